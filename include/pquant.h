@@ -369,6 +369,76 @@ int pq_decode_ffn(const pq_decode_ffn_desc* desc, const void* X, const uint32_t*
                   const uint32_t* packed_down, const uint16_t* scale_down, const void* UpGate, const void* Down,
                   const void* Wr, void* Y, int32_t* acc_upgate, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Paged key-value cache of one attention layer, and the attention over it: what stands between the q/k/v projections and the
+ * o projection when a prompt is read or tokens are generated.
+ *
+ * Tokens of a sequence lie in pages of page_tokens tokens; page_table [n_seqs][max_pages] int32 names the page of tokens
+ * i * page_tokens .. of sequence b in entry [b][i], lens [n_seqs] int32 its tokens in the cache.  The rows of a call (K, V, Q, O) are
+ * given sequence by sequence: rows row_start[b] .. row_start[b + 1] - 1 (row_start [n_seqs + 1] int32, non-decreasing) are the LAST
+ * n_b = row_start[b + 1] - row_start[b] tokens of sequence b, at positions lens[b] - n_b .. lens[b] - 1; lens counts them already, in
+ * all calls alike.  row_start NULL: row b is the last token of sequence b.  Rows that belong to no sequence (behind
+ * row_start[n_seqs]) are neither read nor written, in any call.
+ * lens, row_start and page_table are device memory that no call checks on the host, so that a captured call may be replayed with others;
+ * every access stays inside the buffers whatever they hold: a token whose page is not in [0, n_pages), whose position is negative or
+ * beyond max_pages * page_tokens, is not written, reads back as zeros and is attended by nobody.
+ *
+ * Layout.  A page is one contiguous run of pq_kv_cache_bytes() / n_pages bytes and may be copied as such; in it, head by head, with
+ * Dp = d_head rounded up to a multiple of 32:  keys [page_tokens][Dp], values [page_tokens / 16][Dp][16 tokens], and for PQ_KV_INT8
+ * the fp32 steps of the keys [page_tokens] and of the values [page_tokens].  Key columns d_head .. Dp - 1 are zero (pq_kv_write
+ * writes them so; a cache filled by other means must hold zeros or finite values there); what a page holds behind its last token is
+ * never used, so a fresh cache needs no clearing.
+ * PQ_KV_INT8: every token and head is a row of the AbsMax quantiser of pq_quant_act (codes q; gamma = 128 / max(max|x|, 1e-5)); the
+ * cache keeps step = max(max|x|, 1e-5) / 128, an exact quotient, and a code stands for fl32(q * step).  A row with an infinity or a
+ * NaN in it has the step NaN: all of it reads back as NaN.
+ * PQ_KV_BF16: values rounded to bf16. */
+typedef enum pq_kv_kind { PQ_KV_BF16 = 0, PQ_KV_INT8 = 1 } pq_kv_kind;
+typedef struct pq_kv_desc {
+  int32_t kv_kind;     /* pq_kv_kind */
+  int32_t n_kv_heads;  /* key-value heads */
+  int32_t d_head;      /* even, 2..256 */
+  int32_t page_tokens; /* power of two, 16..1024 */
+  int32_t n_pages;     /* pages in the cache */
+  int32_t n_seqs;      /* sequences of the call */
+  int32_t max_pages;   /* entries of a row of page_table; max_pages * page_tokens <= 2^30 */
+} pq_kv_desc;
+size_t pq_kv_cache_bytes(const pq_kv_desc* desc); /* of n_pages pages; 0 for a bad descriptor */
+/* Writes T rows of keys and values into the cache.
+ *   K, V [T][n_kv_heads][d_head] of `dtype` (PQ_F32 or PQ_BF16), rows k_stride / v_stride elements apart (parts of a fused q/k/v
+ *   projection); both strides even and at least n_kv_heads * d_head.  Both buffers and the cache 16-byte aligned.
+ *   Sequences of one call must not share a page that they write to: which of two rows for one place stays is not defined. */
+int pq_kv_write(const pq_kv_desc* desc, const void* K, const void* V, int32_t dtype, int32_t T, int64_t k_stride, int64_t v_stride,
+                const int32_t* row_start, const int32_t* lens, const int32_t* page_table, void* cache, size_t cache_bytes, void* stream);
+/* Reads the last n_b tokens of every sequence back into T rows of K and V (either may be NULL), same shapes and strides as written;
+ * elements between the rows are left as they are. */
+int pq_kv_read(const pq_kv_desc* desc, const void* cache, size_t cache_bytes, const int32_t* row_start, const int32_t* lens,
+               const int32_t* page_table, int32_t T, void* K, void* V, int32_t dtype, int64_t k_stride, int64_t v_stride, void* stream);
+
+/* Attention over the cache.  Query head h reads key-value head h / (n_heads / n_kv_heads).  A row at position p sees the tokens 0 .. p of its
+ * sequence (causal), of these the last `window` if window > 0, or with causal == 0 all lens[b] of them (a row at a negative
+ * position sees none):
+ *     s_t = scale * q . k_t,    o = sum_t exp(s_t - lse) v_t,    lse = log sum_t exp(s_t),
+ * k_t, v_t the values that the cache stands for; scores, sums and lse in fp32, one rounding of o to bf16.  A row that sees nothing has
+ * o = 0 and lse = -infinity.  Tokens that a row does not see have no effect on it, whatever they hold. */
+typedef struct pq_attn_desc {
+  pq_kv_desc kv;
+  int32_t n_heads; /* query heads, a multiple of kv.n_kv_heads */
+  int32_t causal;  /* pq_attn_prefill: 1, or 0 for rows that see their whole sequence (then window must be 0) */
+  int32_t window;  /* 0: none */
+  int32_t max_len; /* pq_attn_decode: an upper bound of lens that the caller knows (0: max_pages * page_tokens).  How the work is
+                      split and the size of the workspace go by it; longer sequences are still handled in full. */
+  float scale;     /* finite; usually 1 / sqrt(d_head) */
+} pq_attn_desc;
+/* One new token of every sequence: Q [n_seqs][n_heads][d_head] bf16 (rows q_stride elements apart, even), written to the cache already, at
+ * position lens[b] - 1;  O [n_seqs][n_heads][d_head] bf16 out, contiguous;  lse [n_seqs][n_heads] fp32 out or NULL.
+ * workspace: pq_attn_decode_workspace_bytes() bytes of scratch; calls that may overlap need one each. */
+size_t pq_attn_decode_workspace_bytes(const pq_attn_desc* desc);
+int pq_attn_decode(const pq_attn_desc* desc, const void* Q, int64_t q_stride, const void* cache, size_t cache_bytes, const int32_t* lens,
+                   const int32_t* page_table, void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/* The rows of prompts: Q [T][n_heads][d_head] bf16 (rows q_stride elements apart, even), their keys and values written to the cache already;
+ * O [T][n_heads][d_head] bf16 out, contiguous;  lse [T][n_heads] fp32 out or NULL. */
+int pq_attn_prefill(const pq_attn_desc* desc, const void* Q, int64_t q_stride, int32_t T, const int32_t* row_start, const void* cache,
+                    size_t cache_bytes, const int32_t* lens, const int32_t* page_table, void* O, float* lse, void* stream);
+
 /* Glue for chaining the linears into a layer stack; not part of the method.
  * pq_glue_lincomb: out = c0 x0 + c1 x1 + c2 x2 + c3 x3 over n bf16 elements (x1..x3 may be NULL;
  * fp32 arithmetic, one rounding; n % 8 == 0) -- residual adds and the mean that stands in for the

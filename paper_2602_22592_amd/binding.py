@@ -19,6 +19,7 @@ PQ_W_MASTER, PQ_W_PACKED = 0, 1
 PQ_STE_IDENTITY, PQ_STE_CLIP = 0, 1
 PQ_HP_LOWRANK_BF16, PQ_HP_LOWRANK_INT8 = 0, 1
 PQ_PACKED_ROWMAJOR, PQ_PACKED_TILED64 = 0, 1
+PQ_KV_BF16, PQ_KV_INT8 = 0, 1
 
 EXPORTS = [
     "pq_version", "pq_last_error_string", "pq_quant_act", "pq_pack_workspace_bytes", "pq_pack_sign",
@@ -31,6 +32,7 @@ EXPORTS = [
     "pq_hp_int8_ctx_bytes", "pq_hp_int8_workspace_bytes", "pq_hp_int8_fwd", "pq_hp_int8_bwd", "pq_decode_gemv_int8",
     "pq_decode_ffn_workspace_bytes", "pq_decode_ffn", "pq_rmsnorm_bwd_static_max_bytes", "pq_rmsnorm_bwd_static",
     "pq_groupwise_workspace_bytes", "pq_groupwise_fwd", "pq_ffn_ctx_section",
+    "pq_kv_cache_bytes", "pq_kv_write", "pq_kv_read", "pq_attn_decode_workspace_bytes", "pq_attn_decode", "pq_attn_prefill",
 ]
 
 
@@ -58,6 +60,15 @@ class DecodeFFNDesc(C.Structure):
                 ("top_k", C.c_int32), ("n_layers", C.c_int32), ("alpha", C.c_float), ("batch", C.c_int32)]
 
 
+class KVDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("kv_kind", "n_kv_heads", "d_head", "page_tokens", "n_pages", "n_seqs", "max_pages")]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("kv", KVDesc), ("n_heads", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32), ("max_len", C.c_int32),
+                ("scale", C.c_float)]
+
+
 class PQError(RuntimeError):
     pass
 
@@ -78,7 +89,8 @@ def lib():
                      "pq_decode_workspace_bytes", "pq_pack_tiled64_bytes", "pq_ffn_ctx_bytes",
                      "pq_ffn_workspace_bytes", "pq_rmsnorm_bwd_workspace_bytes", "pq_linear_norm_ctx_bytes",
                      "pq_linear_norm_workspace_bytes", "pq_hp_int8_ctx_bytes", "pq_hp_int8_workspace_bytes",
-                     "pq_decode_ffn_workspace_bytes", "pq_rmsnorm_bwd_static_max_bytes"):
+                     "pq_decode_ffn_workspace_bytes", "pq_rmsnorm_bwd_static_max_bytes", "pq_kv_cache_bytes",
+                     "pq_attn_decode_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         _lib = L
     return _lib
@@ -437,6 +449,133 @@ def ffn_bwd(desc, dY, X, Up, Gate, Down, Wr, bufs, dX, dW_up, dW_gate, dW_down, 
     _check(lib().pq_ffn_bwd(C.byref(desc), _p(dY), _p(X), _p(Up), _p(Gate), _p(Down), _p(Wr), _p(bufs.ctx),
                             C.c_size_t(bufs.ctx.numel()), _p(dX), _p(dW_up), _p(dW_gate), _p(dW_down), _p(dUp),
                             _p(dGate), _p(dDown), _p(dWr), _p(d_ab), _p(bufs.ws), C.c_size_t(bufs.ws.numel()), _stream()))
+
+
+def make_kv_desc(kv_kind, n_kv_heads, d_head, page_tokens, n_pages, n_seqs, max_pages):
+    return KVDesc(kv_kind, n_kv_heads, d_head, page_tokens, n_pages, n_seqs, max_pages)
+
+
+def make_attn_desc(kv, n_heads, scale=None, causal=True, window=0, max_len=0):
+    """scale: 1 / sqrt(d_head) unless given.  max_len: an upper bound of the sequences' lengths (0: what the page table can hold)."""
+    return AttnDesc(kv, n_heads, int(causal), window, max_len, kv.d_head ** -0.5 if scale is None else scale)
+
+
+def kv_cache(desc, device="cuda"):
+    n = lib().pq_kv_cache_bytes(C.byref(desc))
+    if n == 0:
+        raise PQError(f"bad cache descriptor: {lib().pq_last_error_string().decode()}")
+    return _bytes(n, device)
+
+
+def attn_decode_workspace(desc, device="cuda"):
+    n = lib().pq_attn_decode_workspace_bytes(C.byref(desc))
+    if n == 0:
+        raise PQError(f"bad attention descriptor: {lib().pq_last_error_string().decode()}")
+    return _bytes(n, device)
+
+
+def _kv_stream(kv, cache, lens, page_table, row_start, *others):
+    """The stream of a cache call, after the checks that the C side cannot make: devices, types and sizes of the tensors.  The call
+    goes to the cache's device (its current stream), whichever device is current."""
+    dev = cache.device
+    for t in (lens, page_table, row_start):
+        if t is not None and (t.dtype != torch.int32 or t.device != dev or not t.is_contiguous()):
+            raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
+    for t in others:
+        if t is not None and t.device != dev:
+            raise PQError(f"a tensor on {t.device}, the cache on {dev}")
+    if dev.type != "cuda" or cache.dtype != torch.uint8 or not cache.is_contiguous():
+        raise PQError("the cache is a contiguous uint8 tensor on a GPU")
+    B = kv.n_seqs
+    if lens.numel() < B or page_table.numel() < B * kv.max_pages or (row_start is not None and row_start.numel() < B + 1):
+        raise PQError("lens, page_table or row_start is smaller than the descriptor says")
+    return C.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _rows(t, heads, d):
+    """Row stride of a [T][heads][d] tensor whose rows are contiguous."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        raise PQError(f"a tensor of shape {tuple(t.shape)}: [rows, {heads}, {d}] is wanted")
+    T = t.shape[0]
+    if T and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+        raise PQError("the heads of a row must be contiguous")
+    return t.stride(0) if T > 1 else heads * d
+
+
+class _on_device:
+    """Makes a tensor's device the current one for a call, if it is not already."""
+
+    def __init__(self, t):
+        self.dev = t.device
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.dev.index != self.before:
+            torch.cuda.set_device(self.dev)
+
+    def __exit__(self, *a):
+        if self.dev.index != self.before:
+            torch.cuda.set_device(self.before)
+
+
+def kv_write(desc, K, V, cache, lens, page_table, row_start=None):
+    """K, V [T, n_kv_heads, d_head] (bf16 or fp32, any even row stride) into the cache at the last positions of their sequences."""
+    s = _kv_stream(desc, cache, lens, page_table, row_start, K, V)
+    ks, vs = _rows(K, desc.n_kv_heads, desc.d_head), _rows(V, desc.n_kv_heads, desc.d_head)
+    if K.dtype != V.dtype or K.shape[0] != V.shape[0]:
+        raise PQError("K and V differ in type or rows")
+    with _on_device(cache):
+        _check(lib().pq_kv_write(C.byref(desc), _p(K), _p(V), _dt(K), K.shape[0], C.c_int64(ks), C.c_int64(vs), _p(row_start), _p(lens),
+                                 _p(page_table), _p(cache), C.c_size_t(cache.numel()), s))
+    return cache
+
+
+def kv_read(desc, cache, lens, page_table, K, V, row_start=None):
+    """The inverse of kv_write, into K and V (either may be None)."""
+    s = _kv_stream(desc, cache, lens, page_table, row_start, K, V)
+    X = K if K is not None else V
+    if X is None:
+        raise PQError("neither keys nor values are asked for")
+    if K is not None and V is not None and (K.dtype != V.dtype or K.shape[0] != V.shape[0]):
+        raise PQError("K and V differ in type or rows")
+    ks, vs = (0 if t is None else _rows(t, desc.n_kv_heads, desc.d_head) for t in (K, V))
+    with _on_device(cache):
+        _check(lib().pq_kv_read(C.byref(desc), _p(cache), C.c_size_t(cache.numel()), _p(row_start), _p(lens), _p(page_table), X.shape[0],
+                                _p(K), _p(V), _dt(X), C.c_int64(ks), C.c_int64(vs), s))
+    return K, V
+
+
+def _attn_rows(desc, Q, O, lse):
+    qs = _rows(Q, desc.n_heads, desc.kv.d_head)
+    if Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16:
+        raise PQError("Q and O are bf16")
+    if O.numel() != Q.numel() or not O.is_contiguous():
+        raise PQError("O is contiguous and of Q's size")
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != Q.shape[0] * desc.n_heads or not lse.is_contiguous()):
+        raise PQError("lse is a contiguous fp32 tensor of one value per row and head")
+    return qs
+
+
+def attn_decode(desc, Q, cache, lens, page_table, O, ws, lse=None):
+    """Q [n_seqs, n_heads, d_head] bf16: the last token of every sequence over its whole cache."""
+    s = _kv_stream(desc.kv, cache, lens, page_table, None, Q, O, lse, ws)
+    qs = _attn_rows(desc, Q, O, lse)
+    if Q.shape[0] != desc.kv.n_seqs:
+        raise PQError(f"{Q.shape[0]} rows for {desc.kv.n_seqs} sequences")
+    with _on_device(cache):
+        _check(lib().pq_attn_decode(C.byref(desc), _p(Q), C.c_int64(qs), _p(cache), C.c_size_t(cache.numel()), _p(lens), _p(page_table),
+                                    _p(O), _p(lse), _p(ws), C.c_size_t(ws.numel()), s))
+    return O
+
+
+def attn_prefill(desc, Q, cache, lens, page_table, row_start, O, lse=None):
+    """Q [T, n_heads, d_head] bf16: the rows of prompts, sequence by sequence (row_start [n_seqs + 1])."""
+    s = _kv_stream(desc.kv, cache, lens, page_table, row_start, Q, O, lse)
+    qs = _attn_rows(desc, Q, O, lse)
+    with _on_device(cache):
+        _check(lib().pq_attn_prefill(C.byref(desc), _p(Q), C.c_int64(qs), Q.shape[0], _p(row_start), _p(cache), C.c_size_t(cache.numel()),
+                                     _p(lens), _p(page_table), _p(O), _p(lse), s))
+    return O
 
 
 def glue_lincomb(out, xs, cs):
