@@ -75,6 +75,446 @@ __global__ __launch_bounds__(64) void attn_row_kernel(kv_view v, const uint16_t*
   if (lse && lane == 0) lse[(size_t)t * heads + h] = any ? m + logf(l) : -INFINITY;
 }
 
+// ---------------------------------------------------------------------------------------------
+// One new token of every sequence
+// ---------------------------------------------------------------------------------------------
+// x of the neighbours in a quad of lanes (xor 1, xor 2), without the LDS.
+template <int CTRL>
+__device__ __forceinline__ float quad_swap(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += quad_swap<0xB1>(x);
+  return x + quad_swap<0x4E>(x);
+}
+// over the four groups of 16 lanes
+__device__ __forceinline__ float groups_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+__device__ __forceinline__ float groups_sum(float x) {
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+__device__ __forceinline__ uint32_t groups_max_u(uint32_t x) {
+  x = max(x, (uint32_t)__shfl_xor((int)x, 16, 64));
+  return max(x, (uint32_t)__shfl_xor((int)x, 32, 64));
+}
+
+constexpr int DECODE_WAVES = 4;
+struct decode_args {
+  kv_view v;
+  const uint16_t* Q;
+  int64_t qs;
+  int heads, group, head_blocks, block_heads, window, chunk, n_chunks;
+  float scale;                   // times log2 e
+  uint16_t* O;
+  float* lse;
+  float *part_o, *part_ml;       // [b][head][chunk][dp], [b][head][chunk][2]: pieces of sequences that are cut
+};
+
+// The tokens of sequence b that its row sees, and where its pieces begin: pieces of `chunk` tokens from lo rounded down to a tile.
+struct decode_range { int lo, hi, t0, pieces; };
+__device__ __forceinline__ decode_range decode_seq(const decode_args& a, int b) {
+  const int len = max(a.v.lens[b], 0);
+  decode_range r;
+  r.hi = min(len, a.v.max_pages << a.v.page_shift);
+  r.lo = a.window > 0 ? max(0, len - a.window) : 0;
+  r.t0 = r.lo & ~63;
+  r.pieces = r.hi <= r.lo ? 1 : min((r.hi - r.t0 + a.chunk - 1) / a.chunk, a.n_chunks);
+  return r;
+}
+
+template <int KIND, int NK, int NC>
+__global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_args a) {
+  constexpr bool I8 = KIND == PQ_KV_INT8;
+  constexpr int DP = NK * 32, ND = DP / 16;
+  constexpr int TT = 64;                                      // tokens of a tile
+  constexpr int KS = I8 ? DP / 64 : NK, TAIL = I8 ? NK % 2 : 0;
+  const kv_view& v = a.v;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int col = lane & 15, g = lane >> 4;
+  // (b, key-value head, piece), with the head blocks of one of them 8 workgroups apart: on the same XCD, whose L2 holds the tiles
+  const int blk = blockIdx.x, r = (blk / (8 * a.head_blocks)) * 8 + (blk & 7), hb = (blk >> 3) % a.head_blocks;
+  const int z = r % a.n_chunks, bh = r / a.n_chunks, kvh = bh % v.n_kv_heads, b = bh / v.n_kv_heads;
+  if (b >= v.n_seqs) return;
+  const decode_range R = decode_seq(a, b);
+  if (z >= R.pieces) return;
+  const int begin = R.t0 + z * a.chunk, end = z + 1 == R.pieces ? R.hi : begin + a.chunk;
+  const int n_heads = min(a.block_heads, a.group - hb * a.block_heads);   // of this workgroup
+  const int first_head = kvh * a.group + hb * a.block_heads;
+
+  // ---- the queries as the matrix instructions' second operand: column = head (bf16) or head and digit (INT8)
+  i32x4_t qf[NC][KS > 0 ? KS : 1];
+  long qt[NC];
+  float qw[NC];                                               // what one unit of a score's integer stands for, for this column's digit
+  const int digit = lane & 3;
+  const float digit_w = digit == 0 ? 1.0f : digit == 1 ? 256.0f : digit == 2 ? 65536.0f : 0.0f;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int hl = I8 ? c * 4 + (col >> 2) : c * 16 + col;
+    const bool mine = hl < n_heads;
+    const uint16_t* q = a.Q + b * a.qs + (size_t)(first_head + (mine ? hl : 0)) * v.d;
+    if constexpr (I8) {
+      // q in 23 bits relative to the power of two above its largest element, in three digits of base 256
+      float x[NK * 8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int d = ks * 64 + g * 16 + j;
+          x[ks * 16 + j] = mine && d < v.d ? bf16_to_f32(q[d]) : 0.0f;
+        }
+      if constexpr (TAIL)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int d = KS * 64 + g * 8 + j;
+          x[KS * 16 + j] = mine && d < v.d ? bf16_to_f32(q[d]) : 0.0f;
+        }
+#pragma unroll
+      for (int j = 0; j < NK * 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+      top = groups_max_u(top);
+      const bool bad = top >= 0x7f800000u;
+      const int eb = max((int)(top >> 23), 27);                // |x| < 2^(eb - 126)
+      const float fac = bad ? 0.0f : __uint_as_float((uint32_t)(275 - eb) << 23);
+      qw[c] = bad ? __uint_as_float(0x7fc00000u) : digit_w * a.scale * __uint_as_float((uint32_t)(eb - 21) << 23);
+      auto digits4 = [&](int at) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int n = bad ? 0 : (int)rintf(x[at + j] * fac);
+          w |= ((((uint32_t)(n + 0x808080) >> (8 * digit)) & 0xff) ^ 0x80) << (8 * j);
+        }
+        return digit == 3 ? 0u : w;
+      };
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qf[c][ks][j] = (int)digits4(ks * 16 + 4 * j);
+      if constexpr (TAIL) qt[c] = (long)(((uint64_t)digits4(KS * 16 + 4) << 32) | digits4(KS * 16));
+    } else {
+      qw[c] = a.scale;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = ks * 32 + g * 8 + 2 * j;
+          qf[c][ks][j] = mine && d < v.d ? *reinterpret_cast<const int*>(q + d) : 0;
+        }
+    }
+  }
+
+  f32x4_t acc[NC][ND];
+  float m[NC], l[NC];
+  uint32_t seen = 0;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    m[c] = -INFINITY; l[c] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) acc[c][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int slot_mask = (1 << v.page_shift) - 1;
+  const int32_t* table = v.table + (size_t)b * v.max_pages;
+  const size_t kvh_at = (size_t)kvh * v.head_bytes, page_bytes = v.head_bytes * v.n_kv_heads;
+
+  for (int t0 = begin + wave * TT; t0 < end; t0 += waves * TT) {
+    // group g of lanes looks up the page of tokens t0 + 16 g ..
+    const int tg = t0 + 16 * g;
+    int page = -1;
+    if (tg < R.hi) page = table[tg >> v.page_shift];
+    const bool there = (unsigned)page < (unsigned)v.n_pages;
+    if (!there) page = 0;
+    const bool full = t0 >= R.lo && t0 + TT <= end && __all(there);
+    i32x4_t S[NC][4];
+    i32x4_t vf[ND * (I8 ? 1 : 2)];
+    float ks_[16], vs_[16];
+    if constexpr (I8) {
+      const int pk = __shfl(page, 16 * (col >> 2), 64);
+      const uint8_t* kp = v.cache + (size_t)pk * page_bytes + kvh_at +
+                          (size_t)((t0 + 16 * (col >> 2) + (col & 3)) & slot_mask) * DP;
+      const uint8_t* base = v.cache + (size_t)page * page_bytes + kvh_at;
+      const uint8_t* vp = base + v.part_bytes + (size_t)(tg & slot_mask) * DP + col * 16;
+      const float* sp = reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes) + (tg & slot_mask);
+      i32x4_t kf[4][KS > 0 ? KS : 1];
+      long kt[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[c][ks] = *reinterpret_cast<const i32x4_t*>(kp + c * 4 * DP + ks * 64 + g * 16);
+        if constexpr (TAIL) kt[c] = *reinterpret_cast<const long*>(kp + c * 4 * DP + KS * 64 + g * 8);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t x = reinterpret_cast<const f32x4_t*>(sp)[i];
+        const f32x4_t y = reinterpret_cast<const f32x4_t*>(sp + slot_mask + 1)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { ks_[4 * i + j] = x[j]; vs_[4 * i + j] = y[j]; }
+      }
+#pragma unroll
+      for (int i = 0; i < ND; ++i) vf[i] = *reinterpret_cast<const i32x4_t*>(vp + i * 256);
+#pragma unroll
+      for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          i32x4_t s = {0, 0, 0, 0};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[c][ks], qf[n][ks], s, 0, 0, 0);
+          if constexpr (TAIL) s = __builtin_amdgcn_mfma_i32_16x16x32_i8(kt[c], qt[n], s, 0, 0, 0);
+          S[n][c] = s;
+        }
+    } else {
+      // score register [2 u + w][i] of group g is token 32 u + 8 g + 4 w + i: the eight tokens that the group's lanes hold of the values
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int pk = __shfl(page, 16 * (2 * u + (col >> 3)), 64), pv = __shfl(page, 16 * (2 * u + (g >> 1)), 64);
+        const uint8_t* kp = v.cache + (size_t)pk * page_bytes + kvh_at +
+                            (size_t)((t0 + 32 * u + 8 * (col >> 2) + (col & 3)) & slot_mask) * (2 * DP) + g * 16;
+        const uint8_t* vp = v.cache + (size_t)pv * page_bytes + kvh_at + v.part_bytes +
+                            (size_t)((t0 + 32 * u + 16 * (g >> 1)) & slot_mask) * (2 * DP) + col * 32 + (g & 1) * 16;
+        i32x4_t kf[2][NK];
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int ks = 0; ks < NK; ++ks) kf[w][ks] = *reinterpret_cast<const i32x4_t*>(kp + w * 4 * 2 * DP + ks * 64);
+#pragma unroll
+        for (int i = 0; i < ND; ++i) vf[u * ND + i] = *reinterpret_cast<const i32x4_t*>(vp + i * 512);
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks)
+              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[w][ks]), __builtin_bit_cast(bf16x8_t, qf[n][ks]), s, 0, 0, 0);
+            S[n][2 * u + w] = __builtin_bit_cast(i32x4_t, s);
+          }
+      }
+    }
+    // which of the lane's 16 tokens the row sees (all of them in most tiles); token of register k
+    auto token = [&](int k) { return I8 ? 16 * g + k : 32 * (k >> 3) + 8 * g + (k & 7); };
+    uint32_t mask = 0xffff;
+    if (!full) {
+      const uint64_t ok = __ballot(there);
+      mask = 0;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const int t = token(k);
+        if (t0 + t >= R.lo && t0 + t < end && ((ok >> (t & 48)) & 1)) mask |= 1u << k;
+      }
+      if constexpr (!I8) {   // values that nobody sees may be anything: a probability of zero does not silence an infinity
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t two = (mask >> (8 * u + 2 * j)) & 3, keep = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int i = 0; i < ND; ++i) vf[u * ND + i][j] &= (int)keep;
+          }
+      }
+    }
+    seen |= mask;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      float s[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        if constexpr (I8) s[k] = quad_sum((float)S[n][k >> 2][k & 3] * qw[n]) * ks_[k];
+        else s[k] = __int_as_float(S[n][k >> 2][k & 3]) * qw[n];
+      }
+      if (!full)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[k] = (mask >> k) & 1 ? s[k] : -INFINITY;
+      float top = s[0];
+#pragma unroll
+      for (int k = 1; k < 16; ++k) top = fmaxf(top, s[k]);
+      const float mt = fmaxf(m[n], groups_max(top)), mx = mt == -INFINITY ? 0.0f : mt;
+      const float keep = __builtin_amdgcn_exp2f(m[n] - mx);
+      m[n] = mt;
+      float sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        s[k] = __builtin_amdgcn_exp2f(s[k] - mx);
+        sum += s[k];
+      }
+      l[n] = l[n] * keep + sum;
+      if (!__all(keep == 1.0f))
+#pragma unroll
+        for (int i = 0; i < ND; ++i) acc[n][i] *= keep;
+      if constexpr (I8) {
+        // p times the value's step, in 23 bits relative to the power of two above the tile's largest
+        uint32_t big = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          s[k] = full || ((mask >> k) & 1) ? s[k] * vs_[k] : 0.0f;
+          big = max(big, __float_as_uint(s[k]));
+        }
+        big = groups_max_u(big);
+        const int eb = min(max((int)(big >> 23), 27), 254);
+        const float fac = __uint_as_float((uint32_t)(275 - eb) << 23);
+        const float w = big >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : digit_w * __uint_as_float((uint32_t)(eb - 21) << 23);
+        const uint32_t lo_sel = 0x0c0c0400u + 0x0101u * digit, hi_sel = 0x04000c0cu + 0x01010000u * digit;
+        i32x4_t pf;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t u[4];   // the integer in the low bits of 1.5 * 2^23 + x, plus 128 in every digit
+#pragma unroll
+          for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(__builtin_fmaf(s[4 * j + i], fac, 12582912.0f)) + (0x808080u - 0x4B400000u);
+          pf[j] = (int)((__builtin_amdgcn_perm(u[1], u[0], lo_sel) | __builtin_amdgcn_perm(u[3], u[2], hi_sel)) ^ 0x80808080u);
+        }
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+          const i32x4_t o = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[i], pf, i32x4_t{0, 0, 0, 0}, 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[n][i][j] = __builtin_fmaf((float)o[j], w, acc[n][i][j]);
+        }
+      } else {
+        // p as the sum of two bf16 numbers
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          bf16x8_t hi, lo;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            hi[k] = (__bf16)s[8 * u + k];
+            lo[k] = (__bf16)(s[8 * u + k] - (float)hi[k]);
+          }
+#pragma unroll
+          for (int i = 0; i < ND; ++i) {
+            const bf16x8_t x = __builtin_bit_cast(bf16x8_t, vf[u * ND + i]);
+            acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, lo, acc[n][i], 0, 0, 0);
+            acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, hi, acc[n][i], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+
+  // ---- the wavefronts' pieces are joined through the LDS: [wave][head][dp] sums, then maximum, sum and "saw a token"
+  extern __shared__ float lds[];
+  float* ml = lds + (size_t)waves * n_heads * DP;
+  const bool any = __any(seen != 0);
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    const int hl = I8 ? n * 4 + (col >> 2) : n * 16 + col;
+    const float sum = groups_sum(l[n]);
+#pragma unroll
+    for (int i = 0; i < ND; ++i) {
+      f32x4_t x = acc[n][i];
+      if constexpr (I8)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = quad_sum(x[j]);
+      if (hl < n_heads && (!I8 || digit == 0)) *reinterpret_cast<f32x4_t*>(lds + ((size_t)wave * n_heads + hl) * DP + i * 16 + g * 4) = x;
+    }
+    if (hl < n_heads && g == 0 && (!I8 || digit == 0)) {
+      ml[(wave * n_heads + hl) * 2] = m[n];
+      ml[(wave * n_heads + hl) * 2 + 1] = any ? sum : -1.0f;   // (a sum is never negative)
+    }
+  }
+  __syncthreads();
+  const bool whole = R.pieces == 1;
+  for (int e = threadIdx.x; e < n_heads * DP; e += blockDim.x) {
+    const int hl = e / DP, d = e % DP;
+    float M = -INFINITY;
+    for (int w = 0; w < waves; ++w) M = fmaxf(M, ml[(w * n_heads + hl) * 2]);
+    const float mx = M == -INFINITY ? 0.0f : M;
+    float sum = 0.0f, o = 0.0f;
+    bool some = false;
+    for (int w = 0; w < waves; ++w) {
+      const float lw = ml[(w * n_heads + hl) * 2 + 1];
+      if (lw < 0.0f) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[(w * n_heads + hl) * 2] - mx);
+      some = true;
+      sum += lw * f;
+      o += lds[((size_t)w * n_heads + hl) * DP + d] * f;
+    }
+    const int h = first_head + hl;
+    if (whole) {
+      if (d < v.d) a.O[((size_t)b * a.heads + h) * v.d + d] = f32_to_bf16(some ? o / sum : 0.0f);
+      if (d == 0 && a.lse) a.lse[(size_t)b * a.heads + h] = some ? (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
+    } else {
+      const size_t at = ((size_t)b * a.heads + h) * a.n_chunks + z;
+      a.part_o[at * DP + d] = o;
+      if (d == 0) { a.part_ml[at * 2] = M; a.part_ml[at * 2 + 1] = some ? sum : -1.0f; }
+    }
+  }
+}
+
+// Joins the pieces of one row and head in their order.
+__global__ __launch_bounds__(256) void attn_join_kernel(decode_args a) {
+  const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, d = threadIdx.x;
+  const decode_range R = decode_seq(a, b);
+  if (R.pieces == 1) return;                                   // written by the kernel before
+  const size_t at = ((size_t)b * a.heads + h) * a.n_chunks;
+  const float *ml = a.part_ml + at * 2, *po = a.part_o + at * a.v.dp;
+  float M = -INFINITY;
+  for (int z = 0; z < R.pieces; ++z) M = fmaxf(M, ml[2 * z]);
+  const float mx = M == -INFINITY ? 0.0f : M;
+  float sum = 0.0f, o = 0.0f;
+  bool some = false;
+  for (int z = 0; z < R.pieces; ++z) {
+    const float lz = ml[2 * z + 1];
+    if (lz < 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml[2 * z] - mx);
+    some = true;
+    sum += lz * f;
+    if (d < a.v.dp) o += po[(size_t)z * a.v.dp + d] * f;
+  }
+  if (d < a.v.d) a.O[((size_t)b * a.heads + h) * a.v.d + d] = f32_to_bf16(some ? o / sum : 0.0f);
+  if (d == 0 && a.lse) a.lse[(size_t)b * a.heads + h] = some ? (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
+}
+
+// How a decode call is cut: query heads a workgroup, pieces of a sequence.
+struct decode_plan { int nc, head_blocks, block_heads, chunk, n_chunks; size_t part_o, part_ml, total; };
+decode_plan plan_decode(const pq_attn_desc& d) {
+  decode_plan p;
+  const int group = d.n_heads / d.kv.n_kv_heads;
+  const bool i8 = d.kv.kv_kind == PQ_KV_INT8;
+  p.nc = i8 && group > 4 ? 2 : 1;
+  // a column of the matrix instructions for a head (bf16) or a quad of columns (INT8), and 64 KiB of LDS for the wavefronts' sums
+  const int row = DECODE_WAVES * ((d.kv.d_head + 31) / 32 * 32 + 2) * 4, fit = 65536 / row;
+  const int hb = i8 ? 4 * p.nc : fit < 16 ? fit : 16;
+  p.head_blocks = (group + hb - 1) / hb;
+  p.block_heads = (group + p.head_blocks - 1) / p.head_blocks;
+  const int64_t cap = (int64_t)d.kv.max_pages * d.kv.page_tokens;
+  int64_t most = d.max_len > 0 && d.max_len < cap ? d.max_len : cap;
+  if (d.window > 0 && d.window + 63 < most) most = d.window + 63;
+  const int64_t rows = (int64_t)d.kv.n_seqs * d.kv.n_kv_heads * p.head_blocks;
+  int64_t want = rows > 0 ? (1024 + rows - 1) / rows : 1;      // pieces for 1024 workgroups
+  int64_t chunk = (most + want - 1) / want;
+  if (chunk < 256) chunk = 256;
+  chunk = (chunk + 255) / 256 * 256;
+  p.chunk = (int)chunk;
+  p.n_chunks = (int)((most + chunk - 1) / chunk);
+  const size_t pieces = p.n_chunks > 1 ? (size_t)d.kv.n_seqs * d.n_heads * p.n_chunks : 0;
+  p.part_o = 0;
+  p.part_ml = pq_align_up(pieces * (size_t)((d.kv.d_head + 31) / 32 * 32) * 4, 256);
+  p.total = p.part_ml + pq_align_up(pieces * 8, 256);
+  if (p.total < 256) p.total = 256;
+  return p;
+}
+
+template <int KIND, int NK>
+void launch_decode_nc(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
+  const size_t lds = DECODE_WAVES * (size_t)p.block_heads * (NK * 32 + 2) * 4;
+  constexpr int threads = DECODE_WAVES * 64;
+  if constexpr (KIND == PQ_KV_INT8)
+    if (p.nc == 2) { attn_decode_kernel<KIND, NK, 2><<<grid, threads, lds, s>>>(a); return; }
+  attn_decode_kernel<KIND, NK, 1><<<grid, threads, lds, s>>>(a);
+}
+template <int KIND>
+void launch_decode(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
+  switch (a.v.dp / 32) {
+    case 1: launch_decode_nc<KIND, 1>(a, p, grid, s); break;
+    case 2: launch_decode_nc<KIND, 2>(a, p, grid, s); break;
+    case 3: launch_decode_nc<KIND, 3>(a, p, grid, s); break;
+    case 4: launch_decode_nc<KIND, 4>(a, p, grid, s); break;
+    case 5: launch_decode_nc<KIND, 5>(a, p, grid, s); break;
+    case 6: launch_decode_nc<KIND, 6>(a, p, grid, s); break;
+    case 7: launch_decode_nc<KIND, 7>(a, p, grid, s); break;
+    default: launch_decode_nc<KIND, 8>(a, p, grid, s); break;
+  }
+}
+
 int check_attn(const pq_attn_desc* d) {
   PQ_REQUIRE(d != nullptr, PQ_ERR_BAD_ARG, "desc is NULL");
   if (int e = pq_kv_check(&d->kv)) return e;
@@ -112,7 +552,7 @@ int launch_rows(const pq_attn_desc* d, const kv_view& v, const void* Q, int64_t 
 
 extern "C" size_t pq_attn_decode_workspace_bytes(const pq_attn_desc* d) {
   if (check_attn(d)) return 0;
-  return 256;
+  return plan_decode(*d).total;
 }
 
 extern "C" int pq_attn_decode(const pq_attn_desc* d, const void* Q, int64_t q_stride, const void* cache, size_t cache_bytes,
@@ -126,8 +566,27 @@ extern "C" int pq_attn_decode(const pq_attn_desc* d, const void* Q, int64_t q_st
   PQ_REQUIRE(((uintptr_t)workspace & 15) == 0, PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
   PQ_REQUIRE(workspace_bytes >= pq_attn_decode_workspace_bytes(d), PQ_ERR_WORKSPACE, "workspace %zu < %zu", workspace_bytes,
              pq_attn_decode_workspace_bytes(d));
-  const kv_view v = pq_kv_make_view(d->kv, cache, nullptr, lens, page_table, T);
-  return launch_rows(d, v, Q, q_stride, 1, O, lse, PQP_ATTN_DECODE, (hipStream_t)stream);
+  const decode_plan p = plan_decode(*d);
+  decode_args a;
+  a.v = pq_kv_make_view(d->kv, cache, nullptr, lens, page_table, T);
+  a.Q = (const uint16_t*)Q; a.qs = q_stride;
+  a.heads = d->n_heads; a.group = d->n_heads / d->kv.n_kv_heads; a.head_blocks = p.head_blocks; a.block_heads = p.block_heads;
+  a.window = d->window; a.chunk = p.chunk; a.n_chunks = p.n_chunks;
+  a.scale = d->scale * 1.4426950408889634f;
+  a.O = (uint16_t*)O; a.lse = lse;
+  a.part_o = (float*)((char*)workspace + p.part_o); a.part_ml = (float*)((char*)workspace + p.part_ml);
+  const int64_t pieces = (int64_t)T * d->kv.n_kv_heads * p.n_chunks, grid = (pieces + 7) / 8 * 8 * p.head_blocks;
+  PQ_REQUIRE(grid <= 0x7fffffff, PQ_ERR_SHAPE, "%d sequences of %d heads are too many for one call", T, d->n_heads);
+  hipStream_t s = (hipStream_t)stream;
+  pq_prof_scope prof(PQP_ATTN_DECODE, s);
+  if (d->kv.kv_kind == PQ_KV_INT8) launch_decode<PQ_KV_INT8>(a, p, (unsigned)grid, s);
+  else launch_decode<PQ_KV_BF16>(a, p, (unsigned)grid, s);
+  PQ_CHECK_LAUNCH("attn_decode_kernel");
+  if (p.n_chunks > 1) {
+    attn_join_kernel<<<(unsigned)(T * d->n_heads), 256, 0, s>>>(a);
+    PQ_CHECK_LAUNCH("attn_join_kernel");
+  }
+  return PQ_OK;
 }
 
 extern "C" int pq_attn_prefill(const pq_attn_desc* d, const void* Q, int64_t q_stride, int32_t T, const int32_t* row_start, const void* cache,
