@@ -1,79 +1,12 @@
 // Attention over the paged key-value cache: one new token of every sequence (pq_attn_decode) and the rows of prompts (pq_attn_prefill).
 #include <math.h>
+#include <mutex>
 #include "pq_kv.h"
 
 namespace {
 
 #define PQ_REQUIRE(cond, code, ...) \
   do { if (!(cond)) return pq_set_error(code, __VA_ARGS__); } while (0)
-
-// One wavefront per row and head: 64 tokens at a time, a lane's token scored from the row in LDS, the values summed with a lane per
-// element of the head.
-template <int KIND>
-__global__ __launch_bounds__(64) void attn_row_kernel(kv_view v, const uint16_t* __restrict__ Q, int64_t qs, int heads, int causal, int window,
-                                                      float scale, uint16_t* __restrict__ O, float* __restrict__ lse) {
-  __shared__ float q[256];
-  const int lane = threadIdx.x;
-  const int h = blockIdx.x % heads, t = blockIdx.x / heads;
-  const int b = v.row_start ? kv_find_seq(v.n_seqs, t, [&](int i) { return v.row_start[i]; }) : t;
-  if (b < 0 || b >= v.n_seqs) return;
-  const kv_rows r = kv_seq_rows(v, b);
-  if (t < r.r0 || t >= r.r0 + r.n) return;
-  const int pos = r.first + t - r.r0, kvh = h / (heads / v.n_kv_heads);
-  const int cap = v.max_pages << v.page_shift;
-  const int hi = min(pos < 0 ? 0 : causal ? pos + 1 : r.len, cap), lo = window > 0 ? max(0, pos + 1 - window) : 0;
-  for (int d = lane; d < v.d; d += 64) q[d] = bf16_to_f32(Q[t * qs + (size_t)h * v.d + d]);
-  __syncthreads();
-  bool any = false;
-  float m = -INFINITY, l = 0.0f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int t0 = lo & ~63; t0 < hi; t0 += 64) {
-    const int p = t0 + lane, page = p < hi ? kv_page_id(v, b, p) : -1, slot = p & ((1 << v.page_shift) - 1);
-    float s = -INFINITY;
-    const uint8_t* base = nullptr;
-    float vstep = 1.0f;
-    if (p >= lo && page >= 0) {
-      base = kv_head(v, page, kvh);
-      float a = 0.0f;
-      if constexpr (KIND == PQ_KV_INT8) {
-        const int8_t* k = reinterpret_cast<const int8_t*>(base) + (size_t)slot * v.dp;
-        for (int d = 0; d < v.d; ++d) a = fmaf(q[d], (float)k[d], a);
-        const float* steps = reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes);
-        a *= steps[slot];
-        vstep = steps[(1 << v.page_shift) + slot];
-      } else {
-        const uint16_t* k = reinterpret_cast<const uint16_t*>(base) + (size_t)slot * v.dp;
-        for (int d = 0; d < v.d; ++d) a = fmaf(q[d], bf16_to_f32(k[d]), a);
-      }
-      s = a * scale;
-    }
-    const uint64_t seen = __ballot(base != nullptr);
-    if (!seen) continue;
-    any = true;
-    const float mt = fmaxf(m, wave_max(s)), mx = mt == -INFINITY ? 0.0f : mt;
-    const float keep = expf(m - mx), pr = base ? expf(s - mx) : 0.0f;
-    l = l * keep + wave_sum(pr);
-    m = mt;
-    for (int i = 0; i < 4; ++i) acc[i] *= keep;
-    for (int j = 0; j < 64; ++j) {
-      if (!((seen >> j) & 1)) continue;
-      const float pj = __shfl(pr, j, 64) * __shfl(vstep, j, 64);
-      const int sj = (t0 + j) & ((1 << v.page_shift) - 1);
-      const uint8_t* bj = reinterpret_cast<const uint8_t*>((uintptr_t)__shfl((unsigned long long)(uintptr_t)base, j, 64)) + v.part_bytes;
-      for (int i = 0; i < 4; ++i) {
-        const int d = lane + 64 * i;
-        if (d >= v.d) break;
-        const size_t at = ((size_t)(sj / KV_BLOCK) * v.dp + d) * KV_BLOCK + sj % KV_BLOCK;
-        const float x = KIND == PQ_KV_INT8 ? (float)reinterpret_cast<const int8_t*>(bj)[at] : bf16_to_f32(reinterpret_cast<const uint16_t*>(bj)[at]);
-        acc[i] = fmaf(pj, x, acc[i]);
-      }
-    }
-  }
-  for (int i = 0; i < 4; ++i) {
-    const int d = lane + 64 * i;
-    if (d < v.d) O[((size_t)t * heads + h) * v.d + d] = f32_to_bf16(any ? acc[i] / l : 0.0f);
-  }
-  if (lse && lane == 0) lse[(size_t)t * heads + h] = any ? m + logf(l) : -INFINITY;
-}
 
 // ---------------------------------------------------------------------------------------------
 // One new token of every sequence
@@ -537,15 +470,365 @@ int check_attn_call(const pq_attn_desc* d, const void* Q, int64_t qs, int T, con
   return PQ_OK;
 }
 
-int launch_rows(const pq_attn_desc* d, const kv_view& v, const void* Q, int64_t qs, int causal, void* O, float* lse, int label, hipStream_t s) {
-  pq_prof_scope prof(label, s);
-  const unsigned grid = (unsigned)v.T * (unsigned)d->n_heads;
-  if (d->kv.kv_kind == PQ_KV_INT8)
-    attn_row_kernel<PQ_KV_INT8><<<grid, 64, 0, s>>>(v, (const uint16_t*)Q, qs, d->n_heads, causal, d->window, d->scale, (uint16_t*)O, lse);
-  else
-    attn_row_kernel<PQ_KV_BF16><<<grid, 64, 0, s>>>(v, (const uint16_t*)Q, qs, d->n_heads, causal, d->window, d->scale, (uint16_t*)O, lse);
-  PQ_CHECK_LAUNCH("attn_row_kernel");
+// ---------------------------------------------------------------------------------------------
+// The rows of prompts
+// ---------------------------------------------------------------------------------------------
+struct prefill_args {
+  kv_view v;
+  const uint16_t* Q;
+  int64_t qs;
+  int heads, group, causal, window, tiles;
+  float scale;                   // times log2 e
+  uint16_t* O;
+  float* lse;
+};
+
+constexpr int PF_ROWS = 128, PF_TOKENS = 64, PF_VROW = 2 * PF_TOKENS + 16;   // rows of a workgroup, tokens of a stage, bytes of a value row in the LDS
+template <int NK> constexpr int prefill_krow() { return NK * 64 + 16; }
+template <int NK> constexpr int prefill_stage() { return PF_TOKENS * prefill_krow<NK>() + NK * 32 * PF_VROW + 2 * PF_TOKENS * 4 + 16; }
+
+// Four codes as bf16 (every code has at most eight significant bits: exact).
+__device__ __forceinline__ uint2 codes_bf16(int w) {
+  const uint32_t a = __float_as_uint((float)(int8_t)w), b = __float_as_uint((float)(int8_t)(w >> 8)), c = __float_as_uint((float)(int8_t)(w >> 16)),
+                 d = __float_as_uint((float)(w >> 24));
+  return make_uint2(__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u));
+}
+__device__ __forceinline__ bool has_nonfinite(uint32_t two) { return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u; }
+
+template <int KIND, int NK>
+__global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
+  constexpr bool I8 = KIND == PQ_KV_INT8;
+  constexpr int DP = NK * 32, ES = I8 ? 1 : 2, KROW = prefill_krow<NK>(), STAGE = prefill_stage<NK>(), NS = NK * 2;
+  constexpr int CHUNKS = PF_TOKENS * DP * ES / 16, CT = (CHUNKS + 255) / 256;   // 16-byte pieces of a stage's keys (or values), and of a thread
+  extern __shared__ uint8_t lds8[];
+  const kv_view& v = a.v;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
+  // the last tiles of a sequence see the most tokens and come first; one key-value head of every eight on an XCD
+  const int kvh = blockIdx.x % v.n_kv_heads, vt = a.tiles - 1 - (int)(blockIdx.x / v.n_kv_heads);
+  // Virtual tiles: sequence b owns those from floor(first row / PF_ROWS) + b, at least as many as it has; what it does not need is empty.
+  auto start = [&](int i) { return (int)(((int64_t)(v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / PF_ROWS) + i; };
+  const int b = kv_find_seq(v.n_seqs, vt, start);
+  if (b < 0) return;
+  const kv_rows r = kv_seq_rows(v, b);
+  const int64_t all_rows = (int64_t)r.n * a.group, row0 = (int64_t)(vt - start(b)) * PF_ROWS;
+  if (row0 >= all_rows) return;
+  const int cap = v.max_pages << v.page_shift, hi = min(r.len, cap);
+  auto pos_of = [&](int64_t row) { return r.first + (int)(row / a.group); };
+  const int64_t last_row = min(row0 + PF_ROWS, all_rows) - 1;
+  const int pos_first = pos_of(row0), pos_last = pos_of(last_row);
+  const int t_begin = (a.window > 0 ? max(0, pos_first + 1 - a.window) : 0) & ~(PF_TOKENS - 1);
+  const int t_end = pos_last < 0 ? 0 : a.causal ? min(pos_last + 1, hi) : hi;
+
+  // this lane's row, and what the wavefront's rows see between them
+  const int64_t wrow = row0 + wave * 32, row = wrow + col;
+  const bool active = wrow < all_rows, mine = row < all_rows;
+  const int pos = mine ? pos_of(row) : -1, head = kvh * a.group + (mine ? (int)(row % a.group) : 0);
+  const int64_t trow = r.r0 + (mine ? row / a.group : 0);
+  const int lim = pos < 0 ? -1 : a.causal ? min(pos, hi - 1) : hi - 1, low = a.window > 0 ? max(0, pos + 1 - a.window) : 0;
+  const int wfirst = active ? pos_of(wrow) : 0, wlast = active ? pos_of(min(wrow + 31, all_rows - 1)) : -1;
+  const int w_end = wlast < 0 ? 0 : a.causal ? min(wlast + 1, hi) : hi;                 // some row sees up to here
+  const int w_all_end = wfirst < 0 ? 0 : a.causal ? min(wfirst + 1, hi) : hi;           // every row sees up to here ..
+  const int w_begin = a.window > 0 ? max(0, wfirst + 1 - a.window) : 0, w_all_begin = a.window > 0 ? max(0, wlast + 1 - a.window) : 0;   // .. from here
+
+  i32x4_t qf[NS];
+  {
+    const uint16_t* q = a.Q + trow * a.qs + (size_t)head * v.d;
+    const bool wide = v.d % 8 == 0 && a.qs % 8 == 0;
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) {
+      const int d = ks * 16 + h * 8;
+      i32x4_t x = {0, 0, 0, 0};
+      if (mine) {
+        if (wide) {
+          if (d < v.d) x = *reinterpret_cast<const i32x4_t*>(q + d);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (d + 2 * j < v.d) x[j] = *reinterpret_cast<const int*>(q + d + 2 * j);
+        }
+      }
+      qf[ks] = x;
+    }
+  }
+  f32x16_t acc[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+  uint32_t seen = 0;
+
+  // ---- staging: pages of a stage's four blocks of 16 tokens in lanes 0..3 of every wavefront, one stage ahead of the loads
+  const int slot_mask = (1 << v.page_shift) - 1;
+  const int32_t* table = v.table + (size_t)b * v.max_pages;
+  const size_t kvh_at = (size_t)kvh * v.head_bytes, page_bytes = v.head_bytes * v.n_kv_heads;
+  auto pages_at = [&](int t0) {
+    const int t = t0 + 16 * (lane & 3);
+    int p = -1;
+    if (t < t_end) p = table[t >> v.page_shift];
+    return (unsigned)p < (unsigned)v.n_pages ? p : -1;
+  };
+  i32x4_t kreg[CT], vreg[CT];
+  float steps = 0.0f;
+  uint32_t there = 0;            // which of the four blocks of the loaded stage have a page
+  auto load_stage = [&](int t0, int pages) {
+    there = (uint32_t)__ballot(pages >= 0) & 15;
+    const int safe = max(pages, 0);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const int i = threadIdx.x + 256 * c;
+      const int t = min(i / (DP * ES / 16), PF_TOKENS - 1), piece = i % (DP * ES / 16);        // keys: token by token
+      const int bk = __shfl(safe, t >> 4, 64);
+      const int vb = min(i / (DP * ES), 3), vpiece = i % (DP * ES);                            // values: block by block
+      const int bv = __shfl(safe, vb, 64);
+      if (CHUNKS % 256 == 0 || i < CHUNKS) {
+        kreg[c] = *reinterpret_cast<const i32x4_t*>(v.cache + (size_t)bk * page_bytes + kvh_at + (size_t)((t0 + t) & slot_mask) * (DP * ES) + piece * 16);
+        vreg[c] = *reinterpret_cast<const i32x4_t*>(v.cache + (size_t)bv * page_bytes + kvh_at + v.part_bytes + (size_t)((t0 + 16 * vb) & slot_mask) * (DP * ES) + vpiece * 16);
+      }
+    }
+    if constexpr (I8) {
+      const int t = threadIdx.x & 63, bs = __shfl(safe, t >> 4, 64);
+      if (wave < 2)
+        steps = reinterpret_cast<const float*>(v.cache + (size_t)bs * page_bytes + kvh_at + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + ((t0 + t) & slot_mask)];
+    }
+  };
+  // `check`: whether some row of the workgroup does not see some of the stage's tokens
+  auto store_stage = [&](int t0, uint8_t* buf, bool check) {
+    uint8_t *lk = buf, *lv = buf + PF_TOKENS * KROW;
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const int i = threadIdx.x + 256 * c;
+      if (CHUNKS % 256 != 0 && i >= CHUNKS) continue;
+      const int t = i / (DP * ES / 16), piece = i % (DP * ES / 16), vb = i / (DP * ES), vpiece = i % (DP * ES);
+      const int rk = (t & 0x33) | ((t & 4) << 1) | ((t & 8) >> 1);     // see the scores' tokens below
+      if constexpr (I8) {
+        const uint2 x0 = codes_bf16(kreg[c][0]), x1 = codes_bf16(kreg[c][1]), x2 = codes_bf16(kreg[c][2]), x3 = codes_bf16(kreg[c][3]);
+        *reinterpret_cast<uint4*>(lk + rk * KROW + piece * 32) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+        *reinterpret_cast<uint4*>(lk + rk * KROW + piece * 32 + 16) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+        const uint2 y0 = codes_bf16(vreg[c][0]), y1 = codes_bf16(vreg[c][1]), y2 = codes_bf16(vreg[c][2]), y3 = codes_bf16(vreg[c][3]);
+        *reinterpret_cast<uint4*>(lv + vpiece * PF_VROW + vb * 32) = make_uint4(y0.x, y0.y, y1.x, y1.y);
+        *reinterpret_cast<uint4*>(lv + vpiece * PF_VROW + vb * 32 + 16) = make_uint4(y2.x, y2.y, y3.x, y3.y);
+      } else {
+        *reinterpret_cast<i32x4_t*>(lk + rk * KROW + piece * 16) = kreg[c];
+        i32x4_t x = vreg[c];
+        if (check || there != 15) {          // tokens that are not there become zeros: a probability of zero does not silence an infinity
+          const int tv = t0 + 16 * vb + 8 * (vpiece & 1);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bool in = (there >> vb) & 1;
+            uint32_t keep = (in && tv + 2 * j < t_end ? 0xffffu : 0u) | (in && tv + 2 * j + 1 < t_end ? 0xffff0000u : 0u);
+            x[j] &= (int)keep;
+            bad |= has_nonfinite((uint32_t)x[j]);
+          }
+        }
+        *reinterpret_cast<i32x4_t*>(lv + (vpiece >> 1) * PF_VROW + vb * 32 + (vpiece & 1) * 16) = x;
+      }
+    }
+    float* ls = reinterpret_cast<float*>(lv + DP * PF_VROW);
+    if constexpr (I8) {
+      if (wave < 2) ls[threadIdx.x] = wave == 0 ? steps * a.scale : steps;
+    } else {
+      if (lane == 0) reinterpret_cast<int*>(ls + 2 * PF_TOKENS)[wave] = 0;
+      if (__any(bad) && lane == 0) reinterpret_cast<int*>(ls + 2 * PF_TOKENS)[wave] = 1;
+    }
+  };
+  auto partly = [&](int t0) {    // some row of the workgroup does not see all of the stage
+    return t0 + PF_TOKENS > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || (a.window > 0 && t0 < pos_last + 1 - a.window);
+  };
+
+  if (t_begin < t_end) {
+    load_stage(t_begin, pages_at(t_begin));
+    store_stage(t_begin, lds8, partly(t_begin));
+  }
+  uint32_t there_now = there;
+  int next_pages = pages_at(t_begin + PF_TOKENS);
+  int buf = 0;
+  for (int t0 = t_begin; t0 < t_end; t0 += PF_TOKENS, buf ^= 1) {
+    __syncthreads();
+    const bool more = t0 + PF_TOKENS < t_end;
+    if (more) {
+      load_stage(t0 + PF_TOKENS, next_pages);
+      next_pages = pages_at(t0 + 2 * PF_TOKENS);
+    }
+    const uint8_t *lk = lds8 + buf * STAGE, *lv = lk + PF_TOKENS * KROW;
+    const float* ls = reinterpret_cast<const float*>(lv + DP * PF_VROW);
+    if (t0 < w_end && t0 + PF_TOKENS > w_begin) {
+      // Scores, transposed (a column is a row of Q): register k of half h is token 32 u + 16 (k / 8) + 8 h + k % 8, the eight tokens
+      // that the half's lanes hold of the values' second operand; the keys' rows lie in the LDS in the order that makes it so.
+      float s[32];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x16_t S;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) S[j] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < NS; ++ks) {
+          const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(lk + (32 * u + col) * KROW + ks * 32 + h * 16);
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8_t, qf[ks]), S, 0, 0, 0);
+        }
+        if constexpr (I8) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[16 * u + 4 * q + j] = S[4 * q + j] * x[j];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[16 * u + j] = S[j] * a.scale;
+        }
+      }
+      const bool full = t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there_now == 15;
+      uint32_t mask = 0xffffffffu;
+      if (!full) {
+        const int top = lim - t0 - 8 * h, bot = low - t0 - 8 * h;
+        mask = 0;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const int c = 32 * (k >> 4) + 16 * ((k >> 3) & 1) + (k & 7);
+          if (c <= top && c >= bot && ((there_now >> (c >> 4)) & 1)) mask |= 1u << k;
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k) s[k] = (mask >> k) & 1 ? s[k] : -INFINITY;
+      }
+      seen |= mask;
+      float top = fmaxf(s[0], s[1]);
+#pragma unroll
+      for (int k = 2; k < 32; ++k) top = fmaxf(top, s[k]);
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float mt = fmaxf(m, top), mx = mt == -INFINITY ? 0.0f : mt;
+      const float keep = __builtin_amdgcn_exp2f(m - mx);
+      m = mt;
+      float sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        s[k] = __builtin_amdgcn_exp2f(s[k] - mx);
+        sum += s[k];
+      }
+      l = l * keep + sum;
+      if (!__all(keep == 1.0f))
+#pragma unroll
+        for (int i = 0; i < NK; ++i) acc[i] *= keep;
+      if constexpr (I8) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + PF_TOKENS + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[16 * u + 4 * q + j] *= x[j];
+          }
+        if (!full)
+#pragma unroll
+          for (int k = 0; k < 32; ++k) s[k] = (mask >> k) & 1 ? s[k] : 0.0f;    // (a step that nobody sees may be NaN)
+      }
+      bf16x8_t p[4];             // rounded to bf16, the operand's type; the sum l is of the unrounded ones
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[q][j] = (__bf16)s[8 * q + j];
+      bool bad = false;
+      if constexpr (!I8)
+        if (!full) {
+          const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
+          bad = (f[0] | f[1] | f[2] | f[3]) != 0;
+        }
+      if (!bad) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[q], acc[i], 0, 0, 0);
+          }
+      } else {
+        // Infinities or NaN among the values of a stage that some row sees a part of: the product without them, and their own
+        // contributions to the rows that see them, token by token.
+#pragma unroll
+        for (int i = 0; i < NK; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
+              if ((x[j] & 0x7f800000) == 0x7f800000) x[j] &= 0xffff;
+            }
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), p[q], acc[i], 0, 0, 0);
+          }
+#pragma unroll 1
+        for (int k = 0; k < 32; ++k) {
+          const float p0 = s[0], p1 = __shfl_xor(p0, 32, 64);
+          const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
+#pragma unroll
+          for (int j = 0; j < 31; ++j) s[j] = s[j + 1];
+          mask >>= 1;
+          const int c = 32 * (k >> 4) + 16 * ((k >> 3) & 1) + (k & 7);
+#pragma unroll
+          for (int i = 0; i < NK; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const uint16_t* x = reinterpret_cast<const uint16_t*>(lv + (32 * i + 8 * (j >> 2) + 4 * h + (j & 3)) * PF_VROW) + c;
+              const float x0 = bf16_to_f32(x[8 * h]), x1 = bf16_to_f32(x[8 * (h ^ 1)]);
+              if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
+              if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
+            }
+        }
+      }
+    }
+    if (more) store_stage(t0 + PF_TOKENS, lds8 + (buf ^ 1) * STAGE, partly(t0 + PF_TOKENS));
+    there_now = there;
+  }
+  if (!mine) return;
+  // ---- every column is a row: register 4 q + j of half h is element 8 q + 4 h + j of each 32
+  l += __shfl_xor(l, 32, 64);
+  const bool any = (seen | (uint32_t)__shfl_xor((int)seen, 32, 64)) != 0;
+  const float inv = any ? 1.0f / l : 0.0f;
+  uint16_t* o = a.O + ((size_t)trow * a.heads + head) * v.d;
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int d = 32 * i + 8 * q + 4 * h;
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = any ? acc[i][4 * q + j] * inv : 0.0f;
+      const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+      if (v.d % 4 == 0) {
+        if (d < v.d) *reinterpret_cast<uint2*>(o + d) = w;
+      } else {
+        if (d < v.d) *reinterpret_cast<uint32_t*>(o + d) = w.x;
+        if (d + 2 < v.d) *reinterpret_cast<uint32_t*>(o + d + 2) = w.y;
+      }
+    }
+  if (a.lse && h == 0) a.lse[(size_t)trow * a.heads + head] = any ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+template <int KIND, int NK>
+int launch_prefill_nk(const prefill_args& a, unsigned grid, hipStream_t s) {
+  static std::once_flag once;
+  static int rc = PQ_OK;
+  std::call_once(once, [] {
+    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * prefill_stage<NK>()) != hipSuccess)
+      rc = PQ_ERR_HIP;
+  });
+  if (rc) return pq_set_error(rc, "hipFuncSetAttribute failed for attn_prefill_kernel");
+  attn_prefill_kernel<KIND, NK><<<grid, 256, 2 * prefill_stage<NK>(), s>>>(a);
   return PQ_OK;
+}
+template <int KIND>
+int launch_prefill(const prefill_args& a, unsigned grid, hipStream_t s) {
+  switch (a.v.dp / 32) {
+    case 1: return launch_prefill_nk<KIND, 1>(a, grid, s);
+    case 2: return launch_prefill_nk<KIND, 2>(a, grid, s);
+    case 3: return launch_prefill_nk<KIND, 3>(a, grid, s);
+    case 4: return launch_prefill_nk<KIND, 4>(a, grid, s);
+    case 5: return launch_prefill_nk<KIND, 5>(a, grid, s);
+    case 6: return launch_prefill_nk<KIND, 6>(a, grid, s);
+    case 7: return launch_prefill_nk<KIND, 7>(a, grid, s);
+    default: return launch_prefill_nk<KIND, 8>(a, grid, s);
+  }
 }
 
 }  // namespace
@@ -595,6 +878,20 @@ extern "C" int pq_attn_prefill(const pq_attn_desc* d, const void* Q, int64_t q_s
   PQ_REQUIRE(T >= 0, PQ_ERR_BAD_ARG, "T=%d is negative", T);
   if (T == 0 || d->kv.n_seqs == 0) return PQ_OK;
   if (int e = check_attn_call(d, Q, q_stride, T, cache, cache_bytes, lens, page_table, O)) return e;
-  const kv_view v = pq_kv_make_view(d->kv, cache, row_start, lens, page_table, T);
-  return launch_rows(d, v, Q, q_stride, d->causal, O, lse, PQP_ATTN_PREFILL, (hipStream_t)stream);
+  prefill_args a;
+  a.v = pq_kv_make_view(d->kv, cache, row_start, lens, page_table, T);
+  a.Q = (const uint16_t*)Q; a.qs = q_stride;
+  a.heads = d->n_heads; a.group = d->n_heads / d->kv.n_kv_heads;
+  a.causal = d->causal; a.window = d->window;
+  a.scale = d->scale * 1.4426950408889634f;
+  a.O = (uint16_t*)O; a.lse = lse;
+  const int64_t tiles = (int64_t)T * a.group / PF_ROWS + d->kv.n_seqs, grid = tiles * d->kv.n_kv_heads;
+  PQ_REQUIRE(grid <= 0x7fffffff, PQ_ERR_SHAPE, "%d rows of %d heads are too many for one call", T, d->n_heads);
+  a.tiles = (int)tiles;
+  hipStream_t s = (hipStream_t)stream;
+  pq_prof_scope prof(PQP_ATTN_PREFILL, s);
+  if (int e = d->kv.kv_kind == PQ_KV_INT8 ? launch_prefill<PQ_KV_INT8>(a, (unsigned)grid, s) : launch_prefill<PQ_KV_BF16>(a, (unsigned)grid, s))
+    return e;
+  PQ_CHECK_LAUNCH("attn_prefill_kernel");
+  return PQ_OK;
 }
