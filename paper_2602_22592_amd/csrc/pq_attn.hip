@@ -466,7 +466,7 @@ int check_attn_call(const pq_attn_desc* d, const void* Q, int64_t qs, int T, con
              (long long)qs, (long long)d->n_heads * d->kv.d_head);
   PQ_REQUIRE((((uintptr_t)Q | (uintptr_t)O | (uintptr_t)cache) & 15) == 0, PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
   PQ_REQUIRE(cache_bytes >= pq_kv_cache_bytes(&d->kv), PQ_ERR_WORKSPACE, "cache %zu < %zu bytes", cache_bytes, pq_kv_cache_bytes(&d->kv));
-  PQ_REQUIRE((int64_t)T * d->n_heads <= 0x7fffffff, PQ_ERR_SHAPE, "%d rows of %d heads are too many for one call", T, d->n_heads);
+  PQ_REQUIRE(T <= (1 << 29) && (int64_t)T * d->n_heads <= 0x7fffffff, PQ_ERR_SHAPE, "%d rows of %d heads are too many for one call", T, d->n_heads);
   return PQ_OK;
 }
 

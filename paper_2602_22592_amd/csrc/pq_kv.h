@@ -41,7 +41,7 @@ __device__ __forceinline__ kv_rows kv_seq_rows(const kv_view& v, int b) {
     r.r0 = b;
     r.n = b < v.T ? 1 : 0;
   }
-  r.len = max(v.lens[b], 0);
+  r.len = min(max(v.lens[b], 0), (1 << 30) + r.n);   // (beyond 2^30 no table has a page; T <= 2^29: no position overflows)
   r.first = r.len - r.n;
   return r;
 }

@@ -1,4 +1,5 @@
 // The paged key-value cache: rows quantised (or rounded to 16 bits) as they are written, and read back.
+#include <type_traits>
 #include "pq_kv.h"
 
 namespace {
@@ -6,78 +7,269 @@ namespace {
 #define PQ_REQUIRE(cond, code, ...) \
   do { if (!(cond)) return pq_set_error(code, __VA_ARGS__); } while (0)
 
-template <typename T, int KIND>
-__global__ __launch_bounds__(256) void kv_write_kernel(kv_view v, const T* __restrict__ K, const T* __restrict__ V, int64_t ks, int64_t vs) {
-  const int lane = threadIdx.x & 63;
+// Sixteen values a lane, each the maximum over the wavefront's rows of 16 lanes: every exchange halves what a lane carries, lane l ends
+// with value l % 16 in v[0].
+template <int N, int OFF>
+__device__ __forceinline__ void max_transposed(uint32_t* v, int lane) {
+  const bool up = (lane & OFF) != 0;
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const uint32_t send = up ? v[i] : v[i + N / 2], keep = up ? v[i + N / 2] : v[i];
+    v[i] = max(keep, (uint32_t)__shfl_xor((int)send, OFF, 64));
+  }
+  if constexpr (N > 2) max_transposed<N / 2, OFF / 2>(v, lane);
+}
+
+// What a wavefront of both kernels works on: the keys or the values of one block of 16 tokens of a sequence and of 1, 2 or 4 heads (LPH lanes
+// a head, E pairs of elements a lane).  Tokens s0 .. s1 - 1 of the block are rows of the call, from row t0 on.
+struct kv_unit { int which, head, page, slot, s0, s1; int64_t t0; };
+template <int LPH>
+__device__ __forceinline__ bool kv_find_unit(const kv_view& v, kv_unit& u) {
+  constexpr int HPU = 64 / LPH;
+  const int lane = threadIdx.x & 63, groups = (v.n_kv_heads + HPU - 1) / HPU;
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int which = (int)(unit & 1), h = (int)((unit >> 1) % v.n_kv_heads);
-  const int64_t t = (unit >> 1) / v.n_kv_heads;
-  if (t >= v.T) return;
-  const int b = v.row_start ? kv_find_seq(v.n_seqs, (int)t, [&](int i) { return v.row_start[i]; }) : (int)t;
-  if (b < 0 || b >= v.n_seqs) return;
+  u.which = (int)(unit & 1);
+  u.head = (int)((unit >> 1) % groups) * HPU + lane / LPH;
+  const int64_t vb = (unit >> 1) / groups;
+  // Virtual blocks: sequence b owns those from floor(first row / 16) + 2 b, which are at least as many as its rows touch.
+  int b = (int)vb, j = 0;
+  if (v.row_start) {
+    auto start = [&](int i) { return (min(max(v.row_start[i], 0), v.T) >> 4) + 2 * i; };
+    if (vb > 0x7fffffff) return false;
+    b = kv_find_seq(v.n_seqs, (int)vb, start);
+    if (b < 0) return false;
+    j = (int)vb - start(b);
+  } else if (vb >= v.n_seqs) {
+    return false;
+  }
   const kv_rows r = kv_seq_rows(v, b);
-  if (t < r.r0 || t >= r.r0 + r.n) return;
-  const int pos = r.first + (int)t - r.r0;
-  const int page = kv_page_id(v, b, pos);
-  if (page < 0) return;
-  const int slot = pos & ((1 << v.page_shift) - 1);
-  const T* src = which ? V + t * vs + (size_t)h * v.d : K + t * ks + (size_t)h * v.d;
-  float x[4];
-  uint32_t amax = 0;
+  if (r.n == 0) return false;
+  const int from = max(r.first, 0), block = (from >> 4) + j, p0 = block << 4;
+  // rows at negative positions belong to no block: the sequence's first virtual block has them too (they read back as zeros)
+  u.s0 = j == 0 ? min(r.first, 0) + (from - p0) : 0;
+  u.s1 = (int)min((int64_t)16, (int64_t)r.len - p0);
+  if (u.s1 <= u.s0) return false;
+  u.t0 = (int64_t)r.r0 + (p0 + u.s0 - r.first);
+  u.page = kv_page_id(v, b, p0);
+  u.slot = p0 & ((1 << v.page_shift) - 1);
+  return true;
+}
+
+template <typename T> __device__ __forceinline__ float2 load_pair(const T* p);
+template <> __device__ __forceinline__ float2 load_pair<float>(const float* p) { return *reinterpret_cast<const float2*>(p); }
+template <> __device__ __forceinline__ float2 load_pair<uint16_t>(const uint16_t* p) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
+__device__ __forceinline__ void store_pair(uint16_t* p, float x, float y) { *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(x, y); }
+
+// A lane holds two neighbouring elements (four beyond 128: E = 2) of all 16 tokens: rows are read a pair of elements a lane, a token's maximum
+// is taken over the lanes for all 16 tokens together, keys leave token by token and values, 16 tokens of an element side by side, as
+// 16-byte pieces.  A block that the call does not fill is written token by token, so that its other tokens stay as they are.
+template <typename T, int KIND, int LPH, int E>
+__global__ __launch_bounds__(256) void kv_write_kernel(kv_view v, const T* __restrict__ K, const T* __restrict__ V, int64_t ks, int64_t vs) {
+  constexpr bool I8 = KIND == PQ_KV_INT8;
+  const int lane = threadIdx.x & 63;
+  kv_unit u;
+  if (!kv_find_unit<LPH>(v, u) || u.page < 0) return;
+  u.t0 -= u.s0;                                     // (row of the block's first token)
+  const int s0 = max(u.s0, 0), s1 = u.s1;
+  const int d0 = 2 * (lane % LPH);
+  const bool head_ok = u.head < v.n_kv_heads;
+  const int64_t stride = u.which ? vs : ks;
+  const T* src = (u.which ? V : K) + (size_t)(head_ok ? u.head : 0) * v.d;
+  float2 x[16][E];
+  uint32_t top[16];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int d = lane + 64 * i;
-    x[i] = d < v.d ? io_traits<T>::load(src, d) : 0.0f;
-    amax = max(amax, __float_as_uint(x[i]) & 0x7fffffffu);
-  }
-  for (int o = 32; o > 0; o >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, 64));
-  uint8_t* base = kv_head(v, page, h);
-  float gamma = 0.0f, step = 0.0f;
-  if constexpr (KIND == PQ_KV_INT8) {
-    kv_scales(amax, gamma, step);
-    if (lane == 0) reinterpret_cast<float*>(base + 2 * (size_t)v.part_bytes)[(which << v.page_shift) + slot] = step;
-  }
-  uint8_t* part = base + (which ? v.part_bytes : 0);
+  for (int s = 0; s < 16; ++s) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int d = lane + 64 * i;
+    for (int e = 0; e < E; ++e) {
+      x[s][e] = make_float2(0.f, 0.f);
+      if (s >= s0 && s < s1 && d0 + 128 * e < v.d) x[s][e] = load_pair<T>(src + (u.t0 + s) * stride + d0 + 128 * e);
+    }
+  }
+  uint8_t* base = kv_head(v, u.page, head_ok ? u.head : 0);
+  if constexpr (I8) {
+#pragma unroll
+    for (int s = 0; s < 16; ++s) {
+      top[s] = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        top[s] = max(top[s], max(__float_as_uint(x[s][e].x) & 0x7fffffffu, __float_as_uint(x[s][e].y) & 0x7fffffffu));
+    }
+    max_transposed<16, 8>(top, lane);
+    uint32_t most = top[0];
+    if constexpr (LPH >= 32) most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
+    if constexpr (LPH >= 64) most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
+    float gamma, step;
+    kv_scales(most, gamma, step);
+    const int s = lane & 15;
+    if (head_ok && lane % LPH < 16 && s >= s0 && s < s1)
+      reinterpret_cast<float*>(base + 2 * (size_t)v.part_bytes)[(u.which << v.page_shift) + u.slot + s] = step;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float g = __shfl(gamma, (lane & ~(LPH - 1)) | i, 64);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x[i][e].x = __int_as_float(kv_code(x[i][e].x, g));
+        x[i][e].y = __int_as_float(kv_code(x[i][e].y, g));
+      }
+    }
+  }
+  if (!head_ok) return;
+  // the two stored numbers of a token, in the low and the high half of a word
+  auto two = [&](int s, int e) {
+    if constexpr (I8) return (__float_as_uint(x[s][e].x) & 0xffu) | (__float_as_uint(x[s][e].y) << 16);
+    else return pack_bf16x2(x[s][e].x, x[s][e].y);
+  };
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int d = d0 + 128 * e;
     if (d >= v.dp) continue;
-    const size_t at = which ? ((size_t)(slot / KV_BLOCK) * v.dp + d) * KV_BLOCK + slot % KV_BLOCK : (size_t)slot * v.dp + d;
-    if constexpr (KIND == PQ_KV_INT8) reinterpret_cast<int8_t*>(part)[at] = (int8_t)kv_code(x[i], gamma);
-    else reinterpret_cast<uint16_t*>(part)[at] = f32_to_bf16(x[i]);
+    if (u.which == 0) {
+#pragma unroll
+      for (int s = 0; s < 16; ++s) {
+        if (s < s0 || s >= s1) continue;
+        const uint32_t w = two(s, e);
+        const size_t at = (size_t)(u.slot + s) * v.dp + d;
+        if constexpr (I8) *reinterpret_cast<uint16_t*>(base + at) = (uint16_t)((w & 0xffu) | ((w >> 8) & 0xff00u));
+        else *reinterpret_cast<uint32_t*>(base + 2 * at) = w;
+      }
+    } else if (s1 - s0 == 16) {
+      constexpr int PER = I8 ? 4 : 2, WORDS = 16 / PER;             // tokens a word, words an element
+      uint32_t lo[WORDS], hi[WORDS];
+#pragma unroll
+      for (int j = 0; j < WORDS; ++j) {
+        lo[j] = hi[j] = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const uint32_t w = two(PER * j + i, e);
+          const uint32_t m = I8 ? 0xffu : 0xffffu;
+          lo[j] |= (w & m) << (32 / PER * i);
+          hi[j] |= ((w >> 16) & m) << (32 / PER * i);
+        }
+      }
+      uint4* out = reinterpret_cast<uint4*>(base + v.part_bytes + ((size_t)(u.slot / KV_BLOCK) * v.dp + d) * KV_BLOCK * (I8 ? 1 : 2));
+#pragma unroll
+      for (int j = 0; j < WORDS / 4; ++j) {
+        out[j] = make_uint4(lo[4 * j], lo[4 * j + 1], lo[4 * j + 2], lo[4 * j + 3]);
+        out[WORDS / 4 + j] = make_uint4(hi[4 * j], hi[4 * j + 1], hi[4 * j + 2], hi[4 * j + 3]);
+      }
+    } else {
+      const size_t at = ((size_t)(u.slot / KV_BLOCK) * v.dp + d) * KV_BLOCK;
+#pragma unroll
+      for (int s = 0; s < 16; ++s) {
+        if (s < s0 || s >= s1) continue;
+        const uint32_t w = two(s, e);
+        if constexpr (I8) {
+          base[v.part_bytes + at + s] = (uint8_t)w;
+          base[v.part_bytes + at + KV_BLOCK + s] = (uint8_t)(w >> 16);
+        } else {
+          uint16_t* out = reinterpret_cast<uint16_t*>(base + v.part_bytes) + at + s;
+          out[0] = (uint16_t)w;
+          out[KV_BLOCK] = (uint16_t)(w >> 16);
+        }
+      }
+    }
   }
 }
 
-template <typename T, int KIND>
+template <typename T, int KIND, int LPH, int E>
 __global__ __launch_bounds__(256) void kv_read_kernel(kv_view v, T* __restrict__ K, T* __restrict__ V, int64_t ks, int64_t vs) {
+  constexpr bool I8 = KIND == PQ_KV_INT8;
   const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int which = (int)(unit & 1), h = (int)((unit >> 1) % v.n_kv_heads);
-  const int64_t t = (unit >> 1) / v.n_kv_heads;
-  if (t >= v.T) return;
-  T* dst = which ? V : K;
-  if (!dst) return;
-  const int b = v.row_start ? kv_find_seq(v.n_seqs, (int)t, [&](int i) { return v.row_start[i]; }) : (int)t;
-  if (b < 0 || b >= v.n_seqs) return;
-  const kv_rows r = kv_seq_rows(v, b);
-  if (t < r.r0 || t >= r.r0 + r.n) return;
-  const int pos = r.first + (int)t - r.r0;
-  const int page = kv_page_id(v, b, pos);
-  const int slot = pos & ((1 << v.page_shift) - 1);
-  dst += t * (which ? vs : ks) + (size_t)h * v.d;
-  const uint8_t* base = page < 0 ? nullptr : kv_head(v, page, h);
-  const uint8_t* part = base + (which ? v.part_bytes : 0);
-  for (int d = lane; d < v.d; d += 64) {
-    float x = 0.0f;
-    if (page >= 0) {
-      const size_t at = which ? ((size_t)(slot / KV_BLOCK) * v.dp + d) * KV_BLOCK + slot % KV_BLOCK : (size_t)slot * v.dp + d;
-      if constexpr (KIND == PQ_KV_INT8)
-        x = (float)reinterpret_cast<const int8_t*>(part)[at] *
-            reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes)[(which << v.page_shift) + slot];
-      else x = bf16_to_f32(reinterpret_cast<const uint16_t*>(part)[at]);
+  kv_unit u;
+  if (!kv_find_unit<LPH>(v, u)) return;
+  T* dst = u.which ? V : K;
+  if (!dst || u.head >= v.n_kv_heads) return;
+  const int64_t stride = u.which ? vs : ks;
+  const int d0 = 2 * (lane % LPH);
+  dst += (size_t)u.head * v.d;
+  // rows at negative positions and those without a page
+  for (int s = u.s0; s < (u.page < 0 ? u.s1 : min(u.s1, 0)); ++s)
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (d0 + 128 * e < v.d) store_pair(dst + (u.t0 + s - u.s0) * stride + d0 + 128 * e, 0.0f, 0.0f);
+  if (u.page < 0) return;
+  u.t0 -= u.s0;
+  const int s0 = max(u.s0, 0), s1 = u.s1;
+  const uint8_t* base = kv_head(v, u.page, u.head);
+  float step[16];
+  if constexpr (I8) {
+    const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes) + (u.which << v.page_shift) + u.slot);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 x = p[j];
+      step[4 * j] = x.x; step[4 * j + 1] = x.y; step[4 * j + 2] = x.z; step[4 * j + 3] = x.w;
     }
-    io_traits<T>::store(dst, d, x);
   }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int d = d0 + 128 * e;
+    if (d >= v.d) continue;
+    float2 x[16];
+    if (u.which == 0) {
+#pragma unroll
+      for (int s = 0; s < 16; ++s) {
+        const size_t at = (size_t)(u.slot + s) * v.dp + d;
+        if constexpr (I8) {
+          const uint16_t w = *reinterpret_cast<const uint16_t*>(base + at);
+          x[s] = make_float2((float)(int8_t)w, (float)(int8_t)(w >> 8));
+        } else {
+          x[s] = load_pair<uint16_t>(reinterpret_cast<const uint16_t*>(base) + at);
+        }
+      }
+    } else {
+      constexpr int PER = I8 ? 4 : 2, WORDS = 16 / PER;
+      const uint4* p = reinterpret_cast<const uint4*>(base + v.part_bytes + ((size_t)(u.slot / KV_BLOCK) * v.dp + d) * KV_BLOCK * (I8 ? 1 : 2));
+      uint32_t w[2 * WORDS];
+#pragma unroll
+      for (int j = 0; j < WORDS / 2; ++j) {
+        const uint4 y = p[j];
+        w[4 * j] = y.x; w[4 * j + 1] = y.y; w[4 * j + 2] = y.z; w[4 * j + 3] = y.w;
+      }
+#pragma unroll
+      for (int s = 0; s < 16; ++s) {
+        const uint32_t a = w[s / PER] >> (32 / PER * (s % PER)), b = w[WORDS + s / PER] >> (32 / PER * (s % PER));
+        x[s] = I8 ? make_float2((float)(int8_t)a, (float)(int8_t)b) : make_float2(__uint_as_float(a << 16), __uint_as_float(b << 16));
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < 16; ++s) {
+      if (s < s0 || s >= s1) continue;
+      if constexpr (I8) { x[s].x *= step[s]; x[s].y *= step[s]; }
+      store_pair(dst + (u.t0 + s) * stride + d, x[s].x, x[s].y);
+    }
+  }
+}
+
+template <typename F>
+void by_width(int dp, F f) {      // lanes a head, pairs of elements a lane
+  if (dp <= 32) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+  else if (dp <= 64) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+  else if (dp <= 128) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  else f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+}
+// Wavefronts of a call: blocks of 16 tokens (see kv_find_unit), groups of heads, keys and values.
+int64_t kv_units(const kv_view& v) {
+  const int hpu = v.dp <= 32 ? 4 : v.dp <= 64 ? 2 : 1;
+  const int64_t blocks = v.row_start ? (int64_t)v.T / 16 + 2 * (int64_t)v.n_seqs : (v.T < v.n_seqs ? v.T : v.n_seqs);
+  return blocks * ((v.n_kv_heads + hpu - 1) / hpu) * 2;
+}
+template <int KIND, typename T>
+void launch_write(const kv_view& v, const void* K, const void* V, int64_t ks, int64_t vs, hipStream_t s) {
+  const unsigned grid = (unsigned)((kv_units(v) + 3) / 4);
+  by_width(v.dp, [&](auto lph, auto e) {
+    kv_write_kernel<T, KIND, decltype(lph)::value, decltype(e)::value><<<grid, 256, 0, s>>>(v, (const T*)K, (const T*)V, ks, vs);
+  });
+}
+template <int KIND, typename T>
+void launch_read(const kv_view& v, void* K, void* V, int64_t ks, int64_t vs, hipStream_t s) {
+  const unsigned grid = (unsigned)((kv_units(v) + 3) / 4);
+  by_width(v.dp, [&](auto lph, auto e) {
+    kv_read_kernel<T, KIND, decltype(lph)::value, decltype(e)::value><<<grid, 256, 0, s>>>(v, (T*)K, (T*)V, ks, vs);
+  });
 }
 
 }  // namespace
@@ -127,8 +319,9 @@ static int kv_check_call(const pq_kv_desc* d, const void* K, const void* V, int 
              "row strides %lld and %lld must be even and at least n_kv_heads * d_head = %lld", (long long)ks, (long long)vs, (long long)row);
   PQ_REQUIRE((((uintptr_t)K | (uintptr_t)V | (uintptr_t)cache) & 15) == 0, PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
   PQ_REQUIRE(cache_bytes >= pq_kv_cache_bytes(d), PQ_ERR_WORKSPACE, "cache %zu < %zu bytes", cache_bytes, pq_kv_cache_bytes(d));
-  PQ_REQUIRE(((int64_t)T * d->n_kv_heads * 2 + 3) / 4 <= 0x7fffffff, PQ_ERR_SHAPE, "T=%d rows of %d heads are too many for one call", T,
-             d->n_kv_heads);
+  kv_view v = pq_kv_make_view(*d, cache, lens, lens, table, T);      // (with a row_start: the larger count)
+  PQ_REQUIRE(T <= (1 << 29) && d->n_seqs < (1 << 28) && (kv_units(v) + 3) / 4 <= 0x7fffffff, PQ_ERR_SHAPE,
+             "T=%d rows of %d heads in %d sequences are too many for one call", T, d->n_kv_heads, d->n_seqs);
   return PQ_OK;
 }
 
@@ -141,15 +334,9 @@ extern "C" int pq_kv_write(const pq_kv_desc* d, const void* K, const void* V, in
   const kv_view v = pq_kv_make_view(*d, cache, row_start, lens, page_table, T);
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_KV, s);
-  const unsigned grid = (unsigned)(((int64_t)T * d->n_kv_heads * 2 + 3) / 4);
   const bool i8 = d->kv_kind == PQ_KV_INT8;
-  if (dtype == PQ_F32) {
-    if (i8) kv_write_kernel<float, PQ_KV_INT8><<<grid, 256, 0, s>>>(v, (const float*)K, (const float*)V, k_stride, v_stride);
-    else kv_write_kernel<float, PQ_KV_BF16><<<grid, 256, 0, s>>>(v, (const float*)K, (const float*)V, k_stride, v_stride);
-  } else {
-    if (i8) kv_write_kernel<uint16_t, PQ_KV_INT8><<<grid, 256, 0, s>>>(v, (const uint16_t*)K, (const uint16_t*)V, k_stride, v_stride);
-    else kv_write_kernel<uint16_t, PQ_KV_BF16><<<grid, 256, 0, s>>>(v, (const uint16_t*)K, (const uint16_t*)V, k_stride, v_stride);
-  }
+  if (dtype == PQ_F32) i8 ? launch_write<PQ_KV_INT8, float>(v, K, V, k_stride, v_stride, s) : launch_write<PQ_KV_BF16, float>(v, K, V, k_stride, v_stride, s);
+  else i8 ? launch_write<PQ_KV_INT8, uint16_t>(v, K, V, k_stride, v_stride, s) : launch_write<PQ_KV_BF16, uint16_t>(v, K, V, k_stride, v_stride, s);
   PQ_CHECK_LAUNCH("kv_write_kernel");
   return PQ_OK;
 }
@@ -163,15 +350,9 @@ extern "C" int pq_kv_read(const pq_kv_desc* d, const void* cache, size_t cache_b
   const kv_view v = pq_kv_make_view(*d, cache, row_start, lens, page_table, T);
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_KV, s);
-  const unsigned grid = (unsigned)(((int64_t)T * d->n_kv_heads * 2 + 3) / 4);
   const bool i8 = d->kv_kind == PQ_KV_INT8;
-  if (dtype == PQ_F32) {
-    if (i8) kv_read_kernel<float, PQ_KV_INT8><<<grid, 256, 0, s>>>(v, (float*)K, (float*)V, k_stride, v_stride);
-    else kv_read_kernel<float, PQ_KV_BF16><<<grid, 256, 0, s>>>(v, (float*)K, (float*)V, k_stride, v_stride);
-  } else {
-    if (i8) kv_read_kernel<uint16_t, PQ_KV_INT8><<<grid, 256, 0, s>>>(v, (uint16_t*)K, (uint16_t*)V, k_stride, v_stride);
-    else kv_read_kernel<uint16_t, PQ_KV_BF16><<<grid, 256, 0, s>>>(v, (uint16_t*)K, (uint16_t*)V, k_stride, v_stride);
-  }
+  if (dtype == PQ_F32) i8 ? launch_read<PQ_KV_INT8, float>(v, K, V, k_stride, v_stride, s) : launch_read<PQ_KV_BF16, float>(v, K, V, k_stride, v_stride, s);
+  else i8 ? launch_read<PQ_KV_INT8, uint16_t>(v, K, V, k_stride, v_stride, s) : launch_read<PQ_KV_BF16, uint16_t>(v, K, V, k_stride, v_stride, s);
   PQ_CHECK_LAUNCH("kv_read_kernel");
   return PQ_OK;
 }
