@@ -1,6 +1,8 @@
 // Attention over the paged key-value cache: one new token of every sequence (pq_attn_decode) and the rows of prompts (pq_attn_prefill).
 #include <math.h>
 #include <mutex>
+#include <stdlib.h>
+#include <type_traits>
 #include "pq_kv.h"
 
 namespace {
@@ -483,9 +485,9 @@ struct prefill_args {
   float* lse;
 };
 
-constexpr int PF_ROWS = 128, PF_TOKENS = 64, PF_VROW = 2 * PF_TOKENS + 16;   // rows of a workgroup, tokens of a stage, bytes of a value row in the LDS
+constexpr int PF_TOKENS = 64, PF_VROW = 2 * PF_TOKENS + 16;   // tokens of a stage, bytes of a value row in the LDS
 template <int NK> constexpr int prefill_krow() { return NK * 64 + 16; }
-template <int NK> constexpr int prefill_stage() { return PF_TOKENS * prefill_krow<NK>() + NK * 32 * PF_VROW + 2 * PF_TOKENS * 4 + 16; }
+template <int NK> constexpr int prefill_stage() { return PF_TOKENS * prefill_krow<NK>() + NK * 32 * PF_VROW + 2 * PF_TOKENS * 4 + 32; }
 
 // Four codes as bf16 (every code has at most eight significant bits: exact).
 __device__ __forceinline__ uint2 codes_bf16(int w) {
@@ -495,42 +497,45 @@ __device__ __forceinline__ uint2 codes_bf16(int w) {
 }
 __device__ __forceinline__ bool has_nonfinite(uint32_t two) { return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u; }
 
-template <int KIND, int NK>
-__global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
+template <int KIND, int NK, int W>
+__global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(prefill_args a) {
   constexpr bool I8 = KIND == PQ_KV_INT8;
   constexpr int DP = NK * 32, ES = I8 ? 1 : 2, KROW = prefill_krow<NK>(), STAGE = prefill_stage<NK>(), NS = NK * 2;
-  constexpr int CHUNKS = PF_TOKENS * DP * ES / 16, CT = (CHUNKS + 255) / 256;   // 16-byte pieces of a stage's keys (or values), and of a thread
+  constexpr int THREADS = W * 64, ROWS = W * 32, ROW_PIECES = DP * ES / 16, BLOCK_PIECES = DP * ES;   // pieces of 16 bytes of a key, of 16 tokens' values
+  constexpr int PIECES = PF_TOKENS * ROW_PIECES, CT = (PIECES + THREADS - 1) / THREADS;               // of a stage's keys (or values), and of a thread
   extern __shared__ uint8_t lds8[];
   const kv_view& v = a.v;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
   // the last tiles of a sequence see the most tokens and come first; one key-value head of every eight on an XCD
   const int kvh = blockIdx.x % v.n_kv_heads, vt = a.tiles - 1 - (int)(blockIdx.x / v.n_kv_heads);
-  // Virtual tiles: sequence b owns those from floor(first row / PF_ROWS) + b, at least as many as it has; what it does not need is empty.
-  auto start = [&](int i) { return (int)(((int64_t)(v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / PF_ROWS) + i; };
+  // Virtual tiles: sequence b owns those from floor(first row / ROWS) + b, at least as many as it has; what it does not need is empty.
+  // (rows times heads stay below 2^31)
+  auto start = [&](int i) { return ((v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / ROWS + i; };
   const int b = kv_find_seq(v.n_seqs, vt, start);
   if (b < 0) return;
   const kv_rows r = kv_seq_rows(v, b);
-  const int64_t all_rows = (int64_t)r.n * a.group, row0 = (int64_t)(vt - start(b)) * PF_ROWS;
-  if (row0 >= all_rows) return;
+  const int all_rows = r.n * a.group;
+  if (vt - start(b) > (all_rows - 1) / ROWS || all_rows == 0) return;
+  const int row0 = (vt - start(b)) * ROWS;
   const int cap = v.max_pages << v.page_shift, hi = min(r.len, cap);
-  auto pos_of = [&](int64_t row) { return r.first + (int)(row / a.group); };
-  const int64_t last_row = min(row0 + PF_ROWS, all_rows) - 1;
-  const int pos_first = pos_of(row0), pos_last = pos_of(last_row);
+  auto pos_of = [&](int row) { return r.first + row / a.group; };
+  const int rows_here = min(ROWS, all_rows - row0);
+  const int pos_first = pos_of(row0), pos_last = pos_of(row0 + rows_here - 1);
   const int t_begin = (a.window > 0 ? max(0, pos_first + 1 - a.window) : 0) & ~(PF_TOKENS - 1);
   const int t_end = pos_last < 0 ? 0 : a.causal ? min(pos_last + 1, hi) : hi;
 
   // this lane's row, and what the wavefront's rows see between them
-  const int64_t wrow = row0 + wave * 32, row = wrow + col;
-  const bool active = wrow < all_rows, mine = row < all_rows;
-  const int pos = mine ? pos_of(row) : -1, head = kvh * a.group + (mine ? (int)(row % a.group) : 0);
-  const int64_t trow = r.r0 + (mine ? row / a.group : 0);
+  const bool active = wave * 32 < rows_here, mine = wave * 32 + col < rows_here;
+  const int row = row0 + (mine ? wave * 32 + col : 0);
+  const int pos = mine ? pos_of(row) : -1, head = kvh * a.group + row % a.group;
+  const size_t trow = (size_t)r.r0 + row / a.group;
   const int lim = pos < 0 ? -1 : a.causal ? min(pos, hi - 1) : hi - 1, low = a.window > 0 ? max(0, pos + 1 - a.window) : 0;
-  const int wfirst = active ? pos_of(wrow) : 0, wlast = active ? pos_of(min(wrow + 31, all_rows - 1)) : -1;
+  const int wfirst = active ? pos_of(row0 + wave * 32) : 0, wlast = active ? pos_of(row0 + min(wave * 32 + 32, rows_here) - 1) : -1;
   const int w_end = wlast < 0 ? 0 : a.causal ? min(wlast + 1, hi) : hi;                 // some row sees up to here
   const int w_all_end = wfirst < 0 ? 0 : a.causal ? min(wfirst + 1, hi) : hi;           // every row sees up to here ..
   const int w_begin = a.window > 0 ? max(0, wfirst + 1 - a.window) : 0, w_all_begin = a.window > 0 ? max(0, wlast + 1 - a.window) : 0;   // .. from here
 
-  i32x4_t qf[NS];
+  bf16x8_t qf[NS];
   {
     const uint16_t* q = a.Q + trow * a.qs + (size_t)head * v.d;
     const bool wide = v.d % 8 == 0 && a.qs % 8 == 0;
@@ -547,7 +552,7 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
             if (d + 2 * j < v.d) x[j] = *reinterpret_cast<const int*>(q + d + 2 * j);
         }
       }
-      qf[ks] = x;
+      qf[ks] = __builtin_bit_cast(bf16x8_t, x);
     }
   }
   f32x16_t acc[NK];
@@ -561,7 +566,8 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
   // ---- staging: pages of a stage's four blocks of 16 tokens in lanes 0..3 of every wavefront, one stage ahead of the loads
   const int slot_mask = (1 << v.page_shift) - 1;
   const int32_t* table = v.table + (size_t)b * v.max_pages;
-  const size_t kvh_at = (size_t)kvh * v.head_bytes, page_bytes = v.head_bytes * v.n_kv_heads;
+  const uint8_t* pool = v.cache + (size_t)kvh * v.head_bytes;
+  const size_t page_bytes = v.head_bytes * v.n_kv_heads;
   auto pages_at = [&](int t0) {
     const int t = t0 + 16 * (lane & 3);
     int p = -1;
@@ -574,33 +580,46 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
   auto load_stage = [&](int t0, int pages) {
     there = (uint32_t)__ballot(pages >= 0) & 15;
     const int safe = max(pages, 0);
+    if (v.page_shift >= 6) {     // the whole stage in one page: its address is the wavefront's, a thread's place in it does not change
+      const uint8_t* base = pool + (size_t)__builtin_amdgcn_readfirstlane(safe) * page_bytes;
+      const uint8_t* at = base + (size_t)((t0 & slot_mask) * (DP * ES));
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const int i = threadIdx.x + 256 * c;
-      const int t = min(i / (DP * ES / 16), PF_TOKENS - 1), piece = i % (DP * ES / 16);        // keys: token by token
-      const int bk = __shfl(safe, t >> 4, 64);
-      const int vb = min(i / (DP * ES), 3), vpiece = i % (DP * ES);                            // values: block by block
-      const int bv = __shfl(safe, vb, 64);
-      if (CHUNKS % 256 == 0 || i < CHUNKS) {
-        kreg[c] = *reinterpret_cast<const i32x4_t*>(v.cache + (size_t)bk * page_bytes + kvh_at + (size_t)((t0 + t) & slot_mask) * (DP * ES) + piece * 16);
-        vreg[c] = *reinterpret_cast<const i32x4_t*>(v.cache + (size_t)bv * page_bytes + kvh_at + v.part_bytes + (size_t)((t0 + 16 * vb) & slot_mask) * (DP * ES) + vpiece * 16);
+      for (int c = 0; c < CT; ++c) {
+        const int i = threadIdx.x + THREADS * c;
+        if (PIECES % THREADS == 0 || i < PIECES) {
+          kreg[c] = *reinterpret_cast<const i32x4_t*>(at + i * 16);
+          vreg[c] = *reinterpret_cast<const i32x4_t*>(at + v.part_bytes + i * 16);
+        }
       }
-    }
-    if constexpr (I8) {
-      const int t = threadIdx.x & 63, bs = __shfl(safe, t >> 4, 64);
-      if (wave < 2)
-        steps = reinterpret_cast<const float*>(v.cache + (size_t)bs * page_bytes + kvh_at + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + ((t0 + t) & slot_mask)];
+      if constexpr (I8)
+        if (wave < 2) steps = reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + (t0 & slot_mask) + lane];
+    } else {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const int i = threadIdx.x + THREADS * c;
+        const int t = min(i / ROW_PIECES, PF_TOKENS - 1), vb = min(i / BLOCK_PIECES, 3);           // keys token by token, values block by block
+        const int bk = __shfl(safe, t >> 4, 64), bv = __shfl(safe, vb, 64);
+        if (PIECES % THREADS == 0 || i < PIECES) {
+          kreg[c] = *reinterpret_cast<const i32x4_t*>(pool + (size_t)bk * page_bytes + ((t0 + t) & slot_mask) * (DP * ES) + (i % ROW_PIECES) * 16);
+          vreg[c] = *reinterpret_cast<const i32x4_t*>(pool + (size_t)bv * page_bytes + v.part_bytes + ((t0 + 16 * vb) & slot_mask) * (DP * ES) + (i % BLOCK_PIECES) * 16);
+        }
+      }
+      if constexpr (I8) {
+        const int bs = __shfl(safe, lane >> 4, 64);
+        if (wave < 2) steps = reinterpret_cast<const float*>(pool + (size_t)bs * page_bytes + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + ((t0 + lane) & slot_mask)];
+      }
     }
   };
   // `check`: whether some row of the workgroup does not see some of the stage's tokens
   auto store_stage = [&](int t0, uint8_t* buf, bool check) {
     uint8_t *lk = buf, *lv = buf + PF_TOKENS * KROW;
     bool bad = false;
+    const bool clean = check || there != 15;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      const int i = threadIdx.x + 256 * c;
-      if (CHUNKS % 256 != 0 && i >= CHUNKS) continue;
-      const int t = i / (DP * ES / 16), piece = i % (DP * ES / 16), vb = i / (DP * ES), vpiece = i % (DP * ES);
+      const int i = threadIdx.x + THREADS * c;
+      if (PIECES % THREADS != 0 && i >= PIECES) continue;
+      const int t = i / ROW_PIECES, piece = i % ROW_PIECES, vb = i / BLOCK_PIECES, vpiece = i % BLOCK_PIECES;
       const int rk = (t & 0x33) | ((t & 4) << 1) | ((t & 8) >> 1);     // see the scores' tokens below
       if constexpr (I8) {
         const uint2 x0 = codes_bf16(kreg[c][0]), x1 = codes_bf16(kreg[c][1]), x2 = codes_bf16(kreg[c][2]), x3 = codes_bf16(kreg[c][3]);
@@ -612,13 +631,11 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
       } else {
         *reinterpret_cast<i32x4_t*>(lk + rk * KROW + piece * 16) = kreg[c];
         i32x4_t x = vreg[c];
-        if (check || there != 15) {          // tokens that are not there become zeros: a probability of zero does not silence an infinity
-          const int tv = t0 + 16 * vb + 8 * (vpiece & 1);
+        if (clean) {                       // tokens that are not there become zeros: a probability of zero does not silence an infinity
+          const int left = (there >> vb) & 1 ? t_end - (t0 + 16 * vb + 8 * (vpiece & 1)) : 0;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const bool in = (there >> vb) & 1;
-            uint32_t keep = (in && tv + 2 * j < t_end ? 0xffffu : 0u) | (in && tv + 2 * j + 1 < t_end ? 0xffff0000u : 0u);
-            x[j] &= (int)keep;
+            x[j] &= (int)((left > 2 * j ? 0xffffu : 0u) | (left > 2 * j + 1 ? 0xffff0000u : 0u));
             bad |= has_nonfinite((uint32_t)x[j]);
           }
         }
@@ -628,13 +645,151 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
     float* ls = reinterpret_cast<float*>(lv + DP * PF_VROW);
     if constexpr (I8) {
       if (wave < 2) ls[threadIdx.x] = wave == 0 ? steps * a.scale : steps;
-    } else {
-      if (lane == 0) reinterpret_cast<int*>(ls + 2 * PF_TOKENS)[wave] = 0;
-      if (__any(bad) && lane == 0) reinterpret_cast<int*>(ls + 2 * PF_TOKENS)[wave] = 1;
+    } else if (clean) {
+      const bool any = __any(bad);
+      if (lane == 0) reinterpret_cast<int*>(ls + 2 * PF_TOKENS)[wave] = any;
     }
   };
   auto partly = [&](int t0) {    // some row of the workgroup does not see all of the stage
     return t0 + PF_TOKENS > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || (a.window > 0 && t0 < pos_last + 1 - a.window);
+  };
+
+  // One stage for one wavefront, 32 tokens at a time.  Scores are formed transposed (a column is a row of Q): register k of half h is token
+  // 32 u + 16 (k / 8) + 8 h + k % 8, the eight tokens that the half's lanes hold of the values' second operand; the keys' rows lie in
+  // the LDS in the order that makes it so.  The maximum of a row is taken where its exponentials, relative to the maximum so far, sum to
+  // more than 2^16 (and in the first stage, and where tokens are hidden): any reference gives the same quotient, and bf16 and fp32
+  // have the range.
+  auto stage = [&](auto full_, int t0, const uint8_t* lk, uint32_t blocks) {
+    constexpr bool FULL = decltype(full_)::value;
+    const uint8_t* lv = lk + PF_TOKENS * KROW;
+    const float* ls = reinterpret_cast<const float*>(lv + DP * PF_VROW);
+    f32x16_t S[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) S[u][j] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < NS; ++ks) {
+        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(lk + (32 * u + col) * KROW + ks * 32 + h * 16);
+        S[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], S[u], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float ks[16], p[16];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4_t x = {a.scale, a.scale, a.scale, a.scale};
+        if constexpr (I8) x = *reinterpret_cast<const f32x4_t*>(ls + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ks[4 * q + j] = x[j];
+      }
+      uint32_t mask = 0xffffu;
+      float sum = 0.0f;
+      bool fresh = !FULL;
+      if constexpr (FULL) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[u][k], ks[k], -m));
+          sum += p[k];
+        }
+        fresh = !__all(sum <= 65536.0f);
+      } else {
+        const int top = lim - t0 - 8 * h - 32 * u, bot = low - t0 - 8 * h - 32 * u;
+        mask = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const int c = 16 * (k >> 3) + (k & 7);
+          if (c <= top && c >= bot && ((blocks >> (2 * u + (k >> 3))) & 1)) mask |= 1u << k;
+        }
+      }
+      if (fresh) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          p[k] = FULL || ((mask >> k) & 1) ? S[u][k] * ks[k] : -INFINITY;
+          top = fmaxf(top, p[k]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float mt = fmaxf(m, top), mx = mt == -INFINITY ? 0.0f : mt;
+        const float keep = __builtin_amdgcn_exp2f(m - mx);
+        m = mt;
+        sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          p[k] = __builtin_amdgcn_exp2f(p[k] - mx);
+          sum += p[k];
+        }
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) acc[i] *= keep;
+      }
+      l += sum;
+      seen |= mask;
+      if constexpr (I8) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + PF_TOKENS + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p[4 * q + j] = FULL || ((mask >> (4 * q + j)) & 1) ? p[4 * q + j] * x[j] : 0.0f;   // (a step that nobody sees may be NaN)
+        }
+      }
+      bf16x8_t pb[2];            // rounded to bf16, the operand's type; the sum l is of the unrounded ones
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pb[q][j] = (__bf16)p[8 * q + j];
+      bool bad = false;
+      if constexpr (!I8 && !FULL) {
+        const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
+#pragma unroll
+        for (int w = 0; w < W; ++w) bad |= f[w] != 0;
+      }
+      if (!bad) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int i = 0; i < NK; ++i) {
+            const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + (2 * u + q) * 32 + h * 16);
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[q], acc[i], 0, 0, 0);
+          }
+      } else {
+        // Infinities or NaN among the values of a stage that some row sees a part of: the product without them, and their own
+        // contributions to the rows that see them, token by token.
+#pragma unroll
+        for (int i = 0; i < NK; ++i)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + (2 * u + q) * 32 + h * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
+              if ((x[j] & 0x7f800000) == 0x7f800000) x[j] &= 0xffff;
+            }
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), pb[q], acc[i], 0, 0, 0);
+          }
+#pragma unroll 1
+        for (int k = 0; k < 16; ++k) {
+          const float p0 = p[0], p1 = __shfl_xor(p0, 32, 64);
+          const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
+#pragma unroll
+          for (int j = 0; j < 15; ++j) p[j] = p[j + 1];
+          mask >>= 1;
+          const uint8_t* x = lv + 4 * h * PF_VROW + 2 * (32 * u + 16 * (k >> 3) + (k & 7));
+#pragma unroll
+          for (int i = 0; i < NK; ++i) {
+            asm volatile("" ::: "memory");           // (few of the loads at a time)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const uint16_t* y = reinterpret_cast<const uint16_t*>(x + (32 * i + 8 * (j >> 2) + (j & 3)) * PF_VROW);
+              const float x0 = bf16_to_f32(y[8 * h]), x1 = bf16_to_f32(y[8 * (h ^ 1)]);
+              if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
+              if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
+            }
+          }
+        }
+      }
+    }
   };
 
   if (t_begin < t_end) {
@@ -651,131 +806,10 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
       load_stage(t0 + PF_TOKENS, next_pages);
       next_pages = pages_at(t0 + 2 * PF_TOKENS);
     }
-    const uint8_t *lk = lds8 + buf * STAGE, *lv = lk + PF_TOKENS * KROW;
-    const float* ls = reinterpret_cast<const float*>(lv + DP * PF_VROW);
+    const uint8_t* lk = lds8 + buf * STAGE;
     if (t0 < w_end && t0 + PF_TOKENS > w_begin) {
-      // Scores, transposed (a column is a row of Q): register k of half h is token 32 u + 16 (k / 8) + 8 h + k % 8, the eight tokens
-      // that the half's lanes hold of the values' second operand; the keys' rows lie in the LDS in the order that makes it so.
-      float s[32];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x16_t S;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) S[j] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < NS; ++ks) {
-          const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(lk + (32 * u + col) * KROW + ks * 32 + h * 16);
-          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8_t, qf[ks]), S, 0, 0, 0);
-        }
-        if constexpr (I8) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[16 * u + 4 * q + j] = S[4 * q + j] * x[j];
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) s[16 * u + j] = S[j] * a.scale;
-        }
-      }
-      const bool full = t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there_now == 15;
-      uint32_t mask = 0xffffffffu;
-      if (!full) {
-        const int top = lim - t0 - 8 * h, bot = low - t0 - 8 * h;
-        mask = 0;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const int c = 32 * (k >> 4) + 16 * ((k >> 3) & 1) + (k & 7);
-          if (c <= top && c >= bot && ((there_now >> (c >> 4)) & 1)) mask |= 1u << k;
-        }
-#pragma unroll
-        for (int k = 0; k < 32; ++k) s[k] = (mask >> k) & 1 ? s[k] : -INFINITY;
-      }
-      seen |= mask;
-      float top = fmaxf(s[0], s[1]);
-#pragma unroll
-      for (int k = 2; k < 32; ++k) top = fmaxf(top, s[k]);
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float mt = fmaxf(m, top), mx = mt == -INFINITY ? 0.0f : mt;
-      const float keep = __builtin_amdgcn_exp2f(m - mx);
-      m = mt;
-      float sum = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 32; ++k) {
-        s[k] = __builtin_amdgcn_exp2f(s[k] - mx);
-        sum += s[k];
-      }
-      l = l * keep + sum;
-      if (!__all(keep == 1.0f))
-#pragma unroll
-        for (int i = 0; i < NK; ++i) acc[i] *= keep;
-      if constexpr (I8) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + PF_TOKENS + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[16 * u + 4 * q + j] *= x[j];
-          }
-        if (!full)
-#pragma unroll
-          for (int k = 0; k < 32; ++k) s[k] = (mask >> k) & 1 ? s[k] : 0.0f;    // (a step that nobody sees may be NaN)
-      }
-      bf16x8_t p[4];             // rounded to bf16, the operand's type; the sum l is of the unrounded ones
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[q][j] = (__bf16)s[8 * q + j];
-      bool bad = false;
-      if constexpr (!I8)
-        if (!full) {
-          const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
-          bad = (f[0] | f[1] | f[2] | f[3]) != 0;
-        }
-      if (!bad) {
-#pragma unroll
-        for (int i = 0; i < NK; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
-            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[q], acc[i], 0, 0, 0);
-          }
-      } else {
-        // Infinities or NaN among the values of a stage that some row sees a part of: the product without them, and their own
-        // contributions to the rows that see them, token by token.
-#pragma unroll
-        for (int i = 0; i < NK; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
-              if ((x[j] & 0x7f800000) == 0x7f800000) x[j] &= 0xffff;
-            }
-            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), p[q], acc[i], 0, 0, 0);
-          }
-#pragma unroll 1
-        for (int k = 0; k < 32; ++k) {
-          const float p0 = s[0], p1 = __shfl_xor(p0, 32, 64);
-          const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
-#pragma unroll
-          for (int j = 0; j < 31; ++j) s[j] = s[j + 1];
-          mask >>= 1;
-          const int c = 32 * (k >> 4) + 16 * ((k >> 3) & 1) + (k & 7);
-#pragma unroll
-          for (int i = 0; i < NK; ++i)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const uint16_t* x = reinterpret_cast<const uint16_t*>(lv + (32 * i + 8 * (j >> 2) + 4 * h + (j & 3)) * PF_VROW) + c;
-              const float x0 = bf16_to_f32(x[8 * h]), x1 = bf16_to_f32(x[8 * (h ^ 1)]);
-              if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
-              if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
-            }
-        }
-      }
+      if (t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there_now == 15) stage(std::true_type{}, t0, lk, there_now);
+      else stage(std::false_type{}, t0, lk, there_now);
     }
     if (more) store_stage(t0 + PF_TOKENS, lds8 + (buf ^ 1) * STAGE, partly(t0 + PF_TOKENS));
     there_now = there;
@@ -785,7 +819,7 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
   l += __shfl_xor(l, 32, 64);
   const bool any = (seen | (uint32_t)__shfl_xor((int)seen, 32, 64)) != 0;
   const float inv = any ? 1.0f / l : 0.0f;
-  uint16_t* o = a.O + ((size_t)trow * a.heads + head) * v.d;
+  uint16_t* o = a.O + (trow * a.heads + head) * v.d;
 #pragma unroll
   for (int i = 0; i < NK; ++i)
 #pragma unroll
@@ -802,32 +836,41 @@ __global__ __launch_bounds__(256) void attn_prefill_kernel(prefill_args a) {
         if (d + 2 < v.d) *reinterpret_cast<uint32_t*>(o + d + 2) = w.y;
       }
     }
-  if (a.lse && h == 0) a.lse[(size_t)trow * a.heads + head] = any ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+  if (a.lse && h == 0) a.lse[trow * a.heads + head] = any ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
 }
 
-template <int KIND, int NK>
-int launch_prefill_nk(const prefill_args& a, unsigned grid, hipStream_t s) {
+template <int KIND, int NK, int W>
+int launch_prefill_w(prefill_args a, int n_kv_heads, hipStream_t s) {
   static std::once_flag once;
   static int rc = PQ_OK;
   std::call_once(once, [] {
-    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * prefill_stage<NK>()) != hipSuccess)
+    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK, W>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * prefill_stage<NK>()) != hipSuccess)
       rc = PQ_ERR_HIP;
   });
   if (rc) return pq_set_error(rc, "hipFuncSetAttribute failed for attn_prefill_kernel");
-  attn_prefill_kernel<KIND, NK><<<grid, 256, 2 * prefill_stage<NK>(), s>>>(a);
+  const int64_t tiles = (int64_t)a.v.T * a.group / (W * 32) + a.v.n_seqs, grid = tiles * n_kv_heads;
+  if (grid > 0x7fffffff) return pq_set_error(PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call", a.v.T, a.heads, a.v.n_seqs);
+  a.tiles = (int)tiles;
+  attn_prefill_kernel<KIND, NK, W><<<(unsigned)grid, W * 64, 2 * prefill_stage<NK>(), s>>>(a);
   return PQ_OK;
 }
+template <int KIND, int NK>
+int launch_prefill_nk(const prefill_args& a, hipStream_t s) {
+  if constexpr (NK <= 4)
+    if (getenv("PFW8")) return launch_prefill_w<KIND, NK, 8>(a, a.v.n_kv_heads, s);
+  return launch_prefill_w<KIND, NK, 4>(a, a.v.n_kv_heads, s);
+}
 template <int KIND>
-int launch_prefill(const prefill_args& a, unsigned grid, hipStream_t s) {
+int launch_prefill(const prefill_args& a, hipStream_t s) {
   switch (a.v.dp / 32) {
-    case 1: return launch_prefill_nk<KIND, 1>(a, grid, s);
-    case 2: return launch_prefill_nk<KIND, 2>(a, grid, s);
-    case 3: return launch_prefill_nk<KIND, 3>(a, grid, s);
-    case 4: return launch_prefill_nk<KIND, 4>(a, grid, s);
-    case 5: return launch_prefill_nk<KIND, 5>(a, grid, s);
-    case 6: return launch_prefill_nk<KIND, 6>(a, grid, s);
-    case 7: return launch_prefill_nk<KIND, 7>(a, grid, s);
-    default: return launch_prefill_nk<KIND, 8>(a, grid, s);
+    case 1: return launch_prefill_nk<KIND, 1>(a, s);
+    case 2: return launch_prefill_nk<KIND, 2>(a, s);
+    case 3: return launch_prefill_nk<KIND, 3>(a, s);
+    case 4: return launch_prefill_nk<KIND, 4>(a, s);
+    case 5: return launch_prefill_nk<KIND, 5>(a, s);
+    case 6: return launch_prefill_nk<KIND, 6>(a, s);
+    case 7: return launch_prefill_nk<KIND, 7>(a, s);
+    default: return launch_prefill_nk<KIND, 8>(a, s);
   }
 }
 
@@ -885,13 +928,9 @@ extern "C" int pq_attn_prefill(const pq_attn_desc* d, const void* Q, int64_t q_s
   a.causal = d->causal; a.window = d->window;
   a.scale = d->scale * 1.4426950408889634f;
   a.O = (uint16_t*)O; a.lse = lse;
-  const int64_t tiles = (int64_t)T * a.group / PF_ROWS + d->kv.n_seqs, grid = tiles * d->kv.n_kv_heads;
-  PQ_REQUIRE(grid <= 0x7fffffff, PQ_ERR_SHAPE, "%d rows of %d heads are too many for one call", T, d->n_heads);
-  a.tiles = (int)tiles;
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_ATTN_PREFILL, s);
-  if (int e = d->kv.kv_kind == PQ_KV_INT8 ? launch_prefill<PQ_KV_INT8>(a, (unsigned)grid, s) : launch_prefill<PQ_KV_BF16>(a, (unsigned)grid, s))
-    return e;
+  if (int e = d->kv.kv_kind == PQ_KV_INT8 ? launch_prefill<PQ_KV_INT8>(a, s) : launch_prefill<PQ_KV_BF16>(a, s)) return e;
   PQ_CHECK_LAUNCH("attn_prefill_kernel");
   return PQ_OK;
 }
