@@ -505,7 +505,7 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
   constexpr int PIECES = PF_TOKENS * ROW_PIECES, CT = (PIECES + THREADS - 1) / THREADS;               // of a stage's keys (or values), and of a thread
   extern __shared__ uint8_t lds8[];
   const kv_view& v = a.v;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5, col = lane & 31;
   // the last tiles of a sequence see the most tokens and come first; one key-value head of every eight on an XCD
   const int kvh = blockIdx.x % v.n_kv_heads, vt = a.tiles - 1 - (int)(blockIdx.x / v.n_kv_heads);
   // Virtual tiles: sequence b owns those from floor(first row / ROWS) + b, at least as many as it has; what it does not need is empty.
@@ -560,8 +560,8 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
   for (int i = 0; i < NK; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
-  uint32_t seen = 0;
+  float m = 0.0f, l = 0.0f;      // reference of the exponentials (log2), their sum over this lane's tokens
+  uint32_t seen = 0;             // not zero: the row has seen a token
 
   // ---- staging: pages of a stage's four blocks of 16 tokens in lanes 0..3 of every wavefront, one stage ahead of the loads
   const int slot_mask = (1 << v.page_shift) - 1;
@@ -654,139 +654,140 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
     return t0 + PF_TOKENS > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || (a.window > 0 && t0 < pos_last + 1 - a.window);
   };
 
-  // One stage for one wavefront, 32 tokens at a time.  Scores are formed transposed (a column is a row of Q): register k of half h is token
-  // 32 u + 16 (k / 8) + 8 h + k % 8, the eight tokens that the half's lanes hold of the values' second operand; the keys' rows lie in
-  // the LDS in the order that makes it so.  The maximum of a row is taken where its exponentials, relative to the maximum so far, sum to
-  // more than 2^16 (and in the first stage, and where tokens are hidden): any reference gives the same quotient, and bf16 and fp32
-  // have the range.
-  auto stage = [&](auto full_, int t0, const uint8_t* lk, uint32_t blocks) {
-    constexpr bool FULL = decltype(full_)::value;
+  // One stage for one wavefront.  Scores are formed transposed (a column is a row of Q): register k of half h is token
+  // 16 (k / 8) + 8 h + k % 8, the eight tokens that the half's lanes hold of the values' second operand; the keys' rows lie in
+  // the LDS in the order that makes it so.  The reference m of a row's exponentials moves only where a score exceeds it by 16 (and where
+  // the row sees its first tokens, and in stages with hidden ones): any reference gives the same quotient, and bf16 and fp32 have the range.
+  auto stage = [&](int t0, const uint8_t* lk, uint32_t blocks, bool full) {
     const uint8_t* lv = lk + PF_TOKENS * KROW;
     const float* ls = reinterpret_cast<const float*>(lv + DP * PF_VROW);
-    f32x16_t S[2];
+    bool bad = false;
+    if constexpr (!I8)
+      if (!full) {
+        const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) any |= f[w];
+        bad = __builtin_amdgcn_readfirstlane(any) != 0;
+      }
+    float p[32];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      f32x16_t S;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) S[u][j] = 0.0f;
+      for (int j = 0; j < 16; ++j) S[j] = 0.0f;
 #pragma unroll
       for (int ks = 0; ks < NS; ++ks) {
         const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(lk + (32 * u + col) * KROW + ks * 32 + h * 16);
-        S[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], S[u], 0, 0, 0);
+        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], S, 0, 0, 0);
       }
-    }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      float ks[16], p[16];
+      for (int j = 0; j < 16; ++j) p[16 * u + j] = S[j];
+    }
+    bf16x8_t vf[NK][2];          // the first values, under way while the scores are worked on
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int i = 0; i < NK; ++i) vf[i][q] = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      f32x4_t x = {a.scale, a.scale, a.scale, a.scale};
+      if constexpr (I8) x = *reinterpret_cast<const f32x4_t*>(ls + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[4 * q + j] = __builtin_fmaf(p[4 * q + j], x[j], -m);
+    }
+    uint32_t mask = 0xffffffffu;
+    if (!full) {
+      const int top = lim - t0 - 8 * h, bot = low - t0 - 8 * h;
+      mask = 0;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const int c = 16 * (k >> 3) + (k & 7);
+        if (c <= top && c >= bot && ((blocks >> (k >> 3)) & 1)) mask |= 1u << k;
+      }
+#pragma unroll
+      for (int k = 0; k < 32; ++k) p[k] = (mask >> k) & 1 ? p[k] : -INFINITY;
+    }
+    float top = fmaxf(p[0], p[1]);
+#pragma unroll
+    for (int k = 2; k < 32; ++k) top = fmaxf(top, p[k]);
+    if (!full || !__all(seen != 0 && top <= 16.0f)) {
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      float delta = seen ? fmaxf(top, 0.0f) : top;
+      delta = delta == -INFINITY ? 0.0f : delta;
+      const float keep = seen ? __builtin_amdgcn_exp2f(-delta) : 1.0f;     // (nothing to keep before the first tokens)
+#pragma unroll
+      for (int k = 0; k < 32; ++k) p[k] -= delta;
+      m += delta;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) acc[i] *= keep;
+      seen |= mask | (uint32_t)__shfl_xor((int)mask, 32, 64);
+    }
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      p[k] = __builtin_amdgcn_exp2f(p[k]);
+      sum[k & 1] += p[k];
+    }
+    l += sum[0] + sum[1];
+    if constexpr (I8) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + PF_TOKENS + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[4 * q + j] *= x[j];
+      }
+      if (!full)                 // (a step that nobody sees may be NaN)
+#pragma unroll
+        for (int k = 0; k < 32; ++k) p[k] = (mask >> k) & 1 ? p[k] : 0.0f;
+    }
+    bf16x8_t pb[4];              // rounded to bf16, the operand's type; the sum l is of the unrounded ones
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pb[q][j] = (__bf16)p[8 * q + j];
+    if (!bad) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+          const bf16x8_t x = q < 2 ? vf[i][q & 1] : *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pb[q], acc[i], 0, 0, 0);
+        }
+      return;
+    }
+    // Infinities or NaN among the values of a stage that some row sees a part of: the product without them, and their own
+    // contributions to the rows that see them, token by token.
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        f32x4_t x = {a.scale, a.scale, a.scale, a.scale};
-        if constexpr (I8) x = *reinterpret_cast<const f32x4_t*>(ls + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+        i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) ks[4 * q + j] = x[j];
-      }
-      uint32_t mask = 0xffffu;
-      float sum = 0.0f;
-      bool fresh = !FULL;
-      if constexpr (FULL) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[u][k], ks[k], -m));
-          sum += p[k];
+        for (int j = 0; j < 4; ++j) {
+          if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
+          if ((x[j] & 0x7f800000) == 0x7f800000) x[j] &= 0xffff;
         }
-        fresh = !__all(sum <= 65536.0f);
-      } else {
-        const int top = lim - t0 - 8 * h - 32 * u, bot = low - t0 - 8 * h - 32 * u;
-        mask = 0;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const int c = 16 * (k >> 3) + (k & 7);
-          if (c <= top && c >= bot && ((blocks >> (2 * u + (k >> 3))) & 1)) mask |= 1u << k;
-        }
+        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), pb[q], acc[i], 0, 0, 0);
       }
-      if (fresh) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          p[k] = FULL || ((mask >> k) & 1) ? S[u][k] * ks[k] : -INFINITY;
-          top = fmaxf(top, p[k]);
-        }
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float mt = fmaxf(m, top), mx = mt == -INFINITY ? 0.0f : mt;
-        const float keep = __builtin_amdgcn_exp2f(m - mx);
-        m = mt;
-        sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          p[k] = __builtin_amdgcn_exp2f(p[k] - mx);
-          sum += p[k];
-        }
-        l *= keep;
-#pragma unroll
-        for (int i = 0; i < NK; ++i) acc[i] *= keep;
-      }
-      l += sum;
-      seen |= mask;
-      if constexpr (I8) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + PF_TOKENS + 32 * u + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) p[4 * q + j] = FULL || ((mask >> (4 * q + j)) & 1) ? p[4 * q + j] * x[j] : 0.0f;   // (a step that nobody sees may be NaN)
-        }
-      }
-      bf16x8_t pb[2];            // rounded to bf16, the operand's type; the sum l is of the unrounded ones
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) pb[q][j] = (__bf16)p[8 * q + j];
-      bool bad = false;
-      if constexpr (!I8 && !FULL) {
-        const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
-#pragma unroll
-        for (int w = 0; w < W; ++w) bad |= f[w] != 0;
-      }
-      if (!bad) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-          for (int i = 0; i < NK; ++i) {
-            const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + (2 * u + q) * 32 + h * 16);
-            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[q], acc[i], 0, 0, 0);
-          }
-      } else {
-        // Infinities or NaN among the values of a stage that some row sees a part of: the product without them, and their own
-        // contributions to the rows that see them, token by token.
-#pragma unroll
-        for (int i = 0; i < NK; ++i)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + (2 * u + q) * 32 + h * 16);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
-              if ((x[j] & 0x7f800000) == 0x7f800000) x[j] &= 0xffff;
-            }
-            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), pb[q], acc[i], 0, 0, 0);
-          }
 #pragma unroll 1
-        for (int k = 0; k < 16; ++k) {
-          const float p0 = p[0], p1 = __shfl_xor(p0, 32, 64);
-          const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
+    for (int k = 0; k < 32; ++k) {
+      const float p0 = p[0], p1 = __shfl_xor(p0, 32, 64);
+      const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
 #pragma unroll
-          for (int j = 0; j < 15; ++j) p[j] = p[j + 1];
-          mask >>= 1;
-          const uint8_t* x = lv + 4 * h * PF_VROW + 2 * (32 * u + 16 * (k >> 3) + (k & 7));
+      for (int j = 0; j < 31; ++j) p[j] = p[j + 1];
+      mask >>= 1;
+      const uint8_t* x = lv + 4 * h * PF_VROW + 2 * (16 * (k >> 3) + (k & 7));
 #pragma unroll
-          for (int i = 0; i < NK; ++i) {
-            asm volatile("" ::: "memory");           // (few of the loads at a time)
+      for (int i = 0; i < NK; ++i) {
+        asm volatile("" ::: "memory");               // (few of the loads at a time)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const uint16_t* y = reinterpret_cast<const uint16_t*>(x + (32 * i + 8 * (j >> 2) + (j & 3)) * PF_VROW);
-              const float x0 = bf16_to_f32(y[8 * h]), x1 = bf16_to_f32(y[8 * (h ^ 1)]);
-              if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
-              if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
-            }
-          }
+        for (int j = 0; j < 16; ++j) {
+          const uint16_t* y = reinterpret_cast<const uint16_t*>(x + (32 * i + 8 * (j >> 2) + (j & 3)) * PF_VROW);
+          const float x0 = bf16_to_f32(y[8 * h]), x1 = bf16_to_f32(y[8 * (h ^ 1)]);
+          if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
+          if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
         }
       }
     }
@@ -807,17 +808,15 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
       next_pages = pages_at(t0 + 2 * PF_TOKENS);
     }
     const uint8_t* lk = lds8 + buf * STAGE;
-    if (t0 < w_end && t0 + PF_TOKENS > w_begin) {
-      if (t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there_now == 15) stage(std::true_type{}, t0, lk, there_now);
-      else stage(std::false_type{}, t0, lk, there_now);
-    }
+    if (t0 < w_end && t0 + PF_TOKENS > w_begin)
+      stage(t0, lk, there_now, t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there_now == 15);
     if (more) store_stage(t0 + PF_TOKENS, lds8 + (buf ^ 1) * STAGE, partly(t0 + PF_TOKENS));
     there_now = there;
   }
   if (!mine) return;
   // ---- every column is a row: register 4 q + j of half h is element 8 q + 4 h + j of each 32
   l += __shfl_xor(l, 32, 64);
-  const bool any = (seen | (uint32_t)__shfl_xor((int)seen, 32, 64)) != 0;
+  const bool any = seen != 0;
   const float inv = any ? 1.0f / l : 0.0f;
   uint16_t* o = a.O + (trow * a.heads + head) * v.d;
 #pragma unroll
