@@ -92,6 +92,12 @@ def lib():
                      "pq_decode_ffn_workspace_bytes", "pq_rmsnorm_bwd_static_max_bytes", "pq_kv_cache_bytes",
                      "pq_attn_decode_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
+        p, i, l, n = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+        kv, attn = C.POINTER(KVDesc), C.POINTER(AttnDesc)
+        L.pq_kv_write.argtypes = [kv, p, p, i, i, l, l, p, p, p, p, n, p]
+        L.pq_kv_read.argtypes = [kv, p, n, p, p, p, i, p, p, i, l, l, p]
+        L.pq_attn_decode.argtypes = [attn, p, l, p, n, p, p, p, p, p, n, p]
+        L.pq_attn_prefill.argtypes = [attn, p, l, i, p, p, n, p, p, p, p, p]
         _lib = L
     return _lib
 
@@ -474,74 +480,82 @@ def attn_decode_workspace(desc, device="cuda"):
     return _bytes(n, device)
 
 
-def _kv_stream(kv, cache, lens, page_table, row_start, *others):
-    """The stream of a cache call, after the checks that the C side cannot make: devices, types and sizes of the tensors.  The call
-    goes to the cache's device (its current stream), whichever device is current."""
-    dev = cache.device
-    for t in (lens, page_table, row_start):
-        if t is not None and (t.dtype != torch.int32 or t.device != dev or not t.is_contiguous()):
-            raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
+# the current stream of a device as an integer; the public call builds a Stream object for it, which takes as long as half a launch
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _kv_check(kv, cache, lens, page_table, row_start, *others):
+    """What the C side of a cache call cannot see: devices, types and sizes of the tensors.  Returns the cache's device, whose current
+    stream the call goes to, whichever device is current."""
+    dev, i32 = cache.device, torch.int32
+    B = kv.n_seqs
+    if (lens.dtype != i32 or page_table.dtype != i32 or lens.device != dev or page_table.device != dev or not lens.is_contiguous()
+            or not page_table.is_contiguous() or (row_start is not None and (row_start.dtype != i32 or row_start.device != dev
+                                                                             or not row_start.is_contiguous()))):
+        raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
+    if lens.numel() < B or page_table.numel() < B * kv.max_pages or (row_start is not None and row_start.numel() < B + 1):
+        raise PQError("lens, page_table or row_start is smaller than the descriptor says")
+    if dev.type != "cuda" or cache.dtype != torch.uint8 or not cache.is_contiguous():
+        raise PQError("the cache is a contiguous uint8 tensor on a GPU")
     for t in others:
         if t is not None and t.device != dev:
             raise PQError(f"a tensor on {t.device}, the cache on {dev}")
-    if dev.type != "cuda" or cache.dtype != torch.uint8 or not cache.is_contiguous():
-        raise PQError("the cache is a contiguous uint8 tensor on a GPU")
-    B = kv.n_seqs
-    if lens.numel() < B or page_table.numel() < B * kv.max_pages or (row_start is not None and row_start.numel() < B + 1):
-        raise PQError("lens, page_table or row_start is smaller than the descriptor says")
-    return C.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    return dev.index
+
+
+def _kv_call(dev, f, *args):
+    """f(*args, stream) with the device current."""
+    now = torch.cuda.current_device()
+    if now == dev:
+        _check(f(*args, _raw_stream(dev)))
+        return
+    torch.cuda.set_device(dev)
+    try:
+        _check(f(*args, _raw_stream(dev)))
+    finally:
+        torch.cuda.set_device(now)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _rows(t, heads, d):
     """Row stride of a [T][heads][d] tensor whose rows are contiguous."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+    T, *hd = t.shape
+    if hd != [heads, d]:
         raise PQError(f"a tensor of shape {tuple(t.shape)}: [rows, {heads}, {d}] is wanted")
-    T = t.shape[0]
-    if T and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != d)):
+    if T <= 1 and t.is_contiguous():
+        return heads * d
+    row, head, one = t.stride()
+    if T and (one != 1 or (heads > 1 and head != d)):
         raise PQError("the heads of a row must be contiguous")
-    return t.stride(0) if T > 1 else heads * d
-
-
-class _on_device:
-    """Makes a tensor's device the current one for a call, if it is not already."""
-
-    def __init__(self, t):
-        self.dev = t.device
-
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.dev.index != self.before:
-            torch.cuda.set_device(self.dev)
-
-    def __exit__(self, *a):
-        if self.dev.index != self.before:
-            torch.cuda.set_device(self.before)
+    return row if T > 1 else heads * d
 
 
 def kv_write(desc, K, V, cache, lens, page_table, row_start=None):
     """K, V [T, n_kv_heads, d_head] (bf16 or fp32, any even row stride) into the cache at the last positions of their sequences."""
-    s = _kv_stream(desc, cache, lens, page_table, row_start, K, V)
+    dev = _kv_check(desc, cache, lens, page_table, row_start, K, V)
     ks, vs = _rows(K, desc.n_kv_heads, desc.d_head), _rows(V, desc.n_kv_heads, desc.d_head)
     if K.dtype != V.dtype or K.shape[0] != V.shape[0]:
         raise PQError("K and V differ in type or rows")
-    with _on_device(cache):
-        _check(lib().pq_kv_write(C.byref(desc), _p(K), _p(V), _dt(K), K.shape[0], C.c_int64(ks), C.c_int64(vs), _p(row_start), _p(lens),
-                                 _p(page_table), _p(cache), C.c_size_t(cache.numel()), s))
+    _kv_call(dev, lib().pq_kv_write, C.byref(desc), K.data_ptr(), V.data_ptr(), _dt(K), K.shape[0], ks, vs, _ptr(row_start), lens.data_ptr(),
+             page_table.data_ptr(), cache.data_ptr(), cache.numel())
     return cache
 
 
 def kv_read(desc, cache, lens, page_table, K, V, row_start=None):
     """The inverse of kv_write, into K and V (either may be None)."""
-    s = _kv_stream(desc, cache, lens, page_table, row_start, K, V)
+    dev = _kv_check(desc, cache, lens, page_table, row_start, K, V)
     X = K if K is not None else V
     if X is None:
         raise PQError("neither keys nor values are asked for")
     if K is not None and V is not None and (K.dtype != V.dtype or K.shape[0] != V.shape[0]):
         raise PQError("K and V differ in type or rows")
-    ks, vs = (0 if t is None else _rows(t, desc.n_kv_heads, desc.d_head) for t in (K, V))
-    with _on_device(cache):
-        _check(lib().pq_kv_read(C.byref(desc), _p(cache), C.c_size_t(cache.numel()), _p(row_start), _p(lens), _p(page_table), X.shape[0],
-                                _p(K), _p(V), _dt(X), C.c_int64(ks), C.c_int64(vs), s))
+    ks = 0 if K is None else _rows(K, desc.n_kv_heads, desc.d_head)
+    vs = 0 if V is None else _rows(V, desc.n_kv_heads, desc.d_head)
+    _kv_call(dev, lib().pq_kv_read, C.byref(desc), cache.data_ptr(), cache.numel(), _ptr(row_start), lens.data_ptr(), page_table.data_ptr(),
+             X.shape[0], _ptr(K), _ptr(V), _dt(X), ks, vs)
     return K, V
 
 
@@ -558,23 +572,23 @@ def _attn_rows(desc, Q, O, lse):
 
 def attn_decode(desc, Q, cache, lens, page_table, O, ws, lse=None):
     """Q [n_seqs, n_heads, d_head] bf16: the last token of every sequence over its whole cache."""
-    s = _kv_stream(desc.kv, cache, lens, page_table, None, Q, O, lse, ws)
+    dev = _kv_check(desc.kv, cache, lens, page_table, None, Q, O, lse, ws)
     qs = _attn_rows(desc, Q, O, lse)
     if Q.shape[0] != desc.kv.n_seqs:
         raise PQError(f"{Q.shape[0]} rows for {desc.kv.n_seqs} sequences")
-    with _on_device(cache):
-        _check(lib().pq_attn_decode(C.byref(desc), _p(Q), C.c_int64(qs), _p(cache), C.c_size_t(cache.numel()), _p(lens), _p(page_table),
-                                    _p(O), _p(lse), _p(ws), C.c_size_t(ws.numel()), s))
+    if ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise PQError("the workspace is a contiguous uint8 tensor")
+    _kv_call(dev, lib().pq_attn_decode, C.byref(desc), Q.data_ptr(), qs, cache.data_ptr(), cache.numel(), lens.data_ptr(), page_table.data_ptr(),
+             O.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel())
     return O
 
 
 def attn_prefill(desc, Q, cache, lens, page_table, row_start, O, lse=None):
     """Q [T, n_heads, d_head] bf16: the rows of prompts, sequence by sequence (row_start [n_seqs + 1])."""
-    s = _kv_stream(desc.kv, cache, lens, page_table, row_start, Q, O, lse)
+    dev = _kv_check(desc.kv, cache, lens, page_table, row_start, Q, O, lse)
     qs = _attn_rows(desc, Q, O, lse)
-    with _on_device(cache):
-        _check(lib().pq_attn_prefill(C.byref(desc), _p(Q), C.c_int64(qs), Q.shape[0], _p(row_start), _p(cache), C.c_size_t(cache.numel()),
-                                     _p(lens), _p(page_table), _p(O), _p(lse), s))
+    _kv_call(dev, lib().pq_attn_prefill, C.byref(desc), Q.data_ptr(), qs, Q.shape[0], _ptr(row_start), cache.data_ptr(), cache.numel(),
+             lens.data_ptr(), page_table.data_ptr(), O.data_ptr(), _ptr(lse))
     return O
 
 

@@ -13,6 +13,7 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 // One new token of every sequence
 // ---------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(2))) long i64x2_t;
 // x of the neighbours in a quad of lanes (xor 1, xor 2), without the LDS.
 template <int CTRL>
 __device__ __forceinline__ float quad_swap(float x) {
@@ -22,21 +23,24 @@ __device__ __forceinline__ float quad_sum(float x) {
   x += quad_swap<0xB1>(x);
   return x + quad_swap<0x4E>(x);
 }
-// over the four groups of 16 lanes
+// Over the four groups of 16 lanes.  A swap of x with itself leaves every lane its own value and that of the lane 16 (32) from it.
+template <typename F>
+__device__ __forceinline__ uint32_t groups_fold(uint32_t x, F f) {
+  auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f(y[0], y[1]);
+  auto z = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return f(z[0], z[1]);
+}
 __device__ __forceinline__ float groups_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16, 64));
-  return fmaxf(x, __shfl_xor(x, 32, 64));
+  return __uint_as_float(groups_fold(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
 }
 __device__ __forceinline__ float groups_sum(float x) {
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
+  return __uint_as_float(groups_fold(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 __device__ __forceinline__ uint32_t groups_max_u(uint32_t x) {
-  x = max(x, (uint32_t)__shfl_xor((int)x, 16, 64));
-  return max(x, (uint32_t)__shfl_xor((int)x, 32, 64));
+  return groups_fold(x, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
-constexpr int DECODE_WAVES = 4;
 struct decode_args {
   kv_view v;
   const uint16_t* Q;
@@ -60,24 +64,120 @@ __device__ __forceinline__ decode_range decode_seq(const decode_args& a, int b) 
   return r;
 }
 
-template <int KIND, int NK, int NC>
-__global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_args a) {
+template <int KIND, int NK, int NC, int W>
+__global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
   constexpr bool I8 = KIND == PQ_KV_INT8;
   constexpr int DP = NK * 32, ND = DP / 16;
   constexpr int TT = 64;                                      // tokens of a tile
-  constexpr int KS = I8 ? DP / 64 : NK, TAIL = I8 ? NK % 2 : 0;
+  constexpr int KS = I8 ? DP / 64 : NK, TAIL = I8 ? NK % 2 : 0;   // steps of the scores' contraction, and a half one
   const kv_view& v = a.v;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  // (b, key-value head, piece), with the head blocks of one of them 8 workgroups apart: on the same XCD, whose L2 holds the tiles
+  // element of a lane's j-th word of a row
+  constexpr int QW = NK * 4;
+  auto q_at = [&](int j) { return I8 ? (j < 8 * KS ? (j >> 3) * 64 + g * 16 + 2 * (j & 7) : KS * 64 + g * 8 + 2 * (j - 8 * KS)) : (j >> 2) * 32 + g * 8 + 2 * (j & 3); };
+  // (piece, b, key-value head), with the head blocks of one of them 8 workgroups apart: on the same XCD, whose L2 holds the tiles.  The
+  // last pieces, which only the longest sequences have, come first.
   const int blk = blockIdx.x, r = (blk / (8 * a.head_blocks)) * 8 + (blk & 7), hb = (blk >> 3) % a.head_blocks;
-  const int z = r % a.n_chunks, bh = r / a.n_chunks, kvh = bh % v.n_kv_heads, b = bh / v.n_kv_heads;
-  if (b >= v.n_seqs) return;
+  const int pairs = v.n_seqs * v.n_kv_heads;
+  if (r >= pairs * a.n_chunks) return;
+  const int z = a.n_chunks - 1 - r / pairs, bh = r % pairs, kvh = bh % v.n_kv_heads, b = bh / v.n_kv_heads;
+  const int cap = v.max_pages << v.page_shift;
+  const int32_t* table = v.table + (size_t)b * v.max_pages;
+  // group g of lanes looks up the page of tokens t0 + 16 g ..
+  auto pages_at = [&](int t0) {
+    const int tg = t0 + 16 * g;
+    return tg < cap ? table[tg >> v.page_shift] : -1;
+  };
+  int page_next = a.window == 0 ? pages_at(z * a.chunk + wave * TT) : -1;     // (before the length is there)
+  // the rows of this workgroup's heads, as they lie in memory: all that does not wait for the length is under way before it is there
+  const int n_heads = min(a.block_heads, a.group - hb * a.block_heads);
+  const int first_head = kvh * a.group + hb * a.block_heads;
+  uint32_t qraw[NC][QW];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int hl = I8 ? c * 4 + (col >> 2) : c * 16 + col;
+    const uint16_t* q = a.Q + b * a.qs + (size_t)(first_head + (hl < n_heads ? hl : 0)) * v.d;
+#pragma unroll
+    for (int j = 0; j < QW; ++j) {
+      const int d = q_at(j);
+      qraw[c][j] = *reinterpret_cast<const uint32_t*>(q + (d < v.d ? d : 0));
+    }
+  }
   const decode_range R = decode_seq(a, b);
   if (z >= R.pieces) return;
   const int begin = R.t0 + z * a.chunk, end = z + 1 == R.pieces ? R.hi : begin + a.chunk;
-  const int n_heads = min(a.block_heads, a.group - hb * a.block_heads);   // of this workgroup
-  const int first_head = kvh * a.group + hb * a.block_heads;
+  if (a.window != 0) page_next = pages_at(begin + wave * TT);
+  const int slot_mask = (1 << v.page_shift) - 1;
+  const size_t page_bytes = v.head_bytes * v.n_kv_heads;
+  const uint8_t* pool = v.cache + (size_t)kvh * v.head_bytes;
+
+  // ---- a tile in registers: the keys of the next one are under way while this one's probabilities and values are worked on, its values
+  // while the next scores are
+  constexpr int NF = I8 ? 4 * (KS > 0 ? KS : 1) : 4 * NK;
+  i32x4_t kf[NF], vf[ND * (I8 ? 1 : 2)];
+  long kt[4];
+  float ks_[16], vs_[16];
+  auto load_keys = [&](int t0, int page) {
+    if constexpr (I8) {
+      const uint8_t* kp = pool + (size_t)__shfl(page, 16 * (col >> 2), 64) * page_bytes + (size_t)((t0 + 16 * (col >> 2) + (col & 3)) & slot_mask) * DP;
+      const float* sp = reinterpret_cast<const float*>(pool + (size_t)page * page_bytes + 2 * (size_t)v.part_bytes) + ((t0 + 16 * g) & slot_mask);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[c * KS + ks] = *reinterpret_cast<const i32x4_t*>(kp + c * 4 * DP + ks * 64 + g * 16);
+        if constexpr (TAIL) kt[c] = *reinterpret_cast<const long*>(kp + c * 4 * DP + KS * 64 + g * 8);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t x = reinterpret_cast<const f32x4_t*>(sp)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ks_[4 * i + j] = x[j];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint8_t* kp = pool + (size_t)__shfl(page, 16 * (2 * u + (col >> 3)), 64) * page_bytes +
+                            (size_t)((t0 + 32 * u + 8 * (col >> 2) + (col & 3)) & slot_mask) * (2 * DP) + g * 16;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int ks = 0; ks < NK; ++ks) kf[(2 * u + w) * NK + ks] = *reinterpret_cast<const i32x4_t*>(kp + w * 4 * 2 * DP + ks * 64);
+      }
+    }
+  };
+  auto load_values = [&](int t0, int page) {
+    if constexpr (I8) {
+      const uint8_t* base = pool + (size_t)page * page_bytes;
+      const uint8_t* vp = base + v.part_bytes + (size_t)((t0 + 16 * g) & slot_mask) * DP + col * 16;
+      const float* sp = reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes) + slot_mask + 1 + ((t0 + 16 * g) & slot_mask);
+#pragma unroll
+      for (int i = 0; i < ND; ++i) vf[i] = *reinterpret_cast<const i32x4_t*>(vp + i * 256);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t x = reinterpret_cast<const f32x4_t*>(sp)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vs_[4 * i + j] = x[j];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint8_t* vp = pool + (size_t)__shfl(page, 16 * (2 * u + (g >> 1)), 64) * page_bytes + v.part_bytes +
+                            (size_t)((t0 + 32 * u + 16 * (g >> 1)) & slot_mask) * (2 * DP) + col * 32 + (g & 1) * 16;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) vf[u * ND + i] = *reinterpret_cast<const i32x4_t*>(vp + i * 512);
+      }
+    }
+  };
+  auto there_of = [&](int t0, int page) { return t0 + 16 * g < R.hi && (unsigned)page < (unsigned)v.n_pages; };
+  int t0 = begin + wave * TT;
+  bool there = there_of(t0, page_next);
+  if (t0 < end) {
+    const int page = there ? page_next : 0;
+    load_keys(t0, page);
+    load_values(t0, page);
+    page_next = pages_at(t0 + W * TT);
+  }
 
   // ---- the queries as the matrix instructions' second operand: column = head (bf16) or head and digit (INT8)
   i32x4_t qf[NC][KS > 0 ? KS : 1];
@@ -89,24 +189,16 @@ __global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_a
   for (int c = 0; c < NC; ++c) {
     const int hl = I8 ? c * 4 + (col >> 2) : c * 16 + col;
     const bool mine = hl < n_heads;
-    const uint16_t* q = a.Q + b * a.qs + (size_t)(first_head + (mine ? hl : 0)) * v.d;
     if constexpr (I8) {
       // q in 23 bits relative to the power of two above its largest element, in three digits of base 256
       float x[NK * 8];
       uint32_t top = 0;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int d = ks * 64 + g * 16 + j;
-          x[ks * 16 + j] = mine && d < v.d ? bf16_to_f32(q[d]) : 0.0f;
-        }
-      if constexpr (TAIL)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int d = KS * 64 + g * 8 + j;
-          x[KS * 16 + j] = mine && d < v.d ? bf16_to_f32(q[d]) : 0.0f;
-        }
+      for (int j = 0; j < QW; ++j) {
+        const uint32_t w = mine && q_at(j) < v.d ? qraw[c][j] : 0;
+        x[2 * j] = __uint_as_float(w << 16);
+        x[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
+      }
 #pragma unroll
       for (int j = 0; j < NK * 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
       top = groups_max_u(top);
@@ -133,10 +225,7 @@ __global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_a
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int d = ks * 32 + g * 8 + 2 * j;
-          qf[c][ks][j] = mine && d < v.d ? *reinterpret_cast<const int*>(q + d) : 0;
-        }
+        for (int j = 0; j < 4; ++j) qf[c][ks][j] = mine && q_at(4 * ks + j) < v.d ? (int)qraw[c][4 * ks + j] : 0;
     }
   }
 
@@ -149,83 +238,46 @@ __global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_a
 #pragma unroll
     for (int i = 0; i < ND; ++i) acc[c][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const int slot_mask = (1 << v.page_shift) - 1;
-  const int32_t* table = v.table + (size_t)b * v.max_pages;
-  const size_t kvh_at = (size_t)kvh * v.head_bytes, page_bytes = v.head_bytes * v.n_kv_heads;
 
-  for (int t0 = begin + wave * TT; t0 < end; t0 += waves * TT) {
-    // group g of lanes looks up the page of tokens t0 + 16 g ..
-    const int tg = t0 + 16 * g;
-    int page = -1;
-    if (tg < R.hi) page = table[tg >> v.page_shift];
-    const bool there = (unsigned)page < (unsigned)v.n_pages;
-    if (!there) page = 0;
+  while (t0 < end) {
     const bool full = t0 >= R.lo && t0 + TT <= end && __all(there);
-    i32x4_t S[NC][4];
-    i32x4_t vf[ND * (I8 ? 1 : 2)];
-    float ks_[16], vs_[16];
-    if constexpr (I8) {
-      const int pk = __shfl(page, 16 * (col >> 2), 64);
-      const uint8_t* kp = v.cache + (size_t)pk * page_bytes + kvh_at +
-                          (size_t)((t0 + 16 * (col >> 2) + (col & 3)) & slot_mask) * DP;
-      const uint8_t* base = v.cache + (size_t)page * page_bytes + kvh_at;
-      const uint8_t* vp = base + v.part_bytes + (size_t)(tg & slot_mask) * DP + col * 16;
-      const float* sp = reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes) + (tg & slot_mask);
-      i32x4_t kf[4][KS > 0 ? KS : 1];
-      long kt[4];
+    const int t_next = t0 + W * TT;
+    const bool more = t_next < end, there_next = more && there_of(t_next, page_next);
+    const int page = there_next ? page_next : 0;
+    // Scores: register 4 c + i of group g is the token whose value the group's lanes hold, 16 g + 4 c + i (INT8) or, by 32 tokens,
+    // 8 g + k % 8: the keys' rows are read in the order that makes it so.
+    float sc[NC][16];
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
+        if constexpr (I8) {
+          i32x4_t S = {0, 0, 0, 0};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[c][ks] = *reinterpret_cast<const i32x4_t*>(kp + c * 4 * DP + ks * 64 + g * 16);
-        if constexpr (TAIL) kt[c] = *reinterpret_cast<const long*>(kp + c * 4 * DP + KS * 64 + g * 8);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4_t x = reinterpret_cast<const f32x4_t*>(sp)[i];
-        const f32x4_t y = reinterpret_cast<const f32x4_t*>(sp + slot_mask + 1)[i];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { ks_[4 * i + j] = x[j]; vs_[4 * i + j] = y[j]; }
-      }
-#pragma unroll
-      for (int i = 0; i < ND; ++i) vf[i] = *reinterpret_cast<const i32x4_t*>(vp + i * 256);
-#pragma unroll
-      for (int n = 0; n < NC; ++n)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          i32x4_t s = {0, 0, 0, 0};
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[c][ks], qf[n][ks], s, 0, 0, 0);
-          if constexpr (TAIL) s = __builtin_amdgcn_mfma_i32_16x16x32_i8(kt[c], qt[n], s, 0, 0, 0);
-          S[n][c] = s;
-        }
-    } else {
-      // score register [2 u + w][i] of group g is token 32 u + 8 g + 4 w + i: the eight tokens that the group's lanes hold of the values
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int pk = __shfl(page, 16 * (2 * u + (col >> 3)), 64), pv = __shfl(page, 16 * (2 * u + (g >> 1)), 64);
-        const uint8_t* kp = v.cache + (size_t)pk * page_bytes + kvh_at +
-                            (size_t)((t0 + 32 * u + 8 * (col >> 2) + (col & 3)) & slot_mask) * (2 * DP) + g * 16;
-        const uint8_t* vp = v.cache + (size_t)pv * page_bytes + kvh_at + v.part_bytes +
-                            (size_t)((t0 + 32 * u + 16 * (g >> 1)) & slot_mask) * (2 * DP) + col * 32 + (g & 1) * 16;
-        i32x4_t kf[2][NK];
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int ks = 0; ks < NK; ++ks) kf[w][ks] = *reinterpret_cast<const i32x4_t*>(kp + w * 4 * 2 * DP + ks * 64);
-#pragma unroll
-        for (int i = 0; i < ND; ++i) vf[u * ND + i] = *reinterpret_cast<const i32x4_t*>(vp + i * 512);
-#pragma unroll
-        for (int n = 0; n < NC; ++n)
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < NK; ++ks)
-              s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[w][ks]), __builtin_bit_cast(bf16x8_t, qf[n][ks]), s, 0, 0, 0);
-            S[n][2 * u + w] = __builtin_bit_cast(i32x4_t, s);
+          for (int ks = 0; ks < KS; ++ks) {
+            // (A sum takes one kind of instruction: a 16x16x32 that added to a 16x16x64's result a few instructions behind it read the
+            // result before it was there.  With a half step all of them are 16x16x32, on the halves of a piece.)
+            if constexpr (!TAIL) {
+              S = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[c * KS + ks], qf[n][ks], S, 0, 0, 0);
+            } else {
+              const i64x2_t x = __builtin_bit_cast(i64x2_t, kf[c * KS + ks]), y = __builtin_bit_cast(i64x2_t, qf[n][ks]);
+              S = __builtin_amdgcn_mfma_i32_16x16x32_i8(x[0], y[0], S, 0, 0, 0);
+              S = __builtin_amdgcn_mfma_i32_16x16x32_i8(x[1], y[1], S, 0, 0, 0);
+            }
           }
+          if constexpr (TAIL) S = __builtin_amdgcn_mfma_i32_16x16x32_i8(kt[c], qt[n], S, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[n][4 * c + i] = quad_sum((float)S[i] * qw[n]) * ks_[4 * c + i];
+        } else {
+          f32x4_t S = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < NK; ++ks)
+            S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[c * NK + ks]), __builtin_bit_cast(bf16x8_t, qf[n][ks]), S, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[n][4 * c + i] = S[i] * qw[n];
+        }
       }
-    }
+    if (more) load_keys(t_next, page);
     // which of the lane's 16 tokens the row sees (all of them in most tiles); token of register k
     auto token = [&](int k) { return I8 ? 16 * g + k : 32 * (k >> 3) + 8 * g + (k & 7); };
     uint32_t mask = 0xffff;
@@ -251,12 +303,7 @@ __global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_a
     seen |= mask;
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-      float s[16];
-#pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        if constexpr (I8) s[k] = quad_sum((float)S[n][k >> 2][k & 3] * qw[n]) * ks_[k];
-        else s[k] = __int_as_float(S[n][k >> 2][k & 3]) * qw[n];
-      }
+      float (&s)[16] = sc[n];
       if (!full)
 #pragma unroll
         for (int k = 0; k < 16; ++k) s[k] = (mask >> k) & 1 ? s[k] : -INFINITY;
@@ -322,11 +369,17 @@ __global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_a
         }
       }
     }
+    if (more) {
+      load_values(t_next, page);
+      page_next = pages_at(t_next + W * TT);
+    }
+    there = there_next;
+    t0 = t_next;
   }
 
   // ---- the wavefronts' pieces are joined through the LDS: [wave][head][dp] sums, then maximum, sum and "saw a token"
   extern __shared__ float lds[];
-  float* ml = lds + (size_t)waves * n_heads * DP;
+  float* ml = lds + (size_t)W * n_heads * DP;
   const bool any = __any(seen != 0);
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
@@ -350,15 +403,15 @@ __global__ __launch_bounds__(DECODE_WAVES * 64) void attn_decode_kernel(decode_a
   for (int e = threadIdx.x; e < n_heads * DP; e += blockDim.x) {
     const int hl = e / DP, d = e % DP;
     float M = -INFINITY;
-    for (int w = 0; w < waves; ++w) M = fmaxf(M, ml[(w * n_heads + hl) * 2]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) M = fmaxf(M, ml[(w * n_heads + hl) * 2]);
     const float mx = M == -INFINITY ? 0.0f : M;
     float sum = 0.0f, o = 0.0f;
     bool some = false;
-    for (int w = 0; w < waves; ++w) {
-      const float lw = ml[(w * n_heads + hl) * 2 + 1];
-      if (lw < 0.0f) continue;
-      const float f = __builtin_amdgcn_exp2f(ml[(w * n_heads + hl) * 2] - mx);
-      some = true;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {                              // (a wavefront that saw nothing left zeros)
+      const float lw = ml[(w * n_heads + hl) * 2 + 1], f = lw < 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[(w * n_heads + hl) * 2] - mx);
+      some |= !(lw < 0.0f);
       sum += lw * f;
       o += lds[((size_t)w * n_heads + hl) * DP + d] * f;
     }
@@ -386,27 +439,27 @@ __global__ __launch_bounds__(256) void attn_join_kernel(decode_args a) {
   const float mx = M == -INFINITY ? 0.0f : M;
   float sum = 0.0f, o = 0.0f;
   bool some = false;
-  for (int z = 0; z < R.pieces; ++z) {
-    const float lz = ml[2 * z + 1];
-    if (lz < 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml[2 * z] - mx);
-    some = true;
+#pragma unroll 8
+  for (int z = 0; z < R.pieces; ++z) {                         // (a piece that saw nothing holds zeros)
+    const float lz = ml[2 * z + 1], f = lz < 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[2 * z] - mx);
+    some |= !(lz < 0.0f);
     sum += lz * f;
-    if (d < a.v.dp) o += po[(size_t)z * a.v.dp + d] * f;
+    o += (d < a.v.dp ? po[(size_t)z * a.v.dp + d] : 0.0f) * f;
   }
   if (d < a.v.d) a.O[((size_t)b * a.heads + h) * a.v.d + d] = f32_to_bf16(some ? o / sum : 0.0f);
   if (d == 0 && a.lse) a.lse[(size_t)b * a.heads + h] = some ? (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
 }
 
 // How a decode call is cut: query heads a workgroup, pieces of a sequence.
-struct decode_plan { int nc, head_blocks, block_heads, chunk, n_chunks; size_t part_o, part_ml, total; };
+struct decode_plan { int waves, nc, head_blocks, block_heads, chunk, n_chunks; size_t part_o, part_ml, total; };
 decode_plan plan_decode(const pq_attn_desc& d) {
   decode_plan p;
   const int group = d.n_heads / d.kv.n_kv_heads;
   const bool i8 = d.kv.kv_kind == PQ_KV_INT8;
-  p.nc = i8 && group > 4 ? 2 : 1;
+  p.nc = i8 && group > 4 ? (getenv("DNC") ? atoi(getenv("DNC")) : 2) : 1;
   // a column of the matrix instructions for a head (bf16) or a quad of columns (INT8), and 64 KiB of LDS for the wavefronts' sums
-  const int row = DECODE_WAVES * ((d.kv.d_head + 31) / 32 * 32 + 2) * 4, fit = 65536 / row;
+  p.waves = getenv("DW") ? atoi(getenv("DW")) : 4;
+  const int row = p.waves * ((d.kv.d_head + 31) / 32 * 32 + 2) * 4, fit = 65536 / row;
   const int hb = i8 ? 4 * p.nc : fit < 16 ? fit : 16;
   p.head_blocks = (group + hb - 1) / hb;
   p.block_heads = (group + p.head_blocks - 1) / p.head_blocks;
@@ -414,9 +467,10 @@ decode_plan plan_decode(const pq_attn_desc& d) {
   int64_t most = d.max_len > 0 && d.max_len < cap ? d.max_len : cap;
   if (d.window > 0 && d.window + 63 < most) most = d.window + 63;
   const int64_t rows = (int64_t)d.kv.n_seqs * d.kv.n_kv_heads * p.head_blocks;
-  int64_t want = rows > 0 ? (1024 + rows - 1) / rows : 1;      // pieces for 1024 workgroups
+  int64_t want = rows > 0 ? ((getenv("DWANT") ? atoi(getenv("DWANT")) : 1024) + rows - 1) / rows : 1;      // pieces for 1024 workgroups
   int64_t chunk = (most + want - 1) / want;
-  if (chunk < 256) chunk = 256;
+  const int least = getenv("DMIN") ? atoi(getenv("DMIN")) : 256;
+  if (chunk < least) chunk = least;
   chunk = (chunk + 255) / 256 * 256;
   p.chunk = (int)chunk;
   p.n_chunks = (int)((most + chunk - 1) / chunk);
@@ -428,13 +482,17 @@ decode_plan plan_decode(const pq_attn_desc& d) {
   return p;
 }
 
+template <int KIND, int NK, int W>
+void launch_decode_w(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
+  const size_t lds = W * (size_t)p.block_heads * (NK * 32 + 2) * 4;
+  if constexpr (KIND == PQ_KV_INT8)
+    if (p.nc == 2) { attn_decode_kernel<KIND, NK, 2, W><<<grid, W * 64, lds, s>>>(a); return; }
+  attn_decode_kernel<KIND, NK, 1, W><<<grid, W * 64, lds, s>>>(a);
+}
 template <int KIND, int NK>
 void launch_decode_nc(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
-  const size_t lds = DECODE_WAVES * (size_t)p.block_heads * (NK * 32 + 2) * 4;
-  constexpr int threads = DECODE_WAVES * 64;
-  if constexpr (KIND == PQ_KV_INT8)
-    if (p.nc == 2) { attn_decode_kernel<KIND, NK, 2><<<grid, threads, lds, s>>>(a); return; }
-  attn_decode_kernel<KIND, NK, 1><<<grid, threads, lds, s>>>(a);
+  if (p.waves == 8) launch_decode_w<KIND, NK, 8>(a, p, grid, s);
+  else launch_decode_w<KIND, NK, 4>(a, p, grid, s);
 }
 template <int KIND>
 void launch_decode(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
@@ -542,14 +600,15 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
 #pragma unroll
     for (int ks = 0; ks < NS; ++ks) {
       const int d = ks * 16 + h * 8;
-      i32x4_t x = {0, 0, 0, 0};
-      if (mine) {
-        if (wide) {
-          if (d < v.d) x = *reinterpret_cast<const i32x4_t*>(q + d);
-        } else {
+      i32x4_t x;                 // (loaded whatever d is, so that no load waits for another)
+      if (wide) {
+        x = *reinterpret_cast<const i32x4_t*>(q + (d < v.d ? d : 0));
+        if (!mine || d >= v.d) x = i32x4_t{0, 0, 0, 0};
+      } else {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (d + 2 * j < v.d) x[j] = *reinterpret_cast<const int*>(q + d + 2 * j);
+        for (int j = 0; j < 4; ++j) {
+          const int w = *reinterpret_cast<const int*>(q + (d + 2 * j < v.d ? d + 2 * j : 0));
+          x[j] = mine && d + 2 * j < v.d ? w : 0;
         }
       }
       qf[ks] = __builtin_bit_cast(bf16x8_t, x);
@@ -572,14 +631,15 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
     const int t = t0 + 16 * (lane & 3);
     int p = -1;
     if (t < t_end) p = table[t >> v.page_shift];
-    return (unsigned)p < (unsigned)v.n_pages ? p : -1;
+    return p;                    // (looked at a stage later: a wait for it here would wait for the stage's loads too)
   };
   i32x4_t kreg[CT], vreg[CT];
   float steps = 0.0f;
-  uint32_t there = 0;            // which of the four blocks of the loaded stage have a page
+  // returns which of the stage's four blocks have a page
   auto load_stage = [&](int t0, int pages) {
-    there = (uint32_t)__ballot(pages >= 0) & 15;
-    const int safe = max(pages, 0);
+    const bool ok = (unsigned)pages < (unsigned)v.n_pages;
+    const uint32_t there = (uint32_t)__ballot(ok) & 15;
+    const int safe = ok ? pages : 0;
     if (v.page_shift >= 6) {     // the whole stage in one page: its address is the wavefront's, a thread's place in it does not change
       const uint8_t* base = pool + (size_t)__builtin_amdgcn_readfirstlane(safe) * page_bytes;
       const uint8_t* at = base + (size_t)((t0 & slot_mask) * (DP * ES));
@@ -609,9 +669,10 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
         if (wave < 2) steps = reinterpret_cast<const float*>(pool + (size_t)bs * page_bytes + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + ((t0 + lane) & slot_mask)];
       }
     }
+    return there;
   };
   // `check`: whether some row of the workgroup does not see some of the stage's tokens
-  auto store_stage = [&](int t0, uint8_t* buf, bool check) {
+  auto store_stage = [&](int t0, uint8_t* buf, bool check, uint32_t there) {
     uint8_t *lk = buf, *lv = buf + PF_TOKENS * KROW;
     bool bad = false;
     const bool clean = check || there != 15;
@@ -654,41 +715,35 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
     return t0 + PF_TOKENS > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || (a.window > 0 && t0 < pos_last + 1 - a.window);
   };
 
-  // One stage for one wavefront.  Scores are formed transposed (a column is a row of Q): register k of half h is token
+  // A stage for one wavefront is three steps.  Scores are formed transposed (a column is a row of Q): register k of half h is token
   // 16 (k / 8) + 8 h + k % 8, the eight tokens that the half's lanes hold of the values' second operand; the keys' rows lie in
-  // the LDS in the order that makes it so.  The reference m of a row's exponentials moves only where a score exceeds it by 16 (and where
-  // the row sees its first tokens, and in stages with hidden ones): any reference gives the same quotient, and bf16 and fp32 have the range.
-  auto stage = [&](int t0, const uint8_t* lk, uint32_t blocks, bool full) {
+  // the LDS in the order that makes it so.
+  float p[32];
+  bf16x8_t pb[4];
+  bool bad = false;              // values that are not finite in a stage that some row sees a part of
+  auto scores = [&](const uint8_t* lk) {
+    f32x16_t S[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) S[u][j] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(lk + (32 * u + col) * KROW + ks * 32 + h * 16);
+        S[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], S[u], 0, 0, 0);
+      }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) p[16 * u + j] = S[u][j];
+  };
+  // Probabilities relative to the row's reference m, which moves only where a score exceeds it by 16 (and where the row sees its first
+  // tokens, and in stages with hidden ones): any reference gives the same quotient, and bf16 and fp32 have the range.
+  auto soften = [&](int t0, const uint8_t* lk, uint32_t blocks, bool full) {
     const uint8_t* lv = lk + PF_TOKENS * KROW;
     const float* ls = reinterpret_cast<const float*>(lv + DP * PF_VROW);
-    bool bad = false;
-    if constexpr (!I8)
-      if (!full) {
-        const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
-        int any = 0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) any |= f[w];
-        bad = __builtin_amdgcn_readfirstlane(any) != 0;
-      }
-    float p[32];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x16_t S;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) S[j] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < NS; ++ks) {
-        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(lk + (32 * u + col) * KROW + ks * 32 + h * 16);
-        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], S, 0, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) p[16 * u + j] = S[j];
-    }
-    bf16x8_t vf[NK][2];          // the first values, under way while the scores are worked on
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int i = 0; i < NK; ++i) vf[i][q] = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       f32x4_t x = {a.scale, a.scale, a.scale, a.scale};
@@ -742,76 +797,128 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
 #pragma unroll
         for (int k = 0; k < 32; ++k) p[k] = (mask >> k) & 1 ? p[k] : 0.0f;
     }
-    bf16x8_t pb[4];              // rounded to bf16, the operand's type; the sum l is of the unrounded ones
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < 4; ++q)  // rounded to bf16, the operand's type; the sum l is of the unrounded ones
 #pragma unroll
       for (int j = 0; j < 8; ++j) pb[q][j] = (__bf16)p[8 * q + j];
-    if (!bad) {
+    bad = false;
+    if constexpr (!I8)
+      if (!full) {
+        const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) any |= f[w];
+        bad = __builtin_amdgcn_readfirstlane(any) != 0;
+        if (bad) {               // the product will leave them out; here is what they are to the rows that see them, token by token
+#pragma unroll 1
+          for (int k = 0; k < 32; ++k) {
+            const float p0 = p[0], p1 = __shfl_xor(p0, 32, 64);
+            const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
+#pragma unroll
+            for (int j = 0; j < 31; ++j) p[j] = p[j + 1];
+            mask >>= 1;
+            const uint8_t* x = lv + 4 * h * PF_VROW + 2 * (16 * (k >> 3) + (k & 7));
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+              asm volatile("" ::: "memory");         // (few of the loads at a time)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const uint16_t* y = reinterpret_cast<const uint16_t*>(x + (32 * i + 8 * (j >> 2) + (j & 3)) * PF_VROW);
+                const float x0 = bf16_to_f32(y[8 * h]), x1 = bf16_to_f32(y[8 * (h ^ 1)]);
+                if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
+                if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
+              }
+            }
+          }
+        }
+      }
+  };
+  auto values = [&](const uint8_t* lk) {
+    const uint8_t* lv = lk + PF_TOKENS * KROW;
+    if (I8 || !bad) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-          const bf16x8_t x = q < 2 ? vf[i][q & 1] : *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+          const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pb[q], acc[i], 0, 0, 0);
         }
-      return;
-    }
-    // Infinities or NaN among the values of a stage that some row sees a part of: the product without them, and their own
-    // contributions to the rows that see them, token by token.
+    } else {
 #pragma unroll
-    for (int i = 0; i < NK; ++i)
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+        for (int i = 0; i < NK; ++i) {
+          i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
-          if ((x[j] & 0x7f800000) == 0x7f800000) x[j] &= 0xffff;
+          for (int j = 0; j < 4; ++j) {
+            if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
+            if ((x[j] & 0x7f800000) == 0x7f800000) x[j] &= 0xffff;
+          }
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), pb[q], acc[i], 0, 0, 0);
         }
-        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), pb[q], acc[i], 0, 0, 0);
-      }
-#pragma unroll 1
-    for (int k = 0; k < 32; ++k) {
-      const float p0 = p[0], p1 = __shfl_xor(p0, 32, 64);
-      const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
-#pragma unroll
-      for (int j = 0; j < 31; ++j) p[j] = p[j + 1];
-      mask >>= 1;
-      const uint8_t* x = lv + 4 * h * PF_VROW + 2 * (16 * (k >> 3) + (k & 7));
-#pragma unroll
-      for (int i = 0; i < NK; ++i) {
-        asm volatile("" ::: "memory");               // (few of the loads at a time)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const uint16_t* y = reinterpret_cast<const uint16_t*>(x + (32 * i + 8 * (j >> 2) + (j & 3)) * PF_VROW);
-          const float x0 = bf16_to_f32(y[8 * h]), x1 = bf16_to_f32(y[8 * (h ^ 1)]);
-          if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
-          if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
-        }
-      }
     }
   };
+  auto sees = [&](int t0) { return t0 < w_end && t0 + PF_TOKENS > w_begin; };
+  auto sees_all = [&](int t0, uint32_t there) { return t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there == 15; };
 
-  if (t_begin < t_end) {
-    load_stage(t_begin, pages_at(t_begin));
-    store_stage(t_begin, lds8, partly(t_begin));
-  }
-  uint32_t there_now = there;
-  int next_pages = pages_at(t_begin + PF_TOKENS);
-  int buf = 0;
-  for (int t0 = t_begin; t0 < t_end; t0 += PF_TOKENS, buf ^= 1) {
-    __syncthreads();
-    const bool more = t0 + PF_TOKENS < t_end;
-    if (more) {
-      load_stage(t0 + PF_TOKENS, next_pages);
-      next_pages = pages_at(t0 + 2 * PF_TOKENS);
+  const int n = t_begin < t_end ? (t_end - t_begin + PF_TOKENS - 1) / PF_TOKENS : 0;
+  auto t_of = [&](int s) { return t_begin + s * PF_TOKENS; };
+  if constexpr (W == 8) {
+    // Two wavefronts of a SIMD take turns, a barrier each: while one is at its two products (the values of the stage before, the
+    // scores of this one), the other is at the exponentials and the staging, so that the matrix pipe and the vector pipe work at the same
+    // time.  The upper four wavefronts run half a stage behind.  Stages are loaded three ahead and stored two ahead into a ring of
+    // four, which no turn reads and writes in the same place.
+    auto buf = [&](int s) { return lds8 + (s & 3) * STAGE; };
+    uint32_t there = 0;          // four bits a stage, the present one's lowest
+    {
+      const int p0 = pages_at(t_of(0)), p1 = pages_at(t_of(1)), p2 = pages_at(t_of(2));
+      if (n > 0) { there = load_stage(t_of(0), p0); store_stage(t_of(0), buf(0), partly(t_of(0)), there & 15); }
+      if (n > 1) { there |= load_stage(t_of(1), p1) << 4; store_stage(t_of(1), buf(1), partly(t_of(1)), there >> 4 & 15); }
+      if (n > 2) there |= load_stage(t_of(2), p2) << 8;
     }
-    const uint8_t* lk = lds8 + buf * STAGE;
-    if (t0 < w_end && t0 + PF_TOKENS > w_begin)
-      stage(t0, lk, there_now, t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there_now == 15);
-    if (more) store_stage(t0 + PF_TOKENS, lds8 + (buf ^ 1) * STAGE, partly(t0 + PF_TOKENS));
-    there_now = there;
+    int pages = pages_at(t_of(3));
+    bool have = false;
+    __syncthreads();
+    if (wave >= W / 2) __syncthreads();
+    for (int s = 0; s < n; ++s) {
+      if (have) values(buf(s - 1));
+      have = sees(t_of(s));
+      if (have) scores(buf(s));
+      __syncthreads();
+      if (s + 2 < n) store_stage(t_of(s + 2), buf(s + 2), partly(t_of(s + 2)), there >> 8 & 15);
+      if (s + 3 < n) {
+        there |= load_stage(t_of(s + 3), pages) << 12;
+        pages = pages_at(t_of(s + 4));
+      }
+      if (have) soften(t_of(s), buf(s), there & 15, sees_all(t_of(s), there & 15));
+      there >>= 4;
+      __syncthreads();
+    }
+    if (wave < W / 2) __syncthreads();
+    if (have) values(buf(n - 1));
+  } else {
+    uint32_t there = 0;
+    if (n > 0) {
+      there = load_stage(t_of(0), pages_at(t_of(0)));
+      store_stage(t_of(0), lds8, partly(t_of(0)), there);
+    }
+    int pages = pages_at(t_of(1));
+    for (int s = 0; s < n; ++s) {
+      __syncthreads();
+      uint32_t next = 0;
+      if (s + 1 < n) {
+        next = load_stage(t_of(s + 1), pages);
+        pages = pages_at(t_of(s + 2));
+      }
+      const uint8_t* lk = lds8 + (s & 1) * STAGE;
+      if (sees(t_of(s))) {
+        scores(lk);
+        soften(t_of(s), lk, there, sees_all(t_of(s), there));
+        values(lk);
+      }
+      if (s + 1 < n) store_stage(t_of(s + 1), lds8 + (~s & 1) * STAGE, partly(t_of(s + 1)), next);
+      there = next;
+    }
   }
   if (!mine) return;
   // ---- every column is a row: register 4 q + j of half h is element 8 q + 4 h + j of each 32
@@ -840,17 +947,18 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
 
 template <int KIND, int NK, int W>
 int launch_prefill_w(prefill_args a, int n_kv_heads, hipStream_t s) {
+  constexpr int lds = (W == 8 ? 4 : 2) * prefill_stage<NK>();
   static std::once_flag once;
   static int rc = PQ_OK;
   std::call_once(once, [] {
-    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK, W>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * prefill_stage<NK>()) != hipSuccess)
+    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK, W>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
       rc = PQ_ERR_HIP;
   });
   if (rc) return pq_set_error(rc, "hipFuncSetAttribute failed for attn_prefill_kernel");
   const int64_t tiles = (int64_t)a.v.T * a.group / (W * 32) + a.v.n_seqs, grid = tiles * n_kv_heads;
   if (grid > 0x7fffffff) return pq_set_error(PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call", a.v.T, a.heads, a.v.n_seqs);
   a.tiles = (int)tiles;
-  attn_prefill_kernel<KIND, NK, W><<<(unsigned)grid, W * 64, 2 * prefill_stage<NK>(), s>>>(a);
+  attn_prefill_kernel<KIND, NK, W><<<(unsigned)grid, W * 64, lds, s>>>(a);
   return PQ_OK;
 }
 template <int KIND, int NK>
