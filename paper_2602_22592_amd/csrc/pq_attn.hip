@@ -64,7 +64,7 @@ __device__ __forceinline__ decode_range decode_seq(const decode_args& a, int b) 
   return r;
 }
 
-template <int KIND, int NK, int NC, int W>
+template <int KIND, int NK, int W>
 __global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
   constexpr bool I8 = KIND == PQ_KV_INT8;
   constexpr int DP = NK * 32, ND = DP / 16;
@@ -93,16 +93,14 @@ __global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
   // the rows of this workgroup's heads, as they lie in memory: all that does not wait for the length is under way before it is there
   const int n_heads = min(a.block_heads, a.group - hb * a.block_heads);
   const int first_head = kvh * a.group + hb * a.block_heads;
-  uint32_t qraw[NC][QW];
+  const int hl = I8 ? col >> 2 : col;                          // this column's head
+  const bool mine = hl < n_heads;
+  const uint16_t* q = a.Q + b * a.qs + (size_t)(first_head + (mine ? hl : 0)) * v.d;
+  uint32_t qraw[QW];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int hl = I8 ? c * 4 + (col >> 2) : c * 16 + col;
-    const uint16_t* q = a.Q + b * a.qs + (size_t)(first_head + (hl < n_heads ? hl : 0)) * v.d;
-#pragma unroll
-    for (int j = 0; j < QW; ++j) {
-      const int d = q_at(j);
-      qraw[c][j] = *reinterpret_cast<const uint32_t*>(q + (d < v.d ? d : 0));
-    }
+  for (int j = 0; j < QW; ++j) {
+    const int d = q_at(j);
+    qraw[j] = *reinterpret_cast<const uint32_t*>(q + (d < v.d ? d : 0));
   }
   const decode_range R = decode_seq(a, b);
   if (z >= R.pieces) return;
@@ -180,64 +178,55 @@ __global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
   }
 
   // ---- the queries as the matrix instructions' second operand: column = head (bf16) or head and digit (INT8)
-  i32x4_t qf[NC][KS > 0 ? KS : 1];
-  long qt[NC];
-  float qw[NC];                                               // what one unit of a score's integer stands for, for this column's digit
+  i32x4_t qf[KS > 0 ? KS : 1];
+  long qt;
+  float qw;                                               // what one unit of a score's integer stands for, for this column's digit
   const int digit = lane & 3;
   const float digit_w = digit == 0 ? 1.0f : digit == 1 ? 256.0f : digit == 2 ? 65536.0f : 0.0f;
+  if constexpr (I8) {
+    // q in 23 bits relative to the power of two above its largest element, in three digits of base 256
+    float x[NK * 8];
+    uint32_t top = 0;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int hl = I8 ? c * 4 + (col >> 2) : c * 16 + col;
-    const bool mine = hl < n_heads;
-    if constexpr (I8) {
-      // q in 23 bits relative to the power of two above its largest element, in three digits of base 256
-      float x[NK * 8];
-      uint32_t top = 0;
-#pragma unroll
-      for (int j = 0; j < QW; ++j) {
-        const uint32_t w = mine && q_at(j) < v.d ? qraw[c][j] : 0;
-        x[2 * j] = __uint_as_float(w << 16);
-        x[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
-      }
-#pragma unroll
-      for (int j = 0; j < NK * 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-      top = groups_max_u(top);
-      const bool bad = top >= 0x7f800000u;
-      const int eb = max((int)(top >> 23), 27);                // |x| < 2^(eb - 126)
-      const float fac = bad ? 0.0f : __uint_as_float((uint32_t)(275 - eb) << 23);
-      qw[c] = bad ? __uint_as_float(0x7fc00000u) : digit_w * a.scale * __uint_as_float((uint32_t)(eb - 21) << 23);
-      auto digits4 = [&](int at) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int n = bad ? 0 : (int)rintf(x[at + j] * fac);
-          w |= ((((uint32_t)(n + 0x808080) >> (8 * digit)) & 0xff) ^ 0x80) << (8 * j);
-        }
-        return digit == 3 ? 0u : w;
-      };
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) qf[c][ks][j] = (int)digits4(ks * 16 + 4 * j);
-      if constexpr (TAIL) qt[c] = (long)(((uint64_t)digits4(KS * 16 + 4) << 32) | digits4(KS * 16));
-    } else {
-      qw[c] = a.scale;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) qf[c][ks][j] = mine && q_at(4 * ks + j) < v.d ? (int)qraw[c][4 * ks + j] : 0;
+    for (int j = 0; j < QW; ++j) {
+      const uint32_t w = mine && q_at(j) < v.d ? qraw[j] : 0;
+      x[2 * j] = __uint_as_float(w << 16);
+      x[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
     }
+#pragma unroll
+    for (int j = 0; j < NK * 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+    top = groups_max_u(top);
+    const bool bad = top >= 0x7f800000u;
+    const int eb = max((int)(top >> 23), 27);                // |x| < 2^(eb - 126)
+    const float fac = bad ? 0.0f : __uint_as_float((uint32_t)(275 - eb) << 23);
+    qw = bad ? __uint_as_float(0x7fc00000u) : digit_w * a.scale * __uint_as_float((uint32_t)(eb - 21) << 23);
+    auto digits4 = [&](int at) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int n = bad ? 0 : (int)rintf(x[at + j] * fac);
+        w |= ((((uint32_t)(n + 0x808080) >> (8 * digit)) & 0xff) ^ 0x80) << (8 * j);
+      }
+      return digit == 3 ? 0u : w;
+    };
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) qf[ks][j] = (int)digits4(ks * 16 + 4 * j);
+    if constexpr (TAIL) qt = (long)(((uint64_t)digits4(KS * 16 + 4) << 32) | digits4(KS * 16));
+  } else {
+    qw = a.scale;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) qf[ks][j] = mine && q_at(4 * ks + j) < v.d ? (int)qraw[4 * ks + j] : 0;
   }
 
-  f32x4_t acc[NC][ND];
-  float m[NC], l[NC];
+  f32x4_t acc[ND];
+  float m = -INFINITY, l = 0.0f;
   uint32_t seen = 0;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    m[c] = -INFINITY; l[c] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < ND; ++i) acc[c][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int i = 0; i < ND; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   while (t0 < end) {
     const bool full = t0 >= R.lo && t0 + TT <= end && __all(there);
@@ -246,9 +235,7 @@ __global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
     const int page = there_next ? page_next : 0;
     // Scores: register 4 c + i of group g is the token whose value the group's lanes hold, 16 g + 4 c + i (INT8) or, by 32 tokens,
     // 8 g + k % 8: the keys' rows are read in the order that makes it so.
-    float sc[NC][16];
-#pragma unroll
-    for (int n = 0; n < NC; ++n)
+    float s[16];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         if constexpr (I8) {
@@ -258,23 +245,23 @@ __global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
             // (A sum takes one kind of instruction: a 16x16x32 that added to a 16x16x64's result a few instructions behind it read the
             // result before it was there.  With a half step all of them are 16x16x32, on the halves of a piece.)
             if constexpr (!TAIL) {
-              S = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[c * KS + ks], qf[n][ks], S, 0, 0, 0);
+              S = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[c * KS + ks], qf[ks], S, 0, 0, 0);
             } else {
-              const i64x2_t x = __builtin_bit_cast(i64x2_t, kf[c * KS + ks]), y = __builtin_bit_cast(i64x2_t, qf[n][ks]);
+              const i64x2_t x = __builtin_bit_cast(i64x2_t, kf[c * KS + ks]), y = __builtin_bit_cast(i64x2_t, qf[ks]);
               S = __builtin_amdgcn_mfma_i32_16x16x32_i8(x[0], y[0], S, 0, 0, 0);
               S = __builtin_amdgcn_mfma_i32_16x16x32_i8(x[1], y[1], S, 0, 0, 0);
             }
           }
-          if constexpr (TAIL) S = __builtin_amdgcn_mfma_i32_16x16x32_i8(kt[c], qt[n], S, 0, 0, 0);
+          if constexpr (TAIL) S = __builtin_amdgcn_mfma_i32_16x16x32_i8(kt[c], qt, S, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[n][4 * c + i] = quad_sum((float)S[i] * qw[n]) * ks_[4 * c + i];
+          for (int i = 0; i < 4; ++i) s[4 * c + i] = quad_sum((float)S[i] * qw) * ks_[4 * c + i];
         } else {
           f32x4_t S = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ks = 0; ks < NK; ++ks)
-            S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[c * NK + ks]), __builtin_bit_cast(bf16x8_t, qf[n][ks]), S, 0, 0, 0);
+            S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[c * NK + ks]), __builtin_bit_cast(bf16x8_t, qf[ks]), S, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[n][4 * c + i] = S[i] * qw[n];
+          for (int i = 0; i < 4; ++i) s[4 * c + i] = S[i] * qw;
         }
       }
     if (more) load_keys(t_next, page);
@@ -301,71 +288,67 @@ __global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
       }
     }
     seen |= mask;
+    if (!full)
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      float (&s)[16] = sc[n];
-      if (!full)
+      for (int k = 0; k < 16; ++k) s[k] = (mask >> k) & 1 ? s[k] : -INFINITY;
+    float top = s[0];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) s[k] = (mask >> k) & 1 ? s[k] : -INFINITY;
-      float top = s[0];
+    for (int k = 1; k < 16; ++k) top = fmaxf(top, s[k]);
+    const float mt = fmaxf(m, groups_max(top)), mx = mt == -INFINITY ? 0.0f : mt;
+    const float keep = __builtin_amdgcn_exp2f(m - mx);
+    m = mt;
+    float sum = 0.0f;
 #pragma unroll
-      for (int k = 1; k < 16; ++k) top = fmaxf(top, s[k]);
-      const float mt = fmaxf(m[n], groups_max(top)), mx = mt == -INFINITY ? 0.0f : mt;
-      const float keep = __builtin_amdgcn_exp2f(m[n] - mx);
-      m[n] = mt;
-      float sum = 0.0f;
+    for (int k = 0; k < 16; ++k) {
+      s[k] = __builtin_amdgcn_exp2f(s[k] - mx);
+      sum += s[k];
+    }
+    l = l * keep + sum;
+    if (!__all(keep == 1.0f))
+#pragma unroll
+      for (int i = 0; i < ND; ++i) acc[i] *= keep;
+    if constexpr (I8) {
+      // p times the value's step, in 23 bits relative to the power of two above the tile's largest
+      uint32_t big = 0;
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
-        s[k] = __builtin_amdgcn_exp2f(s[k] - mx);
-        sum += s[k];
+        s[k] = full || ((mask >> k) & 1) ? s[k] * vs_[k] : 0.0f;
+        big = max(big, __float_as_uint(s[k]));
       }
-      l[n] = l[n] * keep + sum;
-      if (!__all(keep == 1.0f))
+      big = groups_max_u(big);
+      const int eb = min(max((int)(big >> 23), 27), 254);
+      const float fac = __uint_as_float((uint32_t)(275 - eb) << 23);
+      const float w = big >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : digit_w * __uint_as_float((uint32_t)(eb - 21) << 23);
+      const uint32_t lo_sel = 0x0c0c0400u + 0x0101u * digit, hi_sel = 0x04000c0cu + 0x01010000u * digit;
+      i32x4_t pf;
 #pragma unroll
-        for (int i = 0; i < ND; ++i) acc[n][i] *= keep;
-      if constexpr (I8) {
-        // p times the value's step, in 23 bits relative to the power of two above the tile's largest
-        uint32_t big = 0;
+      for (int j = 0; j < 4; ++j) {
+        uint32_t u[4];   // the integer in the low bits of 1.5 * 2^23 + x, plus 128 in every digit
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          s[k] = full || ((mask >> k) & 1) ? s[k] * vs_[k] : 0.0f;
-          big = max(big, __float_as_uint(s[k]));
-        }
-        big = groups_max_u(big);
-        const int eb = min(max((int)(big >> 23), 27), 254);
-        const float fac = __uint_as_float((uint32_t)(275 - eb) << 23);
-        const float w = big >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : digit_w * __uint_as_float((uint32_t)(eb - 21) << 23);
-        const uint32_t lo_sel = 0x0c0c0400u + 0x0101u * digit, hi_sel = 0x04000c0cu + 0x01010000u * digit;
-        i32x4_t pf;
+        for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(__builtin_fmaf(s[4 * j + i], fac, 12582912.0f)) + (0x808080u - 0x4B400000u);
+        pf[j] = (int)((__builtin_amdgcn_perm(u[1], u[0], lo_sel) | __builtin_amdgcn_perm(u[3], u[2], hi_sel)) ^ 0x80808080u);
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t u[4];   // the integer in the low bits of 1.5 * 2^23 + x, plus 128 in every digit
+      for (int i = 0; i < ND; ++i) {
+        const i32x4_t o = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[i], pf, i32x4_t{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(__builtin_fmaf(s[4 * j + i], fac, 12582912.0f)) + (0x808080u - 0x4B400000u);
-          pf[j] = (int)((__builtin_amdgcn_perm(u[1], u[0], lo_sel) | __builtin_amdgcn_perm(u[3], u[2], hi_sel)) ^ 0x80808080u);
+        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_fmaf((float)o[j], w, acc[i][j]);
+      }
+    } else {
+      // p as the sum of two bf16 numbers
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8_t hi, lo;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          hi[k] = (__bf16)s[8 * u + k];
+          lo[k] = (__bf16)(s[8 * u + k] - (float)hi[k]);
         }
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
-          const i32x4_t o = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[i], pf, i32x4_t{0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[n][i][j] = __builtin_fmaf((float)o[j], w, acc[n][i][j]);
-        }
-      } else {
-        // p as the sum of two bf16 numbers
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          bf16x8_t hi, lo;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            hi[k] = (__bf16)s[8 * u + k];
-            lo[k] = (__bf16)(s[8 * u + k] - (float)hi[k]);
-          }
-#pragma unroll
-          for (int i = 0; i < ND; ++i) {
-            const bf16x8_t x = __builtin_bit_cast(bf16x8_t, vf[u * ND + i]);
-            acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, lo, acc[n][i], 0, 0, 0);
-            acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, hi, acc[n][i], 0, 0, 0);
-          }
+          const bf16x8_t x = __builtin_bit_cast(bf16x8_t, vf[u * ND + i]);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, lo, acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, hi, acc[i], 0, 0, 0);
         }
       }
     }
@@ -381,22 +364,18 @@ __global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
   extern __shared__ float lds[];
   float* ml = lds + (size_t)W * n_heads * DP;
   const bool any = __any(seen != 0);
+  const float sum = groups_sum(l);
 #pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    const int hl = I8 ? n * 4 + (col >> 2) : n * 16 + col;
-    const float sum = groups_sum(l[n]);
+  for (int i = 0; i < ND; ++i) {
+    f32x4_t x = acc[i];
+    if constexpr (I8)
 #pragma unroll
-    for (int i = 0; i < ND; ++i) {
-      f32x4_t x = acc[n][i];
-      if constexpr (I8)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = quad_sum(x[j]);
-      if (hl < n_heads && (!I8 || digit == 0)) *reinterpret_cast<f32x4_t*>(lds + ((size_t)wave * n_heads + hl) * DP + i * 16 + g * 4) = x;
-    }
-    if (hl < n_heads && g == 0 && (!I8 || digit == 0)) {
-      ml[(wave * n_heads + hl) * 2] = m[n];
-      ml[(wave * n_heads + hl) * 2 + 1] = any ? sum : -1.0f;   // (a sum is never negative)
-    }
+      for (int j = 0; j < 4; ++j) x[j] = quad_sum(x[j]);
+    if (hl < n_heads && (!I8 || digit == 0)) *reinterpret_cast<f32x4_t*>(lds + ((size_t)wave * n_heads + hl) * DP + i * 16 + g * 4) = x;
+  }
+  if (hl < n_heads && g == 0 && (!I8 || digit == 0)) {
+    ml[(wave * n_heads + hl) * 2] = m;
+    ml[(wave * n_heads + hl) * 2 + 1] = any ? sum : -1.0f;   // (a sum is never negative)
   }
   __syncthreads();
   const bool whole = R.pieces == 1;
@@ -451,60 +430,55 @@ __global__ __launch_bounds__(256) void attn_join_kernel(decode_args a) {
 }
 
 // How a decode call is cut: query heads a workgroup, pieces of a sequence.
-struct decode_plan { int waves, nc, head_blocks, block_heads, chunk, n_chunks; size_t part_o, part_ml, total; };
+struct decode_plan { int waves, head_blocks, block_heads, chunk, n_chunks; size_t part_o, part_ml, total; };
 decode_plan plan_decode(const pq_attn_desc& d) {
   decode_plan p;
-  const int group = d.n_heads / d.kv.n_kv_heads;
-  const bool i8 = d.kv.kv_kind == PQ_KV_INT8;
-  p.nc = i8 && group > 4 ? (getenv("DNC") ? atoi(getenv("DNC")) : 2) : 1;
+  const int group = d.n_heads / d.kv.n_kv_heads, dp = (d.kv.d_head + 31) / 32 * 32;
+  // Eight wavefronts where two of them on a SIMD hold a tile each in registers, four beyond (heads of 256, INT8: 150 / 510 us for four sequences
+  // of 32768 tokens, 64/8 heads; heads of 128: 200 / 192 us for four of 131072).
+  p.waves = dp <= 128 ? 8 : 4;
   // a column of the matrix instructions for a head (bf16) or a quad of columns (INT8), and 64 KiB of LDS for the wavefronts' sums
-  p.waves = getenv("DW") ? atoi(getenv("DW")) : 4;
-  const int row = p.waves * ((d.kv.d_head + 31) / 32 * 32 + 2) * 4, fit = 65536 / row;
-  const int hb = i8 ? 4 * p.nc : fit < 16 ? fit : 16;
+  const int fit = 65536 / (p.waves * (dp + 2) * 4), hb = d.kv.kv_kind == PQ_KV_INT8 ? 4 : fit < 16 ? fit : 16;
   p.head_blocks = (group + hb - 1) / hb;
   p.block_heads = (group + p.head_blocks - 1) / p.head_blocks;
   const int64_t cap = (int64_t)d.kv.max_pages * d.kv.page_tokens;
   int64_t most = d.max_len > 0 && d.max_len < cap ? d.max_len : cap;
-  if (d.window > 0 && d.window + 63 < most) most = d.window + 63;
+  if (d.window > 0 && d.window + (int64_t)63 < most) most = d.window + (int64_t)63;
+  // Pieces for 1024 workgroups, four a CU, so that ragged lengths spread; a piece is worth its start and the second launch from 1024 tokens on, or
+  // from 2048 where whole sequences already occupy every CU.  (64 ragged sequences up to 8192 tokens, 8 heads of 128 in bf16: 151 us whole, 131 in
+  // pieces of 4096; eight of 2048, 32 heads of 64 in INT8: 14.8 us whole, 21.4 in halves; one of 517: 9.1 us whole, 11.7 in thirds.)
   const int64_t rows = (int64_t)d.kv.n_seqs * d.kv.n_kv_heads * p.head_blocks;
-  int64_t want = rows > 0 ? ((getenv("DWANT") ? atoi(getenv("DWANT")) : 1024) + rows - 1) / rows : 1;      // pieces for 1024 workgroups
+  const int64_t want = rows > 0 ? (1024 + rows - 1) / rows : 1, least = rows >= 256 ? 2048 : 1024;
   int64_t chunk = (most + want - 1) / want;
-  const int least = getenv("DMIN") ? atoi(getenv("DMIN")) : 256;
   if (chunk < least) chunk = least;
-  chunk = (chunk + 255) / 256 * 256;
+  chunk = (chunk + 511) / 512 * 512;
   p.chunk = (int)chunk;
   p.n_chunks = (int)((most + chunk - 1) / chunk);
   const size_t pieces = p.n_chunks > 1 ? (size_t)d.kv.n_seqs * d.n_heads * p.n_chunks : 0;
   p.part_o = 0;
-  p.part_ml = pq_align_up(pieces * (size_t)((d.kv.d_head + 31) / 32 * 32) * 4, 256);
+  p.part_ml = pq_align_up(pieces * (size_t)dp * 4, 256);
   p.total = p.part_ml + pq_align_up(pieces * 8, 256);
   if (p.total < 256) p.total = 256;
   return p;
 }
 
-template <int KIND, int NK, int W>
-void launch_decode_w(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
-  const size_t lds = W * (size_t)p.block_heads * (NK * 32 + 2) * 4;
-  if constexpr (KIND == PQ_KV_INT8)
-    if (p.nc == 2) { attn_decode_kernel<KIND, NK, 2, W><<<grid, W * 64, lds, s>>>(a); return; }
-  attn_decode_kernel<KIND, NK, 1, W><<<grid, W * 64, lds, s>>>(a);
-}
 template <int KIND, int NK>
-void launch_decode_nc(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
-  if (p.waves == 8) launch_decode_w<KIND, NK, 8>(a, p, grid, s);
-  else launch_decode_w<KIND, NK, 4>(a, p, grid, s);
+void launch_decode_nk(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
+  constexpr int W = NK <= 4 ? 8 : 4;
+  const size_t lds = W * (size_t)p.block_heads * (NK * 32 + 2) * 4;
+  attn_decode_kernel<KIND, NK, W><<<grid, W * 64, lds, s>>>(a);
 }
 template <int KIND>
 void launch_decode(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
   switch (a.v.dp / 32) {
-    case 1: launch_decode_nc<KIND, 1>(a, p, grid, s); break;
-    case 2: launch_decode_nc<KIND, 2>(a, p, grid, s); break;
-    case 3: launch_decode_nc<KIND, 3>(a, p, grid, s); break;
-    case 4: launch_decode_nc<KIND, 4>(a, p, grid, s); break;
-    case 5: launch_decode_nc<KIND, 5>(a, p, grid, s); break;
-    case 6: launch_decode_nc<KIND, 6>(a, p, grid, s); break;
-    case 7: launch_decode_nc<KIND, 7>(a, p, grid, s); break;
-    default: launch_decode_nc<KIND, 8>(a, p, grid, s); break;
+    case 1: launch_decode_nk<KIND, 1>(a, p, grid, s); break;
+    case 2: launch_decode_nk<KIND, 2>(a, p, grid, s); break;
+    case 3: launch_decode_nk<KIND, 3>(a, p, grid, s); break;
+    case 4: launch_decode_nk<KIND, 4>(a, p, grid, s); break;
+    case 5: launch_decode_nk<KIND, 5>(a, p, grid, s); break;
+    case 6: launch_decode_nk<KIND, 6>(a, p, grid, s); break;
+    case 7: launch_decode_nk<KIND, 7>(a, p, grid, s); break;
+    default: launch_decode_nk<KIND, 8>(a, p, grid, s); break;
   }
 }
 
