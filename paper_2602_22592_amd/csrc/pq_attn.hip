@@ -1,8 +1,6 @@
 // Attention over the paged key-value cache: one new token of every sequence (pq_attn_decode) and the rows of prompts (pq_attn_prefill).
 #include <math.h>
 #include <mutex>
-#include <stdlib.h>
-#include <type_traits>
 #include "pq_kv.h"
 
 namespace {
@@ -517,9 +515,28 @@ struct prefill_args {
   float* lse;
 };
 
-constexpr int PF_TOKENS = 64, PF_VROW = 2 * PF_TOKENS + 16;   // tokens of a stage, bytes of a value row in the LDS
+// Tokens of a stage.  16-bit heads beyond 64 take half: their stage on its way through the registers beside 64 scores a row spills (8192 tokens,
+// 32/8 heads of 128: 1.72 ms with 64, 0.73 with 32; heads of 64: 139 us for four prompts of 2048 with 64, 153 with 32).
+template <int KIND, int NK> constexpr int prefill_tokens() { return KIND == PQ_KV_BF16 && NK > 2 ? 32 : 64; }
+// Bytes of a key row and a value row of a stage in the LDS (16 more than they hold: sixteen rows' pieces of 16 bytes lie in different
+// banks), and of the stage with both steps and a flag a wavefront.
 template <int NK> constexpr int prefill_krow() { return NK * 64 + 16; }
-template <int NK> constexpr int prefill_stage() { return PF_TOKENS * prefill_krow<NK>() + NK * 32 * PF_VROW + 2 * PF_TOKENS * 4 + 32; }
+template <int KIND, int NK> constexpr int prefill_vrow() { return 2 * prefill_tokens<KIND, NK>() + 16; }
+template <int KIND, int NK> constexpr int prefill_stage() {
+  return prefill_tokens<KIND, NK>() * (prefill_krow<NK>() + 8) + NK * 32 * prefill_vrow<KIND, NK>() + 16;
+}
+
+// Order of a run of N LDS reads and as many products on them: four reads ahead.
+template <int N>
+__device__ __forceinline__ void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+  for (int i = 0; i < N - 4; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
+}
 
 // Four codes as bf16 (every code has at most eight significant bits: exact).
 __device__ __forceinline__ uint2 codes_bf16(int w) {
@@ -529,12 +546,14 @@ __device__ __forceinline__ uint2 codes_bf16(int w) {
 }
 __device__ __forceinline__ bool has_nonfinite(uint32_t two) { return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u; }
 
-template <int KIND, int NK, int W>
-__global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(prefill_args a) {
+template <int KIND, int NK>
+__global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(prefill_args a) {
   constexpr bool I8 = KIND == PQ_KV_INT8;
-  constexpr int DP = NK * 32, ES = I8 ? 1 : 2, KROW = prefill_krow<NK>(), STAGE = prefill_stage<NK>(), NS = NK * 2;
-  constexpr int THREADS = W * 64, ROWS = W * 32, ROW_PIECES = DP * ES / 16, BLOCK_PIECES = DP * ES;   // pieces of 16 bytes of a key, of 16 tokens' values
-  constexpr int PIECES = PF_TOKENS * ROW_PIECES, CT = (PIECES + THREADS - 1) / THREADS;               // of a stage's keys (or values), and of a thread
+  constexpr int TOK = prefill_tokens<KIND, NK>(), DP = NK * 32, ES = I8 ? 1 : 2, NS = NK * 2;
+  constexpr int KROW = prefill_krow<NK>(), VROW = prefill_vrow<KIND, NK>(), STAGE = prefill_stage<KIND, NK>();
+  constexpr int W = 4, THREADS = W * 64, ROWS = W * 32, U = TOK / 32, NB = TOK / 16, ALL = (1 << NB) - 1;
+  constexpr int ROW_PIECES = DP * ES / 16, BLOCK_PIECES = DP * ES;                      // pieces of 16 bytes of a key, of 16 tokens' values
+  constexpr int PIECES = TOK * ROW_PIECES, CT = (PIECES + THREADS - 1) / THREADS;               // of a stage's keys (or values), and of a thread
   extern __shared__ uint8_t lds8[];
   const kv_view& v = a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5, col = lane & 31;
@@ -553,7 +572,7 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
   auto pos_of = [&](int row) { return r.first + row / a.group; };
   const int rows_here = min(ROWS, all_rows - row0);
   const int pos_first = pos_of(row0), pos_last = pos_of(row0 + rows_here - 1);
-  const int t_begin = (a.window > 0 ? max(0, pos_first + 1 - a.window) : 0) & ~(PF_TOKENS - 1);
+  const int t_begin = (a.window > 0 ? max(0, pos_first + 1 - a.window) : 0) & ~(TOK - 1);
   const int t_end = pos_last < 0 ? 0 : a.causal ? min(pos_last + 1, hi) : hi;
 
   // this lane's row, and what the wavefront's rows see between them
@@ -596,27 +615,34 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
   float m = 0.0f, l = 0.0f;      // reference of the exponentials (log2), their sum over this lane's tokens
   uint32_t seen = 0;             // not zero: the row has seen a token
 
-  // ---- staging: pages of a stage's four blocks of 16 tokens in lanes 0..3 of every wavefront, one stage ahead of the loads
+  // ---- staging: pages of a stage's blocks of 16 tokens in the first lanes of every wavefront, one stage ahead of the loads
   const int slot_mask = (1 << v.page_shift) - 1;
   const int32_t* table = v.table + (size_t)b * v.max_pages;
   const uint8_t* pool = v.cache + (size_t)kvh * v.head_bytes;
   const size_t page_bytes = v.head_bytes * v.n_kv_heads;
   auto pages_at = [&](int t0) {
-    const int t = t0 + 16 * (lane & 3);
+    const int t = t0 + 16 * (lane & (NB - 1));
     int p = -1;
     if (t < t_end) p = table[t >> v.page_shift];
     return p;                    // (looked at a stage later: a wait for it here would wait for the stage's loads too)
   };
   i32x4_t kreg[CT], vreg[CT];
   float steps = 0.0f;
-  // returns which of the stage's four blocks have a page
-  auto load_stage = [&](int t0, int pages) {
+  // Where a stage lies: which of its blocks have a page, and the pages with those that are missing as page 0; where a page holds the
+  // whole stage, its address.
+  struct place { int safe; uint32_t there; const uint8_t* at; };
+  const bool one_page = (1 << v.page_shift) >= TOK;
+  auto place_of = [&](int t0, int pages) {
     const bool ok = (unsigned)pages < (unsigned)v.n_pages;
-    const uint32_t there = (uint32_t)__ballot(ok) & 15;
-    const int safe = ok ? pages : 0;
-    if (v.page_shift >= 6) {     // the whole stage in one page: its address is the wavefront's, a thread's place in it does not change
-      const uint8_t* base = pool + (size_t)__builtin_amdgcn_readfirstlane(safe) * page_bytes;
-      const uint8_t* at = base + (size_t)((t0 & slot_mask) * (DP * ES));
+    place w;
+    w.there = (uint32_t)__ballot(ok) & ALL;
+    w.safe = ok ? pages : 0;
+    w.at = pool + (size_t)__builtin_amdgcn_readfirstlane(w.safe) * page_bytes;
+    return w;
+  };
+  auto load_stage = [&](int t0, const place& w) {
+    if (one_page) {              // a thread's place in the stage does not change
+      const uint8_t* at = w.at + (size_t)((t0 & slot_mask) * (DP * ES));
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         const int i = threadIdx.x + THREADS * c;
@@ -626,30 +652,29 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
         }
       }
       if constexpr (I8)
-        if (wave < 2) steps = reinterpret_cast<const float*>(base + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + (t0 & slot_mask) + lane];
+        if (wave < 2) steps = reinterpret_cast<const float*>(w.at + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + (t0 & slot_mask) + (lane & (TOK - 1))];
     } else {
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         const int i = threadIdx.x + THREADS * c;
-        const int t = min(i / ROW_PIECES, PF_TOKENS - 1), vb = min(i / BLOCK_PIECES, 3);           // keys token by token, values block by block
-        const int bk = __shfl(safe, t >> 4, 64), bv = __shfl(safe, vb, 64);
+        const int t = min(i / ROW_PIECES, TOK - 1), vb = min(i / BLOCK_PIECES, NB - 1);           // keys token by token, values block by block
+        const int bk = __shfl(w.safe, t >> 4, 64), bv = __shfl(w.safe, vb, 64);
         if (PIECES % THREADS == 0 || i < PIECES) {
           kreg[c] = *reinterpret_cast<const i32x4_t*>(pool + (size_t)bk * page_bytes + ((t0 + t) & slot_mask) * (DP * ES) + (i % ROW_PIECES) * 16);
           vreg[c] = *reinterpret_cast<const i32x4_t*>(pool + (size_t)bv * page_bytes + v.part_bytes + ((t0 + 16 * vb) & slot_mask) * (DP * ES) + (i % BLOCK_PIECES) * 16);
         }
       }
       if constexpr (I8) {
-        const int bs = __shfl(safe, lane >> 4, 64);
-        if (wave < 2) steps = reinterpret_cast<const float*>(pool + (size_t)bs * page_bytes + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + ((t0 + lane) & slot_mask)];
+        const int bs = __shfl(w.safe, (lane & (TOK - 1)) >> 4, 64);
+        if (wave < 2) steps = reinterpret_cast<const float*>(pool + (size_t)bs * page_bytes + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + ((t0 + (lane & (TOK - 1))) & slot_mask)];
       }
     }
-    return there;
   };
   // `check`: whether some row of the workgroup does not see some of the stage's tokens
   auto store_stage = [&](int t0, uint8_t* buf, bool check, uint32_t there) {
-    uint8_t *lk = buf, *lv = buf + PF_TOKENS * KROW;
+    uint8_t *lk = buf, *lv = buf + TOK * KROW;
     bool bad = false;
-    const bool clean = check || there != 15;
+    const bool clean = check || there != ALL;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const int i = threadIdx.x + THREADS * c;
@@ -661,8 +686,8 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
         *reinterpret_cast<uint4*>(lk + rk * KROW + piece * 32) = make_uint4(x0.x, x0.y, x1.x, x1.y);
         *reinterpret_cast<uint4*>(lk + rk * KROW + piece * 32 + 16) = make_uint4(x2.x, x2.y, x3.x, x3.y);
         const uint2 y0 = codes_bf16(vreg[c][0]), y1 = codes_bf16(vreg[c][1]), y2 = codes_bf16(vreg[c][2]), y3 = codes_bf16(vreg[c][3]);
-        *reinterpret_cast<uint4*>(lv + vpiece * PF_VROW + vb * 32) = make_uint4(y0.x, y0.y, y1.x, y1.y);
-        *reinterpret_cast<uint4*>(lv + vpiece * PF_VROW + vb * 32 + 16) = make_uint4(y2.x, y2.y, y3.x, y3.y);
+        *reinterpret_cast<uint4*>(lv + vpiece * VROW + vb * 32) = make_uint4(y0.x, y0.y, y1.x, y1.y);
+        *reinterpret_cast<uint4*>(lv + vpiece * VROW + vb * 32 + 16) = make_uint4(y2.x, y2.y, y3.x, y3.y);
       } else {
         *reinterpret_cast<i32x4_t*>(lk + rk * KROW + piece * 16) = kreg[c];
         i32x4_t x = vreg[c];
@@ -674,79 +699,85 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
             bad |= has_nonfinite((uint32_t)x[j]);
           }
         }
-        *reinterpret_cast<i32x4_t*>(lv + (vpiece >> 1) * PF_VROW + vb * 32 + (vpiece & 1) * 16) = x;
+        *reinterpret_cast<i32x4_t*>(lv + (vpiece >> 1) * VROW + vb * 32 + (vpiece & 1) * 16) = x;
       }
     }
-    float* ls = reinterpret_cast<float*>(lv + DP * PF_VROW);
+    float* ls = reinterpret_cast<float*>(lv + DP * VROW);
     if constexpr (I8) {
-      if (wave < 2) ls[threadIdx.x] = wave == 0 ? steps * a.scale : steps;
+      if (wave < 2 && lane < TOK) ls[wave * TOK + lane] = wave == 0 ? steps * a.scale : steps;
     } else if (clean) {
       const bool any = __any(bad);
-      if (lane == 0) reinterpret_cast<int*>(ls + 2 * PF_TOKENS)[wave] = any;
+      if (lane == 0) reinterpret_cast<int*>(ls + 2 * TOK)[wave] = any;
     }
   };
   auto partly = [&](int t0) {    // some row of the workgroup does not see all of the stage
-    return t0 + PF_TOKENS > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || (a.window > 0 && t0 < pos_last + 1 - a.window);
+    return t0 + TOK > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || (a.window > 0 && t0 < pos_last + 1 - a.window);
   };
 
   // A stage for one wavefront is three steps.  Scores are formed transposed (a column is a row of Q): register k of half h is token
   // 16 (k / 8) + 8 h + k % 8, the eight tokens that the half's lanes hold of the values' second operand; the keys' rows lie in
   // the LDS in the order that makes it so.
-  float p[32];
-  bf16x8_t pb[4];
+  constexpr int P = 16 * U;      // tokens of a lane in a stage
+  float p[P];
+  bf16x8_t pb[NB];
   bool bad = false;              // values that are not finite in a stage that some row sees a part of
-  auto scores = [&](const uint8_t* lk) {
-    f32x16_t S[2];
+  uint32_t reach[NK];            // the elements that +infinity (low half) and -infinity reach there; NaN is both
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+  for (int i = 0; i < NK; ++i) reach[i] = 0;
+  auto scores = [&](const uint8_t* lk) {
+    f32x16_t S[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int j = 0; j < 16; ++j) S[u][j] = 0.0f;
 #pragma unroll
     for (int ks = 0; ks < NS; ++ks)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < U; ++u) {
         const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(lk + (32 * u + col) * KROW + ks * 32 + h * 16);
         S[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], S[u], 0, 0, 0);
       }
+
+    reads_ahead<NS * U>();
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int j = 0; j < 16; ++j) p[16 * u + j] = S[u][j];
   };
   // Probabilities relative to the row's reference m, which moves only where a score exceeds it by 16 (and where the row sees its first
   // tokens, and in stages with hidden ones): any reference gives the same quotient, and bf16 and fp32 have the range.
   auto soften = [&](int t0, const uint8_t* lk, uint32_t blocks, bool full) {
-    const uint8_t* lv = lk + PF_TOKENS * KROW;
-    const float* ls = reinterpret_cast<const float*>(lv + DP * PF_VROW);
+    const uint8_t* lv = lk + TOK * KROW;
+    const float* ls = reinterpret_cast<const float*>(lv + DP * VROW);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
+    for (int q = 0; q < 4 * U; ++q) {
       f32x4_t x = {a.scale, a.scale, a.scale, a.scale};
       if constexpr (I8) x = *reinterpret_cast<const f32x4_t*>(ls + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
 #pragma unroll
       for (int j = 0; j < 4; ++j) p[4 * q + j] = __builtin_fmaf(p[4 * q + j], x[j], -m);
     }
-    uint32_t mask = 0xffffffffu;
+    uint32_t mask = (uint32_t)(((uint64_t)1 << P) - 1);
     if (!full) {
       const int top = lim - t0 - 8 * h, bot = low - t0 - 8 * h;
       mask = 0;
 #pragma unroll
-      for (int k = 0; k < 32; ++k) {
+      for (int k = 0; k < P; ++k) {
         const int c = 16 * (k >> 3) + (k & 7);
         if (c <= top && c >= bot && ((blocks >> (k >> 3)) & 1)) mask |= 1u << k;
       }
 #pragma unroll
-      for (int k = 0; k < 32; ++k) p[k] = (mask >> k) & 1 ? p[k] : -INFINITY;
+      for (int k = 0; k < P; ++k) p[k] = (mask >> k) & 1 ? p[k] : -INFINITY;
     }
     float top = fmaxf(p[0], p[1]);
 #pragma unroll
-    for (int k = 2; k < 32; ++k) top = fmaxf(top, p[k]);
+    for (int k = 2; k < P; ++k) top = fmaxf(top, p[k]);
     if (!full || !__all(seen != 0 && top <= 16.0f)) {
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       float delta = seen ? fmaxf(top, 0.0f) : top;
       delta = delta == -INFINITY ? 0.0f : delta;
       const float keep = seen ? __builtin_amdgcn_exp2f(-delta) : 1.0f;     // (nothing to keep before the first tokens)
 #pragma unroll
-      for (int k = 0; k < 32; ++k) p[k] -= delta;
+      for (int k = 0; k < P; ++k) p[k] -= delta;
       m += delta;
       l *= keep;
 #pragma unroll
@@ -755,74 +786,72 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
     }
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
+    for (int k = 0; k < P; ++k) {
       p[k] = __builtin_amdgcn_exp2f(p[k]);
       sum[k & 1] += p[k];
     }
     l += sum[0] + sum[1];
     if constexpr (I8) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + PF_TOKENS + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
+      for (int q = 0; q < 4 * U; ++q) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(ls + TOK + 16 * (q >> 1) + 8 * h + 4 * (q & 1));
 #pragma unroll
         for (int j = 0; j < 4; ++j) p[4 * q + j] *= x[j];
       }
       if (!full)                 // (a step that nobody sees may be NaN)
 #pragma unroll
-        for (int k = 0; k < 32; ++k) p[k] = (mask >> k) & 1 ? p[k] : 0.0f;
+        for (int k = 0; k < P; ++k) p[k] = (mask >> k) & 1 ? p[k] : 0.0f;
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q)  // rounded to bf16, the operand's type; the sum l is of the unrounded ones
+    for (int q = 0; q < NB; ++q) // rounded to bf16, the operand's type; the sum l is of the unrounded ones
 #pragma unroll
       for (int j = 0; j < 8; ++j) pb[q][j] = (__bf16)p[8 * q + j];
     bad = false;
     if constexpr (!I8)
       if (!full) {
-        const int* f = reinterpret_cast<const int*>(ls + 2 * PF_TOKENS);
+        const int* f = reinterpret_cast<const int*>(ls + 2 * TOK);
         int any = 0;
 #pragma unroll
         for (int w = 0; w < W; ++w) any |= f[w];
         bad = __builtin_amdgcn_readfirstlane(any) != 0;
-        if (bad) {               // the product will leave them out; here is what they are to the rows that see them, token by token
+        if (bad) {               // the product leaves them out; which elements of which rows they reach is noted
+          const uint32_t other = (uint32_t)__shfl_xor((int)mask, 32, 64);
+#pragma unroll
+          for (int i = 0; i < NK; ++i)
 #pragma unroll 1
-          for (int k = 0; k < 32; ++k) {
-            const float p0 = p[0], p1 = __shfl_xor(p0, 32, 64);
-            const bool see0 = mask & 1, see1 = __shfl_xor((int)(mask & 1), 32, 64) != 0;
-#pragma unroll
-            for (int j = 0; j < 31; ++j) p[j] = p[j + 1];
-            mask >>= 1;
-            const uint8_t* x = lv + 4 * h * PF_VROW + 2 * (16 * (k >> 3) + (k & 7));
-#pragma unroll
-            for (int i = 0; i < NK; ++i) {
-              asm volatile("" ::: "memory");         // (few of the loads at a time)
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const uint16_t* y = reinterpret_cast<const uint16_t*>(x + (32 * i + 8 * (j >> 2) + (j & 3)) * PF_VROW);
-                const float x0 = bf16_to_f32(y[8 * h]), x1 = bf16_to_f32(y[8 * (h ^ 1)]);
-                if (see0 && !(fabsf(x0) < INFINITY)) acc[i][j] += p0 * x0;
-                if (see1 && !(fabsf(x1) < INFINITY)) acc[i][j] += p1 * x1;
+            for (int j = 0; j < 16; ++j) {
+              const uint16_t* x = reinterpret_cast<const uint16_t*>(lv + (32 * i + 8 * (j >> 2) + 4 * h + (j & 3)) * VROW);
+              bool up = false, down = false;
+#pragma unroll 1
+              for (int k = 0; k < P; ++k) {
+                const float x0 = bf16_to_f32(x[16 * (k >> 3) + (k & 7) + 8 * h]), x1 = bf16_to_f32(x[16 * (k >> 3) + (k & 7) + 8 * (h ^ 1)]);
+                const bool see0 = (mask >> k) & 1, see1 = (other >> k) & 1;
+                up |= (see0 && !(x0 < INFINITY)) || (see1 && !(x1 < INFINITY));
+                down |= (see0 && !(x0 > -INFINITY)) || (see1 && !(x1 > -INFINITY));
               }
+              reach[i] |= ((uint32_t)up | (uint32_t)down << 16) << j;
             }
-          }
         }
       }
   };
   auto values = [&](const uint8_t* lk) {
-    const uint8_t* lv = lk + PF_TOKENS * KROW;
+    const uint8_t* lv = lk + TOK * KROW;
     if (I8 || !bad) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < NB; ++q)
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-          const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+          const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(lv + (32 * i + col) * VROW + q * 32 + h * 16);
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pb[q], acc[i], 0, 0, 0);
         }
+
+    reads_ahead<NB * NK>();
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < NB; ++q)
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-          i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * PF_VROW + q * 32 + h * 16);
+          i32x4_t x = *reinterpret_cast<const i32x4_t*>(lv + (32 * i + col) * VROW + q * 32 + h * 16);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if ((x[j] & 0x7f80) == 0x7f80) x[j] &= (int)0xffff0000;
@@ -832,67 +861,36 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
         }
     }
   };
-  auto sees = [&](int t0) { return t0 < w_end && t0 + PF_TOKENS > w_begin; };
-  auto sees_all = [&](int t0, uint32_t there) { return t0 >= w_all_begin && t0 + PF_TOKENS <= w_all_end && there == 15; };
+  auto sees = [&](int t0) { return t0 < w_end && t0 + TOK > w_begin; };
+  auto sees_all = [&](int t0, uint32_t there) { return t0 >= w_all_begin && t0 + TOK <= w_all_end && there == ALL; };
 
-  const int n = t_begin < t_end ? (t_end - t_begin + PF_TOKENS - 1) / PF_TOKENS : 0;
-  auto t_of = [&](int s) { return t_begin + s * PF_TOKENS; };
-  if constexpr (W == 8) {
-    // Two wavefronts of a SIMD take turns, a barrier each: while one is at its two products (the values of the stage before, the
-    // scores of this one), the other is at the exponentials and the staging, so that the matrix pipe and the vector pipe work at the same
-    // time.  The upper four wavefronts run half a stage behind.  Stages are loaded three ahead and stored two ahead into a ring of
-    // four, which no turn reads and writes in the same place.
-    auto buf = [&](int s) { return lds8 + (s & 3) * STAGE; };
-    uint32_t there = 0;          // four bits a stage, the present one's lowest
-    {
-      const int p0 = pages_at(t_of(0)), p1 = pages_at(t_of(1)), p2 = pages_at(t_of(2));
-      if (n > 0) { there = load_stage(t_of(0), p0); store_stage(t_of(0), buf(0), partly(t_of(0)), there & 15); }
-      if (n > 1) { there |= load_stage(t_of(1), p1) << 4; store_stage(t_of(1), buf(1), partly(t_of(1)), there >> 4 & 15); }
-      if (n > 2) there |= load_stage(t_of(2), p2) << 8;
-    }
-    int pages = pages_at(t_of(3));
-    bool have = false;
+  const int n = t_begin < t_end ? (t_end - t_begin + TOK - 1) / TOK : 0;
+  auto t_of = [&](int s) { return t_begin + s * TOK; };
+  place here{0, 0, nullptr};
+  if (n > 0) {
+    here = place_of(t_of(0), pages_at(t_of(0)));
+    load_stage(t_of(0), here);
+    store_stage(t_of(0), lds8, partly(t_of(0)), here.there);
+  }
+  int pages = pages_at(t_of(1));
+  uint32_t there = here.there;
+  for (int s = 0; s < n; ++s) {
     __syncthreads();
-    if (wave >= W / 2) __syncthreads();
-    for (int s = 0; s < n; ++s) {
-      if (have) values(buf(s - 1));
-      have = sees(t_of(s));
-      if (have) scores(buf(s));
-      __syncthreads();
-      if (s + 2 < n) store_stage(t_of(s + 2), buf(s + 2), partly(t_of(s + 2)), there >> 8 & 15);
-      if (s + 3 < n) {
-        there |= load_stage(t_of(s + 3), pages) << 12;
-        pages = pages_at(t_of(s + 4));
-      }
-      if (have) soften(t_of(s), buf(s), there & 15, sees_all(t_of(s), there & 15));
-      there >>= 4;
-      __syncthreads();
+    uint32_t next = 0;
+    if (s + 1 < n) {
+      here = place_of(t_of(s + 1), pages);
+      next = here.there;
+      load_stage(t_of(s + 1), here);
+      pages = pages_at(t_of(s + 2));
     }
-    if (wave < W / 2) __syncthreads();
-    if (have) values(buf(n - 1));
-  } else {
-    uint32_t there = 0;
-    if (n > 0) {
-      there = load_stage(t_of(0), pages_at(t_of(0)));
-      store_stage(t_of(0), lds8, partly(t_of(0)), there);
+    const uint8_t* lk = lds8 + (s & 1) * STAGE;
+    if (sees(t_of(s))) {
+      scores(lk);
+      soften(t_of(s), lk, there, sees_all(t_of(s), there));
+      values(lk);
     }
-    int pages = pages_at(t_of(1));
-    for (int s = 0; s < n; ++s) {
-      __syncthreads();
-      uint32_t next = 0;
-      if (s + 1 < n) {
-        next = load_stage(t_of(s + 1), pages);
-        pages = pages_at(t_of(s + 2));
-      }
-      const uint8_t* lk = lds8 + (s & 1) * STAGE;
-      if (sees(t_of(s))) {
-        scores(lk);
-        soften(t_of(s), lk, there, sees_all(t_of(s), there));
-        values(lk);
-      }
-      if (s + 1 < n) store_stage(t_of(s + 1), lds8 + (~s & 1) * STAGE, partly(t_of(s + 1)), next);
-      there = next;
-    }
+    if (s + 1 < n) store_stage(t_of(s + 1), lds8 + (~s & 1) * STAGE, partly(t_of(s + 1)), next);
+    there = next;
   }
   if (!mine) return;
   // ---- every column is a row: register 4 q + j of half h is element 8 q + 4 h + j of each 32
@@ -907,7 +905,13 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
       const int d = 32 * i + 8 * q + 4 * h;
       float x[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = any ? acc[i][4 * q + j] * inv : 0.0f;
+      for (int j = 0; j < 4; ++j) {
+        x[j] = any ? acc[i][4 * q + j] * inv : 0.0f;
+        if constexpr (!I8) {
+          if ((reach[i] >> (4 * q + j)) & 1) x[j] += INFINITY;
+          if ((reach[i] >> (16 + 4 * q + j)) & 1) x[j] -= INFINITY;
+        }
+      }
       const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
       if (v.d % 4 == 0) {
         if (d < v.d) *reinterpret_cast<uint2*>(o + d) = w;
@@ -919,27 +923,21 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_prefill_kernel(p
   if (a.lse && h == 0) a.lse[trow * a.heads + head] = any ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
 }
 
-template <int KIND, int NK, int W>
-int launch_prefill_w(prefill_args a, int n_kv_heads, hipStream_t s) {
-  constexpr int lds = (W == 8 ? 4 : 2) * prefill_stage<NK>();
+template <int KIND, int NK>
+int launch_prefill_nk(prefill_args a, hipStream_t s) {
+  constexpr int lds = 2 * prefill_stage<KIND, NK>();
   static std::once_flag once;
   static int rc = PQ_OK;
   std::call_once(once, [] {
-    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK, W>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
       rc = PQ_ERR_HIP;
   });
   if (rc) return pq_set_error(rc, "hipFuncSetAttribute failed for attn_prefill_kernel");
-  const int64_t tiles = (int64_t)a.v.T * a.group / (W * 32) + a.v.n_seqs, grid = tiles * n_kv_heads;
+  const int64_t tiles = (int64_t)a.v.T * a.group / 128 + a.v.n_seqs, grid = tiles * a.v.n_kv_heads;
   if (grid > 0x7fffffff) return pq_set_error(PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call", a.v.T, a.heads, a.v.n_seqs);
   a.tiles = (int)tiles;
-  attn_prefill_kernel<KIND, NK, W><<<(unsigned)grid, W * 64, lds, s>>>(a);
+  attn_prefill_kernel<KIND, NK><<<(unsigned)grid, 256, lds, s>>>(a);
   return PQ_OK;
-}
-template <int KIND, int NK>
-int launch_prefill_nk(const prefill_args& a, hipStream_t s) {
-  if constexpr (NK <= 4)
-    if (getenv("PFW8")) return launch_prefill_w<KIND, NK, 8>(a, a.v.n_kv_heads, s);
-  return launch_prefill_w<KIND, NK, 4>(a, a.v.n_kv_heads, s);
 }
 template <int KIND>
 int launch_prefill(const prefill_args& a, hipStream_t s) {
