@@ -1,12 +1,21 @@
-"""A stack of transformer-shaped layers made of pQuant linears only (no attention core, no norms):
+"""Drivers that chain the library's calls into layers.
+
+Stack: a stack of transformer-shaped layers made of pQuant linears only (no attention core, no norms):
 
     per layer:  q,k,v = L_q(h), L_k(h), L_v(h)      pure 1-bit linears (Sec. 3.1: the MHA projections)
                 m = (q + k + v) / 3                 stand-in for the attention core (glue)
                 h1 = h + L_o(m)                     residual (glue)
                 h2 = h1 + FFN(h1)                   decoupled FFN with routed experts (Sec. 3.2, 3.3)
 
-This module only sequences C-ABI calls (pq_linear_*, pq_ffn_*, pq_glue_*); PyTorch provides the
-device buffers.  It exists to time the linears of a 24-layer 1.3B-shaped model end to end.
+It exists to time the linears of a 24-layer 1.3B-shaped model end to end.
+
+CachedAttention: the attention half of a layer at inference, on packed weights and a paged key-value cache:
+
+    q, k, v = L_q(x), L_k(x), L_v(x)                pure 1-bit linears (Sec. 3.1)
+    out = x + L_o(attention(q, cache + k, v))       prompts row by row, then one token of every sequence at a time
+
+This module only sequences C-ABI calls (pq_linear_*, pq_ffn_*, pq_decode_gemv, pq_kv_*, pq_attn_*, pq_glue_*); PyTorch provides the
+device buffers.
 """
 from __future__ import annotations
 
@@ -73,3 +82,61 @@ class Stack:
                 pq.linear_bwd(self.lin_desc, dm, ly["h"], w["W" + n], ly["lin_buf"][n], dxn, g["W" + n], self.dab)
             pq.glue_lincomb(d_cur, [d_tmp, dq, dk, dv], [1.0, 1.0, 1.0, 1.0])
         return d_cur
+
+
+class CachedAttention:
+    """One layer's attention over a cache of `n_pages` pages for `n_seqs` sequences (decoding: at most 16, the packed product's limit).
+
+    Weights: latent Wq [d][d], Wk, Wv [n_kv_heads * d_head][d], Wo [d][d] (bf16, d = d_model), packed here once.  The caller keeps the pages:
+    page_table [n_seqs, max_pages] int32 and lens [n_seqs] int32, which count the tokens of a call before it is made.  A prompt's
+    buffers are made by the call; those of a decoding step are the object's, so that a step can be captured into a graph."""
+
+    def __init__(self, weights, n_heads, n_kv_heads, n_pages, n_seqs, max_pages, page_tokens=64, kv_kind=pq.PQ_KV_INT8, max_len=0,
+                 device="cuda"):
+        d = weights["Wq"].shape[1]
+        self.d, self.H, self.Hk, self.dh, self.B = d, n_heads, n_kv_heads, d // n_heads, n_seqs
+        self.packed = {}
+        for n in ("q", "k", "v", "o"):
+            P, _, ml = pq.pack_sign(weights["W" + n])
+            scale = ml[1:2].to(torch.float16).view(torch.int16)          # the one stored scale of a packed layer
+            self.packed[n] = (weights["W" + n].shape[0], P, ml, pq.pack_retile64(P, d), scale)
+        self.kv = pq.make_kv_desc(kv_kind, n_kv_heads, self.dh, page_tokens, n_pages, n_seqs, max_pages)
+        self.attn = pq.make_attn_desc(self.kv, n_heads, max_len=max_len)
+        self.cache = pq.kv_cache(self.kv, device)
+        e = lambda n: torch.empty((n_seqs, n), dtype=torch.bfloat16, device=device)
+        self.step = {n: e(p[0]) for n, p in self.packed.items()}
+        self.step["a"] = e(d)
+        self.decode = {n: pq.DecodeDesc(n_seqs, d, p[0], 0, 1, 1, 1, pq.PQ_PACKED_TILED64, 0.0) for n, p in self.packed.items()}
+        self.decode_ws = {n: pq.decode_workspace(dd, device) for n, dd in self.decode.items()}
+        self.attn_ws = pq.attn_decode_workspace(self.attn, device)
+
+    def _heads(self, x, heads):
+        return x.view(x.shape[0], heads, self.dh)
+
+    def prompt(self, x, lens, page_table, row_start):
+        """x [T, d] bf16: the last row_start[b + 1] - row_start[b] tokens of every sequence.  Returns [T, d]."""
+        T = x.shape[0]
+
+        def linear(n, x):
+            N, P, ml, _, _ = self.packed[n]
+            desc = pq.make_desc(T, self.d, N, w_kind=pq.PQ_W_PACKED, alpha=0.0, beta=1.0)
+            y = torch.empty((T, N), dtype=torch.bfloat16, device=x.device)
+            return pq.linear_fwd(desc, x, P, y, pq.LinearBuffers(desc, x.device), mu_lambda=ml, save=False)
+        q, k, v = linear("q", x), linear("k", x), linear("v", x)
+        pq.kv_write(self.kv, self._heads(k, self.Hk), self._heads(v, self.Hk), self.cache, lens, page_table, row_start=row_start)
+        a = torch.empty_like(q)
+        pq.attn_prefill(self.attn, self._heads(q, self.H), self.cache, lens, page_table, row_start, self._heads(a, self.H))
+        return pq.glue_lincomb(torch.empty_like(x), [x, linear("o", a)], [1.0, 1.0])
+
+    def token(self, x, lens, page_table, out):
+        """x [n_seqs, d] bf16: the newest token of every sequence, counted in lens already.  Writes out [n_seqs, d]."""
+        s = self.step
+
+        def linear(n, x):
+            _, _, _, tiled, scale = self.packed[n]
+            return pq.decode_gemv(self.decode[n], x, tiled, scale, s[n], self.decode_ws[n])
+        for n in ("q", "k", "v"):
+            linear(n, x)
+        pq.kv_write(self.kv, self._heads(s["k"], self.Hk), self._heads(s["v"], self.Hk), self.cache, lens, page_table)
+        pq.attn_decode(self.attn, self._heads(s["q"], self.H), self.cache, lens, page_table, self._heads(s["a"], self.H), self.attn_ws)
+        return pq.glue_lincomb(out, [x, linear("o", s["a"])], [1.0, 1.0])
