@@ -33,7 +33,8 @@ def test_quantiser():
     x[5, 2] = np.inf
     x[6, 1] = np.nan
     codes, step = ao.quantise(x)
-    assert np.isnan(step[5:7]).all() and not codes[3:7].any() and (step[3:5] == np.float32(1e-5) / 128).all()
+    assert not codes[3].any() and (codes[4] == 1).all() and not codes[5:7].any()        # (1e-7 is 1.28 steps of 1e-5 / 128)
+    assert np.isnan(step[5:7]).all() and (step[3:5] == np.float32(1e-5) / 128).all()
     good = [i for i in range(64) if i not in (5, 6)]
     y = ao.stored(x, True)
     top = np.abs(x[good]).max(1)
