@@ -1,6 +1,6 @@
 // Attention over the paged key-value cache: one new token of every sequence (pq_attn_decode) and the rows of prompts (pq_attn_prefill).
 #include <math.h>
-#include <mutex>
+#include <atomic>
 #include "pq_kv.h"
 
 namespace {
@@ -614,6 +614,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
     for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
   float m = 0.0f, l = 0.0f;      // reference of the exponentials (log2), their sum over this lane's tokens
   uint32_t seen = 0;             // not zero: the row has seen a token
+  bool set = false;              // .. and one whose score is not -infinity: m is a score's
 
   // ---- staging: pages of a stage's blocks of 16 tokens in the first lanes of every wavefront, one stage ahead of the loads
   const int slot_mask = (1 << v.page_shift) - 1;
@@ -771,11 +772,11 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
     float top = fmaxf(p[0], p[1]);
 #pragma unroll
     for (int k = 2; k < P; ++k) top = fmaxf(top, p[k]);
-    if (!full || !__all(seen != 0 && top <= 16.0f)) {
+    if (!full || !__all(set && top <= 16.0f)) {
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      float delta = seen ? fmaxf(top, 0.0f) : top;
-      delta = delta == -INFINITY ? 0.0f : delta;
-      const float keep = seen ? __builtin_amdgcn_exp2f(-delta) : 1.0f;     // (nothing to keep before the first tokens)
+      const float delta = set ? fmaxf(top, 0.0f) : top == -INFINITY ? 0.0f : top;
+      const float keep = set ? __builtin_amdgcn_exp2f(-delta) : 1.0f;      // (nothing to keep before the first scores)
+      set |= top != -INFINITY;
 #pragma unroll
       for (int k = 0; k < P; ++k) p[k] -= delta;
       m += delta;
@@ -926,13 +927,15 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
 template <int KIND, int NK>
 int launch_prefill_nk(prefill_args a, hipStream_t s) {
   constexpr int lds = 2 * prefill_stage<KIND, NK>();
-  static std::once_flag once;
-  static int rc = PQ_OK;
-  std::call_once(once, [] {
+  static std::atomic<uint64_t> set{0};                            // devices where the LDS beyond 64 KiB is asked for
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return pq_set_error(PQ_ERR_HIP, "hipGetDevice failed");
+  const uint64_t bit = (uint64_t)1 << (dev & 63);
+  if (!(set.load(std::memory_order_relaxed) & bit)) {
     if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
-      rc = PQ_ERR_HIP;
-  });
-  if (rc) return pq_set_error(rc, "hipFuncSetAttribute failed for attn_prefill_kernel");
+      return pq_set_error(PQ_ERR_HIP, "hipFuncSetAttribute failed for attn_prefill_kernel");
+    set.fetch_or(bit, std::memory_order_relaxed);
+  }
   const int64_t tiles = (int64_t)a.v.T * a.group / 128 + a.v.n_seqs, grid = tiles * a.v.n_kv_heads;
   if (grid > 0x7fffffff) return pq_set_error(PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call", a.v.T, a.heads, a.v.n_seqs);
   a.tiles = (int)tiles;

@@ -294,3 +294,15 @@ def test_calls_on_other_streams_and_a_fused_projection():
     for O, lse, _ in got:
         assert torch.equal(O, got[0][0]) and torch.equal(lse, got[0][1])
     assert (got[0][0].float() - want[0].float()).abs().max() <= 2.0 ** -7 * want[0].float().abs().max()
+
+
+def test_scores_of_minus_infinity_come_first():
+    """64 seen tokens whose scores are -infinity, then scores around -600: the softmax is that of the later ones."""
+    c = Paged(BF, [200], 1, 64, 16, 3)
+    c.K[0][:, 0, 0], c.K[0][:, 0, 1] = 0.0, -600.0
+    c.K[0][:64, 0, 0] = -np.inf
+    Q, q = queries(100, 2, 64, 6)
+    Q[..., :2], q[..., :2] = 1.0, 1.0
+    later = [np.arange(200) >= 64]                             # what counts
+    check(*run_prefill(c, Q, [100], 2, scale=1.0), expected(c, q, [100], 1.0, present=later, p_bits=8), "prefill")
+    check(*run_decode(c, Q[99:], 2, scale=1.0), expected(c, q[99:], [1], 1.0, present=later, p_bits=15), "decode")
