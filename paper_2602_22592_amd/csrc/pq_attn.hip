@@ -924,22 +924,371 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
   if (a.lse && h == 0) a.lse[trow * a.heads + head] = any ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
 }
 
+// ---------------------------------------------------------------------------------------------
+// Few rows: 32 a workgroup, the wavefronts share the tokens
+// ---------------------------------------------------------------------------------------------
+// The same products as above with the keys and values read straight from the cache into the matrix instructions' registers: wavefront w takes
+// the tiles w, w + W, .. of 32 tokens, so that a row's tokens pass W times as fast, and what the wavefronts found is joined through
+// the LDS.  For calls too small to fill the chip with tiles of 128 rows, whose time is that of the longest row's chain of tiles.
+template <int NK> constexpr int rows_waves() { return NK <= 4 ? 8 : 4; }
+template <int NK> constexpr int rows_pitch() { return NK * 32 + 4; }       // floats: sixteen rows' pieces of 16 bytes lie in different banks
+template <int KIND, int NK> constexpr int rows_lds() {                     // sums, maximum and sum of a row, elements that infinities reach
+  return rows_waves<NK>() * (32 * rows_pitch<NK>() * 4 + 32 * 8 + (KIND == PQ_KV_BF16 ? NK * 256 : 0));
+}
+
 template <int KIND, int NK>
-int launch_prefill_nk(prefill_args a, hipStream_t s) {
-  constexpr int lds = 2 * prefill_stage<KIND, NK>();
-  static std::atomic<uint64_t> set{0};                            // devices where the LDS beyond 64 KiB is asked for
+__global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_rows_kernel(prefill_args a) {
+  constexpr bool I8 = KIND == PQ_KV_INT8;
+  constexpr int W = rows_waves<NK>(), DP = NK * 32, ES = I8 ? 1 : 2, NS = NK * 2, NF = I8 ? NK : NS, PITCH = rows_pitch<NK>();
+  constexpr int ROWS = 32, TT = 32;
+  const kv_view& v = a.v;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5, col = lane & 31;
+  const int kvh = blockIdx.x % v.n_kv_heads, vt = a.tiles - 1 - (int)(blockIdx.x / v.n_kv_heads);
+  auto start = [&](int i) { return ((v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / ROWS + i; };
+  const int b = kv_find_seq(v.n_seqs, vt, start);
+  if (b < 0) return;
+  const kv_rows r = kv_seq_rows(v, b);
+  const int all_rows = r.n * a.group;
+  if (vt - start(b) > (all_rows - 1) / ROWS || all_rows == 0) return;
+  const int row0 = (vt - start(b)) * ROWS;
+  const int cap = v.max_pages << v.page_shift, hi = min(r.len, cap);
+  auto pos_of = [&](int row) { return r.first + row / a.group; };
+  const int rows_here = min(ROWS, all_rows - row0);
+  const int pos_first = pos_of(row0), pos_last = pos_of(row0 + rows_here - 1);
+  const int t_end = pos_last < 0 ? 0 : a.causal ? min(pos_last + 1, hi) : hi;                        // some row sees up to here
+  const int all_end = pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi;                    // every row sees up to here ..
+  const int all_begin = a.window > 0 ? max(0, pos_last + 1 - a.window) : 0;                          // .. from here
+  const int t_begin = (a.window > 0 ? max(0, pos_first + 1 - a.window) : 0) & ~(TT - 1);
+  const int tiles = t_begin < t_end ? (t_end - t_begin + TT - 1) / TT : 0;
+
+  const bool mine = col < rows_here;
+  const int row = row0 + (mine ? col : 0);
+  const int pos = mine ? pos_of(row) : -1, head = kvh * a.group + row % a.group;
+  const size_t trow = (size_t)r.r0 + row / a.group;
+  const int lim = pos < 0 ? -1 : a.causal ? min(pos, hi - 1) : hi - 1, low = a.window > 0 ? max(0, pos + 1 - a.window) : 0;
+
+  // ---- a tile in registers: keys and values of the lane's row of the operand, and (INT8) the steps of the half's sixteen tokens
+  const int slot_mask = (1 << v.page_shift) - 1;
+  const int32_t* table = v.table + (size_t)b * v.max_pages;
+  const uint8_t* pool = v.cache + (size_t)kvh * v.head_bytes;
+  const size_t page_bytes = v.head_bytes * v.n_kv_heads;
+  struct pages { int id[2]; };                   // of the tile's two blocks of 16 tokens
+  auto pages_at = [&](int t0) {
+    pages g;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) g.id[i] = t0 + 16 * i < t_end ? table[(t0 + 16 * i) >> v.page_shift] : -1;
+    return g;
+  };
+  auto there_of = [&](const pages& g) {
+    return ((unsigned)g.id[0] < (unsigned)v.n_pages ? 1u : 0u) | ((unsigned)g.id[1] < (unsigned)v.n_pages ? 2u : 0u);
+  };
+  auto page_of = [&](const pages& g, uint32_t there, int i) { return pool + (size_t)((there >> i) & 1 ? g.id[i] : 0) * page_bytes; };
+  i32x4_t kf[NF], vf[NF];
+  float ks[16], vs[16];
+  // Key row `col` of the first operand is the token that makes a half's sixteen scores the tokens whose values the half's lanes hold:
+  // 16 h + k (INT8) or 16 (k / 8) + 8 h + k % 8.
+  const int ktok = I8 ? 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3) : 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+  auto load_keys = [&](int t0, const pages& g, uint32_t there) {
+    const uint8_t* p0 = page_of(g, there, 0) + (t0 & slot_mask) * (DP * ES);
+    const uint8_t* p1 = page_of(g, there, 1) + ((t0 + 16) & slot_mask) * (DP * ES);
+    const uint8_t* kp = (ktok >> 4 ? p1 : p0) + (ktok & 15) * (DP * ES) + h * 16;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) kf[i] = *reinterpret_cast<const i32x4_t*>(kp + i * 32);
+    if constexpr (I8) {
+      const float* s0 = reinterpret_cast<const float*>(page_of(g, there, 0) + 2 * (size_t)v.part_bytes) + (t0 & slot_mask);
+      const float* s1 = reinterpret_cast<const float*>(page_of(g, there, 1) + 2 * (size_t)v.part_bytes) + ((t0 + 16) & slot_mask);
+      const f32x4_t* sp = reinterpret_cast<const f32x4_t*>(h ? s1 : s0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t x = sp[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ks[4 * i + j] = x[j];
+      }
+    }
+  };
+  auto load_values = [&](int t0, const pages& g, uint32_t there) {
+    const uint8_t* p0 = page_of(g, there, 0) + v.part_bytes + (t0 & slot_mask) * (DP * ES) + col * (16 * ES);
+    const uint8_t* p1 = page_of(g, there, 1) + v.part_bytes + ((t0 + 16) & slot_mask) * (DP * ES) + col * (16 * ES);
+    if constexpr (I8) {
+      const uint8_t* vp = h ? p1 : p0;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) vf[i] = *reinterpret_cast<const i32x4_t*>(vp + i * 512);
+      const float* s0 = reinterpret_cast<const float*>(page_of(g, there, 0) + 2 * (size_t)v.part_bytes) + slot_mask + 1 + (t0 & slot_mask);
+      const float* s1 = reinterpret_cast<const float*>(page_of(g, there, 1) + 2 * (size_t)v.part_bytes) + slot_mask + 1 + ((t0 + 16) & slot_mask);
+      const f32x4_t* sp = reinterpret_cast<const f32x4_t*>(h ? s1 : s0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4_t x = sp[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vs[4 * i + j] = x[j];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        vf[i] = *reinterpret_cast<const i32x4_t*>(p0 + h * 16 + i * 1024);
+        vf[NK + i] = *reinterpret_cast<const i32x4_t*>(p1 + h * 16 + i * 1024);
+      }
+    }
+  };
+  int t0 = t_begin + wave * TT;
+  pages here = pages_at(t0);
+
+  bf16x8_t qf[NS];               // element of step ks: the keys' pieces of 16 bytes are two steps of INT8, one of bf16
+  {
+    const uint16_t* q = a.Q + trow * a.qs + (size_t)head * v.d;
+    const bool wide = v.d % 8 == 0 && a.qs % 8 == 0;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int d = I8 ? (s >> 1) * 32 + h * 16 + (s & 1) * 8 : s * 16 + h * 8;
+      i32x4_t x;                 // (loaded whatever d is, so that no load waits for another)
+      if (wide) {
+        x = *reinterpret_cast<const i32x4_t*>(q + (d < v.d ? d : 0));
+        if (!mine || d >= v.d) x = i32x4_t{0, 0, 0, 0};
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int w = *reinterpret_cast<const int*>(q + (d + 2 * j < v.d ? d + 2 * j : 0));
+          x[j] = mine && d + 2 * j < v.d ? w : 0;
+        }
+      }
+      qf[s] = __builtin_bit_cast(bf16x8_t, x);
+    }
+  }
+  f32x16_t acc[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+  uint32_t seen = 0, reach[NK];  // (reach: as in the kernel above)
+#pragma unroll
+  for (int i = 0; i < NK; ++i) reach[i] = 0;
+
+  uint32_t there = there_of(here);
+  if (t0 < t_end) {
+    load_keys(t0, here, there);
+    load_values(t0, here, there);
+  }
+  pages next = pages_at(t0 + W * TT);
+  while (t0 < t_end) {
+    const int t_next = t0 + W * TT;
+    const bool more = t_next < t_end, full = t0 >= all_begin && t0 + TT <= all_end && there == 3;
+    const uint32_t there_next = there_of(next);
+    f32x16_t S;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) S[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      if constexpr (I8) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint2 x = codes_bf16(kf[i][2 * j]), y = codes_bf16(kf[i][2 * j + 1]);
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(x.x, x.y, y.x, y.y)), qf[2 * i + j], S, 0, 0, 0);
+        }
+      } else {
+        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), qf[i], S, 0, 0, 0);
+      }
+    }
+    float p[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) p[k] = S[k] * (I8 ? ks[k] * a.scale : a.scale);
+    if (more) load_keys(t_next, next, there_next);
+    uint32_t mask = 0xffff;
+    if (!full) {
+      mask = 0;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const int c = I8 ? 16 * h + k : 16 * (k >> 3) + 8 * h + (k & 7);
+        if (t0 + c <= lim && t0 + c >= low && ((there >> (c >> 4)) & 1)) mask |= 1u << k;
+      }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) p[k] = (mask >> k) & 1 ? p[k] : -INFINITY;
+    }
+    seen |= mask | (uint32_t)__shfl_xor((int)mask, 32, 64);
+    float top = p[0];
+#pragma unroll
+    for (int k = 1; k < 16; ++k) top = fmaxf(top, p[k]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float mt = fmaxf(m, top), mx = mt == -INFINITY ? 0.0f : mt;
+    const float keep = __builtin_amdgcn_exp2f(m - mx);
+    m = mt;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      p[k] = __builtin_amdgcn_exp2f(p[k] - mx);
+      sum += p[k];
+    }
+    l = l * keep + sum;
+    if (!__all(keep == 1.0f))
+#pragma unroll
+      for (int i = 0; i < NK; ++i) acc[i] *= keep;
+    if constexpr (I8)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) p[k] = full || ((mask >> k) & 1) ? p[k] * vs[k] : 0.0f;   // (a step that nobody sees may be NaN)
+    bf16x8_t pb[2];              // rounded to bf16, the operand's type; the sum l is of the unrounded ones
+#pragma unroll
+    for (int k = 0; k < 16; ++k) pb[k >> 3][k & 7] = (__bf16)p[k];
+    if constexpr (!I8) {
+      if (!full) {               // a probability of zero does not silence an infinity
+        bool bad = false;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int left = (there >> q) & 1 ? t_end - (t0 + 16 * q + 8 * h) : 0;
+#pragma unroll
+          for (int i = 0; i < NK; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              vf[q * NK + i][j] &= (int)((left > 2 * j ? 0xffffu : 0u) | (left > 2 * j + 1 ? 0xffff0000u : 0u));
+              bad |= has_nonfinite((uint32_t)vf[q * NK + i][j]);
+            }
+        }
+        if (__any(bad)) {        // the product leaves them out; which elements of which rows they reach is noted
+          const uint32_t other = (uint32_t)__shfl_xor((int)mask, 32, 64);
+          const uint8_t* p0 = page_of(here, there, 0) + v.part_bytes + (t0 & slot_mask) * (DP * ES);
+          const uint8_t* p1 = page_of(here, there, 1) + v.part_bytes + ((t0 + 16) & slot_mask) * (DP * ES);
+#pragma unroll
+          for (int i = 0; i < NK; ++i)
+#pragma unroll 1
+            for (int j = 0; j < 16; ++j) {
+              const int d = 32 * i + 8 * (j >> 2) + 4 * h + (j & 3);
+              bool up = false, down = false;
+#pragma unroll 1
+              for (int k = 0; k < 16; ++k) {
+                const uint16_t* x = reinterpret_cast<const uint16_t*>(k >> 3 ? p1 : p0) + d * 16 + (k & 7);
+                const float x0 = bf16_to_f32(x[8 * h]), x1 = bf16_to_f32(x[8 * (h ^ 1)]);
+                const bool see0 = (mask >> k) & 1, see1 = (other >> k) & 1;
+                up |= (see0 && !(x0 < INFINITY)) || (see1 && !(x1 < INFINITY));
+                down |= (see0 && !(x0 > -INFINITY)) || (see1 && !(x1 > -INFINITY));
+              }
+              reach[i] |= ((uint32_t)up | (uint32_t)down << 16) << j;
+            }
+#pragma unroll
+          for (int i = 0; i < NF; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if ((vf[i][j] & 0x7f80) == 0x7f80) vf[i][j] &= (int)0xffff0000;
+              if ((vf[i][j] & 0x7f800000) == 0x7f800000) vf[i][j] &= 0xffff;
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        if constexpr (I8) {
+          const uint2 x = codes_bf16(vf[i][2 * q]), y = codes_bf16(vf[i][2 * q + 1]);
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, make_uint4(x.x, x.y, y.x, y.y)), pb[q], acc[i], 0, 0, 0);
+        } else {
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vf[q * NK + i]), pb[q], acc[i], 0, 0, 0);
+        }
+      }
+    if (more) {
+      load_values(t_next, next, there_next);
+      here = next;
+      next = pages_at(t_next + W * TT);
+    }
+    there = there_next;
+    t0 = t_next;
+  }
+
+  // ---- the wavefronts' parts, joined in their order: register 4 q + j of half h is element 8 q + 4 h + j of each 32 of row `col`
+  extern __shared__ float lds[];
+  float* ml = lds + W * ROWS * PITCH;
+  uint32_t* lr = reinterpret_cast<uint32_t*>(ml + W * ROWS * 2);
+  if (wave < tiles) {
+    l += __shfl_xor(l, 32, 64);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4_t x = {acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
+        *reinterpret_cast<f32x4_t*>(lds + (wave * ROWS + col) * PITCH + 32 * i + 8 * q + 4 * h) = x;
+      }
+      if constexpr (!I8) lr[(wave * NK + i) * 64 + lane] = reach[i];
+    }
+    if (h == 0) {
+      ml[(wave * ROWS + col) * 2] = m;
+      ml[(wave * ROWS + col) * 2 + 1] = seen ? l : -1.0f;      // (a sum is never negative)
+    }
+  }
+  __syncthreads();
+  const int parts = min(W, tiles);
+  for (int e = threadIdx.x; e < rows_here * (DP / 4); e += W * 64) {
+    const int rr = e / (DP / 4), d = e % (DP / 4) * 4;
+    float M = -INFINITY;
+    for (int w = 0; w < parts; ++w) M = fmaxf(M, ml[(w * ROWS + rr) * 2]);
+    const float mx = M == -INFINITY ? 0.0f : M;
+    float sum = 0.0f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    uint32_t hit = 0;
+    bool some = false;
+    for (int w = 0; w < parts; ++w) {                          // (a wavefront that saw nothing of a row holds zeros)
+      const float lw = ml[(w * ROWS + rr) * 2 + 1], f = lw < 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[(w * ROWS + rr) * 2] - mx);
+      some |= !(lw < 0.0f);
+      sum += lw * f;
+      o += *reinterpret_cast<const f32x4_t*>(lds + (w * ROWS + rr) * PITCH + d) * f;
+      if constexpr (!I8) hit |= lr[(w * NK + (d >> 5)) * 64 + (d & 4) * 8 + rr] >> (4 * ((d & 31) >> 3));
+    }
+    const float inv = some ? 1.0f / sum : 0.0f;
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] = some ? o[j] * inv : 0.0f;
+      if constexpr (!I8) {
+        if ((hit >> j) & 1) x[j] += INFINITY;
+        if ((hit >> (16 + j)) & 1) x[j] -= INFINITY;
+      }
+    }
+    const int row = row0 + rr;
+    const size_t at = ((size_t)r.r0 + row / a.group) * a.heads + kvh * a.group + row % a.group;
+    uint16_t* out = a.O + at * v.d + d;
+    const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+    if (v.d % 4 == 0) {
+      if (d < v.d) *reinterpret_cast<uint2*>(out) = w;
+    } else {
+      if (d < v.d) *reinterpret_cast<uint32_t*>(out) = w.x;
+      if (d + 2 < v.d) *reinterpret_cast<uint32_t*>(out + 2) = w.y;
+    }
+    if (d == 0 && a.lse) a.lse[at] = some ? (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
+  }
+}
+
+// Which of the two: tiles of 32 rows up to 16384 rows times heads, half the CUs' worth of tiles of 128.  (32 / 128 rows a tile, INT8, us: 130 rows of
+// 16 heads of 128 9.3 / 11.9; five sequences of 24 rows behind 2000 tokens, 20/4 heads of 128, 29 / 68; 256, 512 and 1024 rows of 32/8 heads of 128
+// 12.4 / 14.5, 23.7 / 21.7 and 55 / 37; 512 and 1024 rows of 32 heads of 64 15.4 / 17.9 and 35.7 / 29.2; 512 rows behind 7680 tokens, 32/8 heads
+// of 128, 157 / 242.)
+bool few_rows(const prefill_args& a) { return (int64_t)a.v.T * a.heads <= 16384; }
+
+// The LDS beyond 64 KiB of a kernel, asked for once on each device.
+int allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& asked) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return pq_set_error(PQ_ERR_HIP, "hipGetDevice failed");
   const uint64_t bit = (uint64_t)1 << (dev & 63);
-  if (!(set.load(std::memory_order_relaxed) & bit)) {
-    if (hipFuncSetAttribute((const void*)attn_prefill_kernel<KIND, NK>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
-      return pq_set_error(PQ_ERR_HIP, "hipFuncSetAttribute failed for attn_prefill_kernel");
-    set.fetch_or(bit, std::memory_order_relaxed);
-  }
-  const int64_t tiles = (int64_t)a.v.T * a.group / 128 + a.v.n_seqs, grid = tiles * a.v.n_kv_heads;
+  if (asked.load(std::memory_order_relaxed) & bit) return PQ_OK;
+  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
+    return pq_set_error(PQ_ERR_HIP, "hipFuncSetAttribute failed for an attention kernel");
+  asked.fetch_or(bit, std::memory_order_relaxed);
+  return PQ_OK;
+}
+
+template <int KIND, int NK>
+int launch_prefill_nk(prefill_args a, hipStream_t s) {
+  static std::atomic<uint64_t> asked[2];
+  const bool few = few_rows(a);
+  const int rows = few ? 32 : 128;
+  const int64_t tiles = (int64_t)a.v.T * a.group / rows + a.v.n_seqs, grid = tiles * a.v.n_kv_heads;
   if (grid > 0x7fffffff) return pq_set_error(PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call", a.v.T, a.heads, a.v.n_seqs);
   a.tiles = (int)tiles;
-  attn_prefill_kernel<KIND, NK><<<(unsigned)grid, 256, lds, s>>>(a);
+  if (few) {
+    constexpr int lds = rows_lds<KIND, NK>();
+    if (int e = allow_lds((const void*)attn_rows_kernel<KIND, NK>, lds, asked[0])) return e;
+    attn_rows_kernel<KIND, NK><<<(unsigned)grid, rows_waves<NK>() * 64, lds, s>>>(a);
+  } else {
+    constexpr int lds = 2 * prefill_stage<KIND, NK>();
+    if (int e = allow_lds((const void*)attn_prefill_kernel<KIND, NK>, lds, asked[1])) return e;
+    attn_prefill_kernel<KIND, NK><<<(unsigned)grid, 256, lds, s>>>(a);
+  }
   return PQ_OK;
 }
 template <int KIND>
