@@ -546,28 +546,93 @@ __device__ __forceinline__ uint2 codes_bf16(int w) {
 }
 __device__ __forceinline__ bool has_nonfinite(uint32_t two) { return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u; }
 
+// Which sequence and which of its tiles of ROWS rows workgroup `vt` of the call has (b < 0: none).  Up to 8 sequences are taken in the order of the
+// tokens that their last tiles see, most first, and a sequence's last tiles first, so that long tiles do not start when the others end.  Beyond
+// that: virtual tiles, of which sequence b owns those from floor(first row / ROWS) + b on, at least as many as it has, the last ones first.
+// (INT8, heads of 90, 32 of them, sorted / not: seven ragged prompts up to 1500 rows 81 / 84 us with a window, 86 / 91 without; eight of 512
+// 48.8 / 46.5, of 128 12.8 / 14.2; 16 and 32 of 128, 19.7 / 18.1 and 42 / 31: each sequence costs every wavefront a step of the loop.)
+struct tile_place { int b, tile; kv_rows r; };
+template <int ROWS>
+__device__ __forceinline__ tile_place find_tile(const prefill_args& a, int vt) {
+  const kv_view& v = a.v;
+  const int lane = threadIdx.x & 63;
+  tile_place w;
+  w.b = -1;
+  if (v.n_seqs <= 8) {
+    const kv_rows mine = kv_seq_rows(v, min(lane, v.n_seqs - 1));
+    const int tiles = lane < v.n_seqs ? (int)(((int64_t)mine.n * a.group + ROWS - 1) / ROWS) : 0;
+    const int sees = a.window > 0 && a.window < mine.len ? min(mine.len, a.window + ROWS) : mine.len;
+    int before = 0;                    // tiles of the sequences that come first
+    for (int i = 0; i < v.n_seqs; ++i) {
+      const int s = __builtin_amdgcn_readlane(sees, i), n = __builtin_amdgcn_readlane(tiles, i);
+      before += s > sees || (s == sees && i < lane) ? n : 0;
+    }
+    const uint64_t hit = __ballot(vt >= before && vt < before + tiles);
+    if (hit == 0) return w;
+    w.b = __builtin_ctzll(hit);
+    w.r.r0 = __builtin_amdgcn_readlane(mine.r0, w.b);
+    w.r.n = __builtin_amdgcn_readlane(mine.n, w.b);
+    w.r.len = __builtin_amdgcn_readlane(mine.len, w.b);
+    w.r.first = __builtin_amdgcn_readlane(mine.first, w.b);
+    w.tile = __builtin_amdgcn_readlane(before + tiles, w.b) - 1 - vt;
+  } else {
+    vt = a.tiles - 1 - vt;
+    auto start = [&](int i) { return ((v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / ROWS + i; };
+    const int b = kv_find_seq(v.n_seqs, vt, start);
+    if (b < 0) return w;
+    w.r = kv_seq_rows(v, b);
+    w.tile = vt - start(b);
+    if (w.r.n > 0 && w.tile <= (w.r.n * a.group - 1) / ROWS) w.b = b;
+  }
+  return w;
+}
+
+// Eight elements of a row of d from element `at` on, zeros behind its end (rows of 8 and more: one load of 16 bytes that ends with the row).
+typedef int i32x4_a4_t __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ i32x4_t row_piece(const uint16_t* q, int d, int at) {
+  i32x4_t x;
+  if (d >= 8) {
+    const int from = min(at, d - 8), shift = (at - from) >> 1;
+    x = *reinterpret_cast<const i32x4_a4_t*>(q + from);
+    if (shift & 1) x = i32x4_t{x[1], x[2], x[3], 0};
+    if (shift & 2) x = i32x4_t{x[2], x[3], 0, 0};
+    if (shift >= 4) x = i32x4_t{0, 0, 0, 0};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int w = *reinterpret_cast<const int*>(q + (at + 2 * j < d ? at + 2 * j : 0));
+      x[j] = at + 2 * j < d ? w : 0;
+    }
+  }
+  return x;
+}
+// Four outputs from element `at` of a row of d on, as many as it has.
+typedef uint32_t u32x2_a4_t __attribute__((ext_vector_type(2), aligned(4)));
+__device__ __forceinline__ void store_quad(uint16_t* row, int d, int at, const float* x) {
+  const uint32_t lo = pack_bf16x2(x[0], x[1]), hi = pack_bf16x2(x[2], x[3]);
+  if (at + 4 <= d) *reinterpret_cast<u32x2_a4_t*>(row + at) = u32x2_a4_t{lo, hi};
+  else if (at < d) *reinterpret_cast<uint32_t*>(row + at) = lo;
+}
+
 template <int KIND, int NK>
 __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(prefill_args a) {
   constexpr bool I8 = KIND == PQ_KV_INT8;
   constexpr int TOK = prefill_tokens<KIND, NK>(), DP = NK * 32, ES = I8 ? 1 : 2, NS = NK * 2;
   constexpr int KROW = prefill_krow<NK>(), VROW = prefill_vrow<KIND, NK>(), STAGE = prefill_stage<KIND, NK>();
   constexpr int W = 4, THREADS = W * 64, ROWS = W * 32, U = TOK / 32, NB = TOK / 16, ALL = (1 << NB) - 1;
-  constexpr int ROW_PIECES = DP * ES / 16, BLOCK_PIECES = DP * ES;                      // pieces of 16 bytes of a key, of 16 tokens' values
-  constexpr int PIECES = TOK * ROW_PIECES, CT = (PIECES + THREADS - 1) / THREADS;               // of a stage's keys (or values), and of a thread
+  // Pieces of a stage's keys (or values): 16 bytes, or 8 where that gives every thread as many.
+  constexpr int PB = TOK * DP * ES % (16 * THREADS) == 0 ? 16 : 8, CT = TOK * DP * ES / (PB * THREADS);
+  constexpr int ROW_PIECES = DP * ES / PB, BLOCK_PIECES = 16 * DP * ES / PB, PT = PB / ES;      // of a key, of 16 tokens' values; tokens of a piece
+  static_assert(CT * PB * THREADS == TOK * DP * ES, "whole pieces");
+  typedef __attribute__((ext_vector_type(PB / 4))) int piece_t;
   extern __shared__ uint8_t lds8[];
   const kv_view& v = a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5, col = lane & 31;
-  // the last tiles of a sequence see the most tokens and come first; one key-value head of every eight on an XCD
-  const int kvh = blockIdx.x % v.n_kv_heads, vt = a.tiles - 1 - (int)(blockIdx.x / v.n_kv_heads);
-  // Virtual tiles: sequence b owns those from floor(first row / ROWS) + b, at least as many as it has; what it does not need is empty.
-  // (rows times heads stay below 2^31)
-  auto start = [&](int i) { return ((v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / ROWS + i; };
-  const int b = kv_find_seq(v.n_seqs, vt, start);
-  if (b < 0) return;
-  const kv_rows r = kv_seq_rows(v, b);
-  const int all_rows = r.n * a.group;
-  if (vt - start(b) > (all_rows - 1) / ROWS || all_rows == 0) return;
-  const int row0 = (vt - start(b)) * ROWS;
+  const int kvh = blockIdx.x % v.n_kv_heads;                       // (one key-value head of every eight on an XCD)
+  const tile_place w = find_tile<ROWS>(a, blockIdx.x / v.n_kv_heads);
+  if (w.b < 0) return;
+  const kv_rows r = w.r;
+  const int b = w.b, all_rows = r.n * a.group, row0 = w.tile * ROWS;
   const int cap = v.max_pages << v.page_shift, hi = min(r.len, cap);
   auto pos_of = [&](int row) { return r.first + row / a.group; };
   const int rows_here = min(ROWS, all_rows - row0);
@@ -586,36 +651,6 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
   const int w_all_end = wfirst < 0 ? 0 : a.causal ? min(wfirst + 1, hi) : hi;           // every row sees up to here ..
   const int w_begin = a.window > 0 ? max(0, wfirst + 1 - a.window) : 0, w_all_begin = a.window > 0 ? max(0, wlast + 1 - a.window) : 0;   // .. from here
 
-  bf16x8_t qf[NS];
-  {
-    const uint16_t* q = a.Q + trow * a.qs + (size_t)head * v.d;
-    const bool wide = v.d % 8 == 0 && a.qs % 8 == 0;
-#pragma unroll
-    for (int ks = 0; ks < NS; ++ks) {
-      const int d = ks * 16 + h * 8;
-      i32x4_t x;                 // (loaded whatever d is, so that no load waits for another)
-      if (wide) {
-        x = *reinterpret_cast<const i32x4_t*>(q + (d < v.d ? d : 0));
-        if (!mine || d >= v.d) x = i32x4_t{0, 0, 0, 0};
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int w = *reinterpret_cast<const int*>(q + (d + 2 * j < v.d ? d + 2 * j : 0));
-          x[j] = mine && d + 2 * j < v.d ? w : 0;
-        }
-      }
-      qf[ks] = __builtin_bit_cast(bf16x8_t, x);
-    }
-  }
-  f32x16_t acc[NK];
-#pragma unroll
-  for (int i = 0; i < NK; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
-  float m = 0.0f, l = 0.0f;      // reference of the exponentials (log2), their sum over this lane's tokens
-  uint32_t seen = 0;             // not zero: the row has seen a token
-  bool set = false;              // .. and one whose score is not -infinity: m is a score's
-
   // ---- staging: pages of a stage's blocks of 16 tokens in the first lanes of every wavefront, one stage ahead of the loads
   const int slot_mask = (1 << v.page_shift) - 1;
   const int32_t* table = v.table + (size_t)b * v.max_pages;
@@ -627,7 +662,27 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
     if (t < t_end) p = table[t >> v.page_shift];
     return p;                    // (looked at a stage later: a wait for it here would wait for the stage's loads too)
   };
-  i32x4_t kreg[CT], vreg[CT];
+  const int n = t_begin < t_end ? (t_end - t_begin + TOK - 1) / TOK : 0;
+  auto t_of = [&](int s) { return t_begin + s * TOK; };
+  const int pages0 = pages_at(t_of(0));
+  int pages = pages_at(t_of(1));
+
+  bf16x8_t qf[NS];
+#pragma unroll
+  for (int ks = 0; ks < NS; ++ks) {
+    const i32x4_t x = row_piece(a.Q + trow * a.qs + (size_t)head * v.d, v.d, ks * 16 + h * 8);
+    qf[ks] = __builtin_bit_cast(bf16x8_t, mine ? x : i32x4_t{0, 0, 0, 0});
+  }
+  f32x16_t acc[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
+  float m = 0.0f, l = 0.0f;      // reference of the exponentials (log2), their sum over this lane's tokens
+  uint32_t seen = 0;             // not zero: the row has seen a token
+  bool set = !mine;              // .. and one whose score is not -infinity: m is a score's (a lane without a row asks for nothing)
+
+  piece_t kreg[CT], vreg[CT];
   float steps = 0.0f;
   // Where a stage lies: which of its blocks have a page, and the pages with those that are missing as page 0; where a page holds the
   // whole stage, its address.
@@ -647,10 +702,8 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         const int i = threadIdx.x + THREADS * c;
-        if (PIECES % THREADS == 0 || i < PIECES) {
-          kreg[c] = *reinterpret_cast<const i32x4_t*>(at + i * 16);
-          vreg[c] = *reinterpret_cast<const i32x4_t*>(at + v.part_bytes + i * 16);
-        }
+        kreg[c] = *reinterpret_cast<const piece_t*>(at + i * PB);
+        vreg[c] = *reinterpret_cast<const piece_t*>(at + v.part_bytes + i * PB);
       }
       if constexpr (I8)
         if (wave < 2) steps = reinterpret_cast<const float*>(w.at + 2 * (size_t)v.part_bytes)[(wave << v.page_shift) + (t0 & slot_mask) + (lane & (TOK - 1))];
@@ -658,12 +711,10 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         const int i = threadIdx.x + THREADS * c;
-        const int t = min(i / ROW_PIECES, TOK - 1), vb = min(i / BLOCK_PIECES, NB - 1);           // keys token by token, values block by block
+        const int t = i / ROW_PIECES, vb = i / BLOCK_PIECES;           // keys token by token, values block by block
         const int bk = __shfl(w.safe, t >> 4, 64), bv = __shfl(w.safe, vb, 64);
-        if (PIECES % THREADS == 0 || i < PIECES) {
-          kreg[c] = *reinterpret_cast<const i32x4_t*>(pool + (size_t)bk * page_bytes + ((t0 + t) & slot_mask) * (DP * ES) + (i % ROW_PIECES) * 16);
-          vreg[c] = *reinterpret_cast<const i32x4_t*>(pool + (size_t)bv * page_bytes + v.part_bytes + ((t0 + 16 * vb) & slot_mask) * (DP * ES) + (i % BLOCK_PIECES) * 16);
-        }
+        kreg[c] = *reinterpret_cast<const piece_t*>(pool + (size_t)bk * page_bytes + ((t0 + t) & slot_mask) * (DP * ES) + (i % ROW_PIECES) * PB);
+        vreg[c] = *reinterpret_cast<const piece_t*>(pool + (size_t)bv * page_bytes + v.part_bytes + ((t0 + 16 * vb) & slot_mask) * (DP * ES) + (i % BLOCK_PIECES) * PB);
       }
       if constexpr (I8) {
         const int bs = __shfl(w.safe, (lane & (TOK - 1)) >> 4, 64);
@@ -679,28 +730,29 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const int i = threadIdx.x + THREADS * c;
-      if (PIECES % THREADS != 0 && i >= PIECES) continue;
-      const int t = i / ROW_PIECES, piece = i % ROW_PIECES, vb = i / BLOCK_PIECES, vpiece = i % BLOCK_PIECES;
+      const int t = i / ROW_PIECES, vb = i / BLOCK_PIECES, e = i % BLOCK_PIECES / (16 / PT), vt = i % (16 / PT) * PT;   // e, vt: element, first token
       const int rk = (t & 0x33) | ((t & 4) << 1) | ((t & 8) >> 1);     // see the scores' tokens below
+      uint8_t *ko = lk + rk * KROW + i % ROW_PIECES * (PB * 2 / ES), *vo = lv + e * VROW + vb * 32 + vt * 2;
       if constexpr (I8) {
-        const uint2 x0 = codes_bf16(kreg[c][0]), x1 = codes_bf16(kreg[c][1]), x2 = codes_bf16(kreg[c][2]), x3 = codes_bf16(kreg[c][3]);
-        *reinterpret_cast<uint4*>(lk + rk * KROW + piece * 32) = make_uint4(x0.x, x0.y, x1.x, x1.y);
-        *reinterpret_cast<uint4*>(lk + rk * KROW + piece * 32 + 16) = make_uint4(x2.x, x2.y, x3.x, x3.y);
-        const uint2 y0 = codes_bf16(vreg[c][0]), y1 = codes_bf16(vreg[c][1]), y2 = codes_bf16(vreg[c][2]), y3 = codes_bf16(vreg[c][3]);
-        *reinterpret_cast<uint4*>(lv + vpiece * VROW + vb * 32) = make_uint4(y0.x, y0.y, y1.x, y1.y);
-        *reinterpret_cast<uint4*>(lv + vpiece * VROW + vb * 32 + 16) = make_uint4(y2.x, y2.y, y3.x, y3.y);
-      } else {
-        *reinterpret_cast<i32x4_t*>(lk + rk * KROW + piece * 16) = kreg[c];
-        i32x4_t x = vreg[c];
-        if (clean) {                       // tokens that are not there become zeros: a probability of zero does not silence an infinity
-          const int left = (there >> vb) & 1 ? t_end - (t0 + 16 * vb + 8 * (vpiece & 1)) : 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < PB / 4; j += 2) {
+          const uint2 x0 = codes_bf16(kreg[c][j]), x1 = codes_bf16(kreg[c][j + 1]);
+          *reinterpret_cast<uint4*>(ko + 8 * j) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+          const uint2 y0 = codes_bf16(vreg[c][j]), y1 = codes_bf16(vreg[c][j + 1]);
+          *reinterpret_cast<uint4*>(vo + 8 * j) = make_uint4(y0.x, y0.y, y1.x, y1.y);
+        }
+      } else {
+        *reinterpret_cast<piece_t*>(ko) = kreg[c];
+        piece_t x = vreg[c];
+        if (clean) {                       // tokens that are not there become zeros: a probability of zero does not silence an infinity
+          const int left = (there >> vb) & 1 ? t_end - (t0 + 16 * vb + vt) : 0;
+#pragma unroll
+          for (int j = 0; j < PB / 4; ++j) {
             x[j] &= (int)((left > 2 * j ? 0xffffu : 0u) | (left > 2 * j + 1 ? 0xffff0000u : 0u));
             bad |= has_nonfinite((uint32_t)x[j]);
           }
         }
-        *reinterpret_cast<i32x4_t*>(lv + (vpiece >> 1) * VROW + vb * 32 + (vpiece & 1) * 16) = x;
+        *reinterpret_cast<piece_t*>(vo) = x;
       }
     }
     float* ls = reinterpret_cast<float*>(lv + DP * VROW);
@@ -746,7 +798,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
       for (int j = 0; j < 16; ++j) p[16 * u + j] = S[u][j];
   };
   // Probabilities relative to the row's reference m, which moves only where a score exceeds it by 16 (and where the row sees its first
-  // tokens, and in stages with hidden ones): any reference gives the same quotient, and bf16 and fp32 have the range.
+  // tokens): any reference gives the same quotient, and bf16 and fp32 have the range.
   auto soften = [&](int t0, const uint8_t* lk, uint32_t blocks, bool full) {
     const uint8_t* lv = lk + TOK * KROW;
     const float* ls = reinterpret_cast<const float*>(lv + DP * VROW);
@@ -758,23 +810,26 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
       for (int j = 0; j < 4; ++j) p[4 * q + j] = __builtin_fmaf(p[4 * q + j], x[j], -m);
     }
     uint32_t mask = (uint32_t)(((uint64_t)1 << P) - 1);
-    if (!full) {
-      const int top = lim - t0 - 8 * h, bot = low - t0 - 8 * h;
+    if (!full) {                 // the seen tokens of every eight are those from `from` to before `to`
       mask = 0;
 #pragma unroll
-      for (int k = 0; k < P; ++k) {
-        const int c = 16 * (k >> 3) + (k & 7);
-        if (c <= top && c >= bot && ((blocks >> (k >> 3)) & 1)) mask |= 1u << k;
+      for (int q = 0; q < NB; ++q) {
+        const int to = min(max(lim + 1 - t0 - 8 * h - 16 * q, 0), 8), from = min(max(low - t0 - 8 * h - 16 * q, 0), 8);
+        const uint32_t eight = ((1u << to) - 1) & ~((1u << from) - 1);
+        mask |= ((blocks >> q) & 1 ? eight : 0u) << (8 * q);
       }
 #pragma unroll
       for (int k = 0; k < P; ++k) p[k] = (mask >> k) & 1 ? p[k] : -INFINITY;
+      seen |= mask | (uint32_t)__shfl_xor((int)mask, 32, 64);
+    } else {
+      seen = mask;
     }
     float top = fmaxf(p[0], p[1]);
 #pragma unroll
     for (int k = 2; k < P; ++k) top = fmaxf(top, p[k]);
-    if (!full || !__all(set && top <= 16.0f)) {
+    if (!__all(set && top <= 16.0f)) {
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float delta = set ? fmaxf(top, 0.0f) : top == -INFINITY ? 0.0f : top;
+      const float delta = (set ? top > 16.0f : top != -INFINITY) ? top : 0.0f;     // (by the row alone, whatever the wavefront's others do)
       const float keep = set ? __builtin_amdgcn_exp2f(-delta) : 1.0f;      // (nothing to keep before the first scores)
       set |= top != -INFINITY;
 #pragma unroll
@@ -783,7 +838,6 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
       l *= keep;
 #pragma unroll
       for (int i = 0; i < NK; ++i) acc[i] *= keep;
-      seen |= mask | (uint32_t)__shfl_xor((int)mask, 32, 64);
     }
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -865,15 +919,12 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
   auto sees = [&](int t0) { return t0 < w_end && t0 + TOK > w_begin; };
   auto sees_all = [&](int t0, uint32_t there) { return t0 >= w_all_begin && t0 + TOK <= w_all_end && there == ALL; };
 
-  const int n = t_begin < t_end ? (t_end - t_begin + TOK - 1) / TOK : 0;
-  auto t_of = [&](int s) { return t_begin + s * TOK; };
   place here{0, 0, nullptr};
   if (n > 0) {
-    here = place_of(t_of(0), pages_at(t_of(0)));
+    here = place_of(t_of(0), pages0);
     load_stage(t_of(0), here);
     store_stage(t_of(0), lds8, partly(t_of(0)), here.there);
   }
-  int pages = pages_at(t_of(1));
   uint32_t there = here.there;
   for (int s = 0; s < n; ++s) {
     __syncthreads();
@@ -903,7 +954,6 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
   for (int i = 0; i < NK; ++i)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int d = 32 * i + 8 * q + 4 * h;
       float x[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -913,13 +963,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
           if ((reach[i] >> (16 + 4 * q + j)) & 1) x[j] -= INFINITY;
         }
       }
-      const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-      if (v.d % 4 == 0) {
-        if (d < v.d) *reinterpret_cast<uint2*>(o + d) = w;
-      } else {
-        if (d < v.d) *reinterpret_cast<uint32_t*>(o + d) = w.x;
-        if (d + 2 < v.d) *reinterpret_cast<uint32_t*>(o + d + 2) = w.y;
-      }
+      store_quad(o, v.d, 32 * i + 8 * q + 4 * h, x);
     }
   if (a.lse && h == 0) a.lse[trow * a.heads + head] = any ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
 }
@@ -943,14 +987,11 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
   constexpr int ROWS = 32, TT = 32;
   const kv_view& v = a.v;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5, col = lane & 31;
-  const int kvh = blockIdx.x % v.n_kv_heads, vt = a.tiles - 1 - (int)(blockIdx.x / v.n_kv_heads);
-  auto start = [&](int i) { return ((v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / ROWS + i; };
-  const int b = kv_find_seq(v.n_seqs, vt, start);
-  if (b < 0) return;
-  const kv_rows r = kv_seq_rows(v, b);
-  const int all_rows = r.n * a.group;
-  if (vt - start(b) > (all_rows - 1) / ROWS || all_rows == 0) return;
-  const int row0 = (vt - start(b)) * ROWS;
+  const int kvh = blockIdx.x % v.n_kv_heads;
+  const tile_place w = find_tile<ROWS>(a, blockIdx.x / v.n_kv_heads);
+  if (w.b < 0) return;
+  const kv_rows r = w.r;
+  const int b = w.b, all_rows = r.n * a.group, row0 = w.tile * ROWS;
   const int cap = v.max_pages << v.page_shift, hi = min(r.len, cap);
   auto pos_of = [&](int row) { return r.first + row / a.group; };
   const int rows_here = min(ROWS, all_rows - row0);
@@ -1033,26 +1074,11 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
   int t0 = t_begin + wave * TT;
   pages here = pages_at(t0);
 
-  bf16x8_t qf[NS];               // element of step ks: the keys' pieces of 16 bytes are two steps of INT8, one of bf16
-  {
-    const uint16_t* q = a.Q + trow * a.qs + (size_t)head * v.d;
-    const bool wide = v.d % 8 == 0 && a.qs % 8 == 0;
+  bf16x8_t qf[NS];               // element of step s: the keys' pieces of 16 bytes are two steps of INT8, one of bf16
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const int d = I8 ? (s >> 1) * 32 + h * 16 + (s & 1) * 8 : s * 16 + h * 8;
-      i32x4_t x;                 // (loaded whatever d is, so that no load waits for another)
-      if (wide) {
-        x = *reinterpret_cast<const i32x4_t*>(q + (d < v.d ? d : 0));
-        if (!mine || d >= v.d) x = i32x4_t{0, 0, 0, 0};
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int w = *reinterpret_cast<const int*>(q + (d + 2 * j < v.d ? d + 2 * j : 0));
-          x[j] = mine && d + 2 * j < v.d ? w : 0;
-        }
-      }
-      qf[s] = __builtin_bit_cast(bf16x8_t, x);
-    }
+  for (int s = 0; s < NS; ++s) {
+    const i32x4_t x = row_piece(a.Q + trow * a.qs + (size_t)head * v.d, v.d, I8 ? (s >> 1) * 32 + h * 16 + (s & 1) * 8 : s * 16 + h * 8);
+    qf[s] = __builtin_bit_cast(bf16x8_t, mine ? x : i32x4_t{0, 0, 0, 0});
   }
   f32x16_t acc[NK];
 #pragma unroll
@@ -1242,14 +1268,7 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
     }
     const int row = row0 + rr;
     const size_t at = ((size_t)r.r0 + row / a.group) * a.heads + kvh * a.group + row % a.group;
-    uint16_t* out = a.O + at * v.d + d;
-    const uint2 w = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-    if (v.d % 4 == 0) {
-      if (d < v.d) *reinterpret_cast<uint2*>(out) = w;
-    } else {
-      if (d < v.d) *reinterpret_cast<uint32_t*>(out) = w.x;
-      if (d + 2 < v.d) *reinterpret_cast<uint32_t*>(out + 2) = w.y;
-    }
+    store_quad(a.O + at * v.d, v.d, d, x);
     if (d == 0 && a.lse) a.lse[at] = some ? (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
   }
 }
@@ -1257,8 +1276,10 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
 // Which of the two: tiles of 32 rows up to 16384 rows times heads, half the CUs' worth of tiles of 128.  (32 / 128 rows a tile, INT8, us: 130 rows of
 // 16 heads of 128 9.3 / 11.9; five sequences of 24 rows behind 2000 tokens, 20/4 heads of 128, 29 / 68; 256, 512 and 1024 rows of 32/8 heads of 128
 // 12.4 / 14.5, 23.7 / 21.7 and 55 / 37; 512 and 1024 rows of 32 heads of 64 15.4 / 17.9 and 35.7 / 29.2; 512 rows behind 7680 tokens, 32/8 heads
-// of 128, 157 / 242.)
-bool few_rows(const prefill_args& a) { return (int64_t)a.v.T * a.heads <= 16384; }
+// of 128, 157 / 242.)  And for 16-bit heads beyond 128, where one wavefront a SIMD holds the tile and the barriers of the other kernel cost
+// more than its shared reads save (8192 tokens, 16/4 heads of 160, 192, 224 and 256: 0.80 / 1.08, 1.19 / 1.04, 1.08 / 1.56 and 1.90 / 1.95 ms).
+template <int KIND, int NK>
+bool few_rows(const prefill_args& a) { return (KIND == PQ_KV_BF16 && NK > 4) || (int64_t)a.v.T * a.heads <= 16384; }
 
 // The LDS beyond 64 KiB of a kernel, asked for once on each device.
 int allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& asked) {
@@ -1275,16 +1296,15 @@ int allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& asked) {
 template <int KIND, int NK>
 int launch_prefill_nk(prefill_args a, hipStream_t s) {
   static std::atomic<uint64_t> asked[2];
-  const bool few = few_rows(a);
-  const int rows = few ? 32 : 128;
-  const int64_t tiles = (int64_t)a.v.T * a.group / rows + a.v.n_seqs, grid = tiles * a.v.n_kv_heads;
+  const bool few = few_rows<KIND, NK>(a);
+  const int64_t tiles = (int64_t)a.v.T * a.group / (few ? 32 : 128) + a.v.n_seqs, grid = tiles * a.v.n_kv_heads;
   if (grid > 0x7fffffff) return pq_set_error(PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call", a.v.T, a.heads, a.v.n_seqs);
   a.tiles = (int)tiles;
   if (few) {
     constexpr int lds = rows_lds<KIND, NK>();
     if (int e = allow_lds((const void*)attn_rows_kernel<KIND, NK>, lds, asked[0])) return e;
     attn_rows_kernel<KIND, NK><<<(unsigned)grid, rows_waves<NK>() * 64, lds, s>>>(a);
-  } else {
+  } else if constexpr (KIND == PQ_KV_INT8 || NK <= 4) {
     constexpr int lds = 2 * prefill_stage<KIND, NK>();
     if (int e = allow_lds((const void*)attn_prefill_kernel<KIND, NK>, lds, asked[1])) return e;
     attn_prefill_kernel<KIND, NK><<<(unsigned)grid, 256, lds, s>>>(a);

@@ -1,4 +1,6 @@
 """Attention over the paged key-value cache against the definition in fp64: one token per sequence, and the rows of prompts."""
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -36,8 +38,21 @@ def run_decode(c, Q, H, window=0, max_len=0, scale=None, dev=None, lens=None):
     return O, lse
 
 
-def run_prefill(c, Q, rows, H, causal=True, window=0, scale=None, dev=None, extra=0):
+LEAST_ROWS = 0
+
+
+@pytest.fixture(params=["few", "many"])
+def rows_of_call(request, monkeypatch):
+    """Prompts alone, and followed by so many rows of no sequence that the call counts as one of many rows (another kernel)."""
+    monkeypatch.setattr(sys.modules[__name__], "LEAST_ROWS", 0 if request.param == "few" else 16385)
+
+
+def run_prefill(c, Q, rows, H, causal=True, window=0, scale=None, dev=None):
     cache, dlens, table = dev or c.device()
+    if Q.shape[0] * H < LEAST_ROWS:
+        buf = torch.full((-(-LEAST_ROWS // H), Q.stride(0)), float("nan"), dtype=torch.bfloat16, device="cuda")
+        buf[:Q.shape[0], :H * c.d] = Q.reshape(-1, H * c.d)
+        Q = buf[:, :H * c.d].unflatten(1, (H, c.d))
     desc = pq.make_attn_desc(c.desc(), H, scale=scale, causal=causal, window=window)
     O = torch.full((Q.shape[0], H, c.d), 7.0, dtype=torch.bfloat16, device="cuda")
     lse = torch.full((Q.shape[0], H), 7.0, device="cuda")
@@ -110,12 +125,13 @@ PREFILL = [  # lens, rows, Hk, group, d, page
     ([1], [1], 1, 1, 64, 16), ([5, 0, 17, 40], [5, 0, 17, 40], 2, 1, 64, 16), ([130], [130], 1, 2, 128, 32), ([300, 64], [70, 1], 2, 4, 90, 64),
     ([257, 128, 33], [257, 128, 2], 1, 3, 64, 128), ([150], [150], 1, 5, 256, 16), ([96, 31], [96, 31], 2, 1, 32, 16), ([66], [65], 1, 8, 80, 32),
     ([200], [3], 2, 2, 96, 1024), ([65, 64, 63], [65, 64, 63], 1, 1, 2, 16), ([70], [70], 1, 2, 160, 16), ([140], [139], 1, 1, 224, 64),
-    ([90], [90], 1, 2, 192, 32),
+    ([90], [90], 1, 2, 192, 32), ([9, 70, 0, 33, 1, 64, 128, 5, 0, 31, 90, 200], [9, 60, 0, 33, 1, 64, 100, 2, 0, 31, 90, 33], 2, 2, 64, 16),
 ]
 
 
 @pytest.mark.parametrize("kind", [I8, BF])
 @pytest.mark.parametrize("lens,rows,Hk,G,d,page", PREFILL)
+@pytest.mark.usefixtures("rows_of_call")
 def test_prefill(kind, lens, rows, Hk, G, d, page):
     c = Paged(kind, lens, Hk, d, page, 12)
     Q, q = queries(sum(rows) + 3, Hk * G, d, 5, gap=8 if d % 8 == 0 else 2)
@@ -125,6 +141,7 @@ def test_prefill(kind, lens, rows, Hk, G, d, page):
 
 @pytest.mark.parametrize("kind", [I8, BF])
 @pytest.mark.parametrize("causal,window", [(False, 0), (True, 1), (True, 17), (True, 64), (True, 150)])
+@pytest.mark.usefixtures("rows_of_call")
 def test_prefill_masks(kind, causal, window):
     c = Paged(kind, [260, 64, 100], 2, 64, 16, 3)
     rows = [200, 64, 1]
@@ -134,6 +151,7 @@ def test_prefill_masks(kind, causal, window):
 
 
 @pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.usefixtures("rows_of_call")
 def test_prefill_sharp_flat_and_negative_scores(kind):
     c = Paged(kind, [150], 2, 64, 32, 9, key_scale=4.0)
     for scale, mul in ((3.0, 4.0), (0.0, 1.0), (-0.125, 1.0), (2.0 ** -70, 2.0 ** 70)):
@@ -143,6 +161,7 @@ def test_prefill_sharp_flat_and_negative_scores(kind):
 
 
 @pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.usefixtures("rows_of_call")
 def test_absent_pages_are_attended_by_nobody(kind):
     """Pages without an entry in the middle and at the end of sequences; one sequence without any page; a row before position 0."""
     c = Paged(kind, [200, 70, 40], 2, 64, 16, 3)
@@ -159,6 +178,7 @@ def test_absent_pages_are_attended_by_nobody(kind):
 
 
 @pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.usefixtures("rows_of_call")
 def test_rows_before_the_first_position_and_beyond_the_table(kind):
     """More rows than tokens: the first see nothing.  More tokens than the table holds: those that it holds are attended."""
     c = Paged(kind, [20, 64], 1, 64, 16, 3)
@@ -176,6 +196,7 @@ def test_rows_before_the_first_position_and_beyond_the_table(kind):
 
 
 @pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.usefixtures("rows_of_call")
 def test_tokens_that_are_not_seen_have_no_effect(kind):
     """Infinities and NaN in keys and values behind a row (causal), before its window and behind the sequence's end."""
     lens, rows, window = [150, 40], [130, 40], 40
@@ -207,6 +228,7 @@ def test_tokens_that_are_not_seen_have_no_effect(kind):
 
 
 @pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.usefixtures("rows_of_call")
 def test_queries_that_are_not_finite_spoil_their_own_row_alone(kind):
     c = Paged(kind, [90, 40], 2, 64, 16, 3)
     Q, _ = queries(130, 4, 64, 6)
@@ -296,6 +318,7 @@ def test_calls_on_other_streams_and_a_fused_projection():
     assert (got[0][0].float() - want[0].float()).abs().max() <= 2.0 ** -7 * want[0].float().abs().max()
 
 
+@pytest.mark.usefixtures("rows_of_call")
 def test_scores_of_minus_infinity_come_first():
     """64 seen tokens whose scores are -infinity, then scores around -600: the softmax is that of the later ones."""
     c = Paged(BF, [200], 1, 64, 16, 3)
