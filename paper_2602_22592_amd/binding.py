@@ -487,20 +487,20 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 def _kv_check(kv, cache, lens, page_table, row_start, *others):
     """What the C side of a cache call cannot see: devices, types and sizes of the tensors.  Returns the cache's device, whose current
     stream the call goes to, whichever device is current."""
-    dev, i32 = cache.device, torch.int32
-    B = kv.n_seqs
-    if (lens.dtype != i32 or page_table.dtype != i32 or lens.device != dev or page_table.device != dev or not lens.is_contiguous()
-            or not page_table.is_contiguous() or (row_start is not None and (row_start.dtype != i32 or row_start.device != dev
-                                                                             or not row_start.is_contiguous()))):
+    dev, i32, B = cache.get_device(), torch.int32, kv.n_seqs              # (-1: not on a GPU; a device object takes four times as long)
+    if (lens.dtype is not i32 or page_table.dtype is not i32 or lens.get_device() != dev or page_table.get_device() != dev
+            or not lens.is_contiguous() or not page_table.is_contiguous()):
+        raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
+    if row_start is not None and (row_start.dtype is not i32 or row_start.get_device() != dev or not row_start.is_contiguous()):
         raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
     if lens.numel() < B or page_table.numel() < B * kv.max_pages or (row_start is not None and row_start.numel() < B + 1):
         raise PQError("lens, page_table or row_start is smaller than the descriptor says")
-    if dev.type != "cuda" or cache.dtype != torch.uint8 or not cache.is_contiguous():
+    if dev < 0 or cache.dtype is not torch.uint8 or not cache.is_contiguous():
         raise PQError("the cache is a contiguous uint8 tensor on a GPU")
     for t in others:
-        if t is not None and t.device != dev:
-            raise PQError(f"a tensor on {t.device}, the cache on {dev}")
-    return dev.index
+        if t is not None and t.get_device() != dev:
+            raise PQError(f"a tensor on {t.device}, the cache on {cache.device}")
+    return dev
 
 
 def _kv_call(dev, f, *args):
@@ -522,61 +522,65 @@ def _ptr(t):
 
 def _rows(t, heads, d):
     """Row stride of a [T][heads][d] tensor whose rows are contiguous."""
-    T, *hd = t.shape
-    if hd != [heads, d]:
-        raise PQError(f"a tensor of shape {tuple(t.shape)}: [rows, {heads}, {d}] is wanted")
-    if T <= 1 and t.is_contiguous():
+    s = t.shape
+    if len(s) != 3 or s[1] != heads or s[2] != d:
+        raise PQError(f"a tensor of shape {tuple(s)}: [rows, {heads}, {d}] is wanted")
+    if t.is_contiguous():
         return heads * d
     row, head, one = t.stride()
-    if T and (one != 1 or (heads > 1 and head != d)):
+    if one != 1 or (heads > 1 and head != d):
         raise PQError("the heads of a row must be contiguous")
-    return row if T > 1 else heads * d
+    return row if s[0] > 1 else heads * d
 
 
 def kv_write(desc, K, V, cache, lens, page_table, row_start=None):
     """K, V [T, n_kv_heads, d_head] (bf16 or fp32, any even row stride) into the cache at the last positions of their sequences."""
-    dev = _kv_check(desc, cache, lens, page_table, row_start, K, V)
-    ks, vs = _rows(K, desc.n_kv_heads, desc.d_head), _rows(V, desc.n_kv_heads, desc.d_head)
-    if K.dtype != V.dtype or K.shape[0] != V.shape[0]:
+    dev, heads, d = _kv_check(desc, cache, lens, page_table, row_start, K, V), desc.n_kv_heads, desc.d_head
+    ks, vs, T = _rows(K, heads, d), _rows(V, heads, d), len(K)
+    if K.dtype is not V.dtype or T != len(V):
         raise PQError("K and V differ in type or rows")
-    _kv_call(dev, lib().pq_kv_write, C.byref(desc), K.data_ptr(), V.data_ptr(), _dt(K), K.shape[0], ks, vs, _ptr(row_start), lens.data_ptr(),
+    _kv_call(dev, lib().pq_kv_write, C.byref(desc), K.data_ptr(), V.data_ptr(), _dt(K), T, ks, vs, _ptr(row_start), lens.data_ptr(),
              page_table.data_ptr(), cache.data_ptr(), cache.numel())
     return cache
 
 
 def kv_read(desc, cache, lens, page_table, K, V, row_start=None):
     """The inverse of kv_write, into K and V (either may be None)."""
-    dev = _kv_check(desc, cache, lens, page_table, row_start, K, V)
+    dev, heads, d = _kv_check(desc, cache, lens, page_table, row_start, K, V), desc.n_kv_heads, desc.d_head
     X = K if K is not None else V
     if X is None:
         raise PQError("neither keys nor values are asked for")
-    if K is not None and V is not None and (K.dtype != V.dtype or K.shape[0] != V.shape[0]):
-        raise PQError("K and V differ in type or rows")
-    ks = 0 if K is None else _rows(K, desc.n_kv_heads, desc.d_head)
-    vs = 0 if V is None else _rows(V, desc.n_kv_heads, desc.d_head)
+    ks = vs = _rows(X, heads, d)
+    T = len(X)
+    if V is not None and V is not X:
+        vs = _rows(V, heads, d)
+        if T != len(V) or V.dtype is not X.dtype:
+            raise PQError("K and V differ in type or rows")
     _kv_call(dev, lib().pq_kv_read, C.byref(desc), cache.data_ptr(), cache.numel(), _ptr(row_start), lens.data_ptr(), page_table.data_ptr(),
-             X.shape[0], _ptr(K), _ptr(V), _dt(X), ks, vs)
+             T, _ptr(K), _ptr(V), _dt(X), ks, vs)
     return K, V
 
 
 def _attn_rows(desc, Q, O, lse):
-    qs = _rows(Q, desc.n_heads, desc.kv.d_head)
-    if Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16:
+    H = desc.n_heads
+    qs, n = _rows(Q, H, desc.kv.d_head), Q.numel()
+    if Q.dtype is not torch.bfloat16 or O.dtype is not torch.bfloat16:
         raise PQError("Q and O are bf16")
-    if O.numel() != Q.numel() or not O.is_contiguous():
+    if O.numel() != n or not O.is_contiguous():
         raise PQError("O is contiguous and of Q's size")
-    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != Q.shape[0] * desc.n_heads or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != len(Q) * H or not lse.is_contiguous()):
         raise PQError("lse is a contiguous fp32 tensor of one value per row and head")
     return qs
 
 
 def attn_decode(desc, Q, cache, lens, page_table, O, ws, lse=None):
     """Q [n_seqs, n_heads, d_head] bf16: the last token of every sequence over its whole cache."""
-    dev = _kv_check(desc.kv, cache, lens, page_table, None, Q, O, lse, ws)
-    qs = _attn_rows(desc, Q, O, lse)
-    if Q.shape[0] != desc.kv.n_seqs:
-        raise PQError(f"{Q.shape[0]} rows for {desc.kv.n_seqs} sequences")
-    if ws.dtype != torch.uint8 or not ws.is_contiguous():
+    kv = desc.kv
+    dev = _kv_check(kv, cache, lens, page_table, None, Q, O, lse, ws)
+    qs, T = _attn_rows(desc, Q, O, lse), len(Q)
+    if T != kv.n_seqs:
+        raise PQError(f"{T} rows for {kv.n_seqs} sequences")
+    if ws.dtype is not torch.uint8 or not ws.is_contiguous():
         raise PQError("the workspace is a contiguous uint8 tensor")
     _kv_call(dev, lib().pq_attn_decode, C.byref(desc), Q.data_ptr(), qs, cache.data_ptr(), cache.numel(), lens.data_ptr(), page_table.data_ptr(),
              O.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel())
@@ -585,9 +589,10 @@ def attn_decode(desc, Q, cache, lens, page_table, O, ws, lse=None):
 
 def attn_prefill(desc, Q, cache, lens, page_table, row_start, O, lse=None):
     """Q [T, n_heads, d_head] bf16: the rows of prompts, sequence by sequence (row_start [n_seqs + 1])."""
-    dev = _kv_check(desc.kv, cache, lens, page_table, row_start, Q, O, lse)
-    qs = _attn_rows(desc, Q, O, lse)
-    _kv_call(dev, lib().pq_attn_prefill, C.byref(desc), Q.data_ptr(), qs, Q.shape[0], _ptr(row_start), cache.data_ptr(), cache.numel(),
+    kv = desc.kv
+    dev = _kv_check(kv, cache, lens, page_table, row_start, Q, O, lse)
+    qs, T = _attn_rows(desc, Q, O, lse), len(Q)
+    _kv_call(dev, lib().pq_attn_prefill, C.byref(desc), Q.data_ptr(), qs, T, _ptr(row_start), cache.data_ptr(), cache.numel(),
              lens.data_ptr(), page_table.data_ptr(), O.data_ptr(), _ptr(lse))
     return O
 
