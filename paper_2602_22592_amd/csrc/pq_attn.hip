@@ -482,11 +482,13 @@ decode_plan plan_decode(const pq_attn_desc& d) {
   const int64_t cap = (int64_t)d.kv.max_pages * d.kv.page_tokens;
   int64_t most = d.max_len > 0 && d.max_len < cap ? d.max_len : cap;
   if (d.window > 0 && d.window + (int64_t)63 < most) most = d.window + (int64_t)63;
-  // Pieces (at most MAX_PIECES) for 1024 workgroups, four a CU, so that ragged lengths spread; a piece is worth its start and the second launch from 1024 tokens on, or
-  // from 2048 where whole sequences already occupy every CU.  (64 ragged sequences up to 8192 tokens, 8 heads of 128 in bf16: 151 us whole, 131 in
-  // pieces of 4096; eight of 2048, 32 heads of 64 in INT8: 14.8 us whole, 21.4 in halves; one of 517: 9.1 us whole, 11.7 in thirds.)
-  const int64_t rows = (int64_t)d.kv.n_seqs * d.kv.n_kv_heads * p.head_blocks;
-  const int64_t want = rows > 0 ? (1024 + rows - 1) / rows : 1, least = rows >= 256 ? 2048 : 1024;
+  // Pieces (at most MAX_PIECES): for 256 workgroups, one a CU, where few sequences have whole sequences' worth of work for less; for 1024, which
+  // spread ragged lengths, from 65 rows of key-value heads on.  A piece is worth its start and the second launch from 1024 tokens on, or from
+  // 2048 where whole sequences already occupy every CU.  (256 / 1024 workgroups, us: INT8, 8 heads of 128, one and four sequences of 131072 56 / 70
+  // and 193 / 199, ragged ones in bf16, 4 up to 65536 111 / 125, 8 up to 16384 59 / 67, 16 up to 16384 107 / 95, 64 up to 8192 152 / 133; eight
+  // of 2048, 32 heads of 64 in INT8: 14.8 whole, 21.4 in halves; one of 517: 9.1 whole, 11.7 in thirds.)
+  const int64_t rows = (int64_t)d.kv.n_seqs * d.kv.n_kv_heads * p.head_blocks, all = rows <= 64 ? 256 : 1024;
+  const int64_t want = rows > 0 ? (all + rows - 1) / rows : 1, least = rows >= 256 ? 2048 : 1024;
   int64_t chunk = (most + want - 1) / want;
   if (chunk < least) chunk = least;
   chunk = (chunk + 511) / 512 * 512;
