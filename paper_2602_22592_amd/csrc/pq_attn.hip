@@ -63,7 +63,7 @@ __device__ __forceinline__ decode_range decode_seq(const decode_args& a, int b) 
 }
 
 template <int KIND, int NK, int W>
-__global__ __launch_bounds__(W * 64) void attn_decode_kernel(decode_args a) {
+__global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_decode_kernel(decode_args a) {
   constexpr bool I8 = KIND == PQ_KV_INT8;
   constexpr int DP = NK * 32, ND = DP / 16;
   constexpr int TT = 64;                                      // tokens of a tile
@@ -472,16 +472,18 @@ struct decode_plan { int waves, head_blocks, block_heads, chunk, n_chunks; size_
 decode_plan plan_decode(const pq_attn_desc& d) {
   decode_plan p;
   const int group = d.n_heads / d.kv.n_kv_heads, dp = (d.kv.d_head + 31) / 32 * 32;
+  const int64_t cap = (int64_t)d.kv.max_pages * d.kv.page_tokens;
+  int64_t most = d.max_len > 0 && d.max_len < cap ? d.max_len : cap;
+  if (d.window > 0 && d.window + (int64_t)63 < most) most = d.window + (int64_t)63;
   // Eight wavefronts where two of them on a SIMD hold a tile each in registers, four beyond (heads of 256, INT8: 150 / 510 us for four sequences
-  // of 32768 tokens, 64/8 heads; heads of 128: 200 / 192 us for four of 131072).
-  p.waves = dp <= 128 ? 8 : 4;
+  // of 32768 tokens, 64/8 heads; heads of 128: 200 / 192 us for four of 131072), and four where more heads than CUs leave each little to do
+  // (32 heads of 64, INT8, 8 / 4 wavefronts, us: 8 sequences of 2048 tokens 14.7 / 16.6, 16 of 300 and 2048 12.0 / 8.7 and 28.8 / 25.3, 32 of 4096
+  // 108 / 101; 64 ragged ones up to 8192, 8 heads of 128, 85.6 / 91.5).
+  p.waves = dp <= 128 && !((int64_t)d.kv.n_seqs * d.kv.n_kv_heads > 256 && most <= 4096) ? 8 : 4;
   // a column of the matrix instructions for a head (bf16) or a quad of columns (INT8), and 64 KiB of LDS for the wavefronts' sums
   const int fit = 65536 / (p.waves * (dp + 2) * 4), hb = d.kv.kv_kind == PQ_KV_INT8 ? 4 : fit < 16 ? fit : 16;
   p.head_blocks = (group + hb - 1) / hb;
   p.block_heads = (group + p.head_blocks - 1) / p.head_blocks;
-  const int64_t cap = (int64_t)d.kv.max_pages * d.kv.page_tokens;
-  int64_t most = d.max_len > 0 && d.max_len < cap ? d.max_len : cap;
-  if (d.window > 0 && d.window + (int64_t)63 < most) most = d.window + (int64_t)63;
   // Pieces (at most MAX_PIECES): for 256 workgroups, one a CU, where few sequences have whole sequences' worth of work for less; for 1024, which
   // spread ragged lengths, from 65 rows of key-value heads on.  A piece is worth its start and the second launch from 1024 tokens on, or from
   // 2048 where whole sequences already occupy every CU.  (256 / 1024 workgroups, us: INT8, 8 heads of 128, one and four sequences of 131072 56 / 70
@@ -504,9 +506,13 @@ decode_plan plan_decode(const pq_attn_desc& d) {
 
 template <int KIND, int NK>
 void launch_decode_nk(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {
-  constexpr int W = NK <= 4 ? 8 : 4;
-  const size_t lds = W * (size_t)p.block_heads * (NK * 32 + 2) * 4;
-  attn_decode_kernel<KIND, NK, W><<<grid, W * 64, lds, s>>>(a);
+  const size_t lds = p.waves * (size_t)p.block_heads * (NK * 32 + 2) * 4;
+  if constexpr (NK <= 4)
+    if (p.waves == 8) {
+      attn_decode_kernel<KIND, NK, 8><<<grid, 512, lds, s>>>(a);
+      return;
+    }
+  attn_decode_kernel<KIND, NK, 4><<<grid, 256, lds, s>>>(a);
 }
 template <int KIND>
 void launch_decode(const decode_args& a, const decode_plan& p, unsigned grid, hipStream_t s) {

@@ -67,6 +67,7 @@ DECODE = [  # lens, Hk, group, d, page
     ([1], 1, 1, 64, 16), ([0, 1, 15, 16, 17, 63, 64, 65], 2, 1, 64, 16), ([300, 2, 129], 3, 4, 128, 32), ([77, 500], 2, 5, 90, 64),
     ([1000, 31, 0, 257], 1, 8, 64, 128), ([130], 2, 16, 128, 16), ([200, 64], 1, 20, 32, 16), ([95, 700], 2, 2, 256, 64),
     ([33], 4, 3, 2, 16), ([400, 10], 1, 32, 80, 32), ([90, 128], 2, 7, 96, 1024), ([70, 190], 1, 6, 160, 16), ([333], 2, 9, 224, 32),
+    ([65, 0, 300, 1, 129, 64, 63, 200] * 6, 6, 1, 64, 16), ([65, 0, 300, 1, 129] * 6, 9, 3, 90, 32), ([128, 5, 77] * 10, 9, 1, 128, 16), ([9, 70] * 15, 9, 5, 32, 16),
 ]
 
 
