@@ -480,8 +480,10 @@ def attn_decode_workspace(desc, device="cuda"):
     return _bytes(n, device)
 
 
-# the current stream of a device as an integer; the public call builds a Stream object for it, which takes as long as half a launch
+# the current stream of a device as an integer, and the current device; the public calls build a Stream object and look whether the runtime
+# is up, which takes as long as half a launch
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _kv_check(kv, cache, lens, page_table, row_start, *others):
@@ -505,7 +507,7 @@ def _kv_check(kv, cache, lens, page_table, row_start, *others):
 
 def _kv_call(dev, f, *args):
     """f(*args, stream) with the device current."""
-    now = torch.cuda.current_device()
+    now = _current_device()
     if now == dev:
         _check(f(*args, _raw_stream(dev)))
         return
