@@ -647,11 +647,10 @@ __device__ __forceinline__ tile_place find_tile(const prefill_args& a, int vt) {
     w.tile = __builtin_amdgcn_readlane(before + tiles, w.b) - 1 - vt;
   } else {
     vt = a.tiles - 1 - vt;
-    auto start = [&](int i) { return ((v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T)) * a.group) / ROWS + i; };
-    const int b = kv_find_seq(v.n_seqs, vt, start);
+    auto start = [&](int r0, int i) { return r0 * a.group / ROWS + i; };
+    const int b = kv_find_rows(v, vt, w.r, start);
     if (b < 0) return w;
-    w.r = kv_seq_rows(v, b);
-    w.tile = vt - start(b);
+    w.tile = vt - start(w.r.r0, b);
     if (w.r.n > 0 && w.tile <= (w.r.n * a.group - 1) / ROWS) w.b = b;
   }
   return w;

@@ -64,6 +64,27 @@ __device__ __forceinline__ int kv_find_seq(int n_seqs, int x, F start) {
   return -1;
 }
 
+// The same with the sequence's rows; start(first row of a sequence, its number).  Up to 64 sequences: each lane has one, and what belongs to the
+// one that is found comes from its lane instead of a second read behind the first.
+template <typename F>
+__device__ __forceinline__ int kv_find_rows(const kv_view& v, int x, kv_rows& r, F start) {
+  if (v.n_seqs > 64) {
+    const int b = kv_find_seq(v.n_seqs, x, [&](int i) { return start(v.row_start ? min(max(v.row_start[i], 0), v.T) : min(i, v.T), i); });
+    if (b >= 0) r = kv_seq_rows(v, b);
+    return b;
+  }
+  const int lane = threadIdx.x & 63;
+  const kv_rows mine = kv_seq_rows(v, min(lane, v.n_seqs - 1));
+  const uint64_t hit = __ballot(lane < v.n_seqs && start(min(mine.r0, v.T), lane) <= x);
+  if (hit == 0) return -1;
+  const int b = 63 - __builtin_clzll(hit);
+  r.r0 = __builtin_amdgcn_readlane(mine.r0, b);
+  r.n = __builtin_amdgcn_readlane(mine.n, b);
+  r.len = __builtin_amdgcn_readlane(mine.len, b);
+  r.first = __builtin_amdgcn_readlane(mine.first, b);
+  return b;
+}
+
 // AbsMax INT8 of one row of a head: the code of pq_quant_act.
 __device__ __forceinline__ int kv_code(float x, float gamma) {
   const float r = rintf(x * gamma);

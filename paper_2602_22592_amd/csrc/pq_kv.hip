@@ -33,16 +33,17 @@ __device__ __forceinline__ bool kv_find_unit(const kv_view& v, kv_unit& u) {
   const int64_t vb = (unit >> 1) / groups;
   // Virtual blocks: sequence b owns those from floor(first row / 16) + 2 b, which are at least as many as its rows touch.
   int b = (int)vb, j = 0;
+  kv_rows r;
   if (v.row_start) {
-    auto start = [&](int i) { return (min(max(v.row_start[i], 0), v.T) >> 4) + 2 * i; };
+    auto start = [&](int r0, int i) { return (r0 >> 4) + 2 * i; };
     if (vb > 0x7fffffff) return false;
-    b = kv_find_seq(v.n_seqs, (int)vb, start);
+    b = kv_find_rows(v, (int)vb, r, start);
     if (b < 0) return false;
-    j = (int)vb - start(b);
-  } else if (vb >= v.n_seqs) {
-    return false;
+    j = (int)vb - start(r.r0, b);
+  } else {
+    if (vb >= v.n_seqs) return false;
+    r = kv_seq_rows(v, b);
   }
-  const kv_rows r = kv_seq_rows(v, b);
   if (r.n == 0) return false;
   const int from = max(r.first, 0), block = (from >> 4) + j, p0 = block << 4;
   // rows at negative positions belong to no block: the sequence's first virtual block has them too (they read back as zeros)
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(kv_view v, const T* __res
   constexpr bool I8 = KIND == PQ_KV_INT8;
   const int lane = threadIdx.x & 63;
   kv_unit u;
-  if (!kv_find_unit<LPH>(v, u) || u.page < 0) return;
+  if (!kv_find_unit<LPH>(v, u)) return;
   u.t0 -= u.s0;                                     // (row of the block's first token)
   const int s0 = max(u.s0, 0), s1 = u.s1;
   const int d0 = 2 * (lane % LPH);
@@ -96,6 +97,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(kv_view v, const T* __res
       if (s >= s0 && s < s1 && d0 + 128 * e < v.d) x[s][e] = load_pair<T>(src + (u.t0 + s) * stride + d0 + 128 * e);
     }
   }
+  if (u.page < 0) return;                           // (looked at with the rows under way)
   uint8_t* base = kv_head(v, u.page, head_ok ? u.head : 0);
   if constexpr (I8) {
 #pragma unroll

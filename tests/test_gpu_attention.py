@@ -330,3 +330,45 @@ def test_scores_of_minus_infinity_come_first():
     later = [np.arange(200) >= 64]                             # what counts
     check(*run_prefill(c, Q, [100], 2, scale=1.0), expected(c, q, [100], 1.0, present=later, p_bits=8), "prefill")
     check(*run_decode(c, Q[99:], 2, scale=1.0), expected(c, q[99:], [1], 1.0, present=later, p_bits=15), "decode")
+
+
+@pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.parametrize("T", [120, 9000])
+def test_a_prompt_captured_and_replayed_with_other_lengths(kind, T):
+    """The first call of its kind is a captured one (few rows, many rows); every replay, with other rows, lengths and pages, equals the eager calls."""
+    B, Hk, H, d, page, max_pages = 3, 1, 2, 190, 32, 8
+    n_pages = B * max_pages
+    kv = pq.make_kv_desc(kind, Hk, d, page, n_pages, B, max_pages)
+    at = pq.make_attn_desc(kv, H, window=70)
+    bf = lambda *s: torch.randn(s, device="cuda").bfloat16()
+    K, V, Q = bf(T, Hk, d), bf(T, Hk, d), bf(T, H, d)
+    O, lse, K2, V2 = torch.zeros_like(Q), torch.zeros((T, H), device="cuda"), torch.zeros_like(K), torch.zeros_like(V)
+    cache, lens, rows = pq.kv_cache(kv), t32([100, 15, 0]), t32([0, 80, 95, 95])
+    table = torch.arange(n_pages, dtype=torch.int32, device="cuda").view(B, max_pages).contiguous()
+    cache.zero_()
+
+    def calls(cache, O, lse, K2, V2):
+        pq.kv_write(kv, K, V, cache, lens, table, row_start=rows)
+        pq.attn_prefill(at, Q, cache, lens, table, rows, O, lse=lse)
+        pq.kv_read(kv, cache, lens, table, K2, V2, row_start=rows)
+
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        calls(cache, O, lse, K2, V2)
+    for n, r in (([100, 15, 0], [0, 80, 95, 95]), ([0, 256, 33], [0, 0, 87, 120]), ([40, 40, 40], [0, 40, 80, 120]), ([300, 1, 2], [3, 60, 61, 62])):
+        lens.copy_(t32(n)), rows.copy_(t32(r))
+        table.copy_(torch.randperm(n_pages, device="cuda").int().view(B, max_pages))
+        for x in (K, V, Q):
+            x.normal_()
+        for x in (O, lse, K2, V2):
+            x.fill_(7)
+        own = [cache.clone(), *(x.clone() for x in (O, lse, K2, V2))]
+        torch.cuda.synchronize()
+        graph.replay()
+        calls(*own)
+        torch.cuda.synchronize()
+        for x, y in zip((cache, O, lse, K2, V2), own):
+            assert torch.equal(x, y)
+        assert (O[r[-1]:] == 7).all() and (K2[r[-1]:] == 7).all()
