@@ -85,11 +85,9 @@ __device__ __forceinline__ int kv_find_rows(const kv_view& v, int x, kv_rows& r,
   return b;
 }
 
-// AbsMax INT8 of one row of a head: the code of pq_quant_act.
-__device__ __forceinline__ int kv_code(float x, float gamma) {
-  const float r = rintf(x * gamma);
-  return (int)fminf(fmaxf(r, -128.0f), 127.0f);
-}
+// AbsMax INT8 of one row of a head: the code of pq_quant_act, rint(fl32(x gamma)) between -128 and 127, in the low byte of the result's bits (1.5 2^23
+// + x is rounded to a whole number, ties to even; |x gamma| < 128.5 by gamma's definition, so that only 128 has to be held back).
+__device__ __forceinline__ float kv_code(float x, float gamma) { return fminf(x * gamma, 127.0f) + 12582912.0f; }
 // gamma and step from the largest |x| as fp32 bits (the bits of infinities and NaN are above every finite value's): a row that holds
 // one of them has the step NaN and reads back as NaN.
 __device__ __forceinline__ void kv_scales(uint32_t amax_bits, float& gamma, float& step) {

@@ -56,12 +56,9 @@ __device__ __forceinline__ bool kv_find_unit(const kv_view& v, kv_unit& u) {
   return true;
 }
 
-template <typename T> __device__ __forceinline__ float2 load_pair(const T* p);
-template <> __device__ __forceinline__ float2 load_pair<float>(const float* p) { return *reinterpret_cast<const float2*>(p); }
-template <> __device__ __forceinline__ float2 load_pair<uint16_t>(const uint16_t* p) {
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
-  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-}
+template <typename T> using raw_pair_t = std::conditional_t<std::is_same_v<T, float>, float2, uint32_t>;    // two neighbours as they lie in memory
+__device__ __forceinline__ float2 pair_of(float2 w) { return w; }
+__device__ __forceinline__ float2 pair_of(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 // Past the L2: a wavefront writes whole lines that nobody of this kernel reads, and lines left dirty are written back behind the kernel's end,
 // on time of their own (16 ragged histories of up to 8192 tokens, 8 heads of 128: 52.5 us with ordinary stores, 34.6 with these; not for the
 // cache's own pieces of 2 to 32 bytes a lane: four prompts of 2048 tokens written and read 45.8 us with ordinary stores there, 53.2 with these).
@@ -69,8 +66,8 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void store_pair(float* p, float x, float y) { __builtin_nontemporal_store(f32x2_t{x, y}, reinterpret_cast<f32x2_t*>(p)); }
 __device__ __forceinline__ void store_pair(uint16_t* p, float x, float y) { __builtin_nontemporal_store(pack_bf16x2(x, y), reinterpret_cast<uint32_t*>(p)); }
 
-// Bound by memory: every element is read once and written once.  (Four prompts of 2048 tokens, 32 heads of 64, bf16 to INT8: 102 MB in 28 us, 3.6
-// TB/s; nine ragged ones in fp32 to bf16, 32 heads of 90: 23 us.  16 tokens of an element at a time because they are one piece of the values'
+// Bound by memory: every element is read once and written once.  (Four prompts of 2048 tokens, 32 heads of 64, bf16 to INT8: 102 MB in 26 us, 3.9
+// TB/s; nine ragged ones in fp32 to bf16, 32 heads of 90: 26 us.  16 tokens of an element at a time because they are one piece of the values'
 // layout: written and read back token by token, with stores of 1 and 2 bytes, the same prompts took 358 us, so 46.)
 // A lane holds two neighbouring elements (four beyond 128: E = 2) of all 16 tokens: rows are read a pair of elements a lane, a token's maximum
 // is taken over the lanes for all 16 tokens together, keys leave token by token and values, 16 tokens of an element side by side, as
@@ -87,16 +84,20 @@ __global__ __launch_bounds__(256) void kv_write_kernel(kv_view v, const T* __res
   const bool head_ok = u.head < v.n_kv_heads;
   const int64_t stride = u.which ? vs : ks;
   const T* src = (u.which ? V : K) + (size_t)(head_ok ? u.head : 0) * v.d;
+  // Every load is made, of a row and an element that are there (a load in a branch of its own would be waited for at the branch's end, one
+  // after the other: four prompts of 2048 tokens 36 us, so 26).
+  raw_pair_t<T> raw[16][E];
+#pragma unroll
+  for (int s = 0; s < 16; ++s)
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      raw[s][e] = *reinterpret_cast<const raw_pair_t<T>*>(src + (u.t0 + min(max(s, s0), s1 - 1)) * stride + min(d0 + 128 * e, v.d - 2));
   float2 x[16][E];
   uint32_t top[16];
 #pragma unroll
-  for (int s = 0; s < 16; ++s) {
+  for (int s = 0; s < 16; ++s)
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      x[s][e] = make_float2(0.f, 0.f);
-      if (s >= s0 && s < s1 && d0 + 128 * e < v.d) x[s][e] = load_pair<T>(src + (u.t0 + s) * stride + d0 + 128 * e);
-    }
-  }
+    for (int e = 0; e < E; ++e) x[s][e] = d0 + 128 * e < v.d ? pair_of(raw[s][e]) : make_float2(0.f, 0.f);
   if (u.page < 0) return;                           // (looked at with the rows under way)
   uint8_t* base = kv_head(v, u.page, head_ok ? u.head : 0);
   if constexpr (I8) {
@@ -121,15 +122,15 @@ __global__ __launch_bounds__(256) void kv_write_kernel(kv_view v, const T* __res
       const float g = __shfl(gamma, (lane & ~(LPH - 1)) | i, 64);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        x[i][e].x = __int_as_float(kv_code(x[i][e].x, g));
-        x[i][e].y = __int_as_float(kv_code(x[i][e].y, g));
+        x[i][e].x = kv_code(x[i][e].x, g);
+        x[i][e].y = kv_code(x[i][e].y, g);
       }
     }
   }
   if (!head_ok) return;
   // the two stored numbers of a token, in the low and the high half of a word
   auto two = [&](int s, int e) {
-    if constexpr (I8) return (__float_as_uint(x[s][e].x) & 0xffu) | (__float_as_uint(x[s][e].y) << 16);
+    if constexpr (I8) return __builtin_amdgcn_perm(__float_as_uint(x[s][e].y), __float_as_uint(x[s][e].x), 0x0c040c00u);
     else return pack_bf16x2(x[s][e].x, x[s][e].y);
   };
 #pragma unroll
@@ -142,21 +143,24 @@ __global__ __launch_bounds__(256) void kv_write_kernel(kv_view v, const T* __res
         if (s < s0 || s >= s1) continue;
         const uint32_t w = two(s, e);
         const size_t at = (size_t)(u.slot + s) * v.dp + d;
-        if constexpr (I8) *reinterpret_cast<uint16_t*>(base + at) = (uint16_t)((w & 0xffu) | ((w >> 8) & 0xff00u));
+        if constexpr (I8) *reinterpret_cast<uint16_t*>(base + at) = (uint16_t)(w | w >> 8);
         else *reinterpret_cast<uint32_t*>(base + 2 * at) = w;
       }
     } else if (s1 - s0 == 16) {
-      constexpr int PER = I8 ? 4 : 2, WORDS = 16 / PER;             // tokens a word, words an element
+      constexpr int WORDS = I8 ? 4 : 8;                               // of an element's 16 tokens
       uint32_t lo[WORDS], hi[WORDS];
 #pragma unroll
       for (int j = 0; j < WORDS; ++j) {
-        lo[j] = hi[j] = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const uint32_t w = two(PER * j + i, e);
-          const uint32_t m = I8 ? 0xffu : 0xffffu;
-          lo[j] |= (w & m) << (32 / PER * i);
-          hi[j] |= ((w >> 16) & m) << (32 / PER * i);
+        if constexpr (I8) {
+          auto four = [&](float a, float b, float c, float d) {       // the low bytes
+            return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0c0c0400u) |
+                   __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000c0cu);
+          };
+          lo[j] = four(x[4 * j][e].x, x[4 * j + 1][e].x, x[4 * j + 2][e].x, x[4 * j + 3][e].x);
+          hi[j] = four(x[4 * j][e].y, x[4 * j + 1][e].y, x[4 * j + 2][e].y, x[4 * j + 3][e].y);
+        } else {
+          lo[j] = pack_bf16x2(x[2 * j][e].x, x[2 * j + 1][e].x);
+          hi[j] = pack_bf16x2(x[2 * j][e].y, x[2 * j + 1][e].y);
         }
       }
       uint4* out = reinterpret_cast<uint4*>(base + v.part_bytes + ((size_t)(u.slot / KV_BLOCK) * v.dp + d) * KV_BLOCK * (I8 ? 1 : 2));
@@ -227,7 +231,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(kv_view v, T* __restrict__
           const uint16_t w = *reinterpret_cast<const uint16_t*>(base + at);
           x[s] = make_float2((float)(int8_t)w, (float)(int8_t)(w >> 8));
         } else {
-          x[s] = load_pair<uint16_t>(reinterpret_cast<const uint16_t*>(base) + at);
+          x[s] = pair_of(*reinterpret_cast<const uint32_t*>(base + 2 * at));
         }
       }
     } else {
