@@ -376,8 +376,8 @@ int pq_decode_ffn(const pq_decode_ffn_desc* desc, const void* X, const uint32_t*
  * i * page_tokens .. of sequence b in entry [b][i], lens [n_seqs] int32 its tokens in the cache.  The rows of a call (K, V, Q, O) are
  * given sequence by sequence: rows row_start[b] .. row_start[b + 1] - 1 (row_start [n_seqs + 1] int32, non-decreasing) are the LAST
  * n_b = row_start[b + 1] - row_start[b] tokens of sequence b, at positions lens[b] - n_b .. lens[b] - 1; lens counts them already, in
- * all calls alike.  row_start NULL: row b is the last token of sequence b.  Rows that belong to no sequence (behind
- * row_start[n_seqs]) are neither read nor written, in any call.
+ * all calls alike.  row_start NULL: row b is the last token of sequence b.  Rows that belong to no sequence (before
+ * row_start[0], behind row_start[n_seqs]) are neither read nor written, in any call.
  * lens, row_start and page_table are device memory that no call checks on the host, so that a captured call may be replayed with others;
  * every access stays inside the buffers whatever they hold: a token whose page is not in [0, n_pages), whose position is negative or
  * beyond max_pages * page_tokens, is not written, reads back as zeros and is attended by nobody.
