@@ -486,116 +486,131 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _kv_check(kv, cache, lens, page_table, row_start, *others):
+def _kv_check(kv, cache, lens, page_table, row_start):
     """What the C side of a cache call cannot see: devices, types and sizes of the tensors.  Returns the cache's device, whose current
     stream the call goes to, whichever device is current."""
     dev, i32, B = cache.get_device(), torch.int32, kv.n_seqs              # (-1: not on a GPU; a device object takes four times as long)
     if (lens.dtype is not i32 or page_table.dtype is not i32 or lens.get_device() != dev or page_table.get_device() != dev
             or not lens.is_contiguous() or not page_table.is_contiguous()):
         raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
-    if row_start is not None and (row_start.dtype is not i32 or row_start.get_device() != dev or not row_start.is_contiguous()):
-        raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
-    if lens.numel() < B or page_table.numel() < B * kv.max_pages or (row_start is not None and row_start.numel() < B + 1):
+    if lens.numel() < B or page_table.numel() < B * kv.max_pages:
         raise PQError("lens, page_table or row_start is smaller than the descriptor says")
+    if row_start is not None:
+        if row_start.dtype is not i32 or row_start.get_device() != dev or not row_start.is_contiguous():
+            raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
+        if row_start.numel() < B + 1:
+            raise PQError("lens, page_table or row_start is smaller than the descriptor says")
     if dev < 0 or cache.dtype is not torch.uint8 or not cache.is_contiguous():
         raise PQError("the cache is a contiguous uint8 tensor on a GPU")
-    for t in others:
-        if t is not None and t.get_device() != dev:
-            raise PQError(f"a tensor on {t.device}, the cache on {cache.device}")
     return dev
 
 
-def _kv_call(dev, f, *args):
-    """f(*args, stream) with the device current."""
-    now = _current_device()
-    if now == dev:
-        _check(f(*args, _raw_stream(dev)))
-        return
-    torch.cuda.set_device(dev)
-    try:
-        _check(f(*args, _raw_stream(dev)))
-    finally:
-        torch.cuda.set_device(now)
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
 def _rows(t, heads, d):
-    """Row stride of a [T][heads][d] tensor whose rows are contiguous."""
+    """Rows of a [T][heads][d] tensor whose rows are contiguous, and their stride."""
     s = t.shape
-    if len(s) != 3 or s[1] != heads or s[2] != d:
+    if len(s) != 3:
+        raise PQError(f"a tensor of shape {tuple(s)}: [rows, {heads}, {d}] is wanted")
+    T, h, n = s
+    if h != heads or n != d:
         raise PQError(f"a tensor of shape {tuple(s)}: [rows, {heads}, {d}] is wanted")
     if t.is_contiguous():
-        return heads * d
+        return T, heads * d
     row, head, one = t.stride()
     if one != 1 or (heads > 1 and head != d):
         raise PQError("the heads of a row must be contiguous")
-    return row if s[0] > 1 else heads * d
+    return T, row if T > 1 else heads * d
+
+
+_KV_DT = {torch.float32: PQ_F32, torch.bfloat16: PQ_BF16}
 
 
 def kv_write(desc, K, V, cache, lens, page_table, row_start=None):
     """K, V [T, n_kv_heads, d_head] (bf16 or fp32, any even row stride) into the cache at the last positions of their sequences."""
-    dev, heads, d = _kv_check(desc, cache, lens, page_table, row_start, K, V), desc.n_kv_heads, desc.d_head
-    ks, vs, T = _rows(K, heads, d), _rows(V, heads, d), len(K)
-    if K.dtype is not V.dtype or T != len(V):
-        raise PQError("K and V differ in type or rows")
-    _kv_call(dev, lib().pq_kv_write, C.byref(desc), K.data_ptr(), V.data_ptr(), _dt(K), T, ks, vs, _ptr(row_start), lens.data_ptr(),
-             page_table.data_ptr(), cache.data_ptr(), cache.numel())
+    dev, heads, d = _kv_check(desc, cache, lens, page_table, row_start), desc.n_kv_heads, desc.d_head
+    (T, ks), (Tv, vs), dt = _rows(K, heads, d), _rows(V, heads, d), _KV_DT.get(K.dtype)
+    if K.dtype is not V.dtype or T != Tv or dt is None:
+        raise PQError("K and V differ in type or rows, or are neither fp32 nor bf16")
+    if K.get_device() != dev or V.get_device() != dev:
+        raise PQError("K and V are on the cache's device")
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return kv_write(desc, K, V, cache, lens, page_table, row_start)
+    rc = lib().pq_kv_write(C.byref(desc), K.data_ptr(), V.data_ptr(), dt, T, ks, vs, None if row_start is None else row_start.data_ptr(),
+                           lens.data_ptr(), page_table.data_ptr(), cache.data_ptr(), cache.numel(), _raw_stream(dev))
+    if rc:
+        _check(rc)
     return cache
 
 
 def kv_read(desc, cache, lens, page_table, K, V, row_start=None):
     """The inverse of kv_write, into K and V (either may be None)."""
-    dev, heads, d = _kv_check(desc, cache, lens, page_table, row_start, K, V), desc.n_kv_heads, desc.d_head
-    X = K if K is not None else V
+    dev, heads, d = _kv_check(desc, cache, lens, page_table, row_start), desc.n_kv_heads, desc.d_head
+    X = V if K is None else K
     if X is None:
         raise PQError("neither keys nor values are asked for")
-    ks = vs = _rows(X, heads, d)
-    T = len(X)
-    if V is not None and V is not X:
-        vs = _rows(V, heads, d)
-        if T != len(V) or V.dtype is not X.dtype:
-            raise PQError("K and V differ in type or rows")
-    _kv_call(dev, lib().pq_kv_read, C.byref(desc), cache.data_ptr(), cache.numel(), _ptr(row_start), lens.data_ptr(), page_table.data_ptr(),
-             T, _ptr(K), _ptr(V), _dt(X), ks, vs)
+    (T, ks), dt = _rows(X, heads, d), _KV_DT.get(X.dtype)
+    Tv, vs = (T, ks) if V is None or V is X else _rows(V, heads, d)
+    if dt is None or T != Tv or (V is not None and V.dtype is not X.dtype):
+        raise PQError("K and V differ in type or rows, or are neither fp32 nor bf16")
+    if X.get_device() != dev or (V is not None and V.get_device() != dev):
+        raise PQError("K and V are on the cache's device")
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return kv_read(desc, cache, lens, page_table, K, V, row_start)
+    rc = lib().pq_kv_read(C.byref(desc), cache.data_ptr(), cache.numel(), None if row_start is None else row_start.data_ptr(), lens.data_ptr(),
+                          page_table.data_ptr(), T, None if K is None else K.data_ptr(), None if V is None else V.data_ptr(), dt, ks, vs,
+                          _raw_stream(dev))
+    if rc:
+        _check(rc)
     return K, V
 
 
 def _attn_rows(desc, Q, O, lse):
-    H = desc.n_heads
-    qs, n = _rows(Q, H, desc.kv.d_head), Q.numel()
+    H, d = desc.n_heads, desc.kv.d_head
+    T, qs = _rows(Q, H, d)
     if Q.dtype is not torch.bfloat16 or O.dtype is not torch.bfloat16:
         raise PQError("Q and O are bf16")
-    if O.numel() != n or not O.is_contiguous():
+    if O.numel() != T * H * d or not O.is_contiguous():
         raise PQError("O is contiguous and of Q's size")
-    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != len(Q) * H or not lse.is_contiguous()):
+    dev = Q.get_device()
+    if O.get_device() != dev or (lse is not None and lse.get_device() != dev):
+        raise PQError("Q, O and lse are on one device")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != T * H or not lse.is_contiguous()):
         raise PQError("lse is a contiguous fp32 tensor of one value per row and head")
-    return qs
+    return T, qs
 
 
 def attn_decode(desc, Q, cache, lens, page_table, O, ws, lse=None):
     """Q [n_seqs, n_heads, d_head] bf16: the last token of every sequence over its whole cache."""
     kv = desc.kv
-    dev = _kv_check(kv, cache, lens, page_table, None, Q, O, lse, ws)
-    qs, T = _attn_rows(desc, Q, O, lse), len(Q)
+    dev, (T, qs) = _kv_check(kv, cache, lens, page_table, None), _attn_rows(desc, Q, O, lse)
     if T != kv.n_seqs:
         raise PQError(f"{T} rows for {kv.n_seqs} sequences")
-    if ws.dtype is not torch.uint8 or not ws.is_contiguous():
-        raise PQError("the workspace is a contiguous uint8 tensor")
-    _kv_call(dev, lib().pq_attn_decode, C.byref(desc), Q.data_ptr(), qs, cache.data_ptr(), cache.numel(), lens.data_ptr(), page_table.data_ptr(),
-             O.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel())
+    if Q.get_device() != dev or ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise PQError("the rows and the workspace, a contiguous uint8 tensor, are on the cache's device")
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return attn_decode(desc, Q, cache, lens, page_table, O, ws, lse)
+    rc = lib().pq_attn_decode(C.byref(desc), Q.data_ptr(), qs, cache.data_ptr(), cache.numel(), lens.data_ptr(), page_table.data_ptr(),
+                              O.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev))
+    if rc:
+        _check(rc)
     return O
 
 
 def attn_prefill(desc, Q, cache, lens, page_table, row_start, O, lse=None):
     """Q [T, n_heads, d_head] bf16: the rows of prompts, sequence by sequence (row_start [n_seqs + 1])."""
-    kv = desc.kv
-    dev = _kv_check(kv, cache, lens, page_table, row_start, Q, O, lse)
-    qs, T = _attn_rows(desc, Q, O, lse), len(Q)
-    _kv_call(dev, lib().pq_attn_prefill, C.byref(desc), Q.data_ptr(), qs, T, _ptr(row_start), cache.data_ptr(), cache.numel(),
-             lens.data_ptr(), page_table.data_ptr(), O.data_ptr(), _ptr(lse))
+    dev, (T, qs) = _kv_check(desc.kv, cache, lens, page_table, row_start), _attn_rows(desc, Q, O, lse)
+    if Q.get_device() != dev:
+        raise PQError("the rows are on the cache's device")
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return attn_prefill(desc, Q, cache, lens, page_table, row_start, O, lse)
+    rc = lib().pq_attn_prefill(C.byref(desc), Q.data_ptr(), qs, T, None if row_start is None else row_start.data_ptr(), cache.data_ptr(),
+                               cache.numel(), lens.data_ptr(), page_table.data_ptr(), O.data_ptr(), None if lse is None else lse.data_ptr(),
+                               _raw_stream(dev))
+    if rc:
+        _check(rc)
     return O
 
 

@@ -106,7 +106,7 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         pq._rows(torch.zeros(2, 2, 128)[..., ::2], 2, 64)
     with pytest.raises(pq.PQError, match="contiguous"):
         pq._rows(torch.zeros(2, 64, 2).transpose(1, 2), 2, 64)
-    assert pq._rows(torch.zeros(5, 4, 64)[:, 1:3], 2, 64) == 256 and pq._rows(torch.zeros(1, 2, 64), 2, 64) == 128
+    assert pq._rows(torch.zeros(5, 4, 64)[:, 1:3], 2, 64) == (5, 256) and pq._rows(torch.zeros(1, 2, 64), 2, 64) == (1, 128)
     Q = torch.zeros((2, 4, 64), dtype=torch.bfloat16)
     for bad in (dict(Q=Q.float()), dict(O=Q.float()), dict(O=Q[:1]), dict(lse=torch.zeros(7)), dict(lse=torch.zeros(8, dtype=torch.float64))):
         with pytest.raises(pq.PQError):
