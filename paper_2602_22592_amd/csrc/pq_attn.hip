@@ -490,10 +490,8 @@ decode_plan plan_decode(const pq_attn_desc& d) {
   int64_t most = d.max_len > 0 && d.max_len < cap ? d.max_len : cap;
   if (d.window > 0 && d.window + (int64_t)63 < most) most = d.window + (int64_t)63;
   // Eight wavefronts where two of them on a SIMD hold a tile each in registers, four beyond (heads of 256, INT8: 150 / 510 us for four sequences
-  // of 32768 tokens, 64/8 heads; heads of 128: 200 / 192 us for four of 131072), and four where more heads than CUs leave each little to do
-  // (32 heads of 64, INT8, 8 / 4 wavefronts, us: 8 sequences of 2048 tokens 14.7 / 16.6, 16 of 300 and 2048 12.0 / 8.7 and 28.8 / 25.3, 32 of 4096
-  // 108 / 101; 64 ragged ones up to 8192, 8 heads of 128, 85.6 / 91.5).
-  p.waves = dp <= 128 && !((int64_t)d.kv.n_seqs * d.kv.n_kv_heads > 256 && most <= 4096) ? 8 : 4;
+  // of 32768 tokens, 64/8 heads; heads of 128: 200 / 192 us for four of 131072).
+  p.waves = dp <= 128 ? 8 : 4;
   // a column of the matrix instructions for a head (bf16) or a quad of columns (INT8), and 64 KiB of LDS for the wavefronts' sums
   const int fit = 65536 / (p.waves * (dp + 2) * 4), hb = d.kv.kv_kind == PQ_KV_INT8 ? 4 : fit < 16 ? fit : 16;
   p.head_blocks = (group + hb - 1) / hb;
@@ -510,6 +508,11 @@ decode_plan plan_decode(const pq_attn_desc& d) {
   chunk = (chunk + 511) / 512 * 512;
   p.chunk = (int)chunk;
   p.n_chunks = (int)((most + chunk - 1) / chunk);
+  // And four, two workgroups a CU, where there are more workgroups than CUs with less than 4096 tokens each: one starts while the other ends.  (8 / 4
+  // wavefronts, us.  INT8, 32 heads of 64: 8 sequences of 2048 tokens 14.7 / 16.1, 16 of 300 and 2048 12.0 / 8.7 and 28.8 / 25.3; ragged, 8 heads of
+  // 128: 16 up to 4096 25.7 / 22.6, 24 up to 8192 38.9 / 32.3, 64 up to 8192, in pieces of 4096, 85.6 / 90.3; in bf16 16 up to 16384 95 / 78 and
+  // 65536 233 / 239, 64 up to 8192 133 / 144.)
+  if (p.waves == 8 && rows > 64 && rows * p.n_chunks > 256 && (chunk < most ? chunk : most) < 4096) p.waves = 4;
   const size_t pieces = p.n_chunks > 1 ? (size_t)d.kv.n_seqs * d.n_heads * p.n_chunks : 0;
   p.part_o = 0;
   p.part_ml = pq_align_up(pieces * (size_t)dp * 4, 256);
