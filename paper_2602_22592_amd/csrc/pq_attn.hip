@@ -619,6 +619,9 @@ __device__ __forceinline__ uint2 codes_bf16(int w) {
 }
 __device__ __forceinline__ bool has_nonfinite(uint32_t two) { return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u; }
 
+// The first token that a row at `pos` sees; a window is up to 2^31 - 1 and a position may be negative.
+__device__ __forceinline__ int first_seen(const prefill_args& a, int pos) { return a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0; }
+
 // Which sequence and which of its tiles of ROWS rows workgroup `vt` of the call has (b < 0: none).  Up to 8 sequences are taken in the order of the
 // tokens that their last tiles see, most first, and a sequence's last tiles first, so that long tiles do not start when the others end.  Beyond
 // that: virtual tiles, of which sequence b owns those from floor(first row / ROWS) + b on, at least as many as it has, the last ones first.
@@ -709,7 +712,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
   auto pos_of = [&](int row) { return r.first + row / a.group; };
   const int rows_here = min(ROWS, all_rows - row0);
   const int pos_first = pos_of(row0), pos_last = pos_of(row0 + rows_here - 1);
-  const int t_begin = (a.window > 0 ? max(0, pos_first + 1 - a.window) : 0) & ~(TOK - 1);
+  const int t_begin = first_seen(a, pos_first) & ~(TOK - 1);
   const int t_end = pos_last < 0 ? 0 : a.causal ? min(pos_last + 1, hi) : hi;
 
   // this lane's row, and what the wavefront's rows see between them
@@ -717,11 +720,11 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
   const int row = row0 + (mine ? wave * 32 + col : 0);
   const int pos = mine ? pos_of(row) : -1, head = kvh * a.group + row % a.group;
   const size_t trow = (size_t)r.r0 + row / a.group;
-  const int lim = pos < 0 ? -1 : a.causal ? min(pos, hi - 1) : hi - 1, low = a.window > 0 ? max(0, pos + 1 - a.window) : 0;
+  const int lim = pos < 0 ? -1 : a.causal ? min(pos, hi - 1) : hi - 1, low = first_seen(a, pos);
   const int wfirst = active ? pos_of(row0 + wave * 32) : 0, wlast = active ? pos_of(row0 + min(wave * 32 + 32, rows_here) - 1) : -1;
   const int w_end = wlast < 0 ? 0 : a.causal ? min(wlast + 1, hi) : hi;                 // some row sees up to here
   const int w_all_end = wfirst < 0 ? 0 : a.causal ? min(wfirst + 1, hi) : hi;           // every row sees up to here ..
-  const int w_begin = a.window > 0 ? max(0, wfirst + 1 - a.window) : 0, w_all_begin = a.window > 0 ? max(0, wlast + 1 - a.window) : 0;   // .. from here
+  const int w_begin = first_seen(a, wfirst), w_all_begin = first_seen(a, wlast);   // .. from here
 
   // ---- staging: pages of a stage's blocks of 16 tokens in the first lanes of every wavefront, one stage ahead of the loads
   const int slot_mask = (1 << v.page_shift) - 1;
@@ -836,7 +839,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
     }
   };
   auto partly = [&](int t0) {    // some row of the workgroup does not see all of the stage
-    return t0 + TOK > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || (a.window > 0 && t0 < pos_last + 1 - a.window);
+    return t0 + TOK > (pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi) || t0 < first_seen(a, pos_last);
   };
 
   // A stage for one wavefront is three steps.  Scores are formed transposed (a column is a row of Q): register k of half h is token
@@ -1072,15 +1075,15 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
   const int pos_first = pos_of(row0), pos_last = pos_of(row0 + rows_here - 1);
   const int t_end = pos_last < 0 ? 0 : a.causal ? min(pos_last + 1, hi) : hi;                        // some row sees up to here
   const int all_end = pos_first < 0 ? 0 : a.causal ? min(pos_first + 1, hi) : hi;                    // every row sees up to here ..
-  const int all_begin = a.window > 0 ? max(0, pos_last + 1 - a.window) : 0;                          // .. from here
-  const int t_begin = (a.window > 0 ? max(0, pos_first + 1 - a.window) : 0) & ~(TT - 1);
+  const int all_begin = first_seen(a, pos_last);                                                     // .. from here
+  const int t_begin = first_seen(a, pos_first) & ~(TT - 1);
   const int tiles = t_begin < t_end ? (t_end - t_begin + TT - 1) / TT : 0;
 
   const bool mine = col < rows_here;
   const int row = row0 + (mine ? col : 0);
   const int pos = mine ? pos_of(row) : -1, head = kvh * a.group + row % a.group;
   const size_t trow = (size_t)r.r0 + row / a.group;
-  const int lim = pos < 0 ? -1 : a.causal ? min(pos, hi - 1) : hi - 1, low = a.window > 0 ? max(0, pos + 1 - a.window) : 0;
+  const int lim = pos < 0 ? -1 : a.causal ? min(pos, hi - 1) : hi - 1, low = first_seen(a, pos);
 
   // ---- a tile in registers: keys and values of the lane's row of the operand, and (INT8) the steps of the half's sixteen tokens
   const int slot_mask = (1 << v.page_shift) - 1;
