@@ -71,6 +71,7 @@ __device__ __forceinline__ decode_range decode_seq(const decode_args& a, int b) 
   decode_range r;
   r.hi = min(len, a.v.max_pages << a.v.page_shift);
   r.lo = a.window > 0 ? max(0, len - a.window) : 0;
+  if (r.lo >= r.hi) r.lo = r.hi = 0;   // (sees nothing: a window behind what the table holds may lie at the end of 32 bits)
   r.t0 = r.lo & ~63;
   r.pieces = r.hi <= r.lo ? 1 : min((r.hi - r.t0 + a.chunk - 1) / a.chunk, a.n_chunks);
   return r;

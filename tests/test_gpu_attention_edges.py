@@ -30,3 +30,23 @@ def test_the_largest_windows_hide_nothing(kind, window):
     plain = run_decode(c, Q[:3], 2, dev=dev)
     one = run_decode(c, Q[:3], 2, window=window, dev=dev)
     assert torch.equal(one[0], plain[0]) and torch.equal(one[1], plain[1])
+
+
+@pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.usefixtures("rows_of_call")
+def test_lengths_far_beyond_the_table(kind):
+    """Lengths up to 2^31 - 1: a row whose window lies behind what the table holds sees nothing, one without a window sees what it holds."""
+    c = Paged(kind, [64, 40, 33], 1, 64, 16, 3)
+    cache, _, table = c.device()
+    Q, q = queries(3, 2, 64, 6)
+    lens = t32([MOST, 40, MOST - 64])
+    O, lse = run_decode(c, Q, 2, window=40, dev=(cache, lens, table))
+    want = expected(c, q, [1, 1, 1], 0.125, window=40, p_bits=15, fixed_point=kind == I8)
+    check(O[1:2], lse[1:2], tuple(x[1:2] for x in want), "within the table")
+    assert (O[::2] == 0).all() and torch.isneginf(lse[::2]).all()
+    want = expected(c, q, [1, 1, 1], 0.125, p_bits=15, fixed_point=kind == I8)
+    check(*run_decode(c, Q, 2, dev=(cache, t32([MOST, 40, 33]), table)), want, "no window")
+    O, lse = run_prefill(c, Q, [1, 1, 1], 2, window=40, dev=(cache, lens, table))
+    want = expected(c, q, [1, 1, 1], 0.125, window=40, p_bits=8)
+    check(O[1:2], lse[1:2], tuple(x[1:2] for x in want), "a prompt within the table")
+    assert (O[::2] == 0).all() and torch.isneginf(lse[::2]).all()
