@@ -397,7 +397,7 @@ typedef struct pq_kv_desc {
   int32_t n_kv_heads;  /* key-value heads */
   int32_t d_head;      /* even, 2..256 */
   int32_t page_tokens; /* power of two, 16..1024 */
-  int32_t n_pages;     /* pages in the cache */
+  int32_t n_pages;     /* pages in the cache, of 2^62 bytes together at most */
   int32_t n_seqs;      /* sequences of the call */
   int32_t max_pages;   /* entries of a row of page_table; max_pages * page_tokens <= 2^30 */
 } pq_kv_desc;

@@ -301,6 +301,8 @@ int pq_kv_check(const pq_kv_desc* d) {
   PQ_REQUIRE(d->n_kv_heads <= 65535, PQ_ERR_SHAPE, "n_kv_heads=%d exceeds 65535", d->n_kv_heads);
   PQ_REQUIRE((int64_t)d->max_pages * d->page_tokens <= (1 << 30), PQ_ERR_SHAPE, "max_pages=%d of %d tokens exceed 2^30 tokens a sequence",
              d->max_pages, d->page_tokens);
+  const size_t page = pq_kv_make_view(*d, nullptr, nullptr, nullptr, nullptr, 0).head_bytes * d->n_kv_heads;      // (at most 2^36)
+  PQ_REQUIRE((size_t)d->n_pages <= ((size_t)1 << 62) / page, PQ_ERR_SHAPE, "n_pages=%d of %zu bytes exceed 2^62 bytes", d->n_pages, page);
   return PQ_OK;
 }
 
