@@ -419,8 +419,9 @@ int pq_kv_read(const pq_kv_desc* desc, const void* cache, size_t cache_bytes, co
  *     s_t = scale * q . k_t,    o = sum_t exp(s_t - lse) v_t,    lse = log sum_t exp(s_t),
  * k_t, v_t the values that the cache stands for; scores, sums and lse in fp32, one rounding of o to bf16.  A row that sees nothing has
  * o = 0 and lse = -infinity.  Tokens that a row does not see have no effect on it, whatever they hold; infinities and NaN among those that it
- * sees come out as the formula has them (a row all of whose scores are -infinity, or one of which is +infinity or NaN, is NaN).  The sums of
- * exp(s_t - m) v_t are fp32 with m up to 16 powers of two below the largest s_t: they hold |v| up to 2^80 in any case.
+ * sees come out as the formula has them (a row all of whose scores are -infinity, or one of which is +infinity or NaN, is NaN), an infinite
+ * value however little its token weighs.  The sums of exp(s_t - m) v_t are fp32 with m up to 16 powers of two below the largest s_t: they hold
+ * |v| up to 2^80 in any case.
  * Prompts round exp(s_t - m) (times the value's step) to bf16 for the product, decoding to 2^-16 (bf16 cache) or 2^-22 of the largest.
  * A call takes at most 2^29 rows, rows * n_heads < 2^31.  The result does not depend on the order in which workgroups run. */
 typedef struct pq_attn_desc {

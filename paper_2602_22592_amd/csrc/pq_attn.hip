@@ -53,6 +53,52 @@ __device__ __forceinline__ uint32_t groups_max_u(uint32_t x) {
   return groups_fold(x, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
+// Infinities and NaN among the values that rows see, in a 16-bit cache (a row of an INT8 cache that holds one is NaN as a whole).  A product with
+// a weight of zero, of a token that a row does not see or that fp32 holds no more, would make them NaN, so the products need not get them
+// right: a sum that one of them has entered is never finite again, and a wavefront that ends with such a sum, or that has left some of them out,
+// looks at its tokens a second time, without weights.  What it finds decides those elements.
+// Over tiles of 32 tokens from `from` (a multiple of 32) to before `to`, `step` apart: found(t0, up, down) where there are any, of element lane +
+// 64 w in word w: which of the tile's tokens are +infinity or NaN, and which -infinity or NaN.
+template <int NK, typename F>
+__device__ __forceinline__ void find_nonfinite(const kv_view& v, int b, int kvh, int from, int to, int step, F found) {
+  constexpr int NW = (NK + 1) / 2;
+  const int lane = threadIdx.x & 63;
+#pragma unroll 1
+  for (int t0 = from; t0 < to; t0 += step) {
+    uint32_t up[NW], down[NW], any = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) up[w] = down[w] = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = t0 + 16 * i, page = t < to ? kv_page_id(v, b, t) : -1;
+      if (page < 0) continue;
+      const uint8_t* at = kv_head(v, page, kvh) + v.part_bytes + (size_t)(t & ((1 << v.page_shift) - 1)) * (NK * 64);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const int d = lane + 64 * w;
+        if (d >= NK * 32) continue;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const i32x4_t x = reinterpret_cast<const i32x4_t*>(at + d * 32)[j];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float y = __uint_as_float(k & 1 ? (uint32_t)x[k >> 1] & 0xffff0000u : (uint32_t)x[k >> 1] << 16);
+            up[w] |= (uint32_t)!(y < INFINITY) << (16 * i + 8 * j + k);
+            down[w] |= (uint32_t)!(y > -INFINITY) << (16 * i + 8 * j + k);
+          }
+        }
+        any |= up[w] | down[w];
+      }
+    }
+    if (__any(any != 0)) found(t0, up, down);
+  }
+}
+// Tokens t0 .. t0 + 31 as a mask, those from lo to before hi.
+__device__ __forceinline__ uint32_t tokens_within(int t0, int lo, int hi) {
+  const int a = min(max(lo - t0, 0), 32), z = min(max(hi - t0, 0), 32);
+  return (uint32_t)(((uint64_t)1 << z) - 1) & ~(uint32_t)(((uint64_t)1 << a) - 1);
+}
+
 struct decode_args {
   kv_view v;
   const uint16_t* Q;
@@ -623,6 +669,42 @@ __device__ __forceinline__ bool has_nonfinite(uint32_t two) { return (two & 0x7f
 // The first token that a row at `pos` sees; a window is up to 2^31 - 1 and a position may be negative.
 __device__ __forceinline__ int first_seen(const prefill_args& a, int pos) { return a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0; }
 
+// Elements of the 32x32 products' columns (register 4 q + j of half h of block i is element 32 i + 8 q + 4 h + j) that infinities and NaN which
+// the column's row sees reach: bit 4 q + j of reach[i] for +infinity, of its high half for -infinity, both for NaN.  The row sees tokens `low` .. `lim`.
+template <int NK>
+__device__ __forceinline__ void find_reach(const kv_view& v, int b, int kvh, int from, int to, int step, int low, int lim, uint32_t* reach) {
+  const int h = (threadIdx.x & 63) >> 5;
+  find_nonfinite<NK>(v, b, kvh, from, to, step, [&](int t0, const uint32_t* up, const uint32_t* down) {
+    const uint32_t mask = tokens_within(t0, low, lim + 1);
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll 1
+      for (int k = 0; k < 16; ++k) {
+        const int from_lane = 32 * (i & 1) + 8 * (k >> 2) + 4 * h + (k & 3);
+        const uint32_t u = (uint32_t)__shfl((int)up[i >> 1], from_lane, 64) & mask, d = (uint32_t)__shfl((int)down[i >> 1], from_lane, 64) & mask;
+        reach[i] |= ((u ? 1u : 0u) | (d ? 0x10000u : 0u)) << k;
+      }
+  });
+}
+// Whether one of the lane's sums is infinite or NaN.
+template <int NK>
+__device__ __forceinline__ bool any_nonfinite(const f32x16_t* acc) {
+  float z = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) z = __builtin_fmaf(acc[i][j], 0.0f, z);
+  return z != 0.0f;              // (NaN: not equal)
+}
+// An element from its sum and the inverse of the row's: what reaches it decides, in a row that is not NaN by its scores (inv: NaN, or infinite where
+// all of them are -infinity).
+__device__ __forceinline__ float settle(float sum, float inv, bool up, bool down) {
+  float x = up || down ? inv * 0.0f : sum * inv;
+  if (up) x += INFINITY;
+  if (down) x -= INFINITY;
+  return x;
+}
+
 // Which sequence and which of its tiles of ROWS rows workgroup `vt` of the call has (b < 0: none).  Up to 8 sequences are taken in the order of the
 // tokens that their last tiles see, most first, and a sequence's last tiles first, so that long tiles do not start when the others end.  Beyond
 // that: virtual tiles, of which sequence b owns those from floor(first row / ROWS) + b on, at least as many as it has, the last ones first.
@@ -849,10 +931,8 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
   constexpr int P = 16 * U;      // tokens of a lane in a stage
   float p[P];
   bf16x8_t pb[NB];
-  bool bad = false;              // values that are not finite in a stage that some row sees a part of
-  uint32_t reach[NK];            // the elements that +infinity (low half) and -infinity reach there; NaN is both
-#pragma unroll
-  for (int i = 0; i < NK; ++i) reach[i] = 0;
+  bool bad = false;              // values that are not finite in a stage that some row sees a part of: the product leaves them out
+  bool left_out = false;
   auto scores = [&](const uint8_t* lk) {
     f32x16_t S[U];
 #pragma unroll
@@ -945,24 +1025,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
 #pragma unroll
         for (int w = 0; w < W; ++w) any |= f[w];
         bad = __builtin_amdgcn_readfirstlane(any) != 0;
-        if (bad) {               // the product leaves them out; which elements of which rows they reach is noted
-          const uint32_t other = (uint32_t)__shfl_xor((int)mask, 32, 64);
-#pragma unroll
-          for (int i = 0; i < NK; ++i)
-#pragma unroll 1
-            for (int j = 0; j < 16; ++j) {
-              const uint16_t* x = reinterpret_cast<const uint16_t*>(lv + (32 * i + 8 * (j >> 2) + 4 * h + (j & 3)) * VROW);
-              bool up = false, down = false;
-#pragma unroll 1
-              for (int k = 0; k < P; ++k) {
-                const float x0 = bf16_to_f32(x[16 * (k >> 3) + (k & 7) + 8 * h]), x1 = bf16_to_f32(x[16 * (k >> 3) + (k & 7) + 8 * (h ^ 1)]);
-                const bool see0 = (mask >> k) & 1, see1 = (other >> k) & 1;
-                up |= (see0 && !(x0 < INFINITY)) || (see1 && !(x1 < INFINITY));
-                down |= (see0 && !(x0 > -INFINITY)) || (see1 && !(x1 > -INFINITY));
-              }
-              reach[i] |= ((uint32_t)up | (uint32_t)down << 16) << j;
-            }
-        }
+        left_out |= bad;
       }
   };
   auto values = [&](const uint8_t* lk) {
@@ -1020,6 +1083,12 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
     if (s + 1 < n) store_stage(t_of(s + 1), lds8 + (~s & 1) * STAGE, partly(t_of(s + 1)), next);
     there = next;
   }
+  uint32_t reach[NK];
+  if constexpr (!I8) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) reach[i] = 0;
+    if (__any(left_out || any_nonfinite<NK>(acc))) find_reach<NK>(v, b, kvh, w_begin & ~31, w_end, 32, low, lim, reach);
+  }
   if (!mine) return;
   // ---- every column is a row: register 4 q + j of half h is element 8 q + 4 h + j of each 32
   l += __shfl_xor(l, 32, 64);
@@ -1033,11 +1102,8 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
       float x[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[j] = any ? acc[i][4 * q + j] * inv : 0.0f;
-        if constexpr (!I8) {
-          if ((reach[i] >> (4 * q + j)) & 1) x[j] += INFINITY;
-          if ((reach[i] >> (16 + 4 * q + j)) & 1) x[j] -= INFINITY;
-        }
+        if constexpr (I8) x[j] = any ? acc[i][4 * q + j] * inv : 0.0f;
+        else x[j] = any ? settle(acc[i][4 * q + j], inv, (reach[i] >> (4 * q + j)) & 1, (reach[i] >> (16 + 4 * q + j)) & 1) : 0.0f;
       }
       store_quad(o, v.d, 32 * i + 8 * q + 4 * h, x);
     }
@@ -1164,9 +1230,8 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
   float m = -INFINITY, l = 0.0f;
-  uint32_t seen = 0, reach[NK];  // (reach: as in the kernel above)
-#pragma unroll
-  for (int i = 0; i < NK; ++i) reach[i] = 0;
+  uint32_t seen = 0;
+  bool left_out = false;         // values that are not finite in a tile that some row sees a part of: the product leaves them out
 
   uint32_t there = there_of(here);
   if (t0 < t_end) {
@@ -1246,26 +1311,8 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
               bad |= has_nonfinite((uint32_t)vf[q * NK + i][j]);
             }
         }
-        if (__any(bad)) {        // the product leaves them out; which elements of which rows they reach is noted
-          const uint32_t other = (uint32_t)__shfl_xor((int)mask, 32, 64);
-          const uint8_t* p0 = page_of(here, there, 0) + v.part_bytes + (t0 & slot_mask) * (DP * ES);
-          const uint8_t* p1 = page_of(here, there, 1) + v.part_bytes + ((t0 + 16) & slot_mask) * (DP * ES);
-#pragma unroll
-          for (int i = 0; i < NK; ++i)
-#pragma unroll 1
-            for (int j = 0; j < 16; ++j) {
-              const int d = 32 * i + 8 * (j >> 2) + 4 * h + (j & 3);
-              bool up = false, down = false;
-#pragma unroll 1
-              for (int k = 0; k < 16; ++k) {
-                const uint16_t* x = reinterpret_cast<const uint16_t*>(k >> 3 ? p1 : p0) + d * 16 + (k & 7);
-                const float x0 = bf16_to_f32(x[8 * h]), x1 = bf16_to_f32(x[8 * (h ^ 1)]);
-                const bool see0 = (mask >> k) & 1, see1 = (other >> k) & 1;
-                up |= (see0 && !(x0 < INFINITY)) || (see1 && !(x1 < INFINITY));
-                down |= (see0 && !(x0 > -INFINITY)) || (see1 && !(x1 > -INFINITY));
-              }
-              reach[i] |= ((uint32_t)up | (uint32_t)down << 16) << j;
-            }
+        if (__any(bad)) {
+          left_out = true;
 #pragma unroll
           for (int i = 0; i < NF; ++i)
 #pragma unroll
@@ -1302,6 +1349,12 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
   uint32_t* lr = reinterpret_cast<uint32_t*>(ml + W * ROWS * 2);
   if (wave < tiles) {
     l += __shfl_xor(l, 32, 64);
+    uint32_t reach[NK];
+    if constexpr (!I8) {
+#pragma unroll
+      for (int i = 0; i < NK; ++i) reach[i] = 0;
+      if (__any(left_out || any_nonfinite<NK>(acc))) find_reach<NK>(v, b, kvh, t_begin + wave * TT, t_end, W * TT, low, lim, reach);
+    }
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
 #pragma unroll
@@ -1338,11 +1391,8 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
     float x[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      x[j] = some ? o[j] * inv : 0.0f;
-      if constexpr (!I8) {
-        if ((hit >> j) & 1) x[j] += INFINITY;
-        if ((hit >> (16 + j)) & 1) x[j] -= INFINITY;
-      }
+      if constexpr (I8) x[j] = some ? o[j] * inv : 0.0f;
+      else x[j] = some ? settle(o[j], inv, (hit >> j) & 1, (hit >> (16 + j)) & 1) : 0.0f;
     }
     const int row = row0 + rr;
     const size_t at = ((size_t)r.r0 + row / a.group) * a.heads + kvh * a.group + row % a.group;
