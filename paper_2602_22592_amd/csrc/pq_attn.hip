@@ -99,6 +99,11 @@ __device__ __forceinline__ uint32_t tokens_within(int t0, int lo, int hi) {
   return (uint32_t)(((uint64_t)1 << z) - 1) & ~(uint32_t)(((uint64_t)1 << a) - 1);
 }
 
+// Sums of pieces join by weight; one that an infinity or a NaN decides keeps it whatever its piece weighs.
+__device__ __forceinline__ float join_sum(float o, float x, float weight) { return o + (__builtin_isfinite(x) ? x * weight : x); }
+// (a row all of whose scores are -infinity, sum 0, is NaN)
+__device__ __forceinline__ float quotient(float o, float sum) { return sum == 0.0f ? __uint_as_float(0x7fc00000u) : o / sum; }
+
 struct decode_args {
   kv_view v;
   const uint16_t* Q;
@@ -422,11 +427,16 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_decode_kernel(de
   // ---- the wavefronts' pieces are joined through the LDS: [wave][head][dp] sums, then maximum, sum and "saw a token"
   extern __shared__ float lds[];
   float* ml = lds + (size_t)W * n_heads * DP;
+  __shared__ uint32_t marks[I8 ? 1 : DP], odd[W];    // (16 bits) elements that +infinity (1), -infinity (2) or NaN (both) reaches; a wavefront has some
   const bool any = __any(seen != 0);
   const float sum = groups_sum(l);
+  float zero = 0.0f;             // NaN if one of the sums is not finite
 #pragma unroll
   for (int i = 0; i < ND; ++i) {
     f32x4_t x = acc[i];
+    if constexpr (!I8)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) zero = __builtin_fmaf(x[j], 0.0f, zero);
     if constexpr (I8)
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = quad_sum(x[j]);
@@ -436,7 +446,30 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_decode_kernel(de
     ml[(wave * n_heads + hl) * 2] = m;
     ml[(wave * n_heads + hl) * 2 + 1] = any ? sum : -1.0f;   // (a sum is never negative)
   }
+  if constexpr (!I8) {
+    const bool mine_odd = __any(zero != 0.0f);
+    if (lane == 0) odd[wave] = mine_odd;
+  }
   __syncthreads();
+  bool marked = false;
+  if constexpr (!I8) {           // (the same for all heads: they see the same tokens)
+#pragma unroll
+    for (int w = 0; w < W; ++w) marked |= odd[w] != 0;
+    if (marked) {
+      for (int d = threadIdx.x; d < DP; d += W * 64) marks[d] = 0;
+      __syncthreads();
+      const int from = max(R.lo, begin);
+      find_nonfinite<NK>(v, b, kvh, (from & ~31) + 32 * wave, end, 32 * W, [&](int t0, const uint32_t* up, const uint32_t* down) {
+        const uint32_t mask = tokens_within(t0, from, end);
+#pragma unroll
+        for (int w = 0; w < (NK + 1) / 2; ++w) {
+          const uint32_t bits = (up[w] & mask ? 1u : 0u) | (down[w] & mask ? 2u : 0u);
+          if (bits) atomicOr(&marks[lane + 64 * w], bits);
+        }
+      });
+      __syncthreads();
+    }
+  }
   const bool whole = R.pieces == 1;
   for (int e = threadIdx.x; e < n_heads * DP; e += blockDim.x) {
     const int hl = e / DP, d = e % DP;
@@ -453,9 +486,11 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_decode_kernel(de
       sum += lw * f;
       o += lds[((size_t)w * n_heads + hl) * DP + d] * f;
     }
+    if constexpr (!I8)
+      if (marked && marks[d]) o = (marks[d] & 1 ? INFINITY : 0.0f) - (marks[d] & 2 ? INFINITY : 0.0f);
     const int h = first_head + hl;
     if (whole) {
-      if (d < v.d) a.O[((size_t)b * a.heads + h) * v.d + d] = f32_to_bf16(some ? o / sum : 0.0f);
+      if (d < v.d) a.O[((size_t)b * a.heads + h) * v.d + d] = f32_to_bf16(some ? quotient(o, sum) : 0.0f);
       if (d == 0 && a.lse) a.lse[(size_t)b * a.heads + h] = some ? (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
     } else {
       const size_t at = ((size_t)b * a.heads + h) * a.n_chunks + z;
@@ -508,13 +543,13 @@ __global__ __launch_bounds__(256) void attn_join_kernel(decode_args a, int width
     const int z = g0 + i * groups;
     if (z < R.pieces) {
       sum += part_l[z];
-      o += early[i] * weight[z];
+      o = join_sum(o, early[i], weight[z]);
     }
   }
 #pragma unroll 8
   for (int z = g0 + EARLY * groups; z < R.pieces; z += groups) {
     sum += part_l[z];
-    o += po[(size_t)z * a.v.dp + min(d, a.v.dp - 1)] * weight[z];
+    o = join_sum(o, po[(size_t)z * a.v.dp + min(d, a.v.dp - 1)], weight[z]);
   }
   part[0][t] = o;
   part[1][t] = sum;
@@ -524,7 +559,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(decode_args a, int width
     o += part[0][g * width + d];
     sum += part[1][g * width + d];
   }
-  if (d < a.v.d) a.O[((size_t)b * a.heads + h) * a.v.d + d] = f32_to_bf16(some ? o / sum : 0.0f);
+  if (d < a.v.d) a.O[((size_t)b * a.heads + h) * a.v.d + d] = f32_to_bf16(some ? quotient(o, sum) : 0.0f);
   if (d == 0 && a.lse) a.lse[(size_t)b * a.heads + h] = some ? (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
 }
 
@@ -539,8 +574,9 @@ decode_plan plan_decode(const pq_attn_desc& d) {
   // Eight wavefronts where two of them on a SIMD hold a tile each in registers, four beyond (heads of 256, INT8: 150 / 510 us for four sequences
   // of 32768 tokens, 64/8 heads; heads of 128: 200 / 192 us for four of 131072).
   p.waves = dp <= 128 ? 8 : 4;
-  // a column of the matrix instructions for a head (bf16) or a quad of columns (INT8), and 64 KiB of LDS for the wavefronts' sums
-  const int fit = 65536 / (p.waves * (dp + 2) * 4), hb = d.kv.kv_kind == PQ_KV_INT8 ? 4 : fit < 16 ? fit : 16;
+  // a column of the matrix instructions for a head (bf16) or a quad of columns (INT8), and 64 KiB of LDS for the wavefronts' sums and the marks
+  // (at most 1040 bytes)
+  const int fit = (65536 - 2048) / (p.waves * (dp + 2) * 4), hb = d.kv.kv_kind == PQ_KV_INT8 ? 4 : fit < 16 ? fit : 16;
   p.head_blocks = (group + hb - 1) / hb;
   p.block_heads = (group + p.head_blocks - 1) / p.head_blocks;
   // Pieces (at most MAX_PIECES): for 256 workgroups, one a CU, where few sequences have whole sequences' worth of work for less; for 1024, which

@@ -87,6 +87,19 @@ def check_nonfinite(O, lse, ref, name):
 @pytest.mark.filterwarnings("ignore::RuntimeWarning")
 @pytest.mark.parametrize("kind", [I8, BF])
 @pytest.mark.parametrize("weight", list(WEIGHTS))
+@pytest.mark.parametrize("L,shift,d,window", [(200, 0, 64, 0), (200, 0, 64, 90), (203, 0, 90, 0), (2600, 2300, 64, 0), (4500, 100, 64, 0), (200, 0, 160, 0)])
+def test_decode_infinities_that_are_seen(kind, weight, L, shift, d, window):
+    """Whole sequences and pieces, whatever the tokens weigh."""
+    c = with_infinities(kind, L, weight, Hk=2, d=d, shift=shift)
+    Q, q = queries(1, 6, d, 6)
+    Q[..., 0], q[..., 0] = 1.0, 1.0
+    O, lse = run_decode(c, Q, 6, window=window, scale=0.125)
+    check_nonfinite(O, lse, expected(c, q, [1], 0.125, window=window, p_bits=15, fixed_point=kind == I8), f"{weight} {L}")
+
+
+@pytest.mark.filterwarnings("ignore::RuntimeWarning")
+@pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.parametrize("weight", list(WEIGHTS))
 @pytest.mark.parametrize("rows,G,d,causal,window", [(200, 1, 64, True, 0), (61, 3, 64, True, 0), (200, 2, 64, True, 50), (40, 2, 90, False, 0), (70, 1, 160, True, 100)])
 @pytest.mark.usefixtures("rows_of_call")
 def test_prompt_infinities_that_are_seen(kind, weight, rows, G, d, causal, window):
