@@ -94,6 +94,12 @@ class CachedAttention:
     def __init__(self, weights, n_heads, n_kv_heads, n_pages, n_seqs, max_pages, page_tokens=64, kv_kind=pq.PQ_KV_INT8, max_len=0,
                  device="cuda"):
         d = weights["Wq"].shape[1]
+        if n_heads < 1 or n_kv_heads < 1 or d % n_heads or n_heads % n_kv_heads:
+            raise pq.PQError(f"d_model={d} is a multiple of n_heads={n_heads}, and that of n_kv_heads={n_kv_heads}")
+        for n in ("q", "k", "v", "o"):
+            W, rows = weights["W" + n], d if n in "qo" else n_kv_heads * (d // n_heads)
+            if W.shape != (rows, d) or not W.is_contiguous():
+                raise pq.PQError(f"W{n} of shape {tuple(W.shape)}: a contiguous [{rows}, {d}] is wanted")
         self.d, self.H, self.Hk, self.dh, self.B = d, n_heads, n_kv_heads, d // n_heads, n_seqs
         self.packed = {}
         for n in ("q", "k", "v", "o"):
@@ -110,12 +116,17 @@ class CachedAttention:
         self.decode_ws = {n: pq.decode_workspace(dd, device) for n, dd in self.decode.items()}
         self.attn_ws = pq.attn_decode_workspace(self.attn, device)
 
+    def _check(self, x, T):
+        if x.shape != (T, self.d) or x.dtype is not torch.bfloat16 or not x.is_contiguous() or x.get_device() != self.cache.get_device():
+            raise pq.PQError(f"a tensor of shape {tuple(x.shape)}: a contiguous bf16 [{T}, {self.d}] on the cache's device is wanted")
+
     def _heads(self, x, heads):
         return x.view(x.shape[0], heads, self.dh)
 
     def prompt(self, x, lens, page_table, row_start):
-        """x [T, d] bf16: the last row_start[b + 1] - row_start[b] tokens of every sequence.  Returns [T, d]."""
-        T = x.shape[0]
+        """x [T, d] bf16: the last row_start[b + 1] - row_start[b] tokens of every sequence.  Returns [T, d]; rows of no sequence are undefined."""
+        T = x.shape[0] if x.dim() else 0
+        self._check(x, T)
 
         def linear(n, x):
             N, P, ml, _, _ = self.packed[n]
@@ -131,6 +142,8 @@ class CachedAttention:
     def token(self, x, lens, page_table, out):
         """x [n_seqs, d] bf16: the newest token of every sequence, counted in lens already.  Writes out [n_seqs, d]."""
         s = self.step
+        self._check(x, self.B)
+        self._check(out, self.B)
 
         def linear(n, x):
             _, _, _, tiled, scale = self.packed[n]

@@ -2,8 +2,10 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2602_22592_amd import binding as pq
+from paper_2602_22592_amd.stack import CachedAttention
 from test_attention_refusals import BF, big, fake, kv, lib  # noqa: F401  (lib: fixture)
 
 
@@ -22,3 +24,27 @@ def test_caches_whose_size_passes_64_bits_are_refused(lib, Hk, n_pages):  # noqa
 def test_the_largest_cache_is_counted_whole(lib):  # noqa: F811
     d = kv(kind=BF, Hk=32768, d=256, page=1024, n_pages=2 ** 27)
     assert lib.pq_kv_cache_bytes(C.byref(d)) == 2 ** 62
+
+
+def test_the_layer_refuses_weights_and_rows_that_do_not_fit():
+    """Before anything is packed or launched: heads that do not divide the width, weights of another shape, rows that are not contiguous."""
+    W = {"W" + n: torch.zeros((512 if n in "qo" else 128, 512), dtype=torch.bfloat16) for n in "qkvo"}
+    pages = dict(n_pages=4, n_seqs=2, max_pages=2, device="cpu")
+    for heads, kv_heads in ((7, 1), (12, 4), (8, 3), (0, 1), (8, 0)):
+        with pytest.raises(pq.PQError, match="multiple of n_heads"):
+            CachedAttention(W, heads, kv_heads, **pages)
+    with pytest.raises(pq.PQError, match="Wk of shape"):
+        CachedAttention(W, 8, 4, **pages)                                 # (its keys have 256 elements, not 128)
+    with pytest.raises(pq.PQError, match="Wo of shape"):
+        CachedAttention({**W, "Wo": W["Wo"].t()}, 8, 2, **pages)
+    layer = CachedAttention.__new__(CachedAttention)
+    layer.d, layer.B, layer.cache = 512, 2, torch.zeros(256, dtype=torch.uint8)
+    x = torch.zeros((2, 512), dtype=torch.bfloat16)
+    for bad in (torch.zeros((2, 1024), dtype=torch.bfloat16)[:, ::2], x.float(), x[:1], torch.zeros((512, 2), dtype=torch.bfloat16).t(), x[0]):
+        for call in (lambda: layer.token(bad, None, None, x), lambda: layer.token(x, None, None, bad)):
+            layer.step = {}
+            with pytest.raises(pq.PQError, match="is wanted"):
+                call()
+    for bad in (torch.zeros((9, 1024), dtype=torch.bfloat16)[:, :512], x.float(), x[0], x[0, 0]):
+        with pytest.raises(pq.PQError, match="is wanted"):
+            layer.prompt(bad, None, None, None)
