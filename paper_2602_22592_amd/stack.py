@@ -100,6 +100,10 @@ class CachedAttention:
             W, rows = weights["W" + n], d if n in "qo" else n_kv_heads * (d // n_heads)
             if W.shape != (rows, d) or not W.is_contiguous():
                 raise pq.PQError(f"W{n} of shape {tuple(W.shape)}: a contiguous [{rows}, {d}] is wanted")
+        dev, want = weights["Wq"].device, torch.device(device)
+        if dev.type != "cuda" or want.type != "cuda" or want.index not in (None, dev.index) or any(weights["W" + n].device != dev for n in "kvo"):
+            raise pq.PQError(f"the weights are on one GPU, that of device={device}")
+        device = dev
         self.d, self.H, self.Hk, self.dh, self.B = d, n_heads, n_kv_heads, d // n_heads, n_seqs
         self.packed = {}
         for n in ("q", "k", "v", "o"):

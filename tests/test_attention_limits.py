@@ -48,3 +48,10 @@ def test_the_layer_refuses_weights_and_rows_that_do_not_fit():
     for bad in (torch.zeros((9, 1024), dtype=torch.bfloat16)[:, :512], x.float(), x[0], x[0, 0]):
         with pytest.raises(pq.PQError, match="is wanted"):
             layer.prompt(bad, None, None, None)
+
+
+def test_the_layer_refuses_weights_that_are_not_on_one_gpu():
+    W = {"W" + n: torch.zeros((512 if n in "qo" else 128, 512), dtype=torch.bfloat16) for n in "qkvo"}
+    for device in ("cpu", "cuda", "cuda:1"):
+        with pytest.raises(pq.PQError, match="one GPU"):
+            CachedAttention(W, 8, 2, n_pages=4, n_seqs=2, max_pages=2, device=device)
