@@ -103,8 +103,12 @@ class CachedAttention:
         dev, want = weights["Wq"].device, torch.device(device)
         if dev.type != "cuda" or want.type != "cuda" or want.index not in (None, dev.index) or any(weights["W" + n].device != dev for n in "kvo"):
             raise pq.PQError(f"the weights are on one GPU, that of device={device}")
-        device = dev
         self.d, self.H, self.Hk, self.dh, self.B = d, n_heads, n_kv_heads, d // n_heads, n_seqs
+        with torch.cuda.device(dev):                                     # (whichever is current)
+            self._build(weights, n_pages, n_seqs, max_pages, page_tokens, kv_kind, max_len, dev)
+
+    def _build(self, weights, n_pages, n_seqs, max_pages, page_tokens, kv_kind, max_len, device):
+        d, n_heads, n_kv_heads = self.d, self.H, self.Hk
         self.packed = {}
         for n in ("q", "k", "v", "o"):
             P, _, ml = pq.pack_sign(weights["W" + n])
@@ -131,6 +135,9 @@ class CachedAttention:
         """x [T, d] bf16: the last row_start[b + 1] - row_start[b] tokens of every sequence.  Returns [T, d]; rows of no sequence are undefined."""
         T = x.shape[0] if x.dim() else 0
         self._check(x, T)
+        if pq._current_device() != self.cache.get_device():
+            with torch.cuda.device(self.cache.device):
+                return self.prompt(x, lens, page_table, row_start)
 
         def linear(n, x):
             N, P, ml, _, _ = self.packed[n]
@@ -148,6 +155,9 @@ class CachedAttention:
         s = self.step
         self._check(x, self.B)
         self._check(out, self.B)
+        if pq._current_device() != self.cache.get_device():
+            with torch.cuda.device(self.cache.device):
+                return self.token(x, lens, page_table, out)
 
         def linear(n, x):
             _, _, _, tiled, scale = self.packed[n]

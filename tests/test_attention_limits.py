@@ -55,3 +55,35 @@ def test_the_layer_refuses_weights_that_are_not_on_one_gpu():
     for device in ("cpu", "cuda", "cuda:1"):
         with pytest.raises(pq.PQError, match="one GPU"):
             CachedAttention(W, 8, 2, n_pages=4, n_seqs=2, max_pages=2, device=device)
+
+
+def test_the_layer_runs_on_its_caches_device_whichever_is_current(monkeypatch):
+    """Every call of a prompt and of a token finds the cache's device current (here -1, the host's number) though another one, 3, was."""
+    current, found = [3], []
+
+    class Device:
+        def __init__(self, device):
+            self.number = -1 if device == torch.device("cpu") else None
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.number
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(pq, "_current_device", lambda: current[0])
+    monkeypatch.setattr(pq, "LinearBuffers", lambda *a: None)
+    for name, out in (("linear_fwd", 3), ("decode_gemv", 4), ("kv_write", 3), ("attn_prefill", 6), ("attn_decode", 5), ("glue_lincomb", 0)):
+        monkeypatch.setattr(pq, name, lambda *a, name=name, out=out, **k: (found.append((name, current[0])), a[out])[1])
+    layer = CachedAttention.__new__(CachedAttention)
+    layer.d, layer.B, layer.H, layer.Hk, layer.dh, layer.cache = 64, 2, 2, 1, 32, torch.zeros(256, dtype=torch.uint8)
+    layer.kv = layer.attn = layer.attn_ws = None
+    layer.packed = {n: (64 if n in "qo" else 32, None, None, None, None) for n in "qkvo"}
+    layer.step = {n: torch.zeros((2, p[0]), dtype=torch.bfloat16) for n, p in layer.packed.items()}
+    layer.step["a"] = torch.zeros((2, 64), dtype=torch.bfloat16)
+    layer.decode = layer.decode_ws = {n: None for n in "qkvo"}
+    x = torch.zeros((2, 64), dtype=torch.bfloat16)
+    layer.prompt(x, None, None, None)
+    layer.token(x, None, None, x.clone())
+    assert len(found) == 14 and {number for _, number in found} == {-1} and current == [3]
