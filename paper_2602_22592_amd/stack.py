@@ -135,6 +135,8 @@ class CachedAttention:
         """x [T, d] bf16: the last row_start[b + 1] - row_start[b] tokens of every sequence.  Returns [T, d]; rows of no sequence are undefined."""
         T = x.shape[0] if x.dim() else 0
         self._check(x, T)
+        if T == 0:
+            return torch.empty_like(x)
         if pq._current_device() != self.cache.get_device():
             with torch.cuda.device(self.cache.device):
                 return self.prompt(x, lens, page_table, row_start)
