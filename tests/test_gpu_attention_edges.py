@@ -3,9 +3,11 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import attention_oracle as ao
 from paged_cases import Paged, check, expected
 from paper_2602_22592_amd import binding as pq
 from test_gpu_attention import BF, I8, queries, rows_of_call, run_decode, run_prefill, t32  # noqa: F401  (rows_of_call: fixture)
+from test_gpu_kv_cache import as_codes, raw_views
 
 pytestmark = pytest.mark.gpu
 MOST = 2 ** 31 - 1
@@ -126,3 +128,90 @@ def test_rows_all_of_whose_scores_are_minus_infinity_are_nan(kind):
         O, lse = run(c, Q[150 - n:], *args, 2)
         want = run(clean, Q[150 - n:], *args, 2)
         assert torch.isnan(O[:, 0].float()).all() and torch.equal(O[:, 1], want[0][:, 1]) and torch.equal(lse[:, 1], want[1][:, 1])
+
+
+def many_sequences(B, kind, seed, longest=9):
+    """Ragged sequences, every third without rows, many of one token; rows are the last ones of their sequences."""
+    rng = np.random.default_rng(seed)
+    lens = rng.integers(0, longest + 1, B)
+    lens[rng.random(B) < 0.3] = 1
+    rows = np.minimum(lens, rng.integers(0, longest + 1, B))
+    rows[::3] = 0
+    lens[-1] = rows[-1] = longest
+    return Paged(kind, lens.tolist(), 2, 32, 16, seed), lens, rows
+
+
+SEARCHES = [64, 65, 130, 1000, 4097, 4200]                     # sequences: one, two and three steps of 64 entries
+
+
+@pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.parametrize("B", SEARCHES)
+@pytest.mark.parametrize("before", [0, 5])
+def test_cache_calls_of_many_sequences(kind, B, before):
+    """Every row lies where its sequence's table says, nothing else is written, and it reads back; rows before the first sequence's are nobody's."""
+    c, lens, rows = many_sequences(B, kind, B)
+    desc = c.desc()
+    T, page = int(rows.sum()), c.page
+    starts = np.concatenate([[0], np.cumsum(rows)]) + before
+    rng = np.random.default_rng(1)
+    K, V = (torch.from_numpy(rng.standard_normal((before + T + 4, 2, 32)).astype(np.float32)).cuda() for _ in range(2))
+    cache = pq.kv_cache(desc)
+    cache.fill_(255)
+    dev, rs = (t32(lens), torch.from_numpy(c.table).cuda()), t32(starts)
+    pq.kv_write(desc, K, V, cache, *dev, row_start=rs)
+    outs = [torch.full_like(K, 7.0) for _ in range(2)]
+    pq.kv_read(desc, cache, *dev, *outs, row_start=rs)
+    torch.cuda.synchronize()
+    seq = np.repeat(np.arange(B), rows)
+    pos = lens[seq] - rows[seq] + np.arange(T) - (starts[seq] - before)
+    at, slot = c.table[seq, pos // page], pos % page
+    keys, values, ks, vs = raw_views(desc, cache.cpu().numpy())
+    own = slice(before, before + T)
+    (kc, kstep), (vc, vstep) = (as_codes(x[own].cpu().numpy(), c.int8) for x in (K, V))
+    assert np.array_equal(keys[at, :, slot], kc) and np.array_equal(values[at, :, slot // 16, :, slot % 16], vc)
+    if c.int8:
+        assert np.array_equal(ks[at, :, slot], kstep) and np.array_equal(vs[at, :, slot], vstep)
+    mine = np.zeros((c.n_pages, page), bool)
+    mine[at, slot] = True
+    assert mine.sum() == T                                     # (every row has a place of its own)
+    assert (keys.view(np.uint8).reshape(c.n_pages, 2, page, -1).transpose(0, 2, 1, 3)[~mine] == 255).all()
+    assert (np.ascontiguousarray(values.transpose(0, 2, 4, 1, 3)).view(np.uint8).reshape(c.n_pages, page, -1)[~mine] == 255).all()
+    for x, got in zip((K, V), outs):
+        assert np.array_equal(got[own].cpu().numpy(), ao.stored(x[own].cpu().numpy(), c.int8))
+        assert (got[:before] == 7).all() and (got[before + T:] == 7).all()
+
+
+@pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.parametrize("B", SEARCHES)
+@pytest.mark.parametrize("before", [0, 5])
+@pytest.mark.parametrize("many", [False, True])
+def test_prompts_of_many_sequences(kind, B, before, many):
+    """.. in few rows (32 a tile) and in many (128 a tile)."""
+    c, lens, rows = many_sequences(B, kind, B + 1)
+    cache, dlens, table = c.device()
+    T, H = int(rows.sum()), 4 if many else 2
+    total = max(before + T + 2, 16384 // H + 1 if many else 0)
+    assert many == (total * H > 16384)
+    Q, q = queries(total, H, 32, 6)
+    O, lse = torch.full((total, H, 32), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((total, H), 7.0, device="cuda")
+    pq.attn_prefill(pq.make_attn_desc(c.desc(), H), Q, cache, dlens, table, t32(np.concatenate([[0], np.cumsum(rows)]) + before), O, lse=lse)
+    torch.cuda.synchronize()
+    own = slice(before, before + T)
+    check(O[own], lse[own], expected(c, q[own], rows.tolist(), 32 ** -0.5, p_bits=8), f"{B} sequences, {T} rows")
+    for x in (O, lse):
+        assert (x[:before] == 7).all() and (x[before + T:] == 7).all()
+
+
+@pytest.mark.parametrize("kind", [I8, BF])
+@pytest.mark.parametrize("B,T", [(64, 64), (65, 65), (130, 100), (4100, 4100), (4100, 9)])
+def test_last_tokens_of_many_sequences_as_prompts(kind, B, T):
+    """No row_start: row b is the last token of sequence b, as many as there are rows."""
+    c, lens, _ = many_sequences(B, kind, B + 2)
+    cache, dlens, table = c.device()
+    Q, q = queries(T, 4, 32, 6)
+    O, lse = torch.full((T, 4, 32), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((T, 4), 7.0, device="cuda")
+    pq.attn_prefill(pq.make_attn_desc(c.desc(), 4), Q, cache, dlens, table, None, O, lse=lse)
+    torch.cuda.synchronize()
+    few = Paged.__new__(Paged)
+    few.__dict__.update(c.__dict__, B=T)
+    check(O, lse, expected(few, q, [1] * T, 32 ** -0.5, p_bits=8), f"{T} of {B}")
