@@ -1152,7 +1152,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attn_prefill_kernel(pref
 // The same products with the keys and values read straight from the cache into the matrix instructions' registers: wavefront w takes
 // the tiles w, w + W, .. of 32 tokens, so that a row's tokens pass W times as fast, and what the wavefronts found is joined through
 // the LDS.  For calls too small to fill the chip with tiles of 128 rows, whose time is that of the longest row's chain of tiles.  Bound by the
-// chain of reads and products of a wavefront (130 tokens of 16 heads of 128, bf16: 10.6 us, of which a launch is 3.6), in larger calls by
+// chain of reads and products of a wavefront (130 tokens of 16 heads of 128, bf16: 10.5 us, of which a launch is 3.6), in larger calls by
 // the conversions and softmax of 32 rows where the other kernel shares the conversions of 128.
 template <int NK> constexpr int rows_waves() { return NK <= 4 ? 8 : 4; }
 template <int NK> constexpr int rows_pitch() { return NK * 32 + 4; }       // floats: sixteen rows' pieces of 16 bytes lie in different banks
@@ -1441,9 +1441,12 @@ __global__ __launch_bounds__(rows_waves<NK>() * 64, NK <= 4 ? 2 : 1) void attn_r
 // 16 heads of 128 9.3 / 11.9; five sequences of 24 rows behind 2000 tokens, 20/4 heads of 128, 29 / 68; 256, 512 and 1024 rows of 32/8 heads of 128
 // 12.4 / 14.5, 23.7 / 21.7 and 55 / 37; 512 and 1024 rows of 32 heads of 64 15.4 / 17.9 and 35.7 / 29.2; 512 rows behind 7680 tokens, 32/8 heads
 // of 128, 157 / 242.)  And for 16-bit heads beyond 128, where one wavefront a SIMD holds the tile and the barriers of the other kernel cost
-// more than its shared reads save (8192 tokens, 16/4 heads of 160, 192, 224 and 256: 0.80 / 1.08, 1.19 / 1.04, 1.08 / 1.56 and 1.90 / 1.95 ms).
+// more than its shared reads save, or its tile spills, but not for those of 162 to 192, the only ones that are faster shared (8192 and 2048 tokens,
+// 16/4 heads of 160 0.84 / 0.89 ms and 105 / 120 us, of 192 1.08 / 0.83 and 116 / 108, of 224 1.07 / 1.28 and 127 / 165, of 256 1.44 / 1.80 and
+// 154 / 227).
+template <int KIND, int NK> constexpr bool always_few() { return KIND == PQ_KV_BF16 && NK > 4 && NK != 6; }
 template <int KIND, int NK>
-bool few_rows(const prefill_args& a) { return (KIND == PQ_KV_BF16 && NK > 4) || (int64_t)a.v.T * a.heads <= 16384; }
+bool few_rows(const prefill_args& a) { return always_few<KIND, NK>() || (int64_t)a.v.T * a.heads <= 16384; }
 
 // The LDS beyond 64 KiB of a kernel, asked for once on each device.
 int allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& asked) {
@@ -1468,7 +1471,7 @@ int launch_prefill_nk(prefill_args a, hipStream_t s) {
     constexpr int lds = rows_lds<KIND, NK>();
     if (int e = allow_lds((const void*)attn_rows_kernel<KIND, NK>, lds, asked[0])) return e;
     attn_rows_kernel<KIND, NK><<<(unsigned)grid, rows_waves<NK>() * 64, lds, s>>>(a);
-  } else if constexpr (KIND == PQ_KV_INT8 || NK <= 4) {
+  } else if constexpr (!always_few<KIND, NK>()) {
     constexpr int lds = 2 * prefill_stage<KIND, NK>();
     if (int e = allow_lds((const void*)attn_prefill_kernel<KIND, NK>, lds, asked[1])) return e;
     attn_prefill_kernel<KIND, NK><<<(unsigned)grid, 256, lds, s>>>(a);

@@ -102,7 +102,7 @@ def test_decode_infinities_that_are_seen(kind, weight, L, shift, d, window):
 @pytest.mark.filterwarnings("ignore::RuntimeWarning")
 @pytest.mark.parametrize("kind", [I8, BF])
 @pytest.mark.parametrize("weight", list(WEIGHTS))
-@pytest.mark.parametrize("rows,G,d,causal,window", [(200, 1, 64, True, 0), (61, 3, 64, True, 0), (200, 2, 64, True, 50), (40, 2, 90, False, 0), (70, 1, 160, True, 100)])
+@pytest.mark.parametrize("rows,G,d,causal,window", [(200, 1, 64, True, 0), (61, 3, 64, True, 0), (200, 2, 64, True, 50), (40, 2, 90, False, 0), (70, 1, 160, True, 100), (70, 1, 192, True, 100)])
 @pytest.mark.usefixtures("rows_of_call")
 def test_prompt_infinities_that_are_seen(kind, weight, rows, G, d, causal, window):
     """In tiles that all rows see and in those that some rows see a part of."""
