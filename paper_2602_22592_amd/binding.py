@@ -495,6 +495,8 @@ def _kv_check(kv, cache, lens, page_table, row_start):
         raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")
     if lens.numel() < B or page_table.numel() < B * kv.max_pages:
         raise PQError("lens, page_table or row_start is smaller than the descriptor says")
+    if B > 1 and page_table.dim() > 1 and page_table.shape[-1] != kv.max_pages:   # (its rows would be read one behind the other)
+        raise PQError(f"rows of {page_table.shape[-1]} pages in page_table, {kv.max_pages} in the descriptor")
     if row_start is not None:
         if row_start.dtype is not i32 or row_start.get_device() != dev or not row_start.is_contiguous():
             raise PQError("lens, page_table and row_start are contiguous int32 tensors on the cache's device")

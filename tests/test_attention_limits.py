@@ -87,3 +87,18 @@ def test_the_layer_runs_on_its_caches_device_whichever_is_current(monkeypatch):
     layer.prompt(x, None, None, None)
     layer.token(x, None, None, x.clone())
     assert len(found) == 14 and {number for _, number in found} == {-1} and current == [3]
+
+
+def test_page_tables_of_another_width_are_refused():
+    """A table with more entries a row than the descriptor says is large enough, but its rows lie elsewhere."""
+    d = kv()
+    cache, lens = torch.zeros(pq.lib().pq_kv_cache_bytes(C.byref(d)), dtype=torch.uint8), torch.zeros(2, dtype=torch.int32)
+    table = lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    for shape in ((2, 8), (4, 2), (8, 1)):
+        with pytest.raises(pq.PQError, match="4 in the descriptor"):
+            pq._kv_check(d, cache, lens, table(*shape), None)
+    for shape in ((2, 4), (3, 4), (8,), (20,)):                           # (what remains wrong with these is that they are host tensors)
+        with pytest.raises(pq.PQError, match="on a GPU"):
+            pq._kv_check(d, cache, lens, table(*shape), None)
+    with pytest.raises(pq.PQError, match="on a GPU"):
+        pq._kv_check(kv(B=1), cache, lens, table(1, 9), None)            # (one row)
