@@ -380,7 +380,7 @@ int pq_decode_ffn(const pq_decode_ffn_desc* desc, const void* X, const uint32_t*
  * row_start[0], behind row_start[n_seqs]) are neither read nor written, in any call.
  * lens, row_start and page_table are device memory that no call checks on the host, so that a captured call may be replayed with others;
  * every access stays inside the buffers whatever they hold: a token whose page is not in [0, n_pages), whose position is negative or
- * beyond max_pages * page_tokens, is not written, reads back as zeros and is attended by nobody.
+ * beyond max_pages * page_tokens, is not written, reads back as zeros and is attended by nobody.  (A length beyond 2^30 + n_b may count as that.)
  *
  * Layout.  A page is one contiguous run of pq_kv_cache_bytes() / n_pages bytes and may be copied as such; in it, head by head, with
  * Dp = d_head rounded up to a multiple of 32:  keys [page_tokens][Dp], values [page_tokens / 16][Dp][16 tokens], and for PQ_KV_INT8
@@ -417,7 +417,8 @@ int pq_kv_read(const pq_kv_desc* desc, const void* cache, size_t cache_bytes, co
  * sequence (causal), of these the last `window` if window > 0, or with causal == 0 all lens[b] of them (a row at a negative
  * position sees none):
  *     s_t = scale * q . k_t,    o = sum_t exp(s_t - lse) v_t,    lse = log sum_t exp(s_t),
- * k_t, v_t the values that the cache stands for; scores, sums and lse in fp32, one rounding of o to bf16.  A row that sees nothing has
+ * k_t, v_t the values that the cache stands for; scores, sums and lse in fp32 (q . k_t is summed before the scale, of an INT8 cache over the
+ * codes: room for |q| up to 2^100), one rounding of o to bf16.  A row that sees nothing has
  * o = 0 and lse = -infinity.  Tokens that a row does not see have no effect on it, whatever they hold; infinities and NaN among those that it
  * sees come out as the formula has them (a row all of whose scores are -infinity, or one of which is +infinity or NaN, is NaN), an infinite
  * value however little its token weighs.  The sums of exp(s_t - m) v_t are fp32 with m up to 16 powers of two below the largest s_t: they hold
@@ -434,7 +435,8 @@ typedef struct pq_attn_desc {
   float scale;     /* finite; usually 1 / sqrt(d_head) */
 } pq_attn_desc;
 /* One new token of every sequence: Q [n_seqs][n_heads][d_head] bf16 (rows q_stride elements apart, even), written to the cache already, at
- * position lens[b] - 1;  O [n_seqs][n_heads][d_head] bf16 out, contiguous;  lse [n_seqs][n_heads] fp32 out or NULL.
+ * position lens[b] - 1;  O [n_seqs][n_heads][d_head] bf16 out, contiguous;  lse [n_seqs][n_heads] fp32 out or NULL.  Q, O, the cache and the
+ * workspace are 16-byte aligned, in both calls.
  * workspace: pq_attn_decode_workspace_bytes() bytes of scratch; calls that may overlap need one each. */
 size_t pq_attn_decode_workspace_bytes(const pq_attn_desc* desc);
 int pq_attn_decode(const pq_attn_desc* desc, const void* Q, int64_t q_stride, const void* cache, size_t cache_bytes, const int32_t* lens,

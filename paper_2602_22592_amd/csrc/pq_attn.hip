@@ -23,7 +23,7 @@ namespace {
 // relative to their largest, in three digits of base 256 that occupy three of the four columns of a head (error 2^-22 of the largest, far
 // below the quantiser's 2^-8; the fourth column is empty).  For 16 bits p is the sum of two bf16 numbers (2^-16).
 // Measured: four sequences of 131072 tokens, 32/8 heads of 128, INT8: 1.11 GB in 192 us, 5.8 TB/s; 64 ragged ones up to 8192, bf16: 585 MB in
-// 133 us, 4.4 TB/s; one of 517 tokens 9.1 us, of which a launch is 3.6 and the rest five reads that wait for each other.
+// 134 us, 4.4 TB/s; one of 517 tokens 9.1 us, of which a launch is 3.6 and the rest five reads that wait for each other.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(2))) long i64x2_t;
 // x of the neighbours in a quad of lanes (xor 1, xor 2), without the LDS.
@@ -306,8 +306,8 @@ __global__ __launch_bounds__(W * 64, NK <= 4 ? 2 : 1) void attn_decode_kernel(de
           i32x4_t S = {0, 0, 0, 0};
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            // (A sum takes one kind of instruction: a 16x16x32 that added to a 16x16x64's result a few instructions behind it read the
-            // result before it was there.  With a half step all of them are 16x16x32, on the halves of a piece.)
+            // (A sum takes one kind of instruction: one that goes on in the other, 16x16x32 behind 16x16x64 or the reverse, loses two of its four
+            // registers, for want of wait states between them.  With a half step all of them are 16x16x32, on the halves of a piece.)
             if constexpr (!TAIL) {
               S = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[c * KS + ks], qf[ks], S, 0, 0, 0);
             } else {
@@ -658,8 +658,9 @@ int check_attn_call(const pq_attn_desc* d, const void* Q, int64_t qs, int T, con
 // products run on the bf16 instructions.  Scores are formed transposed, a column a row of Q, so that a row's maximum and sum need one
 // exchange between two lanes and the probabilities are the second product's operand as they stand.  Probabilities (times the value's step)
 // are rounded to bf16, 2^-9 of each: what a 16-bit product takes (error of the outputs 2.1e-3, 1.6e-3 of it from their own rounding).
-// Bound by the sum of what a stage costs one after the other with two wavefronts a SIMD.  8192 tokens, 32/8 heads of 128, INT8: 630 us (872
-// TFLOP/s of the causal products); its matrix instructions alone 253, with the LDS reads 354, with the staging 477, with the softmax 630.
+// Bound by the sum of what a stage costs one after the other with two wavefronts a SIMD.  8192 tokens, 32/8 heads of 128, INT8: 623 to 653 us on
+// different cards (842 to 882 TFLOP/s of the causal products); where it took 630, its matrix instructions alone 253, with the LDS reads 354, with
+// the staging 477.
 // ---------------------------------------------------------------------------------------------
 struct prefill_args {
   kv_view v;
