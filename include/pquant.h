@@ -384,8 +384,8 @@ int pq_decode_ffn(const pq_decode_ffn_desc* desc, const void* X, const uint32_t*
  *
  * Layout.  A page is one contiguous run of pq_kv_cache_bytes() / n_pages bytes and may be copied as such; in it, head by head, with
  * Dp = d_head rounded up to a multiple of 32:  keys [page_tokens][Dp], values [page_tokens / 16][Dp][16 tokens], and for PQ_KV_INT8
- * the fp32 steps of the keys [page_tokens] and of the values [page_tokens].  Key columns d_head .. Dp - 1 are zero (pq_kv_write
- * writes them so; a cache filled by other means must hold zeros or finite values there); what a page holds behind its last token is
+ * the fp32 steps of the keys [page_tokens] and of the values [page_tokens].  Columns d_head .. Dp - 1 are zero (pq_kv_write
+ * writes them so; a cache filled by other means must hold zeros or finite numbers there); what a page holds behind its last token is
  * never used, so a fresh cache needs no clearing.
  * PQ_KV_INT8: every token and head is a row of the AbsMax quantiser of pq_quant_act (codes q; gamma = 128 / max(max|x|, 1e-5)); the
  * cache keeps step = max(max|x|, 1e-5) / 128, an exact quotient, and a code stands for fl32(q * step).  A row with an infinity or a
