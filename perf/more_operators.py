@@ -276,14 +276,14 @@ def _own(s):
     if "plan" not in s:
         h = s["hyper"]
         tensors = lambda x, of=1: None if x is None else [x[a // of:a // of + -(-n // of)] for a, n in zip(s["starts"], s["sizes"])]
+        m_values, v_values = s["values"] or (None, None)
         s["plan"] = pq.AdamWTensors(tensors(s["params"]), tensors(s["grads"]), tensors(s["m"]), tensors(s["v"]), steps=tensors(s["steps"], BLOCK),
-                                    masters=tensors(s["masters"]), beta1=h["beta1"], beta2=h["beta2"], eps=h["eps"])
+                                    masters=tensors(s["masters"]), m_values=tensors(m_values), v_values=tensors(v_values), beta1=h["beta1"],
+                                    beta2=h["beta2"], eps=h["eps"])
         s["scalars"] = pq.adamw_scalars(s["plan"], h["step"], h["lr"], h["weight_decay"], h["grad_scale"])
-        if s["values"]:
-            s["moments"] = tensors(s["values"][0]), tensors(s["values"][1])
     pq.adamw_step(s["plan"], s["scalars"])
     if s["values"]:                # 8-bit states are read back as the values they stand for, as a checkpoint takes them
-        pq.adamw_read(s["plan"], *s["moments"])
+        pq.adamw_read(s["plan"])
     return _updated(s)
 
 
