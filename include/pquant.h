@@ -446,6 +446,108 @@ int pq_attn_decode(const pq_attn_desc* desc, const void* Q, int64_t q_stride, co
 int pq_attn_prefill(const pq_attn_desc* desc, const void* Q, int64_t q_stride, int32_t T, const int32_t* row_start, const void* cache,
                     size_t cache_bytes, const int32_t* lens, const int32_t* page_table, void* O, float* lse, void* stream);
 
+/* Rotary positions.  Of every head's d_head elements the first rot_dim are pairs (x_i, y_i), i = 0 .. rot_dim / 2 - 1, that turn by an angle of their
+ * token's position p:
+ *     x'_i = scale (x_i cos a - y_i sin a),   y'_i = scale (y_i cos a + x_i sin a),   a = 2 pi freqs[i] p      (inverse: -a)
+ * PQ_ROPE_HALF pairs elements (i, i + rot_dim / 2), PQ_ROPE_PAIRS (2 i, 2 i + 1); elements rot_dim .. d_head - 1 are copied.  With scale == 1 the
+ * gradient of the call is the inverse call; otherwise, too (it is scale times the transposed turn).
+ * freqs [rot_dim / 2] are TURNS per position in fp64, device memory: the usual table is base^(-2 i / rot_dim) / (2 pi); stretched tables (for
+ * contexts longer than the model was trained on) are other numbers in it.  Turns are formed and reduced in fp64, sine and cosine of what is left
+ * in fp32 (2^-23 of 1), products and their sum in fp32, one rounding to `dtype`.
+ * Rows and positions are those of the cache calls: rows row_start[b] .. row_start[b + 1] - 1 are the LAST rows of sequence b of lens[b] tokens, at
+ * positions lens[b] - n_b .. lens[b] - 1 (row_start NULL: row b is the last token of sequence b); lens NULL: row_start's rows are whole sequences, at
+ * positions 0 .. n_b - 1.  Rows of no sequence are neither read nor written. */
+typedef enum pq_rope_layout { PQ_ROPE_HALF = 0, PQ_ROPE_PAIRS = 1 } pq_rope_layout;
+typedef struct pq_rope_desc {
+  int32_t n_heads;    /* heads of Q */
+  int32_t n_kv_heads; /* heads of K; 0: no K */
+  int32_t d_head;     /* even, 2..256 */
+  int32_t rot_dim;    /* even, 2..d_head */
+  int32_t layout;     /* pq_rope_layout */
+  int32_t inverse;    /* 1: turn backwards */
+  int32_t n_seqs;
+  float scale;        /* finite; usually 1 */
+} pq_rope_desc;
+/* Q [T][n_heads][d_head], K [T][n_kv_heads][d_head] of `dtype` (PQ_F32 or PQ_BF16), rows q_stride / k_stride elements apart (even, at least
+ * the heads' elements); Qr, Kr the same shapes with strides of their own.  Qr may be Q and Kr may be K, with the same stride (in place); otherwise they
+ * must not overlap.  All 16-byte aligned. */
+int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, int32_t dtype, int32_t T,
+            const double* freqs, const int32_t* row_start, const int32_t* lens, void* Qr, int64_t qr_stride, void* Kr, int64_t kr_stride, void* stream);
+
+/* Attention over the rows of a call, for training: packed sequences, no cache.  Rows row_start[b] .. row_start[b + 1] - 1 (int32 [n_seqs + 1],
+ * non-decreasing, device memory that no call checks) are sequence b; a row sees rows of its own sequence only, with causal those up to itself, of
+ * these the last `window` if window > 0.  Query head h reads key-value head h / (n_heads / n_kv_heads).
+ *     s_j = scale q . k_j,   lse = log sum_j exp s_j,   o = sum_j exp(s_j - lse) v_j
+ *   Q [T][n_heads][d_head], K, V [T][n_kv_heads][d_head] bf16, rows *_stride elements apart (even);  O [T][n_heads][d_head] bf16 out and
+ *   lse [T][n_heads] fp32 out, both contiguous.  Rows of no sequence are neither read nor written.  Buffers 16-byte aligned.
+ * Scores, sums and lse are fp32; exp(s_j - m) is rounded to bf16 for the product with v (m: up to 16 powers of two below the largest s_j), o once more at the
+ * end.  Tokens that a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite
+ * or NaN.  At most 2^29 rows, rows * n_heads < 2^31.  The result does not depend on the order in which workgroups run. */
+typedef struct pq_self_attn_desc {
+  int32_t n_heads;    /* query heads, a multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t d_head;     /* even, 2..128 */
+  int32_t n_seqs;
+  int32_t causal;     /* 1, or 0 for rows that see their whole sequence (then window must be 0) */
+  int32_t window;     /* 0: none */
+  float scale;        /* finite; usually 1 / sqrt(d_head) */
+} pq_self_attn_desc;
+int pq_self_attn_fwd(const pq_self_attn_desc* desc, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V, int64_t v_stride,
+                     int32_t T, const int32_t* row_start, void* O, float* lse, void* stream);
+/* Its gradients, from dO [T][n_heads][d_head] bf16 and what the forward call was given and left (O, lse):
+ *     delta = sum_d dO O,   p_j = exp(s_j - lse),   dS_j = p_j (dO . v_j - delta)
+ *     dQ = scale sum_j dS_j k_j,   dK_j = scale sum dS_j q,   dV_j = sum p_j dO      (the last two over the rows that see j, and over the heads
+ *                                                                                      that share it)
+ *   dQ, dK, dV bf16 out with strides of their own (even); p and dS are rounded to bf16 for the products, the sums are fp32.  A row that sees one
+ *   token has dS = 0.  Tokens and rows that do not see each other have no effect on each other, as above.
+ *   workspace: pq_self_attn_bwd_workspace_bytes() bytes of scratch (0: refused arguments); calls that may overlap need one each. */
+size_t pq_self_attn_bwd_workspace_bytes(const pq_self_attn_desc* desc, int32_t T);
+int pq_self_attn_bwd(const pq_self_attn_desc* desc, const void* dO, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
+                     int64_t v_stride, const void* O, const float* lse, int32_t T, const int32_t* row_start, void* dQ, int64_t dq_stride, void* dK,
+                     int64_t dk_stride, void* dV, int64_t dv_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One AdamW step (decoupled weight decay) over many tensors in one launch:
+ *     g = grad_scale grad,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g g,
+ *     w = w (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, each product and sum rounded (no fused multiply-add), the square root correctly rounded; w is the fp32 master where there is one (the
+ * parameter is then its rounding), else the parameter.
+ * PQ_STATE_8BIT keeps m and r = sqrt(v) in 8 bits, blocks of 256 elements with two fp32 steps:
+ *     m = q |q| step_m   (int8 q, -127..127, step_m = max|m| / 127^2),      r = u u step_r   (uint8 u, 0..255, step_r = max r / 255^2),
+ * the nearest code (of a tie the even one; quotients are fl(x * fl(1 / step)), steps at least 2^-126); a root that is not zero takes at least code
+ * 1, since it is divided by.  The step itself uses the unrounded m and r.  A block with an infinity or a NaN in m or r has that step NaN. */
+typedef enum pq_state_kind { PQ_STATE_F32 = 0, PQ_STATE_8BIT = 1 } pq_state_kind;
+typedef struct pq_adamw_tensor {
+  void* param;        /* param_dtype */
+  const void* grad;   /* grad_dtype */
+  float* master;      /* fp32 (has_masters) or NULL */
+  void* m;            /* fp32 or int8 */
+  void* v;            /* fp32 (v), or uint8 (codes of sqrt v) */
+  float* steps;       /* 8 bits: [ceil(n / 256)][2] = step_m, step_r */
+  float* m_values;    /* what pq_adamw_read writes: n values each (has_values), or NULL */
+  float* v_values;
+  int64_t n;          /* elements, may be 0 */
+} pq_adamw_tensor;
+typedef struct pq_adamw_desc {
+  int32_t n_tensors;
+  int32_t param_dtype; /* PQ_F32 or PQ_BF16 */
+  int32_t grad_dtype;  /* PQ_F32 or PQ_BF16 */
+  int32_t state_kind;  /* pq_state_kind */
+  int32_t has_masters; /* 1: every tensor has an fp32 master (bf16 parameters), 0: none has */
+  int32_t has_values;  /* 1: every tensor has m_values and v_values (8-bit states), 0: none has */
+  double beta1, beta2; /* in [0, 1) */
+  double eps;          /* > 0, at least 2^-126 */
+} pq_adamw_desc;
+/* A plan lists the pieces of all tensors.  pq_adamw_plan writes pq_adamw_plan_bytes() bytes of HOST memory (plan, 8-byte aligned); the caller copies them to device
+ * memory and keeps them for as long as the tensors' addresses hold.  Every buffer is 16-byte aligned (steps: 8); written buffers must not overlap.
+ * `tensors` is host memory, read only by these two calls.  (0 bytes: refused arguments.)  pq_adamw_step and pq_adamw_read want exactly that many bytes. */
+size_t pq_adamw_plan_bytes(const pq_adamw_desc* desc, const pq_adamw_tensor* tensors);
+int pq_adamw_plan(const pq_adamw_desc* desc, const pq_adamw_tensor* tensors, void* plan, size_t plan_bytes);
+/* scalars: device memory, so that a captured step can be replayed with others; fp32 { 1 - lr weight_decay, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t),
+ * grad_scale } (formed in double, rounded once).  plan: the device copy.  beta1 and beta2 may change from call to call, the rest of desc is the plan's. */
+int pq_adamw_step(const pq_adamw_desc* desc, const void* plan, size_t plan_bytes, const float* scalars, void* stream);
+/* 8-bit states as the fp32 values that they stand for (m, and v = r r), into m_values and v_values: what a checkpoint keeps. */
+int pq_adamw_read(const pq_adamw_desc* desc, const void* plan, size_t plan_bytes, void* stream);
+
 /* Glue for chaining the linears into a layer stack; not part of the method.
  * pq_glue_lincomb: out = c0 x0 + c1 x1 + c2 x2 + c3 x3 over n bf16 elements (x1..x3 may be NULL;
  * fp32 arithmetic, one rounding; n % 8 == 0) -- residual adds and the mean that stands in for the

@@ -20,6 +20,8 @@ PQ_STE_IDENTITY, PQ_STE_CLIP = 0, 1
 PQ_HP_LOWRANK_BF16, PQ_HP_LOWRANK_INT8 = 0, 1
 PQ_PACKED_ROWMAJOR, PQ_PACKED_TILED64 = 0, 1
 PQ_KV_BF16, PQ_KV_INT8 = 0, 1
+PQ_ROPE_HALF, PQ_ROPE_PAIRS = 0, 1
+PQ_STATE_F32, PQ_STATE_8BIT = 0, 1
 
 EXPORTS = [
     "pq_version", "pq_last_error_string", "pq_quant_act", "pq_pack_workspace_bytes", "pq_pack_sign",
@@ -33,6 +35,8 @@ EXPORTS = [
     "pq_decode_ffn_workspace_bytes", "pq_decode_ffn", "pq_rmsnorm_bwd_static_max_bytes", "pq_rmsnorm_bwd_static",
     "pq_groupwise_workspace_bytes", "pq_groupwise_fwd", "pq_ffn_ctx_section",
     "pq_kv_cache_bytes", "pq_kv_write", "pq_kv_read", "pq_attn_decode_workspace_bytes", "pq_attn_decode", "pq_attn_prefill",
+    "pq_rope", "pq_self_attn_fwd", "pq_self_attn_bwd_workspace_bytes", "pq_self_attn_bwd",
+    "pq_adamw_plan_bytes", "pq_adamw_plan", "pq_adamw_step", "pq_adamw_read",
 ]
 
 
@@ -69,6 +73,23 @@ class AttnDesc(C.Structure):
                 ("scale", C.c_float)]
 
 
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "d_head", "rot_dim", "layout", "inverse", "n_seqs")] + [("scale", C.c_float)]
+
+
+class SelfAttnDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "d_head", "n_seqs", "causal", "window")] + [("scale", C.c_float)]
+
+
+class AdamWTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "master", "m", "v", "steps", "m_values", "v_values")] + [("n", C.c_int64)]
+
+
+class AdamWDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_tensors", "param_dtype", "grad_dtype", "state_kind", "has_masters", "has_values")] + [
+        (n, C.c_double) for n in ("beta1", "beta2", "eps")]
+
+
 class PQError(RuntimeError):
     pass
 
@@ -90,7 +111,7 @@ def lib():
                      "pq_ffn_workspace_bytes", "pq_rmsnorm_bwd_workspace_bytes", "pq_linear_norm_ctx_bytes",
                      "pq_linear_norm_workspace_bytes", "pq_hp_int8_ctx_bytes", "pq_hp_int8_workspace_bytes",
                      "pq_decode_ffn_workspace_bytes", "pq_rmsnorm_bwd_static_max_bytes", "pq_kv_cache_bytes",
-                     "pq_attn_decode_workspace_bytes"):
+                     "pq_attn_decode_workspace_bytes", "pq_self_attn_bwd_workspace_bytes", "pq_adamw_plan_bytes"):
             getattr(L, name).restype = C.c_size_t
         p, i, l, n = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
         kv, attn = C.POINTER(KVDesc), C.POINTER(AttnDesc)
@@ -98,6 +119,15 @@ def lib():
         L.pq_kv_read.argtypes = [kv, p, n, p, p, p, i, p, p, i, l, l, p]
         L.pq_attn_decode.argtypes = [attn, p, l, p, n, p, p, p, p, p, n, p]
         L.pq_attn_prefill.argtypes = [attn, p, l, i, p, p, n, p, p, p, p, p]
+        rope, self_attn, adamw = C.POINTER(RopeDesc), C.POINTER(SelfAttnDesc), C.POINTER(AdamWDesc)
+        L.pq_rope.argtypes = [rope, p, l, p, l, i, i, p, p, p, p, l, p, l, p]
+        L.pq_self_attn_fwd.argtypes = [self_attn, p, l, p, l, p, l, i, p, p, p, p]
+        L.pq_self_attn_bwd_workspace_bytes.argtypes = [self_attn, i]
+        L.pq_self_attn_bwd.argtypes = [self_attn, p, p, l, p, l, p, l, p, p, i, p, p, l, p, l, p, l, p, n, p]
+        L.pq_adamw_plan_bytes.argtypes = [adamw, C.POINTER(AdamWTensor)]
+        L.pq_adamw_plan.argtypes = [adamw, C.POINTER(AdamWTensor), p, n]
+        L.pq_adamw_step.argtypes = [adamw, p, n, p, p]
+        L.pq_adamw_read.argtypes = [adamw, p, n, p]
         _lib = L
     return _lib
 
@@ -614,6 +644,233 @@ def attn_prefill(desc, Q, cache, lens, page_table, row_start, O, lse=None):
     if rc:
         _check(rc)
     return O
+
+
+def make_rope_desc(n_heads, n_kv_heads, d_head, n_seqs, rot_dim=0, layout=PQ_ROPE_HALF, inverse=False, scale=1.0):
+    """rot_dim: elements of a head that turn (0: all of them).  n_kv_heads 0: calls have no keys."""
+    return RopeDesc(n_heads, n_kv_heads, d_head, rot_dim or d_head, layout, int(inverse), n_seqs, scale)
+
+
+def rope_freqs(rot_dim, base=10000.0, factor=1.0, original_len=0, low=1.0, high=32.0, device="cuda"):
+    """Turns per position of every pair [rot_dim / 2], fp64: base^(-2 i / rot_dim) / (2 pi).
+
+    factor > 1 stretches them for contexts that many times longer: all of them by the factor (original_len 0), or by parts: of the pairs that turn r
+    times within original_len tokens those with r >= high are left as they are, those with r <= low are slowed down by the factor, a ramp between."""
+    if rot_dim < 2 or rot_dim % 2 or base <= 0 or factor <= 0 or not low < high:
+        raise PQError(f"rope_freqs: rot_dim={rot_dim} is even, base={base} and factor={factor} are positive, low={low} is below high={high}")
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    f = base ** (-2.0 * i / rot_dim) / 6.283185307179586
+    keep = ((original_len * f - low) / (high - low)).clamp(0.0, 1.0) if original_len else torch.zeros_like(f)
+    return (f * (keep + (1.0 - keep) / factor)).to(device)
+
+
+def _index_check(dev, what, *tensors):
+    for t, n in tensors:
+        if t is not None:
+            if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
+                raise PQError(f"{what} are contiguous int32 tensors on the rows' device")
+            if t.numel() < n:
+                raise PQError(f"{what}: {t.numel()} entries where the descriptor asks for {n}")
+
+
+def rope(desc, Q, K, freqs, Qr, Kr, row_start=None, lens=None):
+    """Q [T, n_heads, d_head] and K [T, n_kv_heads, d_head] (or None) turned into Qr and Kr, which may be Q and K themselves."""
+    d, B, dt = desc.d_head, desc.n_seqs, _KV_DT.get(Q.dtype)
+    dev = Q.get_device()
+    T, qs = _rows(Q, desc.n_heads, d)
+    Tr, qrs = _rows(Qr, desc.n_heads, d)
+    if dev < 0 or dt is None or Qr.dtype is not Q.dtype or T != Tr or Qr.get_device() != dev:
+        raise PQError("Q and Qr are fp32 or bf16 tensors of as many rows on one GPU")
+    ks = krs = 0
+    if desc.n_kv_heads:
+        if K is None or Kr is None:
+            raise PQError("the descriptor has key heads: K and Kr are wanted")
+        Tk, ks = _rows(K, desc.n_kv_heads, d)
+        Tkr, krs = _rows(Kr, desc.n_kv_heads, d)
+        if Tk != T or Tkr != T or K.dtype is not Q.dtype or Kr.dtype is not Q.dtype or K.get_device() != dev or Kr.get_device() != dev:
+            raise PQError("K and Kr have Q's rows, type and device")
+    elif K is not None or Kr is not None:
+        raise PQError("the descriptor has no key heads")
+    if freqs.dtype is not torch.float64 or freqs.get_device() != dev or not freqs.is_contiguous() or freqs.numel() != desc.rot_dim // 2:
+        raise PQError(f"freqs is a contiguous fp64 tensor of rot_dim / 2 = {desc.rot_dim // 2} values on Q's device")
+    _index_check(dev, "row_start and lens", (row_start, B + 1), (lens, B))
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return rope(desc, Q, K, freqs, Qr, Kr, row_start, lens)
+    rc = lib().pq_rope(C.byref(desc), Q.data_ptr(), qs, None if K is None else K.data_ptr(), ks, dt, T, freqs.data_ptr(),
+                       None if row_start is None else row_start.data_ptr(), None if lens is None else lens.data_ptr(), Qr.data_ptr(), qrs,
+                       None if Kr is None else Kr.data_ptr(), krs, _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return Qr, Kr
+
+
+def make_self_attn_desc(n_heads, n_kv_heads, d_head, n_seqs, scale=None, causal=True, window=0):
+    """scale: 1 / sqrt(d_head) unless given."""
+    return SelfAttnDesc(n_heads, n_kv_heads, d_head, n_seqs, int(causal), window, d_head ** -0.5 if scale is None else scale)
+
+
+def self_attn_bwd_workspace(desc, T, device="cuda"):
+    n = lib().pq_self_attn_bwd_workspace_bytes(C.byref(desc), T)
+    if n == 0:
+        raise PQError(f"bad attention descriptor: {lib().pq_last_error_string().decode()}")
+    return _bytes(n, device)
+
+
+def _self_attn_check(desc, Q, K, V, row_start, O, lse):
+    """What the C side of a call cannot see.  Returns the rows, the strides of Q, K and V, and the device."""
+    H, Hk, d, bf, dev = desc.n_heads, desc.n_kv_heads, desc.d_head, torch.bfloat16, Q.get_device()
+    (T, qs), (Tk, ks), (Tv, vs) = _rows(Q, H, d), _rows(K, Hk, d), _rows(V, Hk, d)
+    if Tk != T or Tv != T or Q.dtype is not bf or K.dtype is not bf or V.dtype is not bf:
+        raise PQError("Q, K and V are bf16 and have as many rows")
+    if O.dtype is not bf or O.numel() != T * H * d or not O.is_contiguous():
+        raise PQError("O and dO are contiguous bf16 tensors of Q's size")
+    if lse.dtype is not torch.float32 or lse.numel() != T * H or not lse.is_contiguous():
+        raise PQError("lse is a contiguous fp32 tensor of one value per row and head")
+    if dev < 0 or K.get_device() != dev or V.get_device() != dev or O.get_device() != dev or lse.get_device() != dev:
+        raise PQError("Q, K, V, O and lse are on one GPU")
+    _index_check(dev, "row_start", (row_start, desc.n_seqs + 1))
+    return T, qs, ks, vs, dev
+
+
+def self_attn_fwd(desc, Q, K, V, row_start, O, lse):
+    """Q [T, n_heads, d_head], K, V [T, n_kv_heads, d_head] bf16, sequences packed row by row (row_start [n_seqs + 1] int32)."""
+    T, qs, ks, vs, dev = _self_attn_check(desc, Q, K, V, row_start, O, lse)
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return self_attn_fwd(desc, Q, K, V, row_start, O, lse)
+    rc = lib().pq_self_attn_fwd(C.byref(desc), Q.data_ptr(), qs, K.data_ptr(), ks, V.data_ptr(), vs, T, row_start.data_ptr(), O.data_ptr(),
+                                lse.data_ptr(), _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return O, lse
+
+
+def self_attn_bwd(desc, dO, Q, K, V, O, lse, row_start, dQ, dK, dV, ws):
+    """The gradients of self_attn_fwd's inputs, from what it was given and left."""
+    T, qs, ks, vs, dev = _self_attn_check(desc, Q, K, V, row_start, O, lse)
+    H, Hk, d, bf = desc.n_heads, desc.n_kv_heads, desc.d_head, torch.bfloat16
+    (Tq, dqs), (Tk, dks), (Tv, dvs) = _rows(dQ, H, d), _rows(dK, Hk, d), _rows(dV, Hk, d)
+    if Tq != T or Tk != T or Tv != T or dQ.dtype is not bf or dK.dtype is not bf or dV.dtype is not bf:
+        raise PQError("dQ, dK and dV are bf16 and have Q's rows")
+    if dO.dtype is not bf or dO.numel() != T * H * d or not dO.is_contiguous():
+        raise PQError("O and dO are contiguous bf16 tensors of Q's size")
+    if (dO.get_device() != dev or dQ.get_device() != dev or dK.get_device() != dev or dV.get_device() != dev or ws.get_device() != dev
+            or ws.dtype is not torch.uint8 or not ws.is_contiguous()):
+        raise PQError("the gradients and the workspace, a contiguous uint8 tensor, are on Q's device")
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return self_attn_bwd(desc, dO, Q, K, V, O, lse, row_start, dQ, dK, dV, ws)
+    rc = lib().pq_self_attn_bwd(C.byref(desc), dO.data_ptr(), Q.data_ptr(), qs, K.data_ptr(), ks, V.data_ptr(), vs, O.data_ptr(), lse.data_ptr(), T,
+                                row_start.data_ptr(), dQ.data_ptr(), dqs, dK.data_ptr(), dks, dV.data_ptr(), dvs, ws.data_ptr(), ws.numel(),
+                                _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return dQ, dK, dV
+
+
+class AdamWTensors:
+    """The tensors of an AdamW step and their states, laid out once for adamw_step and adamw_read.
+
+    params: contiguous tensors of one type, fp32 or bf16, on one GPU; grads: of the same sizes, fp32 or bf16, read anew by every step; masters: fp32, of bf16
+    params, or None.  States m and v that are not given are made here and begin at zero, of `state` (PQ_STATE_F32 or PQ_STATE_8BIT: int8 m, uint8 v and
+    steps [ceil(n / 256), 2] fp32); those that are given say by their type which it is.  m_values, v_values: fp32, where adamw_read writes 8-bit
+    states as the values they stand for, or None.  The tensors must stay where they are."""
+
+    def __init__(self, params, grads, m=None, v=None, steps=None, masters=None, m_values=None, v_values=None, beta1=0.9, beta2=0.999, eps=1e-8,
+                 state=PQ_STATE_F32):
+        params, grads = list(params), list(grads)
+        if not params:
+            raise PQError("an optimizer step without tensors")
+        dev = params[0].get_device()
+        if (m is None) != (v is None):
+            raise PQError("m and v are given together")
+        if m is not None:
+            m, v = list(m), list(v)
+            state = PQ_STATE_8BIT if m and m[0].dtype is torch.int8 else PQ_STATE_F32
+        if state not in (PQ_STATE_F32, PQ_STATE_8BIT):
+            raise PQError(f"unknown state {state}")
+        eight = state == PQ_STATE_8BIT
+        zeros = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=params[0].device)
+        if m is None:
+            m = [zeros(p.shape, torch.int8 if eight else torch.float32) for p in params]
+            v = [zeros(p.shape, torch.uint8 if eight else torch.float32) for p in params]
+        if eight and steps is None:
+            if any(bool(x.any()) for x in m + v):
+                raise PQError("8-bit states that are not zero have steps")
+            steps = [zeros((-(-p.numel() // 256), 2), torch.float32) for p in params]
+        if not eight and steps is not None:
+            raise PQError("steps belong to 8-bit states")
+        f32 = torch.float32
+        kinds = [("params", params, params[0].dtype), ("grads", grads, grads[0].dtype if grads else f32), ("masters", masters, f32),
+                 ("m", m, torch.int8 if eight else f32), ("v", v, torch.uint8 if eight else f32), ("steps", steps, f32),
+                 ("m_values", m_values, f32), ("v_values", v_values, f32)]
+        written = []
+        for name, ts, dtype in kinds:
+            if ts is None:
+                continue
+            if len(ts) != len(params):
+                raise PQError(f"{len(ts)} {name} for {len(params)} params")
+            for t, p in zip(ts, params):
+                n = -(-p.numel() // 256) * 2 if name == "steps" else p.numel()
+                if t.dtype is not dtype or t.get_device() != dev or dev < 0 or not t.is_contiguous() or t.numel() != n:
+                    raise PQError(f"{name}: contiguous {dtype} tensors of their params' sizes on one GPU are wanted"
+                                  + (" (steps: [ceil(n / 256), 2])" if name == "steps" else ""))
+                if n:
+                    written.append((t.data_ptr(), t.data_ptr() + n * t.element_size(), name))
+        written.sort()
+        for (_, end, a), (begin, _, b) in zip(written, written[1:]):
+            if begin < end and not a == b == "grads":
+                raise PQError(f"{a} and {b} overlap")
+        self.desc = AdamWDesc(len(params), _dt(params[0]), _dt(grads[0]), state, int(masters is not None), int(m_values is not None), beta1, beta2, eps)
+        lists = [params, grads, masters, m, v, steps, m_values, v_values]
+        self.params, self.grads, self.masters, self.m, self.v, self.steps, self.m_values, self.v_values = lists
+        arr = (AdamWTensor * len(params))(*[AdamWTensor(*[ts[i].data_ptr() if ts is not None else None for ts in lists], params[i].numel())
+                                            for i in range(len(params))])
+        n = lib().pq_adamw_plan_bytes(C.byref(self.desc), arr)
+        if n == 0:
+            raise PQError(f"bad optimizer tensors: {lib().pq_last_error_string().decode()}")
+        host = torch.empty(n, dtype=torch.uint8)
+        _check(lib().pq_adamw_plan(C.byref(self.desc), arr, host.data_ptr(), n))
+        self.plan, self.device, self._bytes = host.to(params[0].device), dev, n
+
+
+def adamw_scalars(tensors, step, lr, weight_decay=0.0, grad_scale=1.0, out=None):
+    """What changes from step to step (counted from 1), as the device tensor that adamw_step reads; `out`: into that tensor, for steps that are captured."""
+    if step < 1 or lr < 0.0 or weight_decay < 0.0:
+        raise PQError(f"step={step} counts from 1, lr={lr} and weight_decay={weight_decay} are not negative")
+    d = tensors.desc
+    x = torch.tensor([1.0 - lr * weight_decay, lr / (1.0 - d.beta1 ** step), (1.0 - d.beta2 ** step) ** -0.5, grad_scale], dtype=torch.float64).float()
+    if out is None:
+        return x.to(tensors.plan.device)
+    if out.dtype is not torch.float32 or out.numel() != 4 or not out.is_contiguous() or out.get_device() != tensors.device:
+        raise PQError("scalars are a contiguous fp32 tensor of four values on the tensors' device")
+    return out.copy_(x)
+
+
+def adamw_step(tensors, scalars):
+    """One step of all tensors, with the gradients as they are now."""
+    dev = tensors.device
+    if scalars.dtype is not torch.float32 or scalars.numel() != 4 or not scalars.is_contiguous() or scalars.get_device() != dev:
+        raise PQError("scalars are a contiguous fp32 tensor of four values on the tensors' device")
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return adamw_step(tensors, scalars)
+    rc = lib().pq_adamw_step(C.byref(tensors.desc), tensors.plan.data_ptr(), tensors._bytes, scalars.data_ptr(), _raw_stream(dev))
+    if rc:
+        _check(rc)
+
+
+def adamw_read(tensors):
+    """8-bit states as the values they stand for, into m_values and v_values."""
+    dev = tensors.device
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return adamw_read(tensors)
+    rc = lib().pq_adamw_read(C.byref(tensors.desc), tensors.plan.data_ptr(), tensors._bytes, _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return tensors.m_values, tensors.v_values
 
 
 def glue_lincomb(out, xs, cs):

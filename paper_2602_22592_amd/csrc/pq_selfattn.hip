@@ -1,0 +1,742 @@
+// Attention over the rows of a call, for training: forward pass and gradients.
+//
+//     s_ij = scale q_i . k_j (visible j),  lse_i = log sum_j exp s_ij,  p_ij = exp(s_ij - lse_i),  o_i = sum_j p_ij v_j
+//     delta_i = sum_d dO_id O_id,  dP_ij = dO_i . v_j,  dS_ij = p_ij (dP_ij - delta_i)
+//     dQ_i = scale sum_j dS_ij k_j,   dK_j = scale sum_i dS_ij q_i,   dV_j = sum_i p_ij dO_i     (j's sums over the heads that share it, too)
+//
+// No tensor of scores exists: tiles of 32 x 32 scores are formed by v_mfma_f32_32x32x16_bf16, used, and formed again from lse in the backward pass.
+#include "pq_kv.h"
+
+#include <atomic>
+#include <cmath>
+
+namespace {
+
+#define PQ_REQUIRE(cond, code, ...) \
+  do { if (!(cond)) return pq_set_error(code, __VA_ARGS__); } while (0)
+
+constexpr int SA_ROWS = 128;      // rows of a workgroup's tile, 32 a wavefront
+constexpr int SA_STAGE = 64;      // rows of a stage in LDS
+constexpr float SA_LOG2E = 1.4426950408889634f;
+
+struct self_args {
+  const uint16_t *Q, *K, *V, *O, *dO;
+  int64_t qs, ks, vs;            // elements between rows
+  uint16_t *out, *dQ, *dK, *dV;
+  int64_t dqs, dks, dvs;
+  float* lse;                    // [T][heads]
+  float2* stats;                 // [heads][T]: lse times log2 e, delta
+  const int32_t* row_start;
+  int T, n_seqs, heads, kv_heads, group, d, causal, window, tiles;
+  float c;                       // |scale| log2 e; the sign is in the operand that stays in registers
+  float scale;
+};
+
+// ---------------------------------------------------------------------------------------------
+// Tiles in LDS: rows of DP elements as they lie in memory, their pieces of 16 bytes exchanged within runs of eight (four where DP is an odd number
+// of 32s) by a number that the row gives, so that both ways of reading go through all banks: eight rows' same piece (operand rows), and
+// two neighbouring pieces of four rows (the transposing reads).
+// ---------------------------------------------------------------------------------------------
+template <int DP> __device__ __forceinline__ int piece_at(int row, int c) {
+  if constexpr (DP % 64 == 0) {
+    const int f = ((row & 3) << 1) | ((row >> 2) & 1);
+    return (c & ~7) | ((c ^ f) & 7);
+  } else {
+    return (c & ~3) | ((c ^ (row >> 2)) & 3);
+  }
+}
+
+typedef int i32x4_u_t __attribute__((ext_vector_type(4), aligned(4)));
+// Eight elements of a row of d from element `at` on, zeros behind its end.
+__device__ __forceinline__ i32x4_t load_piece(const uint16_t* q, int d, int at) {
+  i32x4_t x = {0, 0, 0, 0};
+  if (at + 8 <= d) {
+    x = *reinterpret_cast<const i32x4_u_t*>(q + at);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at + 2 * j < d) x[j] = *reinterpret_cast<const int*>(q + at + 2 * j);
+  }
+  return x;
+}
+
+// Sixteen bytes a lane from memory to LDS, lane by lane from `lds` on.  (Not through the compiler's builtin: it would wait for these loads in
+// front of every later read of LDS, of the other buffer as well.)
+__device__ __forceinline__ void load_to_lds(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+// A stage of SA_STAGE rows of one tensor on its way to LDS.  DIRECT: rows and heads lie at multiples of 16 bytes, the loads go straight there;
+// otherwise through registers.  Rows behind the sequence's last are the last once more: whoever uses the stage hides them.
+template <int DP, bool DIRECT>
+struct stage_t {
+  static constexpr int CPR = DP / 8, N = SA_STAGE * CPR / 256, BYTES = SA_STAGE * DP * 2;
+  i32x4_t hold[DIRECT ? 1 : N];
+
+  __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, int first, int n, int d, unsigned char* lds) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int L = (wave * N + i) * 64 + lane, row = L / CPR, c = piece_at<DP>(row, L % CPR);
+      const uint16_t* p = base + (int64_t)min(first + row, n - 1) * stride;
+      if constexpr (DIRECT) {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (wave * N + i) * 1024);
+        if (c * 8 < d) load_to_lds(p + c * 8, to);
+      } else {
+        hold[i] = load_piece(p, d, c * 8);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char* lds) {
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) *reinterpret_cast<i32x4_t*>(lds + ((threadIdx.x >> 6) * N + i) * 1024 + (threadIdx.x & 63) * 16) = hold[i];
+    }
+  }
+  // Pieces behind d are never written by direct loads: zeros, once.
+  static __device__ __forceinline__ void clear(unsigned char* lds, int d) {
+    if constexpr (DIRECT) {
+      if (d == DP) return;
+      for (int L = threadIdx.x; L < SA_STAGE * CPR; L += 256)
+        if (piece_at<DP>(L / CPR, L % CPR) * 8 >= d) *reinterpret_cast<i32x4_t*>(lds + L * 16) = i32x4_t{0, 0, 0, 0};
+    }
+  }
+};
+
+// Operand of 32 rows (row l % 32) and elements 16 step + 8 (l / 32) .. of the contraction.
+template <int DP> __device__ __forceinline__ bf16x8_t row_operand(const unsigned char* lds, int row0, int step) {
+  const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+  return *reinterpret_cast<const bf16x8_t*>(lds + (row0 + r) * (DP * 2) + (piece_at<DP>(r, 2 * step + h) << 4));
+}
+// Operand of 32 columns (column 32 block + l % 32) whose contraction runs over the 16 rows from row0 on, in the order in which the lanes hold a
+// tile's rows: 4 h + 0 .. 3, 8 + 4 h + 0 .. 3.
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+template <int DP> __device__ __forceinline__ bf16x8_t column_operand(const unsigned char* lds, int row0, int block) {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int r = 4 * h + ((lane & 15) >> 2), c = 4 * block + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), in = (lane & 1) * 8;
+  auto at = [&](int row) { return lds + (row0 + row) * (DP * 2) + (piece_at<DP>(row, c) << 4) + in; };
+  typedef __attribute__((address_space(3))) s16x4_t* p3;
+  const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)at(r));
+  const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)at(r + 8));
+  const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+  return __builtin_bit_cast(bf16x8_t, make_uint4(a.x, a.y, b.x, b.y));
+}
+// The operand that stays in registers: columns are rows `row` (per lane) of a tensor.
+template <int DP> __device__ __forceinline__ void load_columns(bf16x8_t* x, const uint16_t* row, int d, bool negative) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    i32x4_t w = load_piece(row, d, 16 * s + 8 * h);
+    if (negative)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] ^= (int)0x80008000u;
+    x[s] = __builtin_bit_cast(bf16x8_t, w);
+  }
+}
+
+__device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// Register j of a tile is its row 8 (j / 4) + 4 h + j % 4.
+__device__ __forceinline__ constexpr int tile_row(int j) { return 8 * (j >> 2) + (j & 3); }
+
+// Eight rows of a tile as the second product's operand (registers 8 u .. 8 u + 7).
+__device__ __forceinline__ bf16x8_t as_operand(const f32x16_t& x, int u) {
+  uint4 w;
+  w.x = pack_bf16x2(x[8 * u], x[8 * u + 1]);
+  w.y = pack_bf16x2(x[8 * u + 2], x[8 * u + 3]);
+  w.z = pack_bf16x2(x[8 * u + 4], x[8 * u + 5]);
+  w.w = pack_bf16x2(x[8 * u + 6], x[8 * u + 7]);
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+
+// a x b where b holds zeros for what is not seen, which an infinity or a NaN of a must not reach (0 times infinity is NaN): such elements are left
+// out, and where they are seen the sum becomes infinite (twice the largest bf16 number is beyond fp32).
+__device__ __forceinline__ f32x16_t mfma_seen(bf16x8_t a, bf16x8_t b, uint32_t seen /* bits of the operand's eight rows */, f32x16_t c) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+  const uint4 w = __builtin_bit_cast(uint4, a);
+  const bf16x2_t zero = {(__bf16)0.0f, (__bf16)0.0f};
+  float z = 0.0f;
+  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.x), zero, z, false);
+  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.y), zero, z, false);
+  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.z), zero, z, false);
+  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.w), zero, z, false);
+  if (__builtin_expect(__ballot(!(z == 0.0f)) == 0, 1)) return mfma(a, b, c);
+  uint32_t clean[4] = {w.x, w.y, w.z, w.w}, top[4], ones[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t x = clean[j], lo = (x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+    clean[j] = x & ~(lo | hi);
+    top[j] = 0x7f7f7f7fu & (lo | hi);
+    ones[j] = ((seen >> (2 * j)) & 1 ? 0x3f80u : 0u) | ((seen >> (2 * j + 1)) & 1 ? 0x3f800000u : 0u);
+  }
+  const bf16x8_t t = __builtin_bit_cast(bf16x8_t, make_uint4(top[0], top[1], top[2], top[3]));
+  const bf16x8_t s = __builtin_bit_cast(bf16x8_t, make_uint4(ones[0], ones[1], ones[2], ones[3]));
+  c = mfma(__builtin_bit_cast(bf16x8_t, make_uint4(clean[0], clean[1], clean[2], clean[3])), b, c);
+  c = mfma(t, s, c);
+  return mfma(t, s, c);
+}
+
+// The value of the other half's lane joined to a lane's own (both halves hold the same columns).
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+
+// Which sequence and which of its tiles of SA_ROWS rows virtual tile vt is: sequence b owns those from floor(first row / SA_ROWS) + b on, at least as
+// many as it has.
+struct self_tile { int r0, n, at; };     // rows r0 .. r0 + n - 1 of the call, the tile's first row among them (n == 0: none)
+__device__ __forceinline__ self_tile find_self_tile(const self_args& a, int vt) {
+  auto first = [&](int i) { return min(max(a.row_start[i], 0), a.T); };
+  const int b = kv_find_seq(a.n_seqs, vt, [&](int i) { return first(i) / SA_ROWS + i; });
+  self_tile t = {0, 0, 0};
+  if (b < 0) return t;
+  t.r0 = first(b);
+  const int n = max(first(b + 1), t.r0) - t.r0;
+  t.at = (vt - (t.r0 / SA_ROWS + b)) * SA_ROWS;
+  if (t.at < n) t.n = n;
+  return t;
+}
+// Tokens that rows from .. to - 1 of a sequence of n see between them.
+__device__ __forceinline__ int first_token(const self_args& a, int row) { return a.window > 0 && row >= a.window ? row - a.window + 1 : 0; }
+
+// What a wavefront's 32 rows see of tokens j0 .. j0 + count - 1: nothing, a part, all.
+enum { SEES_NONE, SEES_PART, SEES_ALL };
+__device__ __forceinline__ int sees(const self_args& a, int n, int row0, int rows, int j0, int count) {
+  const int last = min(row0 + rows, n) - 1;                // (rows behind the last are nobody's)
+  if (last < row0 || j0 >= n) return SEES_NONE;
+  if (a.causal && j0 > last) return SEES_NONE;
+  if (j0 + count <= first_token(a, row0)) return SEES_NONE;
+  if (j0 + count > n || row0 + rows > n) return SEES_PART;
+  if (a.causal && j0 + count - 1 > row0) return SEES_PART;
+  if (j0 < first_token(a, last)) return SEES_PART;
+  return SEES_ALL;
+}
+
+typedef uint32_t u32x2_u_t __attribute__((ext_vector_type(2), aligned(4)));
+__device__ __forceinline__ void store_four(uint16_t* row, int d, int at, const float* x) {
+  const uint32_t lo = pack_bf16x2(x[0], x[1]), hi = pack_bf16x2(x[2], x[3]);
+  if (at + 4 <= d) *reinterpret_cast<u32x2_u_t*>(row + at) = u32x2_u_t{lo, hi};
+  else if (at < d) *reinterpret_cast<uint32_t*>(row + at) = lo;
+}
+// Accumulators [DP / 32] of a column each lane (elements 32 i + 8 q + 4 h + j) times f into a row.
+template <int DP> __device__ __forceinline__ void store_column(const f32x16_t* acc, float f, uint16_t* row, int d) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float x[4] = {acc[i][4 * q] * f, acc[i][4 * q + 1] * f, acc[i][4 * q + 2] * f, acc[i][4 * q + 3] * f};
+      store_four(row, d, 32 * i + 8 * q + 4 * h, x);
+    }
+}
+
+// Head and tile of a workgroup: the heads first, those of a key-value head a multiple of kv_heads apart (its tokens then stay in one L2).
+struct self_place { int head, kv_head, vt; };
+__device__ __forceinline__ self_place place_of(const self_args& a, bool last_first) {
+  const int t = blockIdx.x / a.heads, x = blockIdx.x - t * a.heads, kv = x % a.kv_heads;
+  return {kv * a.group + x / a.kv_heads, kv, last_first ? a.tiles - 1 - t : t};
+}
+
+// ---------------------------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------------------------
+template <int DP, bool PART>
+__device__ __forceinline__ void forward_stage(const self_args& a, const unsigned char* lk, const unsigned char* lv, const bf16x8_t* q, f32x16_t* o,
+                                              float& m, float& l, int low, int lim) {
+  constexpr int NK = DP / 32;
+  const int h = (threadIdx.x & 63) >> 5;
+  f32x16_t s[2];
+  uint32_t seen[2] = {0xffffu, 0xffffu};
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    f32x16_t x = {};
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) x = mfma(row_operand<DP>(lk, 32 * t, k), q[k], x);
+    if constexpr (PART) {
+      seen[t] = 0;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int at = 32 * t + tile_row(j) + 4 * h;
+        const bool v = at >= low && at <= lim;
+        x[j] = v ? x[j] : -INFINITY;
+        seen[t] |= (v ? 1u : 0u) << j;
+      }
+    }
+    s[t] = x;
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int j = 1; j < 32; ++j) top = fmaxf(top, s[j >> 4][j & 15]);
+  top = fmaxf(top, other_half(top)) * a.c;
+  // the reference moves only when a score exceeds it by 16 powers of two (any reference gives the same quotient)
+  if (__ballot(top > m + 16.0f)) {
+    const float next = fmaxf(m, top), f = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+    m = next;
+    l *= f;
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] *= f;
+  }
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      s[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j], a.c, -ref));
+      if constexpr (PART) s[t][j] = (seen[t] >> j) & 1 ? s[t][j] : 0.0f;      // (a scale of 0 makes NaN of the hidden ones' -infinity)
+      sum[j & 1] += s[t][j];
+    }
+  l += sum[0] + sum[1];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8_t p = as_operand(s[t], u);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const bf16x8_t v = column_operand<DP>(lv, 32 * t + 16 * u, i);
+        if constexpr (PART) o[i] = mfma_seen(v, p, seen[t] >> (8 * u), o[i]);
+        else o[i] = mfma(v, p, o[i]);
+      }
+    }
+}
+
+template <int DP, bool DIRECT>
+__global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
+  constexpr int NK = DP / 32;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  typedef stage_t<DP, DIRECT> stage;
+  const self_place w = place_of(a, true);
+  const self_tile t = find_self_tile(a, w.vt);
+  if (t.n == 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int row0 = t.at + 32 * wave, row = row0 + (lane & 31);
+  const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
+  const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
+  const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n;
+  int j0 = first_token(a, t.at) & ~(SA_STAGE - 1);
+  constexpr int BUF = 2 * stage::BYTES;
+  stage k, v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) stage::clear(lds + i * stage::BYTES, a.d);
+  k.load(K, a.ks, j0, t.n, a.d, lds);
+  v.load(V, a.vs, j0, t.n, a.d, lds + stage::BYTES);
+  bf16x8_t q[DP / 16];
+  load_columns<DP>(q, a.Q + ((int64_t)t.r0 + min(row, t.n - 1)) * a.qs + w.head * a.d, a.d, a.scale < 0.0f);
+  f32x16_t o[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) o[i] = f32x16_t{};
+  float m = -INFINITY, l = 0.0f;
+  k.store(lds);
+  v.store(lds + stage::BYTES);
+  int at = 0;
+  for (; j0 < end; j0 += SA_STAGE, at ^= 1) {
+    wait_loads();
+    __syncthreads();                                  // everybody's loads are there, and nobody reads the other buffer any more
+    const bool more = j0 + SA_STAGE < end;
+    unsigned char *here = lds + at * BUF, *next = lds + (at ^ 1) * BUF;
+    if (more) {
+      k.load(K, a.ks, j0 + SA_STAGE, t.n, a.d, next);
+      v.load(V, a.vs, j0 + SA_STAGE, t.n, a.d, next + stage::BYTES);
+    }
+    const int see = sees(a, t.n, row0, 32, j0, SA_STAGE);
+    const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
+    if (see == SEES_ALL) forward_stage<DP, false>(a, here, here + stage::BYTES, q, o, m, l, low, lim);
+    else if (see == SEES_PART) forward_stage<DP, true>(a, here, here + stage::BYTES, q, o, m, l, low, lim);
+    if (more) {
+      k.store(next);
+      v.store(next + stage::BYTES);
+    }
+  }
+  l += other_half(l);
+  if (row >= t.n) return;
+  const int64_t out = ((int64_t)t.r0 + row) * a.heads + w.head;
+  store_column<DP>(o, 1.0f / l, a.out + out * a.d, a.d);
+  if (lane < 32) a.lse[out] = (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Gradient of the queries.  Leaves lse and delta head by head for the other kernel.
+// ---------------------------------------------------------------------------------------------
+// A row that sees one token has p = 1 whatever its score: no gradient passes through it.
+__device__ __forceinline__ bool sees_one(const self_args& a, int n, int row) { return n == 1 || (a.causal && (row == 0 || a.window == 1)); }
+
+template <int DP, bool PART>
+__device__ __forceinline__ void query_block(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q,
+                                            const bf16x8_t* g, f32x16_t* dq, float lse, float delta, int low, int lim, bool one) {
+  constexpr int NK = DP / 32;
+  const int h = (threadIdx.x & 63) >> 5;
+  f32x16_t s = {}, dp;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) dp[j] = -delta;
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) s = mfma(row_operand<DP>(lk, at, k), q[k], s);
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) dp = mfma(row_operand<DP>(lv, at, k), g[k], dp);
+  uint32_t seen = 0xffffu;
+  if constexpr (PART) seen = 0;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], a.c, -lse));
+    float x = p * dp[j];
+    if constexpr (PART) {
+      const int tok = at + tile_row(j) + 4 * h;
+      const bool v = tok >= low && tok <= lim && !one;
+      x = v ? x : 0.0f;
+      seen |= (v ? 1u : 0u) << j;
+    }
+    s[j] = x;
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const bf16x8_t x = as_operand(s, u);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const bf16x8_t k = column_operand<DP>(lk, at + 16 * u, i);
+      if constexpr (PART) dq[i] = mfma_seen(k, x, seen >> (8 * u), dq[i]);
+      else dq[i] = mfma(k, x, dq[i]);
+    }
+  }
+}
+
+template <int DP, bool DIRECT>
+__global__ __launch_bounds__(256, 2) void self_query_kernel(self_args a) {
+  constexpr int NK = DP / 32;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  typedef stage_t<DP, DIRECT> stage;
+  const self_place w = place_of(a, true);
+  const self_tile t = find_self_tile(a, w.vt);
+  if (t.n == 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int row0 = t.at + 32 * wave, row = row0 + (lane & 31);
+  const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
+  const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
+  const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n;
+  int j0 = first_token(a, t.at) & ~(SA_STAGE - 1);
+  constexpr int BUF = 2 * stage::BYTES;
+  stage k, v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) stage::clear(lds + i * stage::BYTES, a.d);
+  k.load(K, a.ks, j0, t.n, a.d, lds);
+  v.load(V, a.vs, j0, t.n, a.d, lds + stage::BYTES);
+  const int64_t mine = (int64_t)t.r0 + min(row, t.n - 1);
+  bf16x8_t q[DP / 16], g[DP / 16];
+  load_columns<DP>(q, a.Q + mine * a.qs + w.head * a.d, a.d, a.scale < 0.0f);
+  load_columns<DP>(g, a.dO + (mine * a.heads + w.head) * a.d, a.d, false);
+  float delta = 0.0f;
+  {
+    bf16x8_t o[DP / 16];
+    load_columns<DP>(o, a.O + (mine * a.heads + w.head) * a.d, a.d, false);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)o[s][j], (float)g[s][j], delta);
+  }
+  delta += other_half(delta);
+  const float lse = a.lse[mine * a.heads + w.head] * SA_LOG2E;
+  if (row < t.n && lane < 32) a.stats[(int64_t)w.head * a.T + mine] = make_float2(lse, delta);
+  const bool one = sees_one(a, t.n, row);
+  f32x16_t dq[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) dq[i] = f32x16_t{};
+  k.store(lds);
+  v.store(lds + stage::BYTES);
+  int at = 0;
+  for (; j0 < end; j0 += SA_STAGE, at ^= 1) {
+    wait_loads();
+    __syncthreads();
+    const bool more = j0 + SA_STAGE < end;
+    unsigned char *here = lds + at * BUF, *next = lds + (at ^ 1) * BUF;
+    if (more) {
+      k.load(K, a.ks, j0 + SA_STAGE, t.n, a.d, next);
+      v.load(V, a.vs, j0 + SA_STAGE, t.n, a.d, next + stage::BYTES);
+    }
+    const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
+#pragma unroll 1
+    for (int part = 0; part < SA_STAGE; part += 32) {
+      const int see = sees(a, t.n, row0, 32, j0 + part, 32);
+      if (see == SEES_ALL) query_block<DP, false>(a, here, here + stage::BYTES, part, q, g, dq, lse, delta, low, lim, one);
+      else if (see == SEES_PART) query_block<DP, true>(a, here, here + stage::BYTES, part, q, g, dq, lse, delta, low, lim, one);
+    }
+    if (more) {
+      k.store(next);
+      v.store(next + stage::BYTES);
+    }
+  }
+  if (row < t.n) store_column<DP>(dq, a.scale, a.dQ + mine * a.dqs + w.head * a.d, a.d);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Gradients of the keys and values
+// ---------------------------------------------------------------------------------------------
+template <int DP, bool PART>
+__device__ __forceinline__ void token_block(const self_args& a, const unsigned char* lq, const unsigned char* lg, const float* lst, int at, int n, int i0,
+                                            int tok, const bf16x8_t* k, const bf16x8_t* v, f32x16_t* dk, f32x16_t* dv) {
+  constexpr int NK = DP / 32;
+  const int h = (threadIdx.x & 63) >> 5;
+  f32x16_t s = {}, dp;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(lst + SA_STAGE + at + 8 * b + 4 * h);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dp[4 * b + j] = -x[j];
+  }
+#pragma unroll
+  for (int x = 0; x < DP / 16; ++x) s = mfma(row_operand<DP>(lq, at, x), k[x], s);
+#pragma unroll
+  for (int x = 0; x < DP / 16; ++x) dp = mfma(row_operand<DP>(lg, at, x), v[x], dp);
+  uint32_t seen = 0xffffu, through = 0xffffu;
+  if constexpr (PART) seen = through = 0;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const f32x4_t lse = *reinterpret_cast<const f32x4_t*>(lst + at + 8 * b + 4 * h);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int x = 4 * b + j;
+      float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], a.c, -lse[j])), ds = p * dp[x];
+      if constexpr (PART) {
+        const int row = i0 + at + 8 * b + 4 * h + j;
+        const bool vis = row < n && tok < n && (!a.causal || tok <= row) && tok >= first_token(a, row), pass = vis && !sees_one(a, n, row);
+        p = vis ? p : 0.0f;
+        ds = pass ? ds : 0.0f;
+        seen |= (vis ? 1u : 0u) << x;
+        through |= (pass ? 1u : 0u) << x;
+      }
+      s[x] = p;
+      dp[x] = ds;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const bf16x8_t x = as_operand(s, u), y = as_operand(dp, u);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const bf16x8_t g = column_operand<DP>(lg, at + 16 * u, i);
+      if constexpr (PART) dv[i] = mfma_seen(g, x, seen >> (8 * u), dv[i]);
+      else dv[i] = mfma(g, x, dv[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const bf16x8_t q = column_operand<DP>(lq, at + 16 * u, i);
+      if constexpr (PART) dk[i] = mfma_seen(q, y, through >> (8 * u), dk[i]);
+      else dk[i] = mfma(q, y, dk[i]);
+    }
+  }
+}
+
+template <int DP, bool DIRECT>
+__global__ __launch_bounds__(256, DP > 96 ? 1 : 2) void self_token_kernel(self_args a) {
+  constexpr int NK = DP / 32;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  typedef stage_t<DP, DIRECT> stage;
+  const int vt = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - vt * a.kv_heads;
+  const self_tile t = find_self_tile(a, vt);
+  if (t.n == 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int tok0 = t.at + 32 * wave, tok = tok0 + (lane & 31);
+  // rows that see the tile's tokens
+  const int begin = (a.causal ? t.at : 0) & ~(SA_STAGE - 1);
+  const int last = min(t.at + SA_ROWS, t.n) - 1, end = a.window > 0 && a.window < t.n - last ? last + a.window : t.n;
+  const int per_head = (end - begin + SA_STAGE - 1) / SA_STAGE, steps = per_head * a.group;
+  constexpr int BUF = 2 * stage::BYTES + SA_STAGE * 8;
+  const uint16_t* Q = a.Q + (int64_t)t.r0 * a.qs + (int64_t)kv_head * a.group * a.d;
+  const uint16_t* G = a.dO + ((int64_t)t.r0 * a.heads + (int64_t)kv_head * a.group) * a.d;
+  const int64_t gs = (int64_t)a.heads * a.d;
+  stage q, g;
+  float2 st = make_float2(0.0f, 0.0f);
+  auto load = [&](int step, unsigned char* to) {
+    const int head = step / per_head, i0 = begin + (step - head * per_head) * SA_STAGE;
+    q.load(Q + head * a.d, a.qs, i0, t.n, a.d, to);
+    g.load(G + head * a.d, gs, i0, t.n, a.d, to + stage::BYTES);
+    if (threadIdx.x < SA_STAGE)
+      st = a.stats[(int64_t)(kv_head * a.group + head) * a.T + t.r0 + min(i0 + (int)threadIdx.x, t.n - 1)];
+  };
+  auto store = [&](unsigned char* to) {
+    q.store(to);
+    g.store(to + stage::BYTES);
+    if (threadIdx.x < SA_STAGE) {
+      float* s = reinterpret_cast<float*>(to + 2 * stage::BYTES);
+      s[threadIdx.x] = st.x;
+      s[SA_STAGE + threadIdx.x] = st.y;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) stage::clear(lds + (i >> 1) * BUF + (i & 1) * stage::BYTES, a.d);
+  load(0, lds);
+  const int64_t mine = (int64_t)t.r0 + min(tok, t.n - 1);
+  bf16x8_t k[DP / 16], v[DP / 16];
+  load_columns<DP>(k, a.K + mine * a.ks + kv_head * a.d, a.d, a.scale < 0.0f);
+  load_columns<DP>(v, a.V + mine * a.vs + kv_head * a.d, a.d, false);
+  f32x16_t dk[NK], dv[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) dk[i] = dv[i] = f32x16_t{};
+  store(lds);
+  int at = 0;
+  for (int step = 0; step < steps; ++step, at ^= 1) {
+    wait_loads();
+    __syncthreads();
+    const bool more = step + 1 < steps;
+    unsigned char *here = lds + at * BUF, *next = lds + (at ^ 1) * BUF;
+    if (more) load(step + 1, next);
+    const int head = step / per_head, i0 = begin + (step - head * per_head) * SA_STAGE;
+    const float* lst = reinterpret_cast<const float*>(here + 2 * stage::BYTES);
+#pragma unroll 1
+    for (int part = 0; part < SA_STAGE; part += 32) {
+      const int see = sees(a, t.n, i0 + part, 32, tok0, 32);
+      if (see == SEES_ALL) token_block<DP, false>(a, here, here + stage::BYTES, lst, part, t.n, i0, tok, k, v, dk, dv);
+      else if (see == SEES_PART) token_block<DP, true>(a, here, here + stage::BYTES, lst, part, t.n, i0, tok, k, v, dk, dv);
+    }
+    if (more) store(next);
+  }
+  if (tok >= t.n) return;
+  store_column<DP>(dk, a.scale, a.dK + mine * a.dks + kv_head * a.d, a.d);
+  store_column<DP>(dv, 1.0f, a.dV + mine * a.dvs + kv_head * a.d, a.d);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------------------------
+int check_self(const pq_self_attn_desc* d) {
+  PQ_REQUIRE(d, PQ_ERR_BAD_ARG, "NULL descriptor");
+  PQ_REQUIRE(d->n_seqs >= 0, PQ_ERR_BAD_ARG, "n_seqs=%d is negative", d->n_seqs);
+  PQ_REQUIRE(d->n_heads > 0 && d->n_kv_heads > 0 && d->n_heads % d->n_kv_heads == 0, PQ_ERR_SHAPE, "n_heads=%d must be a multiple of n_kv_heads=%d",
+             d->n_heads, d->n_kv_heads);
+  PQ_REQUIRE(d->d_head >= 2 && d->d_head <= 128 && d->d_head % 2 == 0, PQ_ERR_SHAPE, "d_head=%d must be even and in 2..128", d->d_head);
+  PQ_REQUIRE((int64_t)d->n_heads * d->d_head <= 0x7fffffff, PQ_ERR_SHAPE, "n_heads=%d is too many", d->n_heads);
+  PQ_REQUIRE(d->causal == 0 || d->causal == 1, PQ_ERR_BAD_ARG, "causal=%d must be 0 or 1", d->causal);
+  PQ_REQUIRE(d->window >= 0 && (d->causal || d->window == 0), PQ_ERR_BAD_ARG, "window=%d must not be negative, and needs causal", d->window);
+  PQ_REQUIRE(std::isfinite(d->scale), PQ_ERR_BAD_ARG, "scale must be finite");
+  return PQ_OK;
+}
+int check_rows(const pq_self_attn_desc* d, int T) {
+  PQ_REQUIRE(T >= 0, PQ_ERR_BAD_ARG, "T=%d is negative", T);
+  PQ_REQUIRE(T <= (1 << 29) && (int64_t)T * d->n_heads <= 0x7fffffff &&
+                 ((int64_t)T / SA_ROWS + d->n_seqs) * d->n_heads <= 0x7fffffff, PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call",
+             T, d->n_heads, d->n_seqs);
+  return PQ_OK;
+}
+int check_stride(const char* name, int64_t stride, int heads, int d) {
+  PQ_REQUIRE(stride >= (int64_t)heads * d && stride % 2 == 0, PQ_ERR_SHAPE, "%s: row stride %lld must be even and at least %lld", name,
+             (long long)stride, (long long)heads * d);
+  return PQ_OK;
+}
+bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+self_args make_args(const pq_self_attn_desc* d, int T, const int32_t* row_start) {
+  self_args a = {};
+  a.T = T; a.n_seqs = d->n_seqs; a.heads = d->n_heads; a.kv_heads = d->n_kv_heads; a.group = d->n_heads / d->n_kv_heads; a.d = d->d_head;
+  a.causal = d->causal; a.window = d->window; a.tiles = T / SA_ROWS + d->n_seqs;
+  a.c = fabsf(d->scale) * SA_LOG2E;
+  a.scale = d->scale;
+  a.row_start = row_start;
+  return a;
+}
+
+int allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& asked) {
+  if (bytes <= 65536) return PQ_OK;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return pq_set_error(PQ_ERR_HIP, "hipGetDevice failed");
+  const uint64_t bit = (uint64_t)1 << (dev & 63);
+  if (asked.load(std::memory_order_relaxed) & bit) return PQ_OK;
+  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
+    return pq_set_error(PQ_ERR_HIP, "hipFuncSetAttribute failed for an attention kernel");
+  asked.fetch_or(bit, std::memory_order_relaxed);
+  return PQ_OK;
+}
+
+template <int DP, bool DIRECT> int launch_forward(const self_args& a, hipStream_t s) {
+  static std::atomic<uint64_t> asked;
+  constexpr int lds = 4 * stage_t<DP, DIRECT>::BYTES;
+  if (int e = allow_lds((const void*)self_forward_kernel<DP, DIRECT>, lds, asked)) return e;
+  self_forward_kernel<DP, DIRECT><<<(unsigned)(a.tiles * a.heads), 256, lds, s>>>(a);
+  PQ_CHECK_LAUNCH("self_forward_kernel");
+  return PQ_OK;
+}
+template <int DP, bool DIRECT> int launch_backward(const self_args& a, hipStream_t s) {
+  static std::atomic<uint64_t> asked[2];
+  constexpr int lds = 4 * stage_t<DP, DIRECT>::BYTES;
+  if (int e = allow_lds((const void*)self_query_kernel<DP, DIRECT>, lds, asked[0])) return e;
+  if (int e = allow_lds((const void*)self_token_kernel<DP, DIRECT>, lds + SA_STAGE * 16, asked[1])) return e;
+  self_query_kernel<DP, DIRECT><<<(unsigned)(a.tiles * a.heads), 256, lds, s>>>(a);
+  PQ_CHECK_LAUNCH("self_query_kernel");
+  self_token_kernel<DP, DIRECT><<<(unsigned)(a.tiles * a.kv_heads), 256, lds + SA_STAGE * 16, s>>>(a);
+  PQ_CHECK_LAUNCH("self_token_kernel");
+  return PQ_OK;
+}
+template <bool DIRECT> int launch_forward_d(const self_args& a, hipStream_t s) {
+  switch ((a.d + 31) / 32) {
+    case 1: return launch_forward<32, DIRECT>(a, s);
+    case 2: return launch_forward<64, DIRECT>(a, s);
+    case 3: return launch_forward<96, DIRECT>(a, s);
+    default: return launch_forward<128, DIRECT>(a, s);
+  }
+}
+template <bool DIRECT> int launch_backward_d(const self_args& a, hipStream_t s) {
+  switch ((a.d + 31) / 32) {
+    case 1: return launch_backward<32, DIRECT>(a, s);
+    case 2: return launch_backward<64, DIRECT>(a, s);
+    case 3: return launch_backward<96, DIRECT>(a, s);
+    default: return launch_backward<128, DIRECT>(a, s);
+  }
+}
+
+}  // namespace
+
+extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
+                                int64_t v_stride, int32_t T, const int32_t* row_start, void* O, float* lse, void* stream) {
+  if (int e = check_self(d)) return e;
+  if (int e = check_rows(d, T)) return e;
+  if (T == 0 || d->n_seqs == 0) return PQ_OK;
+  PQ_REQUIRE(Q && K && V && O && lse && row_start, PQ_ERR_BAD_ARG, "NULL buffer");
+  if (int e = check_stride("Q", q_stride, d->n_heads, d->d_head)) return e;
+  if (int e = check_stride("K", k_stride, d->n_kv_heads, d->d_head)) return e;
+  if (int e = check_stride("V", v_stride, d->n_kv_heads, d->d_head)) return e;
+  PQ_REQUIRE(at16(Q) && at16(K) && at16(V) && at16(O), PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
+  self_args a = make_args(d, T, row_start);
+  a.Q = (const uint16_t*)Q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
+  a.qs = q_stride; a.ks = k_stride; a.vs = v_stride;
+  a.out = (uint16_t*)O; a.lse = lse;
+  hipStream_t s = (hipStream_t)stream;
+  pq_prof_scope prof(PQP_SELF_ATTN_FWD, s);
+  const bool direct = a.d % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
+  return direct ? launch_forward_d<true>(a, s) : launch_forward_d<false>(a, s);
+}
+
+extern "C" size_t pq_self_attn_bwd_workspace_bytes(const pq_self_attn_desc* d, int32_t T) {
+  if (check_self(d) || check_rows(d, T)) return 0;
+  return pq_align_up((size_t)T * d->n_heads * sizeof(float2), 256) + 256;
+}
+
+extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                                const void* V, int64_t v_stride, const void* O, const float* lse, int32_t T, const int32_t* row_start, void* dQ,
+                                int64_t dq_stride, void* dK, int64_t dk_stride, void* dV, int64_t dv_stride, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  if (int e = check_self(d)) return e;
+  if (int e = check_rows(d, T)) return e;
+  if (T == 0 || d->n_seqs == 0) return PQ_OK;
+  PQ_REQUIRE(dO && Q && K && V && O && lse && row_start && dQ && dK && dV && workspace, PQ_ERR_BAD_ARG, "NULL buffer");
+  if (int e = check_stride("Q", q_stride, d->n_heads, d->d_head)) return e;
+  if (int e = check_stride("K", k_stride, d->n_kv_heads, d->d_head)) return e;
+  if (int e = check_stride("V", v_stride, d->n_kv_heads, d->d_head)) return e;
+  if (int e = check_stride("dQ", dq_stride, d->n_heads, d->d_head)) return e;
+  if (int e = check_stride("dK", dk_stride, d->n_kv_heads, d->d_head)) return e;
+  if (int e = check_stride("dV", dv_stride, d->n_kv_heads, d->d_head)) return e;
+  PQ_REQUIRE(at16(dO) && at16(Q) && at16(K) && at16(V) && at16(O) && at16(dQ) && at16(dK) && at16(dV) && at16(workspace), PQ_ERR_SHAPE,
+             "buffers must be 16-byte aligned");
+  PQ_REQUIRE(workspace_bytes >= pq_self_attn_bwd_workspace_bytes(d, T), PQ_ERR_WORKSPACE, "workspace %zu < %zu", workspace_bytes,
+             pq_self_attn_bwd_workspace_bytes(d, T));
+  self_args a = make_args(d, T, row_start);
+  a.Q = (const uint16_t*)Q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V; a.O = (const uint16_t*)O; a.dO = (const uint16_t*)dO;
+  a.qs = q_stride; a.ks = k_stride; a.vs = v_stride;
+  a.dQ = (uint16_t*)dQ; a.dK = (uint16_t*)dK; a.dV = (uint16_t*)dV;
+  a.dqs = dq_stride; a.dks = dk_stride; a.dvs = dv_stride;
+  a.lse = const_cast<float*>(lse);
+  a.stats = (float2*)workspace;
+  hipStream_t s = (hipStream_t)stream;
+  pq_prof_scope prof(PQP_SELF_ATTN_BWD, s);
+  const bool direct = a.d % 8 == 0 && q_stride % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
+  return direct ? launch_backward_d<true>(a, s) : launch_backward_d<false>(a, s);
+}
