@@ -143,20 +143,34 @@ __device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c) { r
 // Register j of a tile is its row 8 (j / 4) + 4 h + j % 4.
 __device__ __forceinline__ constexpr int tile_row(int j) { return 8 * (j >> 2) + (j & 3); }
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+// Two neighbours rounded by one instruction (v_cvt_pk_bf16_f32).
+__device__ __forceinline__ uint32_t round_two(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x, y}, bf16x2_t)); }
+
+// Order of a run of LDS reads and of the products on them: AHEAD reads in front, then a product and its READS reads in turn, with VALU other
+// instructions between.
+template <int PRODUCTS, int READS, int AHEAD, int VALU>
+__device__ __forceinline__ void in_turn() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    if (i < PRODUCTS - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    if (VALU) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
+  }
+}
+
 // Eight rows of a tile as the second product's operand (registers 8 u .. 8 u + 7).
 __device__ __forceinline__ bf16x8_t as_operand(const f32x16_t& x, int u) {
-  uint4 w;
-  w.x = pack_bf16x2(x[8 * u], x[8 * u + 1]);
-  w.y = pack_bf16x2(x[8 * u + 2], x[8 * u + 3]);
-  w.z = pack_bf16x2(x[8 * u + 4], x[8 * u + 5]);
-  w.w = pack_bf16x2(x[8 * u + 6], x[8 * u + 7]);
+  const uint4 w = make_uint4(round_two(x[8 * u], x[8 * u + 1]), round_two(x[8 * u + 2], x[8 * u + 3]), round_two(x[8 * u + 4], x[8 * u + 5]),
+                             round_two(x[8 * u + 6], x[8 * u + 7]));
   return __builtin_bit_cast(bf16x8_t, w);
 }
 
 // a x b where b holds zeros for what is not seen, which an infinity or a NaN of a must not reach (0 times infinity is NaN): such elements are left
 // out, and where they are seen the sum becomes infinite (twice the largest bf16 number is beyond fp32).
 __device__ __forceinline__ f32x16_t mfma_seen(bf16x8_t a, bf16x8_t b, uint32_t seen /* bits of the operand's eight rows */, f32x16_t c) {
-  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
   const uint4 w = __builtin_bit_cast(uint4, a);
   const bf16x2_t zero = {(__bf16)0.0f, (__bf16)0.0f};
   float z = 0.0f;
@@ -213,9 +227,49 @@ __device__ __forceinline__ int sees(const self_args& a, int n, int row0, int row
   return SEES_ALL;
 }
 
+// The stages of tokens that a tile of rows needs, and of them those that a wavefront's 32 rows from row0 on see: its accumulators change in a loop of
+// their own (a stage that it sees nothing of, passed by in a branch, costs a second copy of all of them).
+struct stages_of { int j0, n, from, to; };
+__device__ __forceinline__ stages_of stages_seen(const self_args& a, const self_tile& t, int row0) {
+  const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n;
+  stages_of g;
+  g.j0 = first_token(a, t.at) & ~(SA_STAGE - 1);
+  g.n = (end - g.j0 + SA_STAGE - 1) / SA_STAGE;
+  const int last = a.causal ? min(row0 + 31, t.n - 1) : t.n - 1;
+  g.from = row0 < t.n ? (first_token(a, row0) - g.j0) / SA_STAGE : 0;
+  g.to = row0 < t.n ? (last - g.j0) / SA_STAGE + 1 : 0;
+  return g;
+}
+// Two buffers: the next stage's loads are under way while the present one is used.
+template <typename L, typename S, typename U>
+__device__ __forceinline__ void in_stages(const stages_of& g, L load, S store, U use) {
+  auto next = [&](int i) {
+    wait_loads();
+    __syncthreads();                                  // everybody's loads are there, and nobody reads the other buffer any more
+    if (i + 1 < g.n) load(i + 1);
+  };
+  int i = 0;
+#pragma unroll 1
+  for (; i < g.from; ++i) {
+    next(i);
+    if (i + 1 < g.n) store(i + 1);
+  }
+#pragma unroll 1
+  for (; i < g.to; ++i) {
+    next(i);
+    use(i);
+    if (i + 1 < g.n) store(i + 1);
+  }
+#pragma unroll 1
+  for (; i < g.n; ++i) {
+    next(i);
+    if (i + 1 < g.n) store(i + 1);
+  }
+}
+
 typedef uint32_t u32x2_u_t __attribute__((ext_vector_type(2), aligned(4)));
 __device__ __forceinline__ void store_four(uint16_t* row, int d, int at, const float* x) {
-  const uint32_t lo = pack_bf16x2(x[0], x[1]), hi = pack_bf16x2(x[2], x[3]);
+  const uint32_t lo = round_two(x[0], x[1]), hi = round_two(x[2], x[3]);
   if (at + 4 <= d) *reinterpret_cast<u32x2_u_t*>(row + at) = u32x2_u_t{lo, hi};
   else if (at < d) *reinterpret_cast<uint32_t*>(row + at) = lo;
 }
@@ -241,67 +295,142 @@ __device__ __forceinline__ self_place place_of(const self_args& a, bool last_fir
 // ---------------------------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------------------------
-template <int DP, bool PART>
+// A stage of tokens.  Any reference m gives the same quotient as long as nothing overflows and the row's largest p is not tiny: the maximum of what a row
+// sees in its first stage serves for all others (it has p = 1, so nothing that counts is lost below; what overflows above ends as infinity or NaN,
+// and the tile is taken once more with care).  So the stages have no maximum to keep and no accumulators to rescale.
+template <int DP>
 __device__ __forceinline__ void forward_stage(const self_args& a, const unsigned char* lk, const unsigned char* lv, const bf16x8_t* q, f32x16_t* o,
-                                              float& m, float& l, int low, int lim) {
+                                              float& m, float& l, bool part, int low, int lim) {
   constexpr int NK = DP / 32;
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[2];
-  uint32_t seen[2] = {0xffffu, 0xffffu};
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    f32x16_t x = {};
+    s[t] = f32x16_t{};
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) x = mfma(row_operand<DP>(lk, 32 * t, k), q[k], x);
-    if constexpr (PART) {
-      seen[t] = 0;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int at = 32 * t + tile_row(j) + 4 * h;
-        const bool v = at >= low && at <= lim;
-        x[j] = v ? x[j] : -INFINITY;
-        seen[t] |= (v ? 1u : 0u) << j;
-      }
-    }
-    s[t] = x;
+    for (int k = 0; k < DP / 16; ++k) s[t] = mfma(row_operand<DP>(lk, 32 * t, k), q[k], s[t]);
   }
-  float top = s[0][0];
+  in_turn<DP / 8, 1, 4, 0>();
+  if (part) {
+    const int from = low - 4 * h, to = lim - 4 * h;
 #pragma unroll
-  for (int j = 1; j < 32; ++j) top = fmaxf(top, s[j >> 4][j & 15]);
-  top = fmaxf(top, other_half(top)) * a.c;
-  // the reference moves only when a score exceeds it by 16 powers of two (any reference gives the same quotient)
-  if (__ballot(top > m + 16.0f)) {
-    const float next = fmaxf(m, top), f = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
-    m = next;
-    l *= f;
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < NK; ++i)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) o[i][j] *= f;
+      for (int j = 0; j < 16; ++j) s[t][j] = 32 * t + tile_row(j) >= from && 32 * t + tile_row(j) <= to ? s[t][j] : -INFINITY;
   }
-  const float ref = m == -INFINITY ? 0.0f : m;
+  if (__ballot(m == -INFINITY)) {
+    float top = s[0][0];
+#pragma unroll
+    for (int j = 1; j < 32; ++j) top = fmaxf(top, s[j >> 4][j & 15]);
+    top = fmaxf(top, other_half(top));
+    if (m == -INFINITY && top > -INFINITY) m = top * a.c;
+  }
+  const float ref = m == -INFINITY ? 0.0f : m, c = a.c == 0.0f ? 1.17549435e-38f : a.c;    // (hidden ones times a scale of 0 would be NaN)
   float sum[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      s[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j], a.c, -ref));
-      if constexpr (PART) s[t][j] = (seen[t] >> j) & 1 ? s[t][j] : 0.0f;      // (a scale of 0 makes NaN of the hidden ones' -infinity)
-      sum[j & 1] += s[t][j];
-    }
-  l += sum[0] + sum[1];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
     for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int j = 8 * u; j < 8 * u + 8; ++j) {
+        s[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j], c, -ref));
+        sum[j & 1] += s[t][j];
+      }
       const bf16x8_t p = as_operand(s[t], u);
 #pragma unroll
-      for (int i = 0; i < NK; ++i) {
-        const bf16x8_t v = column_operand<DP>(lv, 32 * t + 16 * u, i);
-        if constexpr (PART) o[i] = mfma_seen(v, p, seen[t] >> (8 * u), o[i]);
-        else o[i] = mfma(v, p, o[i]);
-      }
+      for (int i = 0; i < NK; ++i) o[i] = mfma(column_operand<DP>(lv, 32 * t + 16 * u, i), p, o[i]);
     }
+  __builtin_amdgcn_sched_group_barrier(0x2, 28, 0);
+  in_turn<4 * NK, 2, NK, 28 / NK>();
+  l += sum[0] + sum[1];
+}
+
+// The same with care, 32 tokens at a time: the reference follows the largest score, and an infinity or a NaN among the values reaches those rows
+// alone that see it.
+template <int DP>
+__device__ __forceinline__ void forward_block(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q, f32x16_t* o,
+                                              float& m, float& l, int low, int lim) {
+  constexpr int NK = DP / 32;
+  const int h = (threadIdx.x & 63) >> 5;
+  f32x16_t s = {};
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) s = mfma(row_operand<DP>(lk, at, k), q[k], s);
+  uint32_t seen = 0;
+  float top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const bool v = at + tile_row(j) + 4 * h >= low && at + tile_row(j) + 4 * h <= lim;
+    seen |= (v ? 1u : 0u) << j;
+    s[j] = v ? s[j] * a.c : -INFINITY;
+    top = fmaxf(top, s[j]);
+  }
+  top = fmaxf(top, other_half(top));
+  const float next = fmaxf(m, top), f = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+  m = next;
+  l *= f;
+#pragma unroll
+  for (int i = 0; i < NK; ++i) o[i] *= f;
+  const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    s[j] = __builtin_amdgcn_exp2f(s[j] - ref);
+    l += s[j];
+  }
+#pragma unroll 1
+  for (int u = 0; u < 2; ++u) {
+    const bf16x8_t p = u ? as_operand(s, 1) : as_operand(s, 0);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) o[i] = mfma_seen(column_operand<DP>(lv, at + 16 * u, i), p, seen >> (8 * u), o[i]);
+  }
+}
+
+// Whether one of the lane's sums is infinite or NaN.
+template <int NK> __device__ __forceinline__ bool any_nonfinite(const f32x16_t* acc) {
+  float z = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) z = __builtin_fmaf(acc[i][j], 0.0f, z);
+  return z != 0.0f;              // (NaN: not equal)
+}
+
+template <int DP, bool DIRECT, bool CAREFUL>
+__device__ __forceinline__ void forward_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, const bf16x8_t* q, f32x16_t* o, float& m,
+                                             float& l, unsigned char* lds) {
+  typedef stage_t<DP, DIRECT> stage;
+  constexpr int BUF = 2 * stage::BYTES;
+  const int row = row0 + (threadIdx.x & 31);
+  const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
+  const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
+  const stages_of g = stages_seen(a, t, row0);
+  stage k, v;
+  auto load = [&](int i) {
+    unsigned char* to = lds + (i & 1) * BUF;
+    k.load(K, a.ks, g.j0 + i * SA_STAGE, t.n, a.d, to);
+    v.load(V, a.vs, g.j0 + i * SA_STAGE, t.n, a.d, to + stage::BYTES);
+  };
+  auto store = [&](int i) {
+    unsigned char* to = lds + (i & 1) * BUF;
+    k.store(to);
+    v.store(to + stage::BYTES);
+  };
+  load(0);
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) o[i] = f32x16_t{};
+  m = -INFINITY;
+  l = 0.0f;
+  store(0);
+  in_stages(g, load, store, [&](int i) {
+    unsigned char* here = lds + (i & 1) * BUF;
+    const int j0 = g.j0 + i * SA_STAGE;
+    const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
+    if constexpr (CAREFUL) {
+#pragma unroll 1
+      for (int part = 0; part < SA_STAGE; part += 32) forward_block<DP>(a, here, here + stage::BYTES, part, q, o, m, l, low, lim);
+    } else {
+      forward_stage<DP>(a, here, here + stage::BYTES, q, o, m, l, sees(a, t.n, row0, 32, j0, SA_STAGE) != SEES_ALL, low, lim);
+    }
+  });
 }
 
 template <int DP, bool DIRECT>
@@ -314,43 +443,15 @@ __global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
   if (t.n == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row0 = t.at + 32 * wave, row = row0 + (lane & 31);
-  const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
-  const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
-  const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n;
-  int j0 = first_token(a, t.at) & ~(SA_STAGE - 1);
-  constexpr int BUF = 2 * stage::BYTES;
-  stage k, v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) stage::clear(lds + i * stage::BYTES, a.d);
-  k.load(K, a.ks, j0, t.n, a.d, lds);
-  v.load(V, a.vs, j0, t.n, a.d, lds + stage::BYTES);
   bf16x8_t q[DP / 16];
   load_columns<DP>(q, a.Q + ((int64_t)t.r0 + min(row, t.n - 1)) * a.qs + w.head * a.d, a.d, a.scale < 0.0f);
   f32x16_t o[NK];
-#pragma unroll
-  for (int i = 0; i < NK; ++i) o[i] = f32x16_t{};
-  float m = -INFINITY, l = 0.0f;
-  k.store(lds);
-  v.store(lds + stage::BYTES);
-  int at = 0;
-  for (; j0 < end; j0 += SA_STAGE, at ^= 1) {
-    wait_loads();
-    __syncthreads();                                  // everybody's loads are there, and nobody reads the other buffer any more
-    const bool more = j0 + SA_STAGE < end;
-    unsigned char *here = lds + at * BUF, *next = lds + (at ^ 1) * BUF;
-    if (more) {
-      k.load(K, a.ks, j0 + SA_STAGE, t.n, a.d, next);
-      v.load(V, a.vs, j0 + SA_STAGE, t.n, a.d, next + stage::BYTES);
-    }
-    const int see = sees(a, t.n, row0, 32, j0, SA_STAGE);
-    const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
-    if (see == SEES_ALL) forward_stage<DP, false>(a, here, here + stage::BYTES, q, o, m, l, low, lim);
-    else if (see == SEES_PART) forward_stage<DP, true>(a, here, here + stage::BYTES, q, o, m, l, low, lim);
-    if (more) {
-      k.store(next);
-      v.store(next + stage::BYTES);
-    }
-  }
+  float m, l;
+  forward_tile<DP, DIRECT, false>(a, w, t, row0, q, o, m, l, lds);
+  // An infinity or a NaN among values that not all rows of a wavefront see has reached all of them (0 times infinity): once more, with care.
+  if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(o) || !(l < INFINITY)), 0)) forward_tile<DP, DIRECT, true>(a, w, t, row0, q, o, m, l, lds);
   l += other_half(l);
   if (row >= t.n) return;
   const int64_t out = ((int64_t)t.r0 + row) * a.heads + w.head;
