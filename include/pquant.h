@@ -495,11 +495,12 @@ typedef struct pq_self_attn_desc {
 int pq_self_attn_fwd(const pq_self_attn_desc* desc, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V, int64_t v_stride,
                      int32_t T, const int32_t* row_start, void* O, float* lse, void* stream);
 /* Its gradients, from dO [T][n_heads][d_head] bf16 and what the forward call was given and left (O, lse):
- *     delta = sum_d dO O,   p_j = exp(s_j - lse),   dS_j = p_j (dO . v_j - delta)
+ *     p_j = exp(s_j - lse),   delta = sum_j p_j dO . v_j,   dS_j = p_j (dO . v_j - delta)
  *     dQ = scale sum_j dS_j k_j,   dK_j = scale sum dS_j q,   dV_j = sum p_j dO      (the last two over the rows that see j, and over the heads
  *                                                                                      that share it)
- *   dQ, dK, dV bf16 out with strides of their own (even); p and dS are rounded to bf16 for the products, the sums are fp32.  A row that sees one
- *   token has dS = 0.  Tokens and rows that do not see each other have no effect on each other, as above.
+ *   dQ, dK, dV bf16 out with strides of their own (even); p and dS are rounded to bf16 for the products, the sums are fp32.  (delta is
+ *   begun as dO . O, with O as it was rounded, and put right by the sum of the dS: O may be off by its rounding, not be something else.)  A row
+ *   that sees one token has dS = 0.  Tokens and rows that do not see each other have no effect on each other, as above.
  *   workspace: pq_self_attn_bwd_workspace_bytes() bytes of scratch (0: refused arguments); calls that may overlap need one each. */
 size_t pq_self_attn_bwd_workspace_bytes(const pq_self_attn_desc* desc, int32_t T);
 int pq_self_attn_bwd(const pq_self_attn_desc* desc, const void* dO, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,

@@ -35,12 +35,12 @@ def self_attention(q, k, v, seen, scale):
     return (e / total) @ np.asarray(v, F64), (top + np.log(total))[:, 0], e / total
 
 
-def self_attention_gradients(do, q, k, v, o, lse, seen, scale):
-    """From what the forward pass left (o, lse).  Returns dq, dk, dv, p and dS."""
+def self_attention_gradients(do, q, k, v, lse, seen, scale):
+    """From the lse that the forward pass left.  Returns dq, dk, dv, p and dS."""
     do, q, k, v = (np.asarray(x, F64) for x in (do, q, k, v))
     p = np.where(seen, np.exp(np.where(seen, scale * (q @ k.T) - np.asarray(lse, F64)[:, None], 0.0)), 0.0)
-    delta = (do * np.asarray(o, F64)).sum(1, keepdims=True)
-    ds = p * (do @ v.T - delta)
+    dp = do @ v.T
+    ds = p * (dp - (p * dp).sum(1, keepdims=True))
     ds[seen.sum(1) == 1] = 0.0                                       # (p is 1 whatever the score)
     return scale * (ds @ k), scale * (ds.T @ q), p.T @ do, p, ds
 

@@ -9,6 +9,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 namespace {
 
@@ -148,16 +149,16 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 // Two neighbours rounded by one instruction (v_cvt_pk_bf16_f32).
 __device__ __forceinline__ uint32_t round_two(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x, y}, bf16x2_t)); }
 
-// Order of a run of LDS reads and of the products on them: AHEAD reads in front, then a product and its READS reads in turn, with VALU other
-// instructions between.
-template <int PRODUCTS, int READS, int AHEAD, int VALU>
-__device__ __forceinline__ void in_turn() {
-  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+// The order of a run of instructions, in steps: PRODUCTS times a product, READS reads of LDS and VALU other vector instructions.  Reads in front of
+// the first step run ahead of the products by as many.
+__device__ __forceinline__ constexpr int at_least_one(int x) { return x < 1 ? 1 : x; }
+template <int READS> __device__ __forceinline__ void reads_first() { __builtin_amdgcn_sched_group_barrier(0x100, READS, 0); }
+template <int PRODUCTS, int READS, int VALU> __device__ __forceinline__ void steps() {
 #pragma unroll
   for (int i = 0; i < PRODUCTS; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-    if (i < PRODUCTS - AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-    if (VALU) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
+    if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
   }
 }
 
@@ -169,16 +170,10 @@ __device__ __forceinline__ bf16x8_t as_operand(const f32x16_t& x, int u) {
 }
 
 // a x b where b holds zeros for what is not seen, which an infinity or a NaN of a must not reach (0 times infinity is NaN): such elements are left
-// out, and where they are seen the sum becomes infinite (twice the largest bf16 number is beyond fp32).
+// out, and where they are seen the sum becomes infinite (twice the largest bf16 number is beyond fp32).  Three products for one, for tiles that hold such
+// elements: a branch would keep two copies of the sums.
 __device__ __forceinline__ f32x16_t mfma_seen(bf16x8_t a, bf16x8_t b, uint32_t seen /* bits of the operand's eight rows */, f32x16_t c) {
   const uint4 w = __builtin_bit_cast(uint4, a);
-  const bf16x2_t zero = {(__bf16)0.0f, (__bf16)0.0f};
-  float z = 0.0f;
-  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.x), zero, z, false);
-  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.y), zero, z, false);
-  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.z), zero, z, false);
-  z = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.w), zero, z, false);
-  if (__builtin_expect(__ballot(!(z == 0.0f)) == 0, 1)) return mfma(a, b, c);
   uint32_t clean[4] = {w.x, w.y, w.z, w.w}, top[4], ones[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -214,57 +209,55 @@ __device__ __forceinline__ self_tile find_self_tile(const self_args& a, int vt) 
 // Tokens that rows from .. to - 1 of a sequence of n see between them.
 __device__ __forceinline__ int first_token(const self_args& a, int row) { return a.window > 0 && row >= a.window ? row - a.window + 1 : 0; }
 
-// What a wavefront's 32 rows see of tokens j0 .. j0 + count - 1: nothing, a part, all.
-enum { SEES_NONE, SEES_PART, SEES_ALL };
-__device__ __forceinline__ int sees(const self_args& a, int n, int row0, int rows, int j0, int count) {
-  const int last = min(row0 + rows, n) - 1;                // (rows behind the last are nobody's)
-  if (last < row0 || j0 >= n) return SEES_NONE;
-  if (a.causal && j0 > last) return SEES_NONE;
-  if (j0 + count <= first_token(a, row0)) return SEES_NONE;
-  if (j0 + count > n || row0 + rows > n) return SEES_PART;
-  if (a.causal && j0 + count - 1 > row0) return SEES_PART;
-  if (j0 < first_token(a, last)) return SEES_PART;
-  return SEES_ALL;
-}
-
-// The stages of tokens that a tile of rows needs, and of them those that a wavefront's 32 rows from row0 on see: its accumulators change in a loop of
-// their own (a stage that it sees nothing of, passed by in a branch, costs a second copy of all of them).
-struct stages_of { int j0, n, from, to; };
-__device__ __forceinline__ stages_of stages_seen(const self_args& a, const self_tile& t, int row0) {
-  const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n;
-  stages_of g;
-  g.j0 = first_token(a, t.at) & ~(SA_STAGE - 1);
-  g.n = (end - g.j0 + SA_STAGE - 1) / SA_STAGE;
-  const int last = a.causal ? min(row0 + 31, t.n - 1) : t.n - 1;
-  g.from = row0 < t.n ? (first_token(a, row0) - g.j0) / SA_STAGE : 0;
-  g.to = row0 < t.n ? (last - g.j0) / SA_STAGE + 1 : 0;
+// The stages that a tile needs, and of them what a wavefront's 32 rows (or tokens) see: nothing before `from` and from `to` on, all of the stages from
+// `all` to `part` - 1, a part of the others.  Each of these is a loop of its own: a branch around accumulators costs a second copy of them all.
+struct stages_of { int first, n, from, all, part, to; };
+__device__ __forceinline__ stages_of clamp_stages(stages_of g) {
+  g.to = min(max(g.to, 0), g.n);
+  g.from = min(max(g.from, 0), g.to);
+  g.all = min(max(g.all, g.from), g.to);
+  g.part = min(max(g.part, g.all), g.to);
   return g;
 }
-// Two buffers: the next stage's loads are under way while the present one is used.
-template <typename L, typename S, typename U>
-__device__ __forceinline__ void in_stages(const stages_of& g, L load, S store, U use) {
-  auto next = [&](int i) {
-    wait_loads();
-    __syncthreads();                                  // everybody's loads are there, and nobody reads the other buffer any more
-    if (i + 1 < g.n) load(i + 1);
-  };
+// Stages of tokens that rows row0 .. row0 + 31 of the tile see.
+__device__ __forceinline__ stages_of token_stages(const self_args& a, const self_tile& t, int row0) {
+  const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n, last = min(row0 + 31, t.n - 1);
+  stages_of g;
+  g.first = first_token(a, t.at) & ~(SA_STAGE - 1);
+  g.n = (end - g.first + SA_STAGE - 1) / SA_STAGE;
+  g.from = (first_token(a, row0) - g.first) / SA_STAGE;
+  g.to = row0 < t.n ? ((a.causal ? last : t.n - 1) - g.first) / SA_STAGE + 1 : 0;
+  g.all = (first_token(a, last) - g.first + SA_STAGE - 1) / SA_STAGE;
+  g.part = ((a.causal ? row0 + 1 : t.n) - g.first) / SA_STAGE;
+  return clamp_stages(g);
+}
+// Stages of rows that see tokens tok0 .. tok0 + 31 of the tile.
+__device__ __forceinline__ stages_of row_stages(const self_args& a, const self_tile& t, int tok0) {
+  const bool window = a.window > 0 && a.window < t.n;
+  auto behind = [&](int tok) { return window && tok < t.n - a.window ? tok + a.window : t.n; };   // the first row that sees no `tok` any more
+  stages_of g;
+  g.first = (a.causal ? t.at : 0) & ~(SA_STAGE - 1);
+  g.n = (behind(min(t.at + SA_ROWS, t.n) - 1) - g.first + SA_STAGE - 1) / SA_STAGE;
+  g.from = a.causal ? (tok0 - g.first) / SA_STAGE : 0;
+  g.to = tok0 < t.n ? (behind(min(tok0 + 31, t.n - 1)) - g.first + SA_STAGE - 1) / SA_STAGE : 0;
+  g.all = a.causal ? (tok0 + 31 - g.first + SA_STAGE - 1) / SA_STAGE : 0;
+  g.part = (behind(tok0) - g.first) / SA_STAGE;
+  return clamp_stages(g);
+}
+// `next` waits for a stage and has the loads of the one behind it started, `store` puts away what came through registers.
+template <typename N, typename S, typename P, typename A>
+__device__ __forceinline__ void in_stages(const stages_of& g, N next, S store, P use_part, A use_all) {
   int i = 0;
 #pragma unroll 1
-  for (; i < g.from; ++i) {
-    next(i);
-    if (i + 1 < g.n) store(i + 1);
-  }
+  for (; i < g.from; ++i) { next(i); store(i); }
 #pragma unroll 1
-  for (; i < g.to; ++i) {
-    next(i);
-    use(i);
-    if (i + 1 < g.n) store(i + 1);
-  }
+  for (; i < g.all; ++i) { next(i); use_part(i); store(i); }
 #pragma unroll 1
-  for (; i < g.n; ++i) {
-    next(i);
-    if (i + 1 < g.n) store(i + 1);
-  }
+  for (; i < g.part; ++i) { next(i); use_all(i); store(i); }
+#pragma unroll 1
+  for (; i < g.to; ++i) { next(i); use_part(i); store(i); }
+#pragma unroll 1
+  for (; i < g.n; ++i) { next(i); store(i); }
 }
 
 typedef uint32_t u32x2_u_t __attribute__((ext_vector_type(2), aligned(4)));
@@ -310,7 +303,8 @@ __device__ __forceinline__ void forward_stage(const self_args& a, const unsigned
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) s[t] = mfma(row_operand<DP>(lk, 32 * t, k), q[k], s[t]);
   }
-  in_turn<DP / 8, 1, 4, 0>();
+  reads_first<4>();
+  steps<DP / 8, 1, 0>();
   if (part) {
     const int from = low - 4 * h, to = lim - 4 * h;
 #pragma unroll
@@ -341,7 +335,9 @@ __device__ __forceinline__ void forward_stage(const self_args& a, const unsigned
       for (int i = 0; i < NK; ++i) o[i] = mfma(column_operand<DP>(lv, 32 * t + 16 * u, i), p, o[i]);
     }
   __builtin_amdgcn_sched_group_barrier(0x2, 28, 0);
-  in_turn<4 * NK, 2, NK, 28 / NK>();
+  reads_first<2 * NK>();
+  steps<3 * NK, 2, 28 / NK>();
+  steps<NK, 0, 0>();
   l += sum[0] + sum[1];
 }
 
@@ -402,35 +398,48 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
   const int row = row0 + (threadIdx.x & 31);
   const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
   const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
-  const stages_of g = stages_seen(a, t, row0);
+  const stages_of g = token_stages(a, t, row0);
   stage k, v;
   auto load = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
-    k.load(K, a.ks, g.j0 + i * SA_STAGE, t.n, a.d, to);
-    v.load(V, a.vs, g.j0 + i * SA_STAGE, t.n, a.d, to + stage::BYTES);
+    k.load(K, a.ks, g.first + i * SA_STAGE, t.n, a.d, to);
+    v.load(V, a.vs, g.first + i * SA_STAGE, t.n, a.d, to + stage::BYTES);
   };
-  auto store = [&](int i) {
+  auto put = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
     k.store(to);
     v.store(to + stage::BYTES);
+  };
+  auto next = [&](int i) {
+    wait_loads();
+    __syncthreads();                                  // everybody's loads are there, and nobody reads the other buffer any more
+    if (i + 1 < g.n) load(i + 1);
+  };
+  auto store = [&](int i) {
+    if (i + 1 < g.n) put(i + 1);
   };
   load(0);
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) o[i] = f32x16_t{};
   m = -INFINITY;
   l = 0.0f;
-  store(0);
-  in_stages(g, load, store, [&](int i) {
+  put(0);
+  auto use = [&](int i, bool part) {
     unsigned char* here = lds + (i & 1) * BUF;
-    const int j0 = g.j0 + i * SA_STAGE;
+    const int j0 = g.first + i * SA_STAGE;
     const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
     if constexpr (CAREFUL) {
 #pragma unroll 1
-      for (int part = 0; part < SA_STAGE; part += 32) forward_block<DP>(a, here, here + stage::BYTES, part, q, o, m, l, low, lim);
+      for (int at = 0; at < SA_STAGE; at += 32) forward_block<DP>(a, here, here + stage::BYTES, at, q, o, m, l, low, lim);
     } else {
-      forward_stage<DP>(a, here, here + stage::BYTES, q, o, m, l, sees(a, t.n, row0, 32, j0, SA_STAGE) != SEES_ALL, low, lim);
+      forward_stage<DP>(a, here, here + stage::BYTES, q, o, m, l, part, low, lim);
     }
-  });
+  };
+  // (one loop for both: the mask changes scores alone)
+  stages_of one = g;
+  one.all = g.from;
+  one.part = g.to;
+  in_stages(one, next, store, [&](int) {}, [&](int i) { use(i, i < g.all || i >= g.part); });
 }
 
 template <int DP, bool DIRECT>
@@ -465,46 +474,156 @@ __global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
 // A row that sees one token has p = 1 whatever its score: no gradient passes through it.
 __device__ __forceinline__ bool sees_one(const self_args& a, int n, int row) { return n == 1 || (a.causal && (row == 0 || a.window == 1)); }
 
-template <int DP, bool PART>
-__device__ __forceinline__ void query_block(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q,
-                                            const bf16x8_t* g, f32x16_t* dq, float lse, float delta, int low, int lim, bool one) {
-  constexpr int NK = DP / 32;
+// Blocks of 32 tokens that a wavefront has in flight at a time: with two the products of one cover the exponentials of the other.
+template <int DP> constexpr int blocks_in_flight() { return DP == 96 ? 1 : 2; }
+// Wavefronts a SIMD of the backward kernels: their accumulators and both operands that stay take 1.5 DP registers, of 256 or 512.
+template <int DP> constexpr int backward_waves() { return DP > 96 ? 1 : 2; }
+
+// delta is dO . O with O as it was rounded to bf16, which costs dS as much as all else together; what is missing to sum_j p_ij dP_ij is the sum of
+// the dS themselves, known at the end.  So the products with p are kept beside those with dS (they share their other operand), and dQ is put right by them.
+template <int DP, bool PART, bool CAREFUL>
+__device__ __forceinline__ void query_blocks(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q,
+                                             const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, int low, int lim,
+                                             bool one) {
+  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : blocks_in_flight<DP>();
   const int h = (threadIdx.x & 63) >> 5;
-  f32x16_t s = {}, dp;
+  f32x16_t s[NB], dp[NB];
+  uint32_t seen[NB];
+  auto scores = [&](int b) {
+    s[b] = f32x16_t{};
 #pragma unroll
-  for (int j = 0; j < 16; ++j) dp[j] = -delta;
+    for (int k = 0; k < DP / 16; ++k) s[b] = mfma(row_operand<DP>(lk, at + 32 * b, k), q[k], s[b]);
+  };
+  auto slopes = [&](int b) {
 #pragma unroll
-  for (int k = 0; k < DP / 16; ++k) s = mfma(row_operand<DP>(lk, at, k), q[k], s);
+    for (int j = 0; j < 16; ++j) dp[b][j] = -delta;
 #pragma unroll
-  for (int k = 0; k < DP / 16; ++k) dp = mfma(row_operand<DP>(lv, at, k), g[k], dp);
-  uint32_t seen = 0xffffu;
-  if constexpr (PART) seen = 0;
+    for (int k = 0; k < DP / 16; ++k) dp[b] = mfma(row_operand<DP>(lv, at + 32 * b, k), g[k], dp[b]);
+  };
+  auto weights = [&](int b) {
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], a.c, -lse));
-    float x = p * dp[j];
-    if constexpr (PART) {
-      const int tok = at + tile_row(j) + 4 * h;
-      const bool v = tok >= low && tok <= lim && !one;
-      x = v ? x : 0.0f;
-      seen |= (v ? 1u : 0u) << j;
+    for (int j = 0; j < 16; ++j) {
+      s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], a.c, -lse));
+      if constexpr (PART || CAREFUL) {
+        const int tok = 32 * b + tile_row(j);
+        s[b][j] = tok >= low - at - 4 * h && tok <= lim - at - 4 * h ? s[b][j] : 0.0f;
+      }
     }
-    s[j] = x;
+  };
+  auto through = [&](int b) {
+    seen[b] = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      float x = s[b][j] * dp[b][j];
+      if constexpr (PART || CAREFUL) {
+        const int tok = 32 * b + tile_row(j);
+        const bool v = tok >= low - at - 4 * h && tok <= lim - at - 4 * h && !one;
+        if constexpr (CAREFUL) x = v ? x : 0.0f;       // (otherwise 0 times what is not finite: the tile is taken with care)
+        else x = one ? 0.0f : x;
+        seen[b] |= (v ? 1u : 0u) << j;
+      }
+      dp[b][j] = x;
+      rest += x;
+    }
+  };
+  auto products = [&](int b) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8_t x = as_operand(dp[b], u), p = as_operand(s[b], u);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const bf16x8_t k = column_operand<DP>(lk, at + 32 * b + 16 * u, i);
+        if constexpr (CAREFUL) {
+          dq[i] = mfma_seen(k, x, seen[b] >> (8 * u), dq[i]);
+          pk[i] = mfma_seen(k, p, seen[b] >> (8 * u), pk[i]);
+        } else {
+          dq[i] = mfma(k, x, dq[i]);
+          pk[i] = mfma(k, p, pk[i]);
+        }
+      }
+    }
+  };
+  scores(0);
+  slopes(0);
+  weights(0);
+  if constexpr (NB == 2) scores(1);
+  through(0);
+  if constexpr (NB == 2) {
+    slopes(1);
+    weights(1);
   }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const bf16x8_t x = as_operand(s, u);
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const bf16x8_t k = column_operand<DP>(lk, at + 16 * u, i);
-      if constexpr (PART) dq[i] = mfma_seen(k, x, seen >> (8 * u), dq[i]);
-      else dq[i] = mfma(k, x, dq[i]);
+  products(0);
+  if constexpr (NB == 2) {
+    through(1);
+    products(1);
+  }
+  if constexpr (!CAREFUL && !PART) {
+    constexpr int S = DP / 16, P = 4 * NK;
+    reads_first<4>();
+    steps<S, 1, 0>();
+    steps<S, 1, at_least_one(32 / S)>();
+    if constexpr (NB == 2) {
+      steps<S, 1, at_least_one(48 / S)>();
+      steps<S, 1, at_least_one(32 / S)>();
+      steps<P, 1, at_least_one(48 / P)>();
+      steps<P - 4, 1, 0>();
+      steps<4, 0, 0>();
+    } else {
+      __builtin_amdgcn_sched_group_barrier(0x2, 40, 0);
+      steps<P - 4, 1, 0>();
+      steps<4, 0, 0>();
     }
   }
 }
 
+template <int DP, bool DIRECT, bool CAREFUL>
+__device__ __forceinline__ void query_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, const bf16x8_t* q, const bf16x8_t* g,
+                                           f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, unsigned char* lds) {
+  typedef stage_t<DP, DIRECT> stage;
+  constexpr int BUF = 2 * stage::BYTES;
+  const int row = row0 + (threadIdx.x & 31);
+  const bool one = sees_one(a, t.n, row);
+  const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
+  const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
+  const stages_of st = token_stages(a, t, row0);
+  stage k, v;
+  auto load = [&](int i) {
+    unsigned char* to = lds + (i & 1) * BUF;
+    k.load(K, a.ks, st.first + i * SA_STAGE, t.n, a.d, to);
+    v.load(V, a.vs, st.first + i * SA_STAGE, t.n, a.d, to + stage::BYTES);
+  };
+  auto put = [&](int i) {
+    unsigned char* to = lds + (i & 1) * BUF;
+    k.store(to);
+    v.store(to + stage::BYTES);
+  };
+  auto next = [&](int i) {
+    wait_loads();
+    __syncthreads();
+    if (i + 1 < st.n) load(i + 1);
+  };
+  auto store = [&](int i) {
+    if (i + 1 < st.n) put(i + 1);
+  };
+  load(0);
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) dq[i] = pk[i] = f32x16_t{};
+  rest = 0.0f;
+  put(0);
+  auto use = [&](int i, auto part) {
+    unsigned char* here = lds + (i & 1) * BUF;
+    const int j0 = st.first + i * SA_STAGE;
+    const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
+    constexpr int NB = CAREFUL ? 1 : blocks_in_flight<DP>();
+#pragma unroll 1
+    for (int at = 0; at < SA_STAGE; at += 32 * NB)
+      query_blocks<DP, decltype(part)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, low, lim, one);
+  };
+  in_stages(st, next, store, [&](int i) { use(i, std::true_type{}); }, [&](int i) { use(i, std::false_type{}); });
+}
+
 template <int DP, bool DIRECT>
-__global__ __launch_bounds__(256, 2) void self_query_kernel(self_args a) {
+__global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(self_args a) {
   constexpr int NK = DP / 32;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   typedef stage_t<DP, DIRECT> stage;
@@ -513,16 +632,8 @@ __global__ __launch_bounds__(256, 2) void self_query_kernel(self_args a) {
   if (t.n == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row0 = t.at + 32 * wave, row = row0 + (lane & 31);
-  const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
-  const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
-  const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n;
-  int j0 = first_token(a, t.at) & ~(SA_STAGE - 1);
-  constexpr int BUF = 2 * stage::BYTES;
-  stage k, v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) stage::clear(lds + i * stage::BYTES, a.d);
-  k.load(K, a.ks, j0, t.n, a.d, lds);
-  v.load(V, a.vs, j0, t.n, a.d, lds + stage::BYTES);
   const int64_t mine = (int64_t)t.r0 + min(row, t.n - 1);
   bf16x8_t q[DP / 16], g[DP / 16];
   load_columns<DP>(q, a.Q + mine * a.qs + w.head * a.d, a.d, a.scale < 0.0f);
@@ -538,98 +649,198 @@ __global__ __launch_bounds__(256, 2) void self_query_kernel(self_args a) {
   }
   delta += other_half(delta);
   const float lse = a.lse[mine * a.heads + w.head] * SA_LOG2E;
-  if (row < t.n && lane < 32) a.stats[(int64_t)w.head * a.T + mine] = make_float2(lse, delta);
-  const bool one = sees_one(a, t.n, row);
-  f32x16_t dq[NK];
+  f32x16_t dq[NK], pk[NK];
+  float rest;
+  query_tile<DP, DIRECT, false>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, lds);
+  if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dq) || any_nonfinite<NK>(pk)), 0))
+    query_tile<DP, DIRECT, true>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, lds);
+  rest += other_half(rest);
+  if (row >= t.n) return;
+  if (lane < 32) a.stats[(int64_t)w.head * a.T + mine] = make_float2(lse, delta + rest);
 #pragma unroll
-  for (int i = 0; i < NK; ++i) dq[i] = f32x16_t{};
-  k.store(lds);
-  v.store(lds + stage::BYTES);
-  int at = 0;
-  for (; j0 < end; j0 += SA_STAGE, at ^= 1) {
-    wait_loads();
-    __syncthreads();
-    const bool more = j0 + SA_STAGE < end;
-    unsigned char *here = lds + at * BUF, *next = lds + (at ^ 1) * BUF;
-    if (more) {
-      k.load(K, a.ks, j0 + SA_STAGE, t.n, a.d, next);
-      v.load(V, a.vs, j0 + SA_STAGE, t.n, a.d, next + stage::BYTES);
-    }
-    const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
-#pragma unroll 1
-    for (int part = 0; part < SA_STAGE; part += 32) {
-      const int see = sees(a, t.n, row0, 32, j0 + part, 32);
-      if (see == SEES_ALL) query_block<DP, false>(a, here, here + stage::BYTES, part, q, g, dq, lse, delta, low, lim, one);
-      else if (see == SEES_PART) query_block<DP, true>(a, here, here + stage::BYTES, part, q, g, dq, lse, delta, low, lim, one);
-    }
-    if (more) {
-      k.store(next);
-      v.store(next + stage::BYTES);
-    }
-  }
-  if (row < t.n) store_column<DP>(dq, a.scale, a.dQ + mine * a.dqs + w.head * a.d, a.d);
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) dq[i][j] -= rest * pk[i][j];
+  store_column<DP>(dq, a.scale, a.dQ + mine * a.dqs + w.head * a.d, a.d);
 }
 
 // ---------------------------------------------------------------------------------------------
 // Gradients of the keys and values
 // ---------------------------------------------------------------------------------------------
-template <int DP, bool PART>
-__device__ __forceinline__ void token_block(const self_args& a, const unsigned char* lq, const unsigned char* lg, const float* lst, int at, int n, int i0,
-                                            int tok, const bf16x8_t* k, const bf16x8_t* v, f32x16_t* dk, f32x16_t* dv) {
-  constexpr int NK = DP / 32;
+template <int DP, bool PART, bool CAREFUL>
+__device__ __forceinline__ void token_blocks(const self_args& a, const unsigned char* lq, const unsigned char* lg, const float* lst, int at, int n, int i0,
+                                             int tok, const bf16x8_t* k, const bf16x8_t* v, f32x16_t* dk, f32x16_t* dv) {
+  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : blocks_in_flight<DP>();
   const int h = (threadIdx.x & 63) >> 5;
-  f32x16_t s = {}, dp;
+  f32x16_t s[NB], dp[NB];
+  uint32_t seen[NB], passed[NB];
+  auto visible = [&](int row) { return (row < n) & (tok < n) & (!a.causal | (tok <= row)) & (tok >= first_token(a, row)); };
+  auto scores = [&](int b) {
+    s[b] = f32x16_t{};
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(lst + SA_STAGE + at + 8 * b + 4 * h);
+    for (int x = 0; x < DP / 16; ++x) s[b] = mfma(row_operand<DP>(lq, at + 32 * b, x), k[x], s[b]);
+  };
+  auto slopes = [&](int b) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dp[4 * b + j] = -x[j];
-  }
+    for (int y = 0; y < 4; ++y) {
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(lst + SA_STAGE + at + 32 * b + 8 * y + 4 * h);
 #pragma unroll
-  for (int x = 0; x < DP / 16; ++x) s = mfma(row_operand<DP>(lq, at, x), k[x], s);
+      for (int j = 0; j < 4; ++j) dp[b][4 * y + j] = x[j];       // (-delta)
+    }
 #pragma unroll
-  for (int x = 0; x < DP / 16; ++x) dp = mfma(row_operand<DP>(lg, at, x), v[x], dp);
-  uint32_t seen = 0xffffu, through = 0xffffu;
-  if constexpr (PART) seen = through = 0;
+    for (int x = 0; x < DP / 16; ++x) dp[b] = mfma(row_operand<DP>(lg, at + 32 * b, x), v[x], dp[b]);
+  };
+  auto weights = [&](int b) {
+    seen[b] = 0;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    const f32x4_t lse = *reinterpret_cast<const f32x4_t*>(lst + at + 8 * b + 4 * h);
+    for (int y = 0; y < 4; ++y) {
+      const f32x4_t lse = *reinterpret_cast<const f32x4_t*>(lst + at + 32 * b + 8 * y + 4 * h);     // (-lse log2 e)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int x = 4 * b + j;
-      float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], a.c, -lse[j])), ds = p * dp[x];
-      if constexpr (PART) {
-        const int row = i0 + at + 8 * b + 4 * h + j;
-        const bool vis = row < n && tok < n && (!a.causal || tok <= row) && tok >= first_token(a, row), pass = vis && !sees_one(a, n, row);
-        p = vis ? p : 0.0f;
-        ds = pass ? ds : 0.0f;
-        seen |= (vis ? 1u : 0u) << x;
-        through |= (pass ? 1u : 0u) << x;
+      for (int j = 0; j < 4; ++j) {
+        const int x = 4 * y + j;
+        s[b][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x], a.c, lse[j]));
+        if constexpr (PART || CAREFUL) {
+          const bool vis = visible(i0 + at + 32 * b + 8 * y + 4 * h + j);
+          s[b][x] = vis ? s[b][x] : 0.0f;
+          seen[b] |= (vis ? 1u : 0u) << x;
+        }
       }
-      s[x] = p;
-      dp[x] = ds;
     }
+  };
+  auto through = [&](int b) {
+    passed[b] = 0;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      float ds = s[b][x] * dp[b][x];
+      if constexpr (PART || CAREFUL) {
+        const int row = i0 + at + 32 * b + tile_row(x) + 4 * h;
+        const bool one = sees_one(a, n, row), pass = ((seen[b] >> x) & 1) && !one;
+        if constexpr (CAREFUL) ds = pass ? ds : 0.0f;   // (otherwise 0 times what is not finite: the tile is taken with care)
+        else ds = one ? 0.0f : ds;
+        passed[b] |= (pass ? 1u : 0u) << x;
+      }
+      dp[b][x] = ds;
+    }
+  };
+  auto products = [&](int b) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8_t x = as_operand(s[b], u);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const bf16x8_t g = column_operand<DP>(lg, at + 32 * b + 16 * u, i);
+        if constexpr (CAREFUL) dv[i] = mfma_seen(g, x, seen[b] >> (8 * u), dv[i]);
+        else dv[i] = mfma(g, x, dv[i]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8_t y = as_operand(dp[b], u);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const bf16x8_t q = column_operand<DP>(lq, at + 32 * b + 16 * u, i);
+        if constexpr (CAREFUL) dk[i] = mfma_seen(q, y, passed[b] >> (8 * u), dk[i]);
+        else dk[i] = mfma(q, y, dk[i]);
+      }
+    }
+  };
+  scores(0);
+  slopes(0);
+  weights(0);
+  if constexpr (NB == 2) scores(1);
+  through(0);
+  if constexpr (NB == 2) {
+    slopes(1);
+    weights(1);
   }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const bf16x8_t x = as_operand(s, u), y = as_operand(dp, u);
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const bf16x8_t g = column_operand<DP>(lg, at + 16 * u, i);
-      if constexpr (PART) dv[i] = mfma_seen(g, x, seen >> (8 * u), dv[i]);
-      else dv[i] = mfma(g, x, dv[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const bf16x8_t q = column_operand<DP>(lq, at + 16 * u, i);
-      if constexpr (PART) dk[i] = mfma_seen(q, y, through >> (8 * u), dk[i]);
-      else dk[i] = mfma(q, y, dk[i]);
+  products(0);
+  if constexpr (NB == 2) {
+    through(1);
+    products(1);
+  }
+  if constexpr (!CAREFUL && !PART) {
+    constexpr int S = DP / 16, P = 4 * NK;
+    reads_first<8>();
+    steps<S, 1, 0>();
+    steps<S, 2, at_least_one(32 / S)>();
+    if constexpr (NB == 2) {
+      steps<S, 2, at_least_one(32 / S)>();
+      steps<S, 2, at_least_one(32 / S)>();
+      steps<P, 2, at_least_one(32 / P)>();
+      steps<P - 4, 2, 0>();
+      steps<4, 0, 0>();
+    } else {
+      __builtin_amdgcn_sched_group_barrier(0x2, 24, 0);
+      steps<P - 4, 2, 0>();
+      steps<4, 0, 0>();
     }
   }
 }
 
+template <int DP, bool DIRECT, bool CAREFUL>
+__device__ __forceinline__ void token_tile(const self_args& a, int kv_head, const self_tile& t, int tok0, const bf16x8_t* k, const bf16x8_t* v,
+                                           f32x16_t* dk, f32x16_t* dv, unsigned char* lds) {
+  typedef stage_t<DP, DIRECT> stage;
+  constexpr int BUF = 2 * stage::BYTES + SA_STAGE * 8;
+  const int tok = tok0 + (threadIdx.x & 31);
+  const stages_of st = row_stages(a, t, tok0);
+  const uint16_t* Q = a.Q + (int64_t)t.r0 * a.qs + (int64_t)kv_head * a.group * a.d;
+  const uint16_t* G = a.dO + ((int64_t)t.r0 * a.heads + (int64_t)kv_head * a.group) * a.d;
+  const int64_t gs = (int64_t)a.heads * a.d;
+  stage q, g;
+  float2 sums = make_float2(0.0f, 0.0f);
+  int at = 0;                                          // the buffer of the present stage
+  auto load = [&](int head, int i, int to_at) {
+    unsigned char* to = lds + to_at * BUF;
+    const int i0 = st.first + i * SA_STAGE;
+    q.load(Q + head * a.d, a.qs, i0, t.n, a.d, to);
+    g.load(G + head * a.d, gs, i0, t.n, a.d, to + stage::BYTES);
+    if (threadIdx.x < SA_STAGE)
+      sums = a.stats[(int64_t)(kv_head * a.group + head) * a.T + t.r0 + min(i0 + (int)threadIdx.x, t.n - 1)];
+  };
+  auto put = [&](int to_at) {
+    unsigned char* to = lds + to_at * BUF;
+    q.store(to);
+    g.store(to + stage::BYTES);
+    if (threadIdx.x < SA_STAGE) {
+      float* s = reinterpret_cast<float*>(to + 2 * stage::BYTES);
+      s[threadIdx.x] = -sums.x;
+      s[SA_STAGE + threadIdx.x] = -sums.y;
+    }
+  };
+  load(0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) dk[i] = dv[i] = f32x16_t{};
+  put(0);
+#pragma unroll 1
+  for (int head = 0; head < a.group; ++head) {
+    auto more = [&](int i) { return i + 1 < st.n || head + 1 < a.group; };
+    auto next = [&](int i) {
+      wait_loads();
+      __syncthreads();
+      if (more(i)) {
+        const bool same = i + 1 < st.n;
+        load(same ? head : head + 1, same ? i + 1 : 0, at ^ 1);
+      }
+    };
+    auto store = [&](int i) {
+      at ^= 1;
+      if (more(i)) put(at);
+    };
+    auto use = [&](int i, auto part) {
+      unsigned char* here = lds + at * BUF;
+      const float* lst = reinterpret_cast<const float*>(here + 2 * stage::BYTES);
+      constexpr int NB = CAREFUL ? 1 : blocks_in_flight<DP>();
+#pragma unroll 1
+      for (int x = 0; x < SA_STAGE; x += 32 * NB)
+        token_blocks<DP, decltype(part)::value, CAREFUL>(a, here, here + stage::BYTES, lst, x, t.n, st.first + i * SA_STAGE, tok, k, v, dk, dv);
+    };
+    in_stages(st, next, store, [&](int i) { use(i, std::true_type{}); }, [&](int i) { use(i, std::false_type{}); });
+  }
+}
+
 template <int DP, bool DIRECT>
-__global__ __launch_bounds__(256, DP > 96 ? 1 : 2) void self_token_kernel(self_args a) {
+__global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(self_args a) {
   constexpr int NK = DP / 32;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   typedef stage_t<DP, DIRECT> stage;
@@ -638,60 +849,17 @@ __global__ __launch_bounds__(256, DP > 96 ? 1 : 2) void self_token_kernel(self_a
   if (t.n == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int tok0 = t.at + 32 * wave, tok = tok0 + (lane & 31);
-  // rows that see the tile's tokens
-  const int begin = (a.causal ? t.at : 0) & ~(SA_STAGE - 1);
-  const int last = min(t.at + SA_ROWS, t.n) - 1, end = a.window > 0 && a.window < t.n - last ? last + a.window : t.n;
-  const int per_head = (end - begin + SA_STAGE - 1) / SA_STAGE, steps = per_head * a.group;
   constexpr int BUF = 2 * stage::BYTES + SA_STAGE * 8;
-  const uint16_t* Q = a.Q + (int64_t)t.r0 * a.qs + (int64_t)kv_head * a.group * a.d;
-  const uint16_t* G = a.dO + ((int64_t)t.r0 * a.heads + (int64_t)kv_head * a.group) * a.d;
-  const int64_t gs = (int64_t)a.heads * a.d;
-  stage q, g;
-  float2 st = make_float2(0.0f, 0.0f);
-  auto load = [&](int step, unsigned char* to) {
-    const int head = step / per_head, i0 = begin + (step - head * per_head) * SA_STAGE;
-    q.load(Q + head * a.d, a.qs, i0, t.n, a.d, to);
-    g.load(G + head * a.d, gs, i0, t.n, a.d, to + stage::BYTES);
-    if (threadIdx.x < SA_STAGE)
-      st = a.stats[(int64_t)(kv_head * a.group + head) * a.T + t.r0 + min(i0 + (int)threadIdx.x, t.n - 1)];
-  };
-  auto store = [&](unsigned char* to) {
-    q.store(to);
-    g.store(to + stage::BYTES);
-    if (threadIdx.x < SA_STAGE) {
-      float* s = reinterpret_cast<float*>(to + 2 * stage::BYTES);
-      s[threadIdx.x] = st.x;
-      s[SA_STAGE + threadIdx.x] = st.y;
-    }
-  };
 #pragma unroll
   for (int i = 0; i < 4; ++i) stage::clear(lds + (i >> 1) * BUF + (i & 1) * stage::BYTES, a.d);
-  load(0, lds);
   const int64_t mine = (int64_t)t.r0 + min(tok, t.n - 1);
   bf16x8_t k[DP / 16], v[DP / 16];
   load_columns<DP>(k, a.K + mine * a.ks + kv_head * a.d, a.d, a.scale < 0.0f);
   load_columns<DP>(v, a.V + mine * a.vs + kv_head * a.d, a.d, false);
   f32x16_t dk[NK], dv[NK];
-#pragma unroll
-  for (int i = 0; i < NK; ++i) dk[i] = dv[i] = f32x16_t{};
-  store(lds);
-  int at = 0;
-  for (int step = 0; step < steps; ++step, at ^= 1) {
-    wait_loads();
-    __syncthreads();
-    const bool more = step + 1 < steps;
-    unsigned char *here = lds + at * BUF, *next = lds + (at ^ 1) * BUF;
-    if (more) load(step + 1, next);
-    const int head = step / per_head, i0 = begin + (step - head * per_head) * SA_STAGE;
-    const float* lst = reinterpret_cast<const float*>(here + 2 * stage::BYTES);
-#pragma unroll 1
-    for (int part = 0; part < SA_STAGE; part += 32) {
-      const int see = sees(a, t.n, i0 + part, 32, tok0, 32);
-      if (see == SEES_ALL) token_block<DP, false>(a, here, here + stage::BYTES, lst, part, t.n, i0, tok, k, v, dk, dv);
-      else if (see == SEES_PART) token_block<DP, true>(a, here, here + stage::BYTES, lst, part, t.n, i0, tok, k, v, dk, dv);
-    }
-    if (more) store(next);
-  }
+  token_tile<DP, DIRECT, false>(a, kv_head, t, tok0, k, v, dk, dv, lds);
+  if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dk) || any_nonfinite<NK>(dv)), 0))
+    token_tile<DP, DIRECT, true>(a, kv_head, t, tok0, k, v, dk, dv, lds);
   if (tok >= t.n) return;
   store_column<DP>(dk, a.scale, a.dK + mine * a.dks + kv_head * a.d, a.d);
   store_column<DP>(dv, 1.0f, a.dV + mine * a.dvs + kv_head * a.d, a.d);

@@ -94,7 +94,7 @@ class Packed:
             assert (np.abs(lse[here, h] - l) <= e[:, 0] + len(q) * F + 2 * F * np.abs(l)).all(), (here, h)
 
     def check_backward(self, O, lse, out):
-        """Against the formula on the O and lse that the call was given."""
+        """Against the formula in 64 bits on the lse that the call was given (O is where delta begins, not what it is)."""
         dQ, dK, dV = (x.float().cpu().numpy() for x in out)
         for x in (dQ, dK, dV):
             assert (x[self.others()] == 7).all()
@@ -106,14 +106,18 @@ class Packed:
             want[name][1][here, head] += error
         for here, h, hk, seen in self.each():
             q, k, v, do, o = (x[here, j].astype(np.float64) for x, j in ((self.q, h), (self.k, hk), (self.v, hk), (self.do, h), (O, h)))
-            dq, dk, dv, p, ds = to.self_attention_gradients(do, q, k, v, o, lse[here, h], seen, self.scale)
+            dq, dk, dv, p, ds = to.self_attention_gradients(do, q, k, v, lse[here, h], seen, self.scale)
             e = self.score_error(q, k, seen)
-            # dP - delta: two sums of d products in fp32
-            diff = (self.d + 2) * F * (np.abs(do) @ np.abs(v).T + (np.abs(do) * np.abs(o)).sum(1, keepdims=True))
+            # dP - delta: a sum of d products in fp32, and delta, a sum of as many products as the row sees, each with its p off by e and n f
+            slopes = np.abs(do) @ np.abs(v).T
+            diff = (self.d + 2) * F * slopes + ((self.d + 2 + len(q)) * F + 2 * e) * (p * slopes).sum(1, keepdims=True)
             diff = np.where(seen & (seen.sum(1) > 1)[:, None], diff, 0)
+            # dQ and the sums behind it: dS is formed with dO . O first (off by `rest`, from O's rounding), and rounded then
+            rest = np.abs((do * o).sum(1, keepdims=True) - (p * (do @ v.T)).sum(1, keepdims=True))
             dse = (np.abs(ds) * (U + e) + p * diff * (1 + e)) * (1 + U)
+            dsq = dse + p * rest * (2 * U + 2 * e) * (seen.sum(1, keepdims=True) > 1)
             n = len(q) * self.H // self.Hk + 4
-            add("dQ", here, h, dq, abs(self.scale) * (dse @ np.abs(k) + n * F * np.abs(ds) @ np.abs(k)))
+            add("dQ", here, h, dq, abs(self.scale) * (dsq @ np.abs(k) + n * F * np.abs(ds) @ np.abs(k)))
             add("dK", here, hk, dk, abs(self.scale) * (dse.T @ np.abs(q) + n * F * np.abs(ds).T @ np.abs(q)))
             add("dV", here, hk, dv, (p * (U + e + n * F)).T @ np.abs(do))
         mine = ~self.others()
