@@ -34,17 +34,15 @@ struct self_args {
 };
 
 // ---------------------------------------------------------------------------------------------
-// Tiles in LDS: rows of DP elements as they lie in memory, their pieces of 16 bytes exchanged within runs of eight (four where DP is an odd number
-// of 32s) by a number that the row gives, so that both ways of reading go through all banks: eight rows' same piece (operand rows), and
-// two neighbouring pieces of four rows (the transposing reads).
+// Tiles in LDS: rows of DP elements as they lie in memory, their pieces of 16 bytes exchanged within a row by a number that the row gives, so that both
+// ways of reading go through all 64 banks: the same piece of eight rows (operand rows), and four neighbouring pieces of four rows (the transposing
+// reads, whose rows therefore lie in different quarters of the banks).
 // ---------------------------------------------------------------------------------------------
 template <int DP> __device__ __forceinline__ int piece_at(int row, int c) {
-  if constexpr (DP % 64 == 0) {
-    const int f = ((row & 3) << 1) | ((row >> 2) & 1);
-    return (c & ~7) | ((c ^ f) & 7);
-  } else {
-    return (c & ~3) | ((c ^ (row >> 2)) & 3);
-  }
+  const int low = (row >> 2) & 3;
+  if constexpr (DP % 128 == 0) return c ^ (4 * (row & 3) + low);
+  else if constexpr (DP % 64 == 0) return c ^ (4 * ((row >> 1) & 1) + low);
+  else return c ^ low;            // (rows an odd number of quarters apart)
 }
 
 typedef int i32x4_u_t __attribute__((ext_vector_type(4), aligned(4)));
@@ -61,10 +59,10 @@ __device__ __forceinline__ i32x4_t load_piece(const uint16_t* q, int d, int at) 
   return x;
 }
 
-// Sixteen bytes a lane from memory to LDS, lane by lane from `lds` on.  (Not through the compiler's builtin: it would wait for these loads in
-// front of every later read of LDS, of the other buffer as well.)
-__device__ __forceinline__ void load_to_lds(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+// Sixteen bytes a lane from memory to LDS, lane by lane from `lds` on: from base + offset, the base and `lds` the same for all lanes.  (Not through the
+// compiler's builtin: it would wait for these loads in front of every later read of LDS, of the other buffer as well.)
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
@@ -76,26 +74,45 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 template <int DP, bool DIRECT>
 struct stage_t {
   static constexpr int CPR = DP / 8, N = SA_STAGE * CPR / 256, BYTES = SA_STAGE * DP * 2;
+  const uint16_t* base;          // the sequence's first row
+  int64_t stride;
+  int d;
+  uint32_t offset[N];            // of the lane's pieces from a stage's first row, in bytes (64 rows of at most 2^23 elements)
   i32x4_t hold[DIRECT ? 1 : N];
 
-  __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, int first, int n, int d, unsigned char* lds) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  __device__ __forceinline__ void begin(const uint16_t* base_, int64_t stride_, int d_) {
+    base = base_; stride = stride_; d = d_;
+    if constexpr (DIRECT)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int L = (wave * N + i) * 64 + lane, row = L / CPR, c = piece_at<DP>(row, L % CPR);
-      const uint16_t* p = base + (int64_t)min(first + row, n - 1) * stride;
-      if constexpr (DIRECT) {
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (wave * N + i) * 1024);
-        if (c * 8 < d) load_to_lds(p + c * 8, to);
+      for (int i = 0; i < N; ++i) offset[i] = (uint32_t)row_of(i) * (uint32_t)stride * 2 + piece_of(i) * 16;
+  }
+  static __device__ __forceinline__ int place(int i) { return (int)((threadIdx.x >> 6) * N + i) * 64 + (int)(threadIdx.x & 63); }
+  static __device__ __forceinline__ int row_of(int i) { return place(i) / CPR; }
+  static __device__ __forceinline__ int piece_of(int i) { return piece_at<DP>(row_of(i), place(i) % CPR); }
+
+  __device__ __forceinline__ void load(int first, int n, unsigned char* lds) {
+    if constexpr (DIRECT) {
+      const uint16_t* from = base + (int64_t)first * stride;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (threadIdx.x >> 6) * N * 1024);
+      if (first + SA_STAGE <= n && d == DP) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_to_lds(from, offset[i], to + i * 1024);
       } else {
-        hold[i] = load_piece(p, d, c * 8);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t x = (uint32_t)min(row_of(i), n - 1 - first) * (uint32_t)stride * 2 + piece_of(i) * 16;
+          if (piece_of(i) * 8 < d) load_to_lds(from, x, to + i * 1024);
+        }
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) hold[i] = load_piece(base + (int64_t)min(first + row_of(i), n - 1) * stride, d, piece_of(i) * 8);
     }
   }
   __device__ __forceinline__ void store(unsigned char* lds) {
     if constexpr (!DIRECT) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) *reinterpret_cast<i32x4_t*>(lds + ((threadIdx.x >> 6) * N + i) * 1024 + (threadIdx.x & 63) * 16) = hold[i];
+      for (int i = 0; i < N; ++i) *reinterpret_cast<i32x4_t*>(lds + place(i) * 16) = hold[i];
     }
   }
   // Pieces behind d are never written by direct loads: zeros, once.
@@ -125,6 +142,17 @@ template <int DP> __device__ __forceinline__ bf16x8_t column_operand(const unsig
   const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p3)at(r + 8));
   const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
   return __builtin_bit_cast(bf16x8_t, make_uint4(a.x, a.y, b.x, b.y));
+}
+// All of a product's operands for 32 rows: DP / 16 of either kind.
+template <int DP> __device__ __forceinline__ void row_operands(bf16x8_t* x, const unsigned char* lds, int row0) {
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) x[s] = row_operand<DP>(lds, row0, s);
+}
+template <int DP> __device__ __forceinline__ void column_operands(bf16x8_t* x, const unsigned char* lds, int row0) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) x[u * (DP / 32) + i] = column_operand<DP>(lds, row0 + 16 * u, i);
 }
 // The operand that stays in registers: columns are rows `row` (per lane) of a tensor.
 template <int DP> __device__ __forceinline__ void load_columns(bf16x8_t* x, const uint16_t* row, int d, bool negative) {
@@ -160,6 +188,11 @@ template <int PRODUCTS, int READS, int VALU> __device__ __forceinline__ void ste
     if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
     if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
   }
+}
+// The same, and nothing moves across its end.
+template <int PRODUCTS, int READS, int VALU> __device__ __forceinline__ void phase() {
+  steps<PRODUCTS, READS, VALU>();
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // Eight rows of a tile as the second product's operand (registers 8 u .. 8 u + 7).
@@ -400,10 +433,12 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
   const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
   const stages_of g = token_stages(a, t, row0);
   stage k, v;
+  k.begin(K, a.ks, a.d);
+  v.begin(V, a.vs, a.d);
   auto load = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
-    k.load(K, a.ks, g.first + i * SA_STAGE, t.n, a.d, to);
-    v.load(V, a.vs, g.first + i * SA_STAGE, t.n, a.d, to + stage::BYTES);
+    k.load(g.first + i * SA_STAGE, t.n, to);
+    v.load(g.first + i * SA_STAGE, t.n, to + stage::BYTES);
   };
   auto put = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
@@ -489,16 +524,18 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
   uint32_t seen[NB];
-  auto scores = [&](int b) {
+  constexpr int N = DP / 16;
+  bf16x8_t x[2][N];              // operands of the present phase and, being read, of the next
+  auto scores = [&](int b, const bf16x8_t* o) {
     s[b] = f32x16_t{};
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) s[b] = mfma(row_operand<DP>(lk, at + 32 * b, k), q[k], s[b]);
+    for (int k = 0; k < N; ++k) s[b] = mfma(o[k], q[k], s[b]);
   };
-  auto slopes = [&](int b) {
+  auto slopes = [&](int b, const bf16x8_t* o) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) dp[b][j] = -delta;
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) dp[b] = mfma(row_operand<DP>(lv, at + 32 * b, k), g[k], dp[b]);
+    for (int k = 0; k < N; ++k) dp[b] = mfma(o[k], g[k], dp[b]);
   };
   auto weights = [&](int b) {
 #pragma unroll
@@ -526,13 +563,13 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
       rest += x;
     }
   };
-  auto products = [&](int b) {
+  auto products = [&](int b, const bf16x8_t* o) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const bf16x8_t x = as_operand(dp[b], u), p = as_operand(s[b], u);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        const bf16x8_t k = column_operand<DP>(lk, at + 32 * b + 16 * u, i);
+        const bf16x8_t k = o[u * NK + i];
         if constexpr (CAREFUL) {
           dq[i] = mfma_seen(k, x, seen[b] >> (8 * u), dq[i]);
           pk[i] = mfma_seen(k, p, seen[b] >> (8 * u), pk[i]);
@@ -543,36 +580,37 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
       }
     }
   };
-  scores(0);
-  slopes(0);
+  // Each phase's operands are read during the one before it; the exponentials and dS of a block run beside the products of another phase.
+  constexpr int VE = at_least_one(40 / N), VD = at_least_one(56 / N);
+  row_operands<DP>(x[0], lk, at);
+  __builtin_amdgcn_sched_barrier(0);
+  row_operands<DP>(x[1], lv, at);
+  scores(0, x[0]);
+  phase<N, 1, 0>();
+  if constexpr (NB == 2) row_operands<DP>(x[0], lk, at + 32);
+  else column_operands<DP>(x[0], lk, at);
+  slopes(0, x[1]);
   weights(0);
-  if constexpr (NB == 2) scores(1);
-  through(0);
+  phase<N, NB == 2 ? 1 : 2, VE>();
   if constexpr (NB == 2) {
-    slopes(1);
+    row_operands<DP>(x[1], lv, at + 32);
+    scores(1, x[0]);
+    through(0);
+    phase<N, 1, VD>();
+    column_operands<DP>(x[0], lk, at);
+    slopes(1, x[1]);
     weights(1);
-  }
-  products(0);
-  if constexpr (NB == 2) {
+    phase<N, 2, VE>();
+    column_operands<DP>(x[1], lk, at + 32);
+    products(0, x[0]);
     through(1);
-    products(1);
-  }
-  if constexpr (!CAREFUL && !PART) {
-    constexpr int S = DP / 16, P = 4 * NK;
-    reads_first<4>();
-    steps<S, 1, 0>();
-    steps<S, 1, at_least_one(32 / S)>();
-    if constexpr (NB == 2) {
-      steps<S, 1, at_least_one(48 / S)>();
-      steps<S, 1, at_least_one(32 / S)>();
-      steps<P, 1, at_least_one(48 / P)>();
-      steps<P - 4, 1, 0>();
-      steps<4, 0, 0>();
-    } else {
-      __builtin_amdgcn_sched_group_barrier(0x2, 40, 0);
-      steps<P - 4, 1, 0>();
-      steps<4, 0, 0>();
-    }
+    phase<2 * N, 1, VD / 2>();
+    products(1, x[1]);
+    __builtin_amdgcn_sched_barrier(0);
+  } else {
+    through(0);
+    products(0, x[0]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -587,10 +625,12 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
   const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
   const stages_of st = token_stages(a, t, row0);
   stage k, v;
+  k.begin(K, a.ks, a.d);
+  v.begin(V, a.vs, a.d);
   auto load = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
-    k.load(K, a.ks, st.first + i * SA_STAGE, t.n, a.d, to);
-    v.load(V, a.vs, st.first + i * SA_STAGE, t.n, a.d, to + stage::BYTES);
+    k.load(st.first + i * SA_STAGE, t.n, to);
+    v.load(st.first + i * SA_STAGE, t.n, to + stage::BYTES);
   };
   auto put = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
@@ -675,30 +715,35 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
   f32x16_t s[NB], dp[NB];
   uint32_t seen[NB], passed[NB];
   auto visible = [&](int row) { return (row < n) & (tok < n) & (!a.causal | (tok <= row)) & (tok >= first_token(a, row)); };
-  auto scores = [&](int b) {
-    s[b] = f32x16_t{};
-#pragma unroll
-    for (int x = 0; x < DP / 16; ++x) s[b] = mfma(row_operand<DP>(lq, at + 32 * b, x), k[x], s[b]);
-  };
-  auto slopes = [&](int b) {
+  constexpr int N = DP / 16;
+  bf16x8_t o[2][N];              // operands of the present phase and, being read, of the next
+  f32x4_t lse[NB][4];            // (-lse log2 e)
+  auto sums = [&](int b) {       // and -delta, which dP begins with
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
+      lse[b][y] = *reinterpret_cast<const f32x4_t*>(lst + at + 32 * b + 8 * y + 4 * h);
       const f32x4_t x = *reinterpret_cast<const f32x4_t*>(lst + SA_STAGE + at + 32 * b + 8 * y + 4 * h);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) dp[b][4 * y + j] = x[j];       // (-delta)
+      for (int j = 0; j < 4; ++j) dp[b][4 * y + j] = x[j];
     }
+  };
+  auto scores = [&](int b, const bf16x8_t* o) {
+    s[b] = f32x16_t{};
 #pragma unroll
-    for (int x = 0; x < DP / 16; ++x) dp[b] = mfma(row_operand<DP>(lg, at + 32 * b, x), v[x], dp[b]);
+    for (int x = 0; x < N; ++x) s[b] = mfma(o[x], k[x], s[b]);
+  };
+  auto slopes = [&](int b, const bf16x8_t* o) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) dp[b] = mfma(o[x], v[x], dp[b]);
   };
   auto weights = [&](int b) {
     seen[b] = 0;
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
-      const f32x4_t lse = *reinterpret_cast<const f32x4_t*>(lst + at + 32 * b + 8 * y + 4 * h);     // (-lse log2 e)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int x = 4 * y + j;
-        s[b][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x], a.c, lse[j]));
+        s[b][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x], a.c, lse[b][y][j]));
         if constexpr (PART || CAREFUL) {
           const bool vis = visible(i0 + at + 32 * b + 8 * y + 4 * h + j);
           s[b][x] = vis ? s[b][x] : 0.0f;
@@ -722,58 +767,73 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
       dp[b][x] = ds;
     }
   };
-  auto products = [&](int b) {
+  auto value_products = [&](int b, const bf16x8_t* o) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const bf16x8_t x = as_operand(s[b], u);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        const bf16x8_t g = column_operand<DP>(lg, at + 32 * b + 16 * u, i);
-        if constexpr (CAREFUL) dv[i] = mfma_seen(g, x, seen[b] >> (8 * u), dv[i]);
-        else dv[i] = mfma(g, x, dv[i]);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const bf16x8_t y = as_operand(dp[b], u);
-#pragma unroll
-      for (int i = 0; i < NK; ++i) {
-        const bf16x8_t q = column_operand<DP>(lq, at + 32 * b + 16 * u, i);
-        if constexpr (CAREFUL) dk[i] = mfma_seen(q, y, passed[b] >> (8 * u), dk[i]);
-        else dk[i] = mfma(q, y, dk[i]);
+        if constexpr (CAREFUL) dv[i] = mfma_seen(o[u * NK + i], x, seen[b] >> (8 * u), dv[i]);
+        else dv[i] = mfma(o[u * NK + i], x, dv[i]);
       }
     }
   };
-  scores(0);
-  slopes(0);
-  weights(0);
-  if constexpr (NB == 2) scores(1);
-  through(0);
-  if constexpr (NB == 2) {
-    slopes(1);
-    weights(1);
-  }
-  products(0);
-  if constexpr (NB == 2) {
-    through(1);
-    products(1);
-  }
-  if constexpr (!CAREFUL && !PART) {
-    constexpr int S = DP / 16, P = 4 * NK;
-    reads_first<8>();
-    steps<S, 1, 0>();
-    steps<S, 2, at_least_one(32 / S)>();
-    if constexpr (NB == 2) {
-      steps<S, 2, at_least_one(32 / S)>();
-      steps<S, 2, at_least_one(32 / S)>();
-      steps<P, 2, at_least_one(32 / P)>();
-      steps<P - 4, 2, 0>();
-      steps<4, 0, 0>();
-    } else {
-      __builtin_amdgcn_sched_group_barrier(0x2, 24, 0);
-      steps<P - 4, 2, 0>();
-      steps<4, 0, 0>();
+  auto key_products = [&](int b, const bf16x8_t* o) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8_t x = as_operand(dp[b], u);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        if constexpr (CAREFUL) dk[i] = mfma_seen(o[u * NK + i], x, passed[b] >> (8 * u), dk[i]);
+        else dk[i] = mfma(o[u * NK + i], x, dk[i]);
+      }
     }
+  };
+  // Each phase's operands are read during the one before it; the exponentials and dS of a block run beside the products of another phase.
+  constexpr int VE = at_least_one(40 / N), VD = at_least_one(36 / N);
+  row_operands<DP>(o[0], lq, at);
+  sums(0);
+  __builtin_amdgcn_sched_barrier(0);
+  row_operands<DP>(o[1], lg, at);
+  scores(0, o[0]);
+  phase<N, 1, 0>();
+  if constexpr (NB == 2) {
+    row_operands<DP>(o[0], lq, at + 32);
+    sums(1);
+    slopes(0, o[1]);
+    weights(0);
+    phase<N, 2, VE>();
+    row_operands<DP>(o[1], lg, at + 32);
+    scores(1, o[0]);
+    through(0);
+    phase<N, 1, VD>();
+    column_operands<DP>(o[0], lg, at);
+    slopes(1, o[1]);
+    weights(1);
+    phase<N, 2, VE>();
+    column_operands<DP>(o[1], lq, at);
+    value_products(0, o[0]);
+    through(1);
+    phase<N, 2, VD>();
+    column_operands<DP>(o[0], lg, at + 32);
+    key_products(0, o[1]);
+    phase<N, 2, 0>();
+    column_operands<DP>(o[1], lq, at + 32);
+    value_products(1, o[0]);
+    phase<N, 2, 0>();
+    key_products(1, o[1]);
+    __builtin_amdgcn_sched_barrier(0);
+  } else {
+    column_operands<DP>(o[0], lg, at);
+    slopes(0, o[1]);
+    weights(0);
+    phase<N, 2, VE>();
+    column_operands<DP>(o[1], lq, at);
+    value_products(0, o[0]);
+    through(0);
+    phase<N, 2, VD>();
+    key_products(0, o[1]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -788,13 +848,17 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
   const uint16_t* G = a.dO + ((int64_t)t.r0 * a.heads + (int64_t)kv_head * a.group) * a.d;
   const int64_t gs = (int64_t)a.heads * a.d;
   stage q, g;
+  q.begin(Q, a.qs, a.d);
+  g.begin(G, gs, a.d);
   float2 sums = make_float2(0.0f, 0.0f);
   int at = 0;                                          // the buffer of the present stage
   auto load = [&](int head, int i, int to_at) {
     unsigned char* to = lds + to_at * BUF;
     const int i0 = st.first + i * SA_STAGE;
-    q.load(Q + head * a.d, a.qs, i0, t.n, a.d, to);
-    g.load(G + head * a.d, gs, i0, t.n, a.d, to + stage::BYTES);
+    q.base = Q + head * a.d;
+    g.base = G + head * a.d;
+    q.load(i0, t.n, to);
+    g.load(i0, t.n, to + stage::BYTES);
     if (threadIdx.x < SA_STAGE)
       sums = a.stats[(int64_t)(kv_head * a.group + head) * a.T + t.r0 + min(i0 + (int)threadIdx.x, t.n - 1)];
   };
@@ -892,6 +956,8 @@ int check_stride(const char* name, int64_t stride, int heads, int d) {
              (long long)stride, (long long)heads * d);
   return PQ_OK;
 }
+// Rows that direct loads take: at multiples of 16 bytes, 64 of them within 2^31 bytes.
+bool direct_stride(int64_t stride) { return stride % 8 == 0 && stride <= (1 << 23); }
 bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 self_args make_args(const pq_self_attn_desc* d, int T, const int32_t* row_start) {
@@ -970,7 +1036,7 @@ extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64
   a.out = (uint16_t*)O; a.lse = lse;
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_FWD, s);
-  const bool direct = a.d % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
+  const bool direct = a.d % 8 == 0 && direct_stride(k_stride) && direct_stride(v_stride);
   return direct ? launch_forward_d<true>(a, s) : launch_forward_d<false>(a, s);
 }
 
@@ -1006,6 +1072,6 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   a.stats = (float2*)workspace;
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_BWD, s);
-  const bool direct = a.d % 8 == 0 && q_stride % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
+  const bool direct = a.d % 8 == 0 && direct_stride(q_stride) && direct_stride(k_stride) && direct_stride(v_stride) && direct_stride((int64_t)a.heads * a.d);
   return direct ? launch_backward_d<true>(a, s) : launch_backward_d<false>(a, s);
 }
