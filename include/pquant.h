@@ -478,7 +478,7 @@ int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const voi
  * non-decreasing, device memory that no call checks) are sequence b; a row sees rows of its own sequence only, with causal those up to itself, of
  * these the last `window` if window > 0.  Query head h reads key-value head h / (n_heads / n_kv_heads).
  *     s_j = scale q . k_j,   lse = log sum_j exp s_j,   o = sum_j exp(s_j - lse) v_j
- *   Q [T][n_heads][d_head], K, V [T][n_kv_heads][d_head] bf16, rows *_stride elements apart (even);  O [T][n_heads][d_head] bf16 out and
+ *   Q [T][n_heads][d_head], K, V [T][n_kv_heads][d_head] bf16, rows *_stride elements apart (even, at most 2^23);  O [T][n_heads][d_head] bf16 out and
  *   lse [T][n_heads] fp32 out, both contiguous.  Rows of no sequence are neither read nor written.  Buffers 16-byte aligned.
  * Scores, sums and lse are fp32; exp(s_j - m) is rounded to bf16 for the product with v (m: up to 16 powers of two below the largest s_j), o once more at the
  * end.  Tokens that a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite

@@ -70,49 +70,74 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 }
 
 // A stage of SA_STAGE rows of one tensor on its way to LDS.  DIRECT: rows and heads lie at multiples of 16 bytes, the loads go straight there;
-// otherwise through registers.  Rows behind the sequence's last are the last once more: whoever uses the stage hides them.
+// otherwise through registers, four bytes aligned.  Rows behind the sequence's last are the last once more: whoever uses the stage hides them.
 template <int DP, bool DIRECT>
 struct stage_t {
   static constexpr int CPR = DP / 8, N = SA_STAGE * CPR / 256, BYTES = SA_STAGE * DP * 2;
   const uint16_t* base;          // the sequence's first row
-  int64_t stride;
+  int64_t stride;                // elements, at most 2^23: 64 rows are within 2^31 bytes
   int d;
-  uint32_t offset[N];            // of the lane's pieces from a stage's first row, in bytes (64 rows of at most 2^23 elements)
+  uint32_t offset[N];            // of the lane's pieces from a stage's first row, in bytes
   i32x4_t hold[DIRECT ? 1 : N];
 
   __device__ __forceinline__ void begin(const uint16_t* base_, int64_t stride_, int d_) {
     base = base_; stride = stride_; d = d_;
-    if constexpr (DIRECT)
 #pragma unroll
-      for (int i = 0; i < N; ++i) offset[i] = (uint32_t)row_of(i) * (uint32_t)stride * 2 + piece_of(i) * 16;
+    for (int i = 0; i < N; ++i) offset[i] = (uint32_t)row_of(i) * (uint32_t)stride * 2 + place_in_row(i);
   }
   static __device__ __forceinline__ int place(int i) { return (int)((threadIdx.x >> 6) * N + i) * 64 + (int)(threadIdx.x & 63); }
   static __device__ __forceinline__ int row_of(int i) { return place(i) / CPR; }
   static __device__ __forceinline__ int piece_of(int i) { return piece_at<DP>(row_of(i), place(i) % CPR); }
+  // Where in its row a piece's load begins: through registers no load passes the row's end (d >= 8; shorter rows are read by halves of it).
+  __device__ __forceinline__ uint32_t place_in_row(int i) const { return 2 * (DIRECT || d < 8 ? piece_of(i) * 8 : min(piece_of(i) * 8, d - 8)); }
 
   __device__ __forceinline__ void load(int first, int n, unsigned char* lds) {
+    const uint16_t* from = base + (int64_t)first * stride;
+    const bool whole = first + SA_STAGE <= n;
     if constexpr (DIRECT) {
-      const uint16_t* from = base + (int64_t)first * stride;
       const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (threadIdx.x >> 6) * N * 1024);
-      if (first + SA_STAGE <= n && d == DP) {
+      if (whole && d == DP) {
 #pragma unroll
         for (int i = 0; i < N; ++i) load_to_lds(from, offset[i], to + i * 1024);
       } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const uint32_t x = (uint32_t)min(row_of(i), n - 1 - first) * (uint32_t)stride * 2 + piece_of(i) * 16;
+          const uint32_t x = (uint32_t)min(row_of(i), n - 1 - first) * (uint32_t)stride * 2 + place_in_row(i);
           if (piece_of(i) * 8 < d) load_to_lds(from, x, to + i * 1024);
         }
       }
     } else {
+      uint32_t x[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) hold[i] = load_piece(base + (int64_t)min(first + row_of(i), n - 1) * stride, d, piece_of(i) * 8);
+      for (int i = 0; i < N; ++i) x[i] = offset[i];
+      if (!whole)
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (uint32_t)min(row_of(i), n - 1 - first) * (uint32_t)stride * 2 + place_in_row(i);
+      const char* bytes = reinterpret_cast<const char*>(from);
+      if (d >= 8) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) hold[i] = *reinterpret_cast<const i32x4_u_t*>(bytes + x[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) hold[i] = load_piece(reinterpret_cast<const uint16_t*>(bytes + (x[i] - place_in_row(i))), d, piece_of(i) * 8);
+      }
     }
   }
   __device__ __forceinline__ void store(unsigned char* lds) {
     if constexpr (!DIRECT) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) *reinterpret_cast<i32x4_t*>(lds + place(i) * 16) = hold[i];
+      for (int i = 0; i < N; ++i) {
+        i32x4_t x = hold[i];
+        if (d >= 8) {                                  // the last piece came d % 8 elements too early; nothing is behind it
+          const int at = piece_of(i) * 8;
+          i32x4_t y = x;
+          for (int k = d & 7; k < 8 && k > 0; k += 2) y = i32x4_t{y[1], y[2], y[3], 0};
+          const bool last = at < d && at + 8 > d, none = at >= d;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = none ? 0 : last ? y[j] : x[j];
+        }
+        *reinterpret_cast<i32x4_t*>(lds + place(i) * 16) = x;
+      }
     }
   }
   // Pieces behind d are never written by direct loads: zeros, once.
@@ -222,6 +247,21 @@ __device__ __forceinline__ f32x16_t mfma_seen(bf16x8_t a, bf16x8_t b, uint32_t s
   return mfma(t, s, c);
 }
 
+// Bits low .. high of 32, as far as there are such.
+__device__ __forceinline__ uint32_t bits_between(int low, int high) {
+  const uint32_t up = high >= 31 ? 0xffffffffu : high < 0 ? 0u : (2u << high) - 1u;
+  return low <= 0 ? up : low > 31 ? 0u : up & (0xffffffffu << low);
+}
+// x where bit k of the mask is set, otherwise 0 (two instructions, no comparison).
+__device__ __forceinline__ float where_set(float x, uint32_t mask, int k) {
+  return __uint_as_float(__float_as_uint(x) & (uint32_t)__builtin_amdgcn_sbfe((int)mask, k, 1));
+}
+// The bits of a tile's registers 8 u .. among those of its rows (shifted by 4 h): what mfma_seen wants.
+__device__ __forceinline__ uint32_t register_bits(uint32_t rows, int u) {
+  const uint32_t x = rows >> (16 * u);
+  return (x & 15u) | ((x >> 8) & 15u) << 4;
+}
+
 // The value of the other half's lane joined to a lane's own (both halves hold the same columns).
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
 
@@ -242,53 +282,64 @@ __device__ __forceinline__ self_tile find_self_tile(const self_args& a, int vt) 
 // Tokens that rows from .. to - 1 of a sequence of n see between them.
 __device__ __forceinline__ int first_token(const self_args& a, int row) { return a.window > 0 && row >= a.window ? row - a.window + 1 : 0; }
 
-// The stages that a tile needs, and of them what a wavefront's 32 rows (or tokens) see: nothing before `from` and from `to` on, all of the stages from
-// `all` to `part` - 1, a part of the others.  Each of these is a loop of its own: a branch around accumulators costs a second copy of them all.
+// The stages that a tile needs, and of them those of which a wavefront's 32 rows (or tokens) see something, from .. to - 1: these are a loop of their own,
+// since a branch around accumulators costs a second copy of them all.  Those from `all` to `part` - 1 are seen by all of its rows.
 struct stages_of { int first, n, from, all, part, to; };
-__device__ __forceinline__ stages_of clamp_stages(stages_of g) {
-  g.to = min(max(g.to, 0), g.n);
-  g.from = min(max(g.from, 0), g.to);
-  g.all = min(max(g.all, g.from), g.to);
-  g.part = min(max(g.part, g.all), g.to);
-  return g;
-}
 // Stages of tokens that rows row0 .. row0 + 31 of the tile see.
 __device__ __forceinline__ stages_of token_stages(const self_args& a, const self_tile& t, int row0) {
   const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n, last = min(row0 + 31, t.n - 1);
   stages_of g;
   g.first = first_token(a, t.at) & ~(SA_STAGE - 1);
   g.n = (end - g.first + SA_STAGE - 1) / SA_STAGE;
-  g.from = (first_token(a, row0) - g.first) / SA_STAGE;
   g.to = row0 < t.n ? ((a.causal ? last : t.n - 1) - g.first) / SA_STAGE + 1 : 0;
+  g.from = min((first_token(a, row0) - g.first) / SA_STAGE, g.to);
   g.all = (first_token(a, last) - g.first + SA_STAGE - 1) / SA_STAGE;
   g.part = ((a.causal ? row0 + 1 : t.n) - g.first) / SA_STAGE;
-  return clamp_stages(g);
+  return g;
 }
 // Stages of rows that see tokens tok0 .. tok0 + 31 of the tile.
+__device__ __forceinline__ int first_blind_row(const self_args& a, int n, int tok) {   // the first that sees `tok` no more
+  return a.window > 0 && a.window < n && tok < n - a.window ? tok + a.window : n;
+}
 __device__ __forceinline__ stages_of row_stages(const self_args& a, const self_tile& t, int tok0) {
-  const bool window = a.window > 0 && a.window < t.n;
-  auto behind = [&](int tok) { return window && tok < t.n - a.window ? tok + a.window : t.n; };   // the first row that sees no `tok` any more
   stages_of g;
   g.first = (a.causal ? t.at : 0) & ~(SA_STAGE - 1);
-  g.n = (behind(min(t.at + SA_ROWS, t.n) - 1) - g.first + SA_STAGE - 1) / SA_STAGE;
-  g.from = a.causal ? (tok0 - g.first) / SA_STAGE : 0;
-  g.to = tok0 < t.n ? (behind(min(tok0 + 31, t.n - 1)) - g.first + SA_STAGE - 1) / SA_STAGE : 0;
+  g.n = (first_blind_row(a, t.n, min(t.at + SA_ROWS, t.n) - 1) - g.first + SA_STAGE - 1) / SA_STAGE;
+  g.to = tok0 < t.n ? (first_blind_row(a, t.n, min(tok0 + 31, t.n - 1)) - g.first + SA_STAGE - 1) / SA_STAGE : 0;
+  g.from = min(a.causal ? (tok0 - g.first) / SA_STAGE : 0, g.to);
   g.all = a.causal ? (tok0 + 31 - g.first + SA_STAGE - 1) / SA_STAGE : 0;
-  g.part = (behind(tok0) - g.first) / SA_STAGE;
-  return clamp_stages(g);
+  g.part = (first_blind_row(a, t.n, tok0) - g.first) / SA_STAGE;
+  return g;
 }
-// `next` waits for a stage and has the loads of the one behind it started, `store` puts away what came through registers.
-template <typename N, typename S, typename P, typename A>
-__device__ __forceinline__ void in_stages(const stages_of& g, N next, S store, P use_part, A use_all) {
+// `next` waits for a stage and has the loads of the one behind it started, `store` puts away what came through registers; `use` is told whether the
+// stage needs its mask.  (Masked and unmasked stages are loops in turn inside a loop, so that each is there once: heads of 128, 8192 and 130 tokens,
+// always masked 2320 and 29.1 us, two masked loops around an unmasked one 2150 and 33.)
+template <typename N, typename S, typename U>
+__device__ __forceinline__ void in_stages(const stages_of& g, N next, S store, U use) {
+  int i = 0;
+#pragma unroll 1
+  for (; i < g.from; ++i) { next(i); store(i); }
+  int masked = min(g.all, g.to);
+  const int part = min(g.part, g.to);
+#pragma unroll 1
+  while (i < g.to) {
+#pragma unroll 1
+    for (; i < masked; ++i) { next(i); use(i, std::true_type{}); store(i); }
+#pragma unroll 1
+    for (; i < part; ++i) { next(i); use(i, std::false_type{}); store(i); }
+    masked = g.to;
+  }
+#pragma unroll 1
+  for (; i < g.n; ++i) { next(i); store(i); }
+}
+// The same where `use` asks by itself.
+template <typename N, typename S, typename U>
+__device__ __forceinline__ void in_stages_alike(const stages_of& g, N next, S store, U use) {
   int i = 0;
 #pragma unroll 1
   for (; i < g.from; ++i) { next(i); store(i); }
 #pragma unroll 1
-  for (; i < g.all; ++i) { next(i); use_part(i); store(i); }
-#pragma unroll 1
-  for (; i < g.part; ++i) { next(i); use_all(i); store(i); }
-#pragma unroll 1
-  for (; i < g.to; ++i) { next(i); use_part(i); store(i); }
+  for (; i < g.to; ++i) { next(i); use(i); store(i); }
 #pragma unroll 1
   for (; i < g.n; ++i) { next(i); store(i); }
 }
@@ -470,11 +521,7 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
       forward_stage<DP>(a, here, here + stage::BYTES, q, o, m, l, part, low, lim);
     }
   };
-  // (one loop for both: the mask changes scores alone)
-  stages_of one = g;
-  one.all = g.from;
-  one.part = g.to;
-  in_stages(one, next, store, [&](int) {}, [&](int i) { use(i, i < g.all || i >= g.part); });
+  in_stages_alike(g, next, store, [&](int i) { use(i, i < g.all || i >= g.part); });
 }
 
 template <int DP, bool DIRECT>
@@ -506,20 +553,19 @@ __global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
 // ---------------------------------------------------------------------------------------------
 // Gradient of the queries.  Leaves lse and delta head by head for the other kernel.
 // ---------------------------------------------------------------------------------------------
-// A row that sees one token has p = 1 whatever its score: no gradient passes through it.
-__device__ __forceinline__ bool sees_one(const self_args& a, int n, int row) { return n == 1 || (a.causal && (row == 0 || a.window == 1)); }
+// Rows that see one token have p = 1 whatever its score: no gradient passes through it.
+__device__ __forceinline__ bool see_one(const self_args& a, int n) { return n == 1 || a.window == 1; }
 
 // Blocks of 32 tokens that a wavefront has in flight at a time: with two the products of one cover the exponentials of the other.
-template <int DP> constexpr int blocks_in_flight() { return DP == 96 ? 1 : 2; }
+template <int DP> constexpr int blocks_in_flight() { return 2; }
 // Wavefronts a SIMD of the backward kernels: their accumulators and both operands that stay take 1.5 DP registers, of 256 or 512.
-template <int DP> constexpr int backward_waves() { return DP > 96 ? 1 : 2; }
+template <int DP> constexpr int backward_waves() { return DP > 64 ? 1 : 2; }
 
 // delta is dO . O with O as it was rounded to bf16, which costs dS as much as all else together; what is missing to sum_j p_ij dP_ij is the sum of
 // the dS themselves, known at the end.  So the products with p are kept beside those with dS (they share their other operand), and dQ is put right by them.
-template <int DP, bool PART, bool CAREFUL>
+template <int DP, bool MASKED, bool CAREFUL>
 __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q,
-                                             const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, int low, int lim,
-                                             bool one) {
+                                             const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, int low, int lim) {
   constexpr int NK = DP / 32, NB = CAREFUL ? 1 : blocks_in_flight<DP>();
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
@@ -538,29 +584,19 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
     for (int k = 0; k < N; ++k) dp[b] = mfma(o[k], g[k], dp[b]);
   };
   auto weights = [&](int b) {
+    seen[b] = bits_between(low - at - 32 * b, lim - at - 32 * b) >> (4 * h);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], a.c, -lse));
-      if constexpr (PART || CAREFUL) {
-        const int tok = 32 * b + tile_row(j);
-        s[b][j] = tok >= low - at - 4 * h && tok <= lim - at - 4 * h ? s[b][j] : 0.0f;
-      }
+      if constexpr (MASKED) s[b][j] = where_set(s[b][j], seen[b], tile_row(j));
     }
   };
   auto through = [&](int b) {
-    seen[b] = 0;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      float x = s[b][j] * dp[b][j];
-      if constexpr (PART || CAREFUL) {
-        const int tok = 32 * b + tile_row(j);
-        const bool v = tok >= low - at - 4 * h && tok <= lim - at - 4 * h && !one;
-        if constexpr (CAREFUL) x = v ? x : 0.0f;       // (otherwise 0 times what is not finite: the tile is taken with care)
-        else x = one ? 0.0f : x;
-        seen[b] |= (v ? 1u : 0u) << j;
-      }
-      dp[b][j] = x;
-      rest += x;
+      // (without care 0 times what is not finite is NaN, and has the tile taken with care)
+      dp[b][j] = CAREFUL ? where_set(s[b][j] * dp[b][j], seen[b], tile_row(j)) : s[b][j] * dp[b][j];
+      rest += dp[b][j];
     }
   };
   auto products = [&](int b, const bf16x8_t* o) {
@@ -571,8 +607,8 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
       for (int i = 0; i < NK; ++i) {
         const bf16x8_t k = o[u * NK + i];
         if constexpr (CAREFUL) {
-          dq[i] = mfma_seen(k, x, seen[b] >> (8 * u), dq[i]);
-          pk[i] = mfma_seen(k, p, seen[b] >> (8 * u), pk[i]);
+          dq[i] = mfma_seen(k, x, register_bits(seen[b], u), dq[i]);
+          pk[i] = mfma_seen(k, p, register_bits(seen[b], u), pk[i]);
         } else {
           dq[i] = mfma(k, x, dq[i]);
           pk[i] = mfma(k, p, pk[i]);
@@ -580,19 +616,18 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
       }
     }
   };
-  // Each phase's operands are read during the one before it; the exponentials and dS of a block run beside the products of another phase.
-  constexpr int VE = at_least_one(40 / N), VD = at_least_one(56 / N);
-  row_operands<DP>(x[0], lk, at);
-  __builtin_amdgcn_sched_barrier(0);
-  row_operands<DP>(x[1], lv, at);
-  scores(0, x[0]);
-  phase<N, 1, 0>();
-  if constexpr (NB == 2) row_operands<DP>(x[0], lk, at + 32);
-  else column_operands<DP>(x[0], lk, at);
-  slopes(0, x[1]);
-  weights(0);
-  phase<N, NB == 2 ? 1 : 2, VE>();
   if constexpr (NB == 2) {
+    // Each phase's operands are read during the one before it; the exponentials and dS of a block run beside the products of another phase.
+    constexpr int VE = at_least_one(40 / N), VD = at_least_one(56 / N);
+    row_operands<DP>(x[0], lk, at);
+    __builtin_amdgcn_sched_barrier(0);
+    row_operands<DP>(x[1], lv, at);
+    scores(0, x[0]);
+    phase<N, 1, 0>();
+    row_operands<DP>(x[0], lk, at + 32);
+    slopes(0, x[1]);
+    weights(0);
+    phase<N, 1, VE>();
     row_operands<DP>(x[1], lv, at + 32);
     scores(1, x[0]);
     through(0);
@@ -608,9 +643,21 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
     products(1, x[1]);
     __builtin_amdgcn_sched_barrier(0);
   } else {
+    // (one block: no registers for a second set of operands, reads run four products ahead)
+    row_operands<DP>(x[0], lk, at);
+    scores(0, x[0]);
+    row_operands<DP>(x[1], lv, at);
+    slopes(0, x[1]);
+    weights(0);
     through(0);
+    column_operands<DP>(x[0], lk, at);
     products(0, x[0]);
-    __builtin_amdgcn_sched_barrier(0);
+    reads_first<4>();
+    steps<N, 1, 0>();
+    steps<N, 1, at_least_one(32 / N)>();
+    __builtin_amdgcn_sched_group_barrier(0x2, 40, 0);
+    steps<2 * N - 4, 1, 0>();
+    steps<4, 0, 0>();
   }
 }
 
@@ -620,7 +667,6 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES;
   const int row = row0 + (threadIdx.x & 31);
-  const bool one = sees_one(a, t.n, row);
   const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
   const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
   const stages_of st = token_stages(a, t, row0);
@@ -650,16 +696,17 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
   for (int i = 0; i < DP / 32; ++i) dq[i] = pk[i] = f32x16_t{};
   rest = 0.0f;
   put(0);
-  auto use = [&](int i, auto part) {
+  auto use = [&](int i, auto masked) {
     unsigned char* here = lds + (i & 1) * BUF;
     const int j0 = st.first + i * SA_STAGE;
     const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
     constexpr int NB = CAREFUL ? 1 : blocks_in_flight<DP>();
 #pragma unroll 1
     for (int at = 0; at < SA_STAGE; at += 32 * NB)
-      query_blocks<DP, decltype(part)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, low, lim, one);
+      query_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, low, lim);
   };
-  in_stages(st, next, store, [&](int i) { use(i, std::true_type{}); }, [&](int i) { use(i, std::false_type{}); });
+  if constexpr (CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
+  else in_stages(st, next, store, use);
 }
 
 template <int DP, bool DIRECT>
@@ -697,24 +744,24 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
   rest += other_half(rest);
   if (row >= t.n) return;
   if (lane < 32) a.stats[(int64_t)w.head * a.T + mine] = make_float2(lse, delta + rest);
+  const bool one = see_one(a, t.n) || (a.causal && row == 0);
 #pragma unroll
   for (int i = 0; i < NK; ++i)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) dq[i][j] -= rest * pk[i][j];
+    for (int j = 0; j < 16; ++j) dq[i][j] = one ? 0.0f : dq[i][j] - rest * pk[i][j];
   store_column<DP>(dq, a.scale, a.dQ + mine * a.dqs + w.head * a.d, a.d);
 }
 
 // ---------------------------------------------------------------------------------------------
 // Gradients of the keys and values
 // ---------------------------------------------------------------------------------------------
-template <int DP, bool PART, bool CAREFUL>
-__device__ __forceinline__ void token_blocks(const self_args& a, const unsigned char* lq, const unsigned char* lg, const float* lst, int at, int n, int i0,
-                                             int tok, const bf16x8_t* k, const bf16x8_t* v, f32x16_t* dk, f32x16_t* dv) {
+template <int DP, bool MASKED, bool CAREFUL>
+__device__ __forceinline__ void token_blocks(const self_args& a, const unsigned char* lq, const unsigned char* lg, const float* lst, int at, int low, int lim,
+                                             const bf16x8_t* k, const bf16x8_t* v, f32x16_t* dk, f32x16_t* dv) {
   constexpr int NK = DP / 32, NB = CAREFUL ? 1 : blocks_in_flight<DP>();
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
-  uint32_t seen[NB], passed[NB];
-  auto visible = [&](int row) { return (row < n) & (tok < n) & (!a.causal | (tok <= row)) & (tok >= first_token(a, row)); };
+  uint32_t seen[NB];
   constexpr int N = DP / 16;
   bf16x8_t o[2][N];              // operands of the present phase and, being read, of the next
   f32x4_t lse[NB][4];            // (-lse log2 e)
@@ -737,35 +784,16 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
     for (int x = 0; x < N; ++x) dp[b] = mfma(o[x], v[x], dp[b]);
   };
   auto weights = [&](int b) {
-    seen[b] = 0;
+    seen[b] = bits_between(low - at - 32 * b, lim - at - 32 * b) >> (4 * h);
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int x = 4 * y + j;
-        s[b][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x], a.c, lse[b][y][j]));
-        if constexpr (PART || CAREFUL) {
-          const bool vis = visible(i0 + at + 32 * b + 8 * y + 4 * h + j);
-          s[b][x] = vis ? s[b][x] : 0.0f;
-          seen[b] |= (vis ? 1u : 0u) << x;
-        }
-      }
+    for (int j = 0; j < 16; ++j) {
+      s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], a.c, lse[b][j >> 2][j & 3]));
+      if constexpr (MASKED) s[b][j] = where_set(s[b][j], seen[b], tile_row(j));
     }
   };
   auto through = [&](int b) {
-    passed[b] = 0;
 #pragma unroll
-    for (int x = 0; x < 16; ++x) {
-      float ds = s[b][x] * dp[b][x];
-      if constexpr (PART || CAREFUL) {
-        const int row = i0 + at + 32 * b + tile_row(x) + 4 * h;
-        const bool one = sees_one(a, n, row), pass = ((seen[b] >> x) & 1) && !one;
-        if constexpr (CAREFUL) ds = pass ? ds : 0.0f;   // (otherwise 0 times what is not finite: the tile is taken with care)
-        else ds = one ? 0.0f : ds;
-        passed[b] |= (pass ? 1u : 0u) << x;
-      }
-      dp[b][x] = ds;
-    }
+    for (int j = 0; j < 16; ++j) dp[b][j] = CAREFUL ? where_set(s[b][j] * dp[b][j], seen[b], tile_row(j)) : s[b][j] * dp[b][j];
   };
   auto value_products = [&](int b, const bf16x8_t* o) {
 #pragma unroll
@@ -773,7 +801,7 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
       const bf16x8_t x = as_operand(s[b], u);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        if constexpr (CAREFUL) dv[i] = mfma_seen(o[u * NK + i], x, seen[b] >> (8 * u), dv[i]);
+        if constexpr (CAREFUL) dv[i] = mfma_seen(o[u * NK + i], x, register_bits(seen[b], u), dv[i]);
         else dv[i] = mfma(o[u * NK + i], x, dv[i]);
       }
     }
@@ -784,20 +812,20 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
       const bf16x8_t x = as_operand(dp[b], u);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        if constexpr (CAREFUL) dk[i] = mfma_seen(o[u * NK + i], x, passed[b] >> (8 * u), dk[i]);
+        if constexpr (CAREFUL) dk[i] = mfma_seen(o[u * NK + i], x, register_bits(seen[b], u), dk[i]);
         else dk[i] = mfma(o[u * NK + i], x, dk[i]);
       }
     }
   };
-  // Each phase's operands are read during the one before it; the exponentials and dS of a block run beside the products of another phase.
-  constexpr int VE = at_least_one(40 / N), VD = at_least_one(36 / N);
-  row_operands<DP>(o[0], lq, at);
-  sums(0);
-  __builtin_amdgcn_sched_barrier(0);
-  row_operands<DP>(o[1], lg, at);
-  scores(0, o[0]);
-  phase<N, 1, 0>();
   if constexpr (NB == 2) {
+    // (as in the other kernel)
+    constexpr int VE = at_least_one(40 / N), VD = at_least_one(36 / N);
+    row_operands<DP>(o[0], lq, at);
+    sums(0);
+    __builtin_amdgcn_sched_barrier(0);
+    row_operands<DP>(o[1], lg, at);
+    scores(0, o[0]);
+    phase<N, 1, 0>();
     row_operands<DP>(o[0], lq, at + 32);
     sums(1);
     slopes(0, o[1]);
@@ -824,16 +852,23 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
     key_products(1, o[1]);
     __builtin_amdgcn_sched_barrier(0);
   } else {
-    column_operands<DP>(o[0], lg, at);
+    row_operands<DP>(o[0], lq, at);
+    scores(0, o[0]);
+    sums(0);
+    row_operands<DP>(o[1], lg, at);
     slopes(0, o[1]);
     weights(0);
-    phase<N, 2, VE>();
-    column_operands<DP>(o[1], lq, at);
-    value_products(0, o[0]);
     through(0);
-    phase<N, 2, VD>();
+    column_operands<DP>(o[0], lg, at);
+    value_products(0, o[0]);
+    column_operands<DP>(o[1], lq, at);
     key_products(0, o[1]);
-    __builtin_amdgcn_sched_barrier(0);
+    reads_first<8>();
+    steps<N, 1, 0>();
+    steps<N, 2, at_least_one(32 / N)>();
+    __builtin_amdgcn_sched_group_barrier(0x2, 24, 0);
+    steps<2 * N - 4, 2, 0>();
+    steps<4, 0, 0>();
   }
 }
 
@@ -891,15 +926,18 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
       at ^= 1;
       if (more(i)) put(at);
     };
-    auto use = [&](int i, auto part) {
+    auto use = [&](int i, auto masked) {
       unsigned char* here = lds + at * BUF;
       const float* lst = reinterpret_cast<const float*>(here + 2 * stage::BYTES);
+      const int i0 = st.first + i * SA_STAGE;
+      const int low = (a.causal ? tok : 0) - i0, lim = first_blind_row(a, t.n, tok) - 1 - i0;      // the rows that see the lane's token
       constexpr int NB = CAREFUL ? 1 : blocks_in_flight<DP>();
 #pragma unroll 1
       for (int x = 0; x < SA_STAGE; x += 32 * NB)
-        token_blocks<DP, decltype(part)::value, CAREFUL>(a, here, here + stage::BYTES, lst, x, t.n, st.first + i * SA_STAGE, tok, k, v, dk, dv);
+        token_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, lst, x, low, lim, k, v, dk, dv);
     };
-    in_stages(st, next, store, [&](int i) { use(i, std::true_type{}); }, [&](int i) { use(i, std::false_type{}); });
+    if constexpr (CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
+    else in_stages(st, next, store, use);
   }
 }
 
@@ -925,7 +963,7 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(s
   if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dk) || any_nonfinite<NK>(dv)), 0))
     token_tile<DP, DIRECT, true>(a, kv_head, t, tok0, k, v, dk, dv, lds);
   if (tok >= t.n) return;
-  store_column<DP>(dk, a.scale, a.dK + mine * a.dks + kv_head * a.d, a.d);
+  store_column<DP>(dk, see_one(a, t.n) ? 0.0f : a.scale, a.dK + mine * a.dks + kv_head * a.d, a.d);
   store_column<DP>(dv, 1.0f, a.dV + mine * a.dvs + kv_head * a.d, a.d);
 }
 
@@ -938,7 +976,7 @@ int check_self(const pq_self_attn_desc* d) {
   PQ_REQUIRE(d->n_heads > 0 && d->n_kv_heads > 0 && d->n_heads % d->n_kv_heads == 0, PQ_ERR_SHAPE, "n_heads=%d must be a multiple of n_kv_heads=%d",
              d->n_heads, d->n_kv_heads);
   PQ_REQUIRE(d->d_head >= 2 && d->d_head <= 128 && d->d_head % 2 == 0, PQ_ERR_SHAPE, "d_head=%d must be even and in 2..128", d->d_head);
-  PQ_REQUIRE((int64_t)d->n_heads * d->d_head <= 0x7fffffff, PQ_ERR_SHAPE, "n_heads=%d is too many", d->n_heads);
+  PQ_REQUIRE((int64_t)d->n_heads * d->d_head <= (1 << 23), PQ_ERR_SHAPE, "n_heads=%d of %d are more than 2^23 elements", d->n_heads, d->d_head);
   PQ_REQUIRE(d->causal == 0 || d->causal == 1, PQ_ERR_BAD_ARG, "causal=%d must be 0 or 1", d->causal);
   PQ_REQUIRE(d->window >= 0 && (d->causal || d->window == 0), PQ_ERR_BAD_ARG, "window=%d must not be negative, and needs causal", d->window);
   PQ_REQUIRE(std::isfinite(d->scale), PQ_ERR_BAD_ARG, "scale must be finite");
@@ -952,12 +990,10 @@ int check_rows(const pq_self_attn_desc* d, int T) {
   return PQ_OK;
 }
 int check_stride(const char* name, int64_t stride, int heads, int d) {
-  PQ_REQUIRE(stride >= (int64_t)heads * d && stride % 2 == 0, PQ_ERR_SHAPE, "%s: row stride %lld must be even and at least %lld", name,
-             (long long)stride, (long long)heads * d);
+  PQ_REQUIRE(stride >= (int64_t)heads * d && stride % 2 == 0 && stride <= (1 << 23), PQ_ERR_SHAPE,
+             "%s: row stride %lld must be even, at least %lld and at most 2^23", name, (long long)stride, (long long)heads * d);
   return PQ_OK;
 }
-// Rows that direct loads take: at multiples of 16 bytes, 64 of them within 2^31 bytes.
-bool direct_stride(int64_t stride) { return stride % 8 == 0 && stride <= (1 << 23); }
 bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 self_args make_args(const pq_self_attn_desc* d, int T, const int32_t* row_start) {
@@ -1036,7 +1072,7 @@ extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64
   a.out = (uint16_t*)O; a.lse = lse;
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_FWD, s);
-  const bool direct = a.d % 8 == 0 && direct_stride(k_stride) && direct_stride(v_stride);
+  const bool direct = a.d % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
   return direct ? launch_forward_d<true>(a, s) : launch_forward_d<false>(a, s);
 }
 
@@ -1072,6 +1108,6 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   a.stats = (float2*)workspace;
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_BWD, s);
-  const bool direct = a.d % 8 == 0 && direct_stride(q_stride) && direct_stride(k_stride) && direct_stride(v_stride) && direct_stride((int64_t)a.heads * a.d);
+  const bool direct = a.d % 8 == 0 && q_stride % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
   return direct ? launch_backward_d<true>(a, s) : launch_backward_d<false>(a, s);
 }
