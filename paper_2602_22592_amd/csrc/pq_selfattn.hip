@@ -227,6 +227,16 @@ __device__ __forceinline__ bf16x8_t as_operand(const f32x16_t& x, int u) {
   return __builtin_bit_cast(bf16x8_t, w);
 }
 
+// The sum of an operand's eight elements and x.
+__device__ __forceinline__ float sum_of(bf16x8_t a, float x) {
+  const uint4 w = __builtin_bit_cast(uint4, a);
+  const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
+  x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.x), ones, x, false);
+  x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.y), ones, x, false);
+  x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.z), ones, x, false);
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w.w), ones, x, false);
+}
+
 // a x b where b holds zeros for what is not seen, which an infinity or a NaN of a must not reach (0 times infinity is NaN): such elements are left
 // out, and where they are seen the sum becomes infinite (twice the largest bf16 number is beyond fp32).  Three products for one, for tiles that hold such
 // elements: a branch would keep two copies of the sums.
@@ -562,10 +572,12 @@ template <int DP> constexpr int blocks_in_flight() { return 2; }
 template <int DP> constexpr int backward_waves() { return DP > 64 ? 1 : 2; }
 
 // delta is dO . O with O as it was rounded to bf16, which costs dS as much as all else together; what is missing to sum_j p_ij dP_ij is the sum of
-// the dS themselves, known at the end.  So the products with p are kept beside those with dS (they share their other operand), and dQ is put right by them.
+// the dS themselves, known at the end.  So the products with p are kept beside those with dS (they share their other operand), and dQ is put right by
+// them: dQ = sum (dS - p sum dS) k.  With the sum of the dS as they were rounded for the product, which takes the part of their roundings that the
+// mean of the k would carry out as well: the true dS add up to nothing.
 template <int DP, bool MASKED, bool CAREFUL>
 __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q,
-                                             const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, int low, int lim) {
+                                             const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, float& rounded, int low, int lim) {
   constexpr int NK = DP / 32, NB = CAREFUL ? 1 : blocks_in_flight<DP>();
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
@@ -603,6 +615,7 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const bf16x8_t x = as_operand(dp[b], u), p = as_operand(s[b], u);
+      rounded = sum_of(x, rounded);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
         const bf16x8_t k = o[u * NK + i];
@@ -663,7 +676,7 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
 
 template <int DP, bool DIRECT, bool CAREFUL>
 __device__ __forceinline__ void query_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, const bf16x8_t* q, const bf16x8_t* g,
-                                           f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, unsigned char* lds) {
+                                           f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, float& rounded, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES;
   const int row = row0 + (threadIdx.x & 31);
@@ -694,7 +707,7 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
   load(0);
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = pk[i] = f32x16_t{};
-  rest = 0.0f;
+  rest = rounded = 0.0f;
   put(0);
   auto use = [&](int i, auto masked) {
     unsigned char* here = lds + (i & 1) * BUF;
@@ -703,7 +716,7 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
     constexpr int NB = CAREFUL ? 1 : blocks_in_flight<DP>();
 #pragma unroll 1
     for (int at = 0; at < SA_STAGE; at += 32 * NB)
-      query_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, low, lim);
+      query_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, rounded, low, lim);
   };
   if constexpr (CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
   else in_stages(st, next, store, use);
@@ -737,18 +750,19 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
   delta += other_half(delta);
   const float lse = a.lse[mine * a.heads + w.head] * SA_LOG2E;
   f32x16_t dq[NK], pk[NK];
-  float rest;
-  query_tile<DP, DIRECT, false>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, lds);
+  float rest, rounded;
+  query_tile<DP, DIRECT, false>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rounded, lds);
   if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dq) || any_nonfinite<NK>(pk)), 0))
-    query_tile<DP, DIRECT, true>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, lds);
+    query_tile<DP, DIRECT, true>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rounded, lds);
   rest += other_half(rest);
+  rounded += other_half(rounded);
   if (row >= t.n) return;
   if (lane < 32) a.stats[(int64_t)w.head * a.T + mine] = make_float2(lse, delta + rest);
   const bool one = see_one(a, t.n) || (a.causal && row == 0);
 #pragma unroll
   for (int i = 0; i < NK; ++i)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) dq[i][j] = one ? 0.0f : dq[i][j] - rest * pk[i][j];
+    for (int j = 0; j < 16; ++j) dq[i][j] = one ? 0.0f : dq[i][j] - rounded * pk[i][j];
   store_column<DP>(dq, a.scale, a.dQ + mine * a.dqs + w.head * a.d, a.d);
 }
 
