@@ -76,22 +76,23 @@ struct stage_t {
   static constexpr int CPR = DP / 8, N = SA_STAGE * CPR / 256, BYTES = SA_STAGE * DP * 2;
   const uint16_t* base;          // the sequence's first row
   int64_t stride;                // elements, at most 2^23: 64 rows are within 2^31 bytes
-  int d;
+  int d, n;
+  bool is_last;                  // the sequence's last row is the call's
   uint32_t offset[N];            // of the lane's pieces from a stage's first row, in bytes
   i32x4_t hold[DIRECT ? 1 : N];
 
-  __device__ __forceinline__ void begin(const uint16_t* base_, int64_t stride_, int d_) {
-    base = base_; stride = stride_; d = d_;
+  __device__ __forceinline__ void begin(const uint16_t* base_, int64_t stride_, int d_, int n_, bool is_last_) {
+    base = base_; stride = stride_; d = d_; n = n_; is_last = is_last_;
 #pragma unroll
     for (int i = 0; i < N; ++i) offset[i] = (uint32_t)row_of(i) * (uint32_t)stride * 2 + place_in_row(i);
   }
   static __device__ __forceinline__ int place(int i) { return (int)((threadIdx.x >> 6) * N + i) * 64 + (int)(threadIdx.x & 63); }
   static __device__ __forceinline__ int row_of(int i) { return place(i) / CPR; }
   static __device__ __forceinline__ int piece_of(int i) { return piece_at<DP>(row_of(i), place(i) % CPR); }
-  // Where in its row a piece's load begins: through registers no load passes the row's end (d >= 8; shorter rows are read by halves of it).
-  __device__ __forceinline__ uint32_t place_in_row(int i) const { return 2 * (DIRECT || d < 8 ? piece_of(i) * 8 : min(piece_of(i) * 8, d - 8)); }
+  // Pieces behind d are not loaded (DIRECT), or are the first once more and cleared afterwards.
+  __device__ __forceinline__ uint32_t place_in_row(int i) const { return DIRECT || piece_of(i) * 8 < d ? piece_of(i) * 16 : 0; }
 
-  __device__ __forceinline__ void load(int first, int n, unsigned char* lds) {
+  __device__ __forceinline__ void load(int first, unsigned char* lds) {
     const uint16_t* from = base + (int64_t)first * stride;
     const bool whole = first + SA_STAGE <= n;
     if constexpr (DIRECT) {
@@ -107,14 +108,13 @@ struct stage_t {
         }
       }
     } else {
+      // A row's last piece takes up to six elements of what follows (cleared by `store`): the next head's, or the next row's.  Not from the call's last
+      // row, behind which nothing need be, nor where rows are shorter than a piece.
+      const char* bytes = reinterpret_cast<const char*>(from);
       uint32_t x[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = offset[i];
-      if (!whole)
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = (uint32_t)min(row_of(i), n - 1 - first) * (uint32_t)stride * 2 + place_in_row(i);
-      const char* bytes = reinterpret_cast<const char*>(from);
-      if (d >= 8) {
+      for (int i = 0; i < N; ++i) x[i] = whole ? offset[i] : (uint32_t)min(row_of(i), n - 1 - first) * (uint32_t)stride * 2 + place_in_row(i);
+      if (d >= 8 && !(is_last && first + SA_STAGE >= n)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) hold[i] = *reinterpret_cast<const i32x4_u_t*>(bytes + x[i]);
       } else {
@@ -128,14 +128,8 @@ struct stage_t {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         i32x4_t x = hold[i];
-        if (d >= 8) {                                  // the last piece came d % 8 elements too early; nothing is behind it
-          const int at = piece_of(i) * 8;
-          i32x4_t y = x;
-          for (int k = d & 7; k < 8 && k > 0; k += 2) y = i32x4_t{y[1], y[2], y[3], 0};
-          const bool last = at < d && at + 8 > d, none = at >= d;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = none ? 0 : last ? y[j] : x[j];
-        }
+        for (int j = 0; j < 4; ++j) x[j] = piece_of(i) * 8 + 2 * j < d ? x[j] : 0;
         *reinterpret_cast<i32x4_t*>(lds + place(i) * 16) = x;
       }
     }
@@ -275,13 +269,40 @@ __device__ __forceinline__ uint32_t register_bits(uint32_t rows, int u) {
 // The value of the other half's lane joined to a lane's own (both halves hold the same columns).
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
 
-// Which sequence and which of its tiles of SA_ROWS rows virtual tile vt is: sequence b owns those from floor(first row / SA_ROWS) + b on, at least as
-// many as it has.
+// Which sequence and which of its tiles of SA_ROWS rows workgroup tile vt is.  Up to 8 sequences: the longest first, of each the tiles with most work
+// first (`down`: its last ones), so that long tiles do not start when the others end.  Up to 63: from one load of all of row_start.  Any number: virtual
+// tiles, of which sequence b owns those from floor(first row / SA_ROWS) + b on, at least as many as it has.
 struct self_tile { int r0, n, at; };     // rows r0 .. r0 + n - 1 of the call, the tile's first row among them (n == 0: none)
-__device__ __forceinline__ self_tile find_self_tile(const self_args& a, int vt) {
+__device__ __forceinline__ self_tile find_self_tile(const self_args& a, int vt, bool down) {
   auto first = [&](int i) { return min(max(a.row_start[i], 0), a.T); };
-  const int b = kv_find_seq(a.n_seqs, vt, [&](int i) { return first(i) / SA_ROWS + i; });
   self_tile t = {0, 0, 0};
+  if (a.n_seqs <= 63) {
+    const int lane = threadIdx.x & 63, at = first(min(lane, a.n_seqs));
+    const int next = __shfl_down(at, 1, 64);               // (of all lanes: one that sits out hands nothing over)
+    const int mine = lane < a.n_seqs ? max(next - at, 0) : 0;
+    int before = at / SA_ROWS + lane;
+    if (a.n_seqs <= 8) {
+      before = 0;
+      for (int i = 0; i < a.n_seqs; ++i) {
+        const int n = __builtin_amdgcn_readlane(mine, i);
+        before += n > mine || (n == mine && i < lane) ? (n + SA_ROWS - 1) / SA_ROWS : 0;
+      }
+    } else if (down) {
+      vt = a.tiles - 1 - vt;
+    }
+    const int tiles = (mine + SA_ROWS - 1) / SA_ROWS;
+    const uint64_t hit = __ballot(vt >= before && vt < before + tiles);
+    if (hit == 0) return t;
+    const int b = __builtin_ctzll(hit);
+    int tile = vt - __builtin_amdgcn_readlane(before, b);
+    if (down && a.n_seqs <= 8) tile = __builtin_amdgcn_readlane(tiles, b) - 1 - tile;
+    t.r0 = __builtin_amdgcn_readlane(at, b);
+    t.n = __builtin_amdgcn_readlane(mine, b);
+    t.at = tile * SA_ROWS;
+    return t;
+  }
+  if (down) vt = a.tiles - 1 - vt;
+  const int b = kv_find_seq(a.n_seqs, vt, [&](int i) { return first(i) / SA_ROWS + i; });
   if (b < 0) return t;
   t.r0 = first(b);
   const int n = max(first(b + 1), t.r0) - t.r0;
@@ -374,9 +395,9 @@ template <int DP> __device__ __forceinline__ void store_column(const f32x16_t* a
 
 // Head and tile of a workgroup: the heads first, those of a key-value head a multiple of kv_heads apart (its tokens then stay in one L2).
 struct self_place { int head, kv_head, vt; };
-__device__ __forceinline__ self_place place_of(const self_args& a, bool last_first) {
+__device__ __forceinline__ self_place place_of(const self_args& a) {
   const int t = blockIdx.x / a.heads, x = blockIdx.x - t * a.heads, kv = x % a.kv_heads;
-  return {kv * a.group + x / a.kv_heads, kv, last_first ? a.tiles - 1 - t : t};
+  return {kv * a.group + x / a.kv_heads, kv, t};
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -494,12 +515,12 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
   const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
   const stages_of g = token_stages(a, t, row0);
   stage k, v;
-  k.begin(K, a.ks, a.d);
-  v.begin(V, a.vs, a.d);
+  k.begin(K, a.ks, a.d, t.n, t.r0 + t.n == a.T);
+  v.begin(V, a.vs, a.d, t.n, t.r0 + t.n == a.T);
   auto load = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
-    k.load(g.first + i * SA_STAGE, t.n, to);
-    v.load(g.first + i * SA_STAGE, t.n, to + stage::BYTES);
+    k.load(g.first + i * SA_STAGE, to);
+    v.load(g.first + i * SA_STAGE, to + stage::BYTES);
   };
   auto put = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
@@ -539,8 +560,8 @@ __global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
   constexpr int NK = DP / 32;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   typedef stage_t<DP, DIRECT> stage;
-  const self_place w = place_of(a, true);
-  const self_tile t = find_self_tile(a, w.vt);
+  const self_place w = place_of(a);
+  const self_tile t = find_self_tile(a, w.vt, a.causal);
   if (t.n == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row0 = t.at + 32 * wave, row = row0 + (lane & 31);
@@ -684,12 +705,12 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
   const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
   const stages_of st = token_stages(a, t, row0);
   stage k, v;
-  k.begin(K, a.ks, a.d);
-  v.begin(V, a.vs, a.d);
+  k.begin(K, a.ks, a.d, t.n, t.r0 + t.n == a.T);
+  v.begin(V, a.vs, a.d, t.n, t.r0 + t.n == a.T);
   auto load = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
-    k.load(st.first + i * SA_STAGE, t.n, to);
-    v.load(st.first + i * SA_STAGE, t.n, to + stage::BYTES);
+    k.load(st.first + i * SA_STAGE, to);
+    v.load(st.first + i * SA_STAGE, to + stage::BYTES);
   };
   auto put = [&](int i) {
     unsigned char* to = lds + (i & 1) * BUF;
@@ -727,8 +748,8 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
   constexpr int NK = DP / 32;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   typedef stage_t<DP, DIRECT> stage;
-  const self_place w = place_of(a, true);
-  const self_tile t = find_self_tile(a, w.vt);
+  const self_place w = place_of(a);
+  const self_tile t = find_self_tile(a, w.vt, a.causal);
   if (t.n == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row0 = t.at + 32 * wave, row = row0 + (lane & 31);
@@ -897,8 +918,8 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
   const uint16_t* G = a.dO + ((int64_t)t.r0 * a.heads + (int64_t)kv_head * a.group) * a.d;
   const int64_t gs = (int64_t)a.heads * a.d;
   stage q, g;
-  q.begin(Q, a.qs, a.d);
-  g.begin(G, gs, a.d);
+  q.begin(Q, a.qs, a.d, t.n, t.r0 + t.n == a.T);
+  g.begin(G, gs, a.d, t.n, t.r0 + t.n == a.T);
   float2 sums = make_float2(0.0f, 0.0f);
   int at = 0;                                          // the buffer of the present stage
   auto load = [&](int head, int i, int to_at) {
@@ -906,8 +927,8 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
     const int i0 = st.first + i * SA_STAGE;
     q.base = Q + head * a.d;
     g.base = G + head * a.d;
-    q.load(i0, t.n, to);
-    g.load(i0, t.n, to + stage::BYTES);
+    q.load(i0, to);
+    g.load(i0, to + stage::BYTES);
     if (threadIdx.x < SA_STAGE)
       sums = a.stats[(int64_t)(kv_head * a.group + head) * a.T + t.r0 + min(i0 + (int)threadIdx.x, t.n - 1)];
   };
@@ -961,7 +982,7 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(s
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   typedef stage_t<DP, DIRECT> stage;
   const int vt = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - vt * a.kv_heads;
-  const self_tile t = find_self_tile(a, vt);
+  const self_tile t = find_self_tile(a, vt, false);
   if (t.n == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int tok0 = t.at + 32 * wave, tok = tok0 + (lane & 31);

@@ -112,12 +112,17 @@ class Packed:
             slopes = np.abs(do) @ np.abs(v).T
             diff = (self.d + 2) * F * slopes + ((self.d + 2 + len(q)) * F + 2 * e) * (p * slopes).sum(1, keepdims=True)
             diff = np.where(seen & (seen.sum(1) > 1)[:, None], diff, 0)
-            # dQ and the sums behind it: dS is formed with dO . O first (off by `rest`, from O's rounding), and rounded then
-            rest = np.abs((do * o).sum(1, keepdims=True) - (p * (do @ v.T)).sum(1, keepdims=True))
+            # dQ = sum_j D_j k_j - (sum_j D_j) m, with D the rounded dS that are formed with dO . O (off by p `rest`, from O's rounding) and m = sum p~ k,
+            # p~ the rounded p.  D_j = x_j + r_j, |r_j| <= U |x_j|, |x_j| <= |dS_j| + p_j rest.  The x_j alone give dQ exactly (sum x_j (k_j - m) with
+            # m exact), so the error is sum r_j (k_j - m), at most U sum |x_j| (|k_j| + |m|), and (sum D_j) (m~ - m), at most (rest + U sum |x_j|) U sum p |k|.
+            many = seen.sum(1, keepdims=True) > 1
+            rest = np.abs((do * o).sum(1, keepdims=True) - (p * (do @ v.T)).sum(1, keepdims=True)) * many
             dse = (np.abs(ds) * (U + e) + p * diff * (1 + e)) * (1 + U)
-            dsq = dse + p * rest * (2 * U + 2 * e) * (seen.sum(1, keepdims=True) > 1)
+            dsq = dse + p * rest * (U + 2 * e)
+            x = (np.abs(ds) + p * rest) * many
+            mean = U * x.sum(1, keepdims=True) * np.abs(p @ k) + (rest + U * x.sum(1, keepdims=True)) * U * (p @ np.abs(k))
             n = len(q) * self.H // self.Hk + 4
-            add("dQ", here, h, dq, abs(self.scale) * (dsq @ np.abs(k) + n * F * np.abs(ds) @ np.abs(k)))
+            add("dQ", here, h, dq, abs(self.scale) * (dsq @ np.abs(k) + mean + n * F * np.abs(ds) @ np.abs(k)))
             add("dK", here, hk, dk, abs(self.scale) * (dse.T @ np.abs(q) + n * F * np.abs(ds).T @ np.abs(q)))
             add("dV", here, hk, dv, (p * (U + e + n * F)).T @ np.abs(do))
         mine = ~self.others()
