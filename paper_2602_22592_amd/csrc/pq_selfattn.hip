@@ -27,8 +27,9 @@ struct self_args {
   int64_t dqs, dks, dvs;
   float* lse;                    // [T][heads]
   float2* stats;                 // [heads][T]: lse times log2 e, delta
+  float* parts;                  // [pieces][T][kv_heads][2][d]: parts of dK and dV where a tile's work is cut
   const int32_t* row_start;
-  int T, n_seqs, heads, kv_heads, group, d, causal, window, tiles;
+  int T, n_seqs, heads, kv_heads, group, d, causal, window, tiles, pieces;
   float c;                       // |scale| log2 e; the sign is in the operand that stays in registers
   float scale;
 };
@@ -315,7 +316,7 @@ __device__ __forceinline__ int first_token(const self_args& a, int row) { return
 
 // The stages that a tile needs, and of them those of which a wavefront's 32 rows (or tokens) see something, from .. to - 1: these are a loop of their own,
 // since a branch around accumulators costs a second copy of them all.  Those from `all` to `part` - 1 are seen by all of its rows.
-struct stages_of { int first, n, from, all, part, to; };
+struct stages_of { int first, n, from, all, part, to, begin; };     // begin: the first of those that are taken at all
 // Stages of tokens that rows row0 .. row0 + 31 of the tile see.
 __device__ __forceinline__ stages_of token_stages(const self_args& a, const self_tile& t, int row0) {
   const int end = a.causal ? min(t.at + SA_ROWS, t.n) : t.n, last = min(row0 + 31, t.n - 1);
@@ -326,6 +327,7 @@ __device__ __forceinline__ stages_of token_stages(const self_args& a, const self
   g.from = min((first_token(a, row0) - g.first) / SA_STAGE, g.to);
   g.all = (first_token(a, last) - g.first + SA_STAGE - 1) / SA_STAGE;
   g.part = ((a.causal ? row0 + 1 : t.n) - g.first) / SA_STAGE;
+  g.begin = 0;
   return g;
 }
 // Stages of rows that see tokens tok0 .. tok0 + 31 of the tile.
@@ -340,6 +342,7 @@ __device__ __forceinline__ stages_of row_stages(const self_args& a, const self_t
   g.from = min(a.causal ? (tok0 - g.first) / SA_STAGE : 0, g.to);
   g.all = a.causal ? (tok0 + 31 - g.first + SA_STAGE - 1) / SA_STAGE : 0;
   g.part = (first_blind_row(a, t.n, tok0) - g.first) / SA_STAGE;
+  g.begin = 0;
   return g;
 }
 // `next` waits for a stage and has the loads of the one behind it started, `store` puts away what came through registers; `use` is told whether the
@@ -347,9 +350,9 @@ __device__ __forceinline__ stages_of row_stages(const self_args& a, const self_t
 // always masked 2320 and 29.1 us, two masked loops around an unmasked one 2150 and 33.)
 template <typename N, typename S, typename U>
 __device__ __forceinline__ void in_stages(const stages_of& g, N next, S store, U use) {
-  int i = 0;
+  int i = g.begin;
 #pragma unroll 1
-  for (; i < g.from; ++i) { next(i); store(i); }
+  for (; i < min(g.from, g.n); ++i) { next(i); store(i); }
   int masked = min(g.all, g.to);
   const int part = min(g.part, g.to);
 #pragma unroll 1
@@ -366,9 +369,9 @@ __device__ __forceinline__ void in_stages(const stages_of& g, N next, S store, U
 // The same where `use` asks by itself.
 template <typename N, typename S, typename U>
 __device__ __forceinline__ void in_stages_alike(const stages_of& g, N next, S store, U use) {
-  int i = 0;
+  int i = g.begin;
 #pragma unroll 1
-  for (; i < g.from; ++i) { next(i); store(i); }
+  for (; i < min(g.from, g.n); ++i) { next(i); store(i); }
 #pragma unroll 1
   for (; i < g.to; ++i) { next(i); use(i); store(i); }
 #pragma unroll 1
@@ -393,6 +396,17 @@ template <int DP> __device__ __forceinline__ void store_column(const f32x16_t* a
     }
 }
 
+template <int DP> __device__ __forceinline__ void store_part(const f32x16_t* acc, float f, float* row, int d) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; j += 2) {
+      const int at = 32 * i + tile_row(j) + 4 * h;
+      if (at < d) *reinterpret_cast<f32x2_t*>(row + at) = f32x2_t{acc[i][j] * f, acc[i][j + 1] * f};
+    }
+}
+
 // Head and tile of a workgroup: the heads first, those of a key-value head a multiple of kv_heads apart (its tokens then stay in one L2).
 struct self_place { int head, kv_head, vt; };
 __device__ __forceinline__ self_place place_of(const self_args& a) {
@@ -406,53 +420,86 @@ __device__ __forceinline__ self_place place_of(const self_args& a) {
 // A stage of tokens.  Any reference m gives the same quotient as long as nothing overflows and the row's largest p is not tiny: the maximum of what a row
 // sees in its first stage serves for all others (it has p = 1, so nothing that counts is lost below; what overflows above ends as infinity or NaN,
 // and the tile is taken once more with care).  So the stages have no maximum to keep and no accumulators to rescale.
-template <int DP>
+// MASKED: stages that some row sees in part, or as its first.
+template <int DP, bool MASKED>
 __device__ __forceinline__ void forward_stage(const self_args& a, const unsigned char* lk, const unsigned char* lv, const bf16x8_t* q, f32x16_t* o,
-                                              float& m, float& l, bool part, int low, int lim) {
-  constexpr int NK = DP / 32;
+                                              float& m, float& l, int low, int lim) {
+  constexpr int NK = DP / 32, N = DP / 16;
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  float sum[2] = {0.0f, 0.0f};
+  auto scores = [&](int t, const bf16x8_t* x) {
     s[t] = f32x16_t{};
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k) s[t] = mfma(row_operand<DP>(lk, 32 * t, k), q[k], s[t]);
-  }
-  reads_first<4>();
-  steps<DP / 8, 1, 0>();
-  if (part) {
-    const int from = low - 4 * h, to = lim - 4 * h;
+    for (int k = 0; k < N; ++k) s[t] = mfma(x[k], q[k], s[t]);
+  };
+  float ref, c = a.c;
+  auto weights = [&](int t) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) s[t][j] = 32 * t + tile_row(j) >= from && 32 * t + tile_row(j) <= to ? s[t][j] : -INFINITY;
-  }
-  if (__ballot(m == -INFINITY)) {
-    float top = s[0][0];
-#pragma unroll
-    for (int j = 1; j < 32; ++j) top = fmaxf(top, s[j >> 4][j & 15]);
-    top = fmaxf(top, other_half(top));
-    if (m == -INFINITY && top > -INFINITY) m = top * a.c;
-  }
-  const float ref = m == -INFINITY ? 0.0f : m, c = a.c == 0.0f ? 1.17549435e-38f : a.c;    // (hidden ones times a scale of 0 would be NaN)
-  float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
+    for (int j = 0; j < 16; ++j) {
+      s[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j], c, -ref));
+      sum[j & 1] += s[t][j];
+    }
+  };
+  auto products = [&](int t, const bf16x8_t* x) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int j = 8 * u; j < 8 * u + 8; ++j) {
-        s[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][j], c, -ref));
-        sum[j & 1] += s[t][j];
-      }
       const bf16x8_t p = as_operand(s[t], u);
 #pragma unroll
-      for (int i = 0; i < NK; ++i) o[i] = mfma(column_operand<DP>(lv, 32 * t + 16 * u, i), p, o[i]);
+      for (int i = 0; i < NK; ++i) o[i] = mfma(x[u * NK + i], p, o[i]);
     }
-  __builtin_amdgcn_sched_group_barrier(0x2, 28, 0);
-  reads_first<2 * NK>();
-  steps<3 * NK, 2, 28 / NK>();
-  steps<NK, 0, 0>();
+  };
+  bf16x8_t x[2][N];
+  if constexpr (MASKED) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      row_operands<DP>(x[0], lk, 32 * t);
+      scores(t, x[0]);
+    }
+    reads_first<4>();
+    steps<2 * N, 1, 0>();
+    const uint32_t seen[2] = {bits_between(low, lim) >> (4 * h), bits_between(low - 32, lim - 32) >> (4 * h)};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[j >> 4][j & 15] = (seen[j >> 4] >> tile_row(j & 15)) & 1 ? s[j >> 4][j & 15] : -INFINITY;
+    if (__ballot(m == -INFINITY)) {
+      float top = s[0][0];
+#pragma unroll
+      for (int j = 1; j < 32; ++j) top = fmaxf(top, s[j >> 4][j & 15]);
+      top = fmaxf(top, other_half(top));
+      if (m == -INFINITY && top > -INFINITY) m = top * a.c;
+    }
+    ref = m == -INFINITY ? 0.0f : m;
+    if (c == 0.0f) c = 1.17549435e-38f;               // (hidden ones times a scale of 0 would be NaN)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      weights(t);
+      column_operands<DP>(x[0], lv, 32 * t);
+      products(t, x[0]);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x2, 28, 0);
+    reads_first<2 * NK>();
+    steps<3 * NK, 2, 28 / NK>();
+    steps<NK, 0, 0>();
+  } else {
+    // each phase's operands are read during the one before it, exponentials run beside products
+    constexpr int VE = at_least_one(56 / N);
+    ref = m;
+    row_operands<DP>(x[0], lk, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    row_operands<DP>(x[1], lk, 32);
+    scores(0, x[0]);
+    phase<N, 1, 0>();
+    column_operands<DP>(x[0], lv, 0);
+    scores(1, x[1]);
+    weights(0);
+    phase<N, 2, VE>();
+    column_operands<DP>(x[1], lv, 32);
+    products(0, x[0]);
+    weights(1);
+    phase<N, 2, VE>();
+    products(1, x[1]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
   l += sum[0] + sum[1];
 }
 
@@ -541,7 +588,7 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
   m = -INFINITY;
   l = 0.0f;
   put(0);
-  auto use = [&](int i, bool part) {
+  auto use = [&](int i, auto masked) {
     unsigned char* here = lds + (i & 1) * BUF;
     const int j0 = g.first + i * SA_STAGE;
     const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
@@ -549,10 +596,17 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
 #pragma unroll 1
       for (int at = 0; at < SA_STAGE; at += 32) forward_block<DP>(a, here, here + stage::BYTES, at, q, o, m, l, low, lim);
     } else {
-      forward_stage<DP>(a, here, here + stage::BYTES, q, o, m, l, part, low, lim);
+      forward_stage<DP, decltype(masked)::value>(a, here, here + stage::BYTES, q, o, m, l, low, lim);
     }
   };
-  in_stages_alike(g, next, store, [&](int i) { use(i, i < g.all || i >= g.part); });
+  if constexpr (CAREFUL) {
+    in_stages_alike(g, next, store, [&](int i) { use(i, std::true_type{}); });
+  } else {
+    // (the stage of the last row's first token is masked as well: there its reference is found)
+    stages_of f = g;
+    f.all = (first_token(a, min(row0 + 31, t.n - 1)) - g.first) / SA_STAGE + 1;
+    in_stages(f, next, store, use);
+  }
 }
 
 template <int DP, bool DIRECT>
@@ -908,12 +962,14 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
 }
 
 template <int DP, bool DIRECT, bool CAREFUL>
-__device__ __forceinline__ void token_tile(const self_args& a, int kv_head, const self_tile& t, int tok0, const bf16x8_t* k, const bf16x8_t* v,
+__device__ __forceinline__ void token_tile(const self_args& a, int kv_head, const self_tile& t, int tok0, int piece, const bf16x8_t* k, const bf16x8_t* v,
                                            f32x16_t* dk, f32x16_t* dv, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES + SA_STAGE * 8;
   const int tok = tok0 + (threadIdx.x & 31);
-  const stages_of st = row_stages(a, t, tok0);
+  const stages_of all = row_stages(a, t, tok0);
+  // The stages of the heads that share the tile one behind the other, and of these the piece's.
+  const int steps = all.n * a.group, begin = (int)((int64_t)steps * piece / a.pieces), end = (int)((int64_t)steps * (piece + 1) / a.pieces);
   const uint16_t* Q = a.Q + (int64_t)t.r0 * a.qs + (int64_t)kv_head * a.group * a.d;
   const uint16_t* G = a.dO + ((int64_t)t.r0 * a.heads + (int64_t)kv_head * a.group) * a.d;
   const int64_t gs = (int64_t)a.heads * a.d;
@@ -924,7 +980,7 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
   int at = 0;                                          // the buffer of the present stage
   auto load = [&](int head, int i, int to_at) {
     unsigned char* to = lds + to_at * BUF;
-    const int i0 = st.first + i * SA_STAGE;
+    const int i0 = all.first + i * SA_STAGE;
     q.base = Q + head * a.d;
     g.base = G + head * a.d;
     q.load(i0, to);
@@ -942,13 +998,19 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
       s[SA_STAGE + threadIdx.x] = -sums.y;
     }
   };
-  load(0, 0, 0);
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dk[i] = dv[i] = f32x16_t{};
+  if (begin == end) return;
+  const int head0 = begin / all.n, head1 = (end - 1) / all.n;
+  load(head0, begin - head0 * all.n, 0);
   put(0);
 #pragma unroll 1
-  for (int head = 0; head < a.group; ++head) {
-    auto more = [&](int i) { return i + 1 < st.n || head + 1 < a.group; };
+  for (int head = head0; head <= head1; ++head) {
+    stages_of st = all;
+    st.begin = max(begin - head * all.n, 0);
+    st.n = min(end - head * all.n, all.n);
+    st.to = min(all.to, st.n);
+    auto more = [&](int i) { return i + 1 < st.n || head < head1; };
     auto next = [&](int i) {
       wait_loads();
       __syncthreads();
@@ -981,7 +1043,7 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(s
   constexpr int NK = DP / 32;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   typedef stage_t<DP, DIRECT> stage;
-  const int vt = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - vt * a.kv_heads;
+  const int per_tile = a.kv_heads * a.pieces, vt = blockIdx.x / per_tile, x = blockIdx.x - vt * per_tile, kv_head = x % a.kv_heads, piece = x / a.kv_heads;
   const self_tile t = find_self_tile(a, vt, false);
   if (t.n == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -994,12 +1056,37 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(s
   load_columns<DP>(k, a.K + mine * a.ks + kv_head * a.d, a.d, a.scale < 0.0f);
   load_columns<DP>(v, a.V + mine * a.vs + kv_head * a.d, a.d, false);
   f32x16_t dk[NK], dv[NK];
-  token_tile<DP, DIRECT, false>(a, kv_head, t, tok0, k, v, dk, dv, lds);
+  token_tile<DP, DIRECT, false>(a, kv_head, t, tok0, piece, k, v, dk, dv, lds);
   if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dk) || any_nonfinite<NK>(dv)), 0))
-    token_tile<DP, DIRECT, true>(a, kv_head, t, tok0, k, v, dk, dv, lds);
+    token_tile<DP, DIRECT, true>(a, kv_head, t, tok0, piece, k, v, dk, dv, lds);
   if (tok >= t.n) return;
-  store_column<DP>(dk, see_one(a, t.n) ? 0.0f : a.scale, a.dK + mine * a.dks + kv_head * a.d, a.d);
-  store_column<DP>(dv, 1.0f, a.dV + mine * a.dvs + kv_head * a.d, a.d);
+  const float f = see_one(a, t.n) ? 0.0f : a.scale;
+  if (a.pieces == 1) {
+    store_column<DP>(dk, f, a.dK + mine * a.dks + kv_head * a.d, a.d);
+    store_column<DP>(dv, 1.0f, a.dV + mine * a.dvs + kv_head * a.d, a.d);
+  } else {
+    float* to = a.parts + (((int64_t)piece * a.T + mine) * a.kv_heads + kv_head) * 2 * a.d;
+    store_part<DP>(dk, f, to, a.d);
+    store_part<DP>(dv, 1.0f, to + a.d, a.d);
+  }
+}
+
+// The pieces' parts of dK and dV added in their order, two neighbouring elements a lane.  Rows of no sequence are left alone.
+__global__ __launch_bounds__(256) void self_join_kernel(self_args a) {
+  const int half = a.d / 2, per_row = a.kv_heads * 2 * half;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, row = x / per_row;
+  if (row >= min(max(a.row_start[a.n_seqs], 0), a.T) || row < max(a.row_start[0], 0)) return;
+  const int y = (int)(x - row * per_row), kv = y / (2 * half), z = y - kv * 2 * half, which = z / half, e = 2 * (z - which * half);
+  const int64_t stride = (int64_t)a.T * a.kv_heads * 2 * a.d;
+  const float* from = a.parts + (row * a.kv_heads + kv) * 2 * a.d + which * a.d + e;
+  float2 sum = *reinterpret_cast<const float2*>(from);
+  for (int i = 1; i < a.pieces; ++i) {
+    const float2 p = *reinterpret_cast<const float2*>(from + i * stride);
+    sum.x += p.x;
+    sum.y += p.y;
+  }
+  uint16_t* to = which ? a.dV + row * a.dvs : a.dK + row * a.dks;
+  *reinterpret_cast<uint32_t*>(to + (int64_t)kv * a.d + e) = round_two(sum.x, sum.y);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1030,6 +1117,16 @@ int check_stride(const char* name, int64_t stride, int heads, int d) {
   return PQ_OK;
 }
 bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Pieces of a token tile's work, where there are fewer tiles than CUs: as many as give 512 workgroups, of 8 stages each at least.
+int token_pieces(const pq_self_attn_desc* d, int T) {
+  const int64_t tiles = ((int64_t)T / SA_ROWS + d->n_seqs) * d->n_kv_heads, steps = (int64_t)d->n_heads / d->n_kv_heads * (T / SA_STAGE + 1);
+  if (tiles == 0 || tiles > 256) return 1;
+  int64_t pieces = 512 / tiles;
+  if (pieces > steps / 8) pieces = steps / 8;
+  return pieces < 1 ? 1 : pieces > 32 ? 32 : (int)pieces;
+}
+size_t stats_bytes(const pq_self_attn_desc* d, int T) { return pq_align_up((size_t)T * d->n_heads * sizeof(float2), 256); }
 
 self_args make_args(const pq_self_attn_desc* d, int T, const int32_t* row_start) {
   self_args a = {};
@@ -1068,8 +1165,12 @@ template <int DP, bool DIRECT> int launch_backward(const self_args& a, hipStream
   if (int e = allow_lds((const void*)self_token_kernel<DP, DIRECT>, lds + SA_STAGE * 16, asked[1])) return e;
   self_query_kernel<DP, DIRECT><<<(unsigned)(a.tiles * a.heads), 256, lds, s>>>(a);
   PQ_CHECK_LAUNCH("self_query_kernel");
-  self_token_kernel<DP, DIRECT><<<(unsigned)(a.tiles * a.kv_heads), 256, lds + SA_STAGE * 16, s>>>(a);
+  self_token_kernel<DP, DIRECT><<<(unsigned)(a.tiles * a.kv_heads * a.pieces), 256, lds + SA_STAGE * 16, s>>>(a);
   PQ_CHECK_LAUNCH("self_token_kernel");
+  if (a.pieces > 1) {
+    self_join_kernel<<<(unsigned)(((int64_t)a.T * a.kv_heads * a.d + 255) / 256), 256, 0, s>>>(a);
+    PQ_CHECK_LAUNCH("self_join_kernel");
+  }
   return PQ_OK;
 }
 template <bool DIRECT> int launch_forward_d(const self_args& a, hipStream_t s) {
@@ -1113,7 +1214,8 @@ extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64
 
 extern "C" size_t pq_self_attn_bwd_workspace_bytes(const pq_self_attn_desc* d, int32_t T) {
   if (check_self(d) || check_rows(d, T)) return 0;
-  return pq_align_up((size_t)T * d->n_heads * sizeof(float2), 256) + 256;
+  const int pieces = token_pieces(d, T);
+  return stats_bytes(d, T) + (pieces > 1 ? (size_t)pieces * T * d->n_kv_heads * 2 * d->d_head * sizeof(float) : 0) + 256;
 }
 
 extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
@@ -1141,6 +1243,8 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   a.dqs = dq_stride; a.dks = dk_stride; a.dvs = dv_stride;
   a.lse = const_cast<float*>(lse);
   a.stats = (float2*)workspace;
+  a.parts = (float*)((char*)workspace + stats_bytes(d, T));
+  a.pieces = token_pieces(d, T);
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_BWD, s);
   const bool direct = a.d % 8 == 0 && q_stride % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;

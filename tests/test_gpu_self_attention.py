@@ -38,6 +38,10 @@ CASES = {
     "sharp": dict(rows=[300], H=2, Hk=1, d=128, size=3.0),
     "group16": dict(rows=[100], H=16, Hk=1, d=64),
     "many": dict(rows=[1 + i % 5 for i in range(100)], H=2, Hk=2, d=64),
+    # (few tiles of tokens and many stages each: their work is cut and joined)
+    "pieces": dict(rows=[300, 5, 400], H=16, Hk=1, d=90, window=100, before=2, behind=3),
+    "pieces_whole": dict(rows=[330, 70], H=8, Hk=1, d=32, causal=False),
+    "pieces_128": dict(rows=[1, 700], H=8, Hk=2, d=128, scale=-0.05),
     "long": dict(rows=[1500], H=2, Hk=1, d=128, seed=3),
 }
 
