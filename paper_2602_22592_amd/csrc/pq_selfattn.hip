@@ -174,16 +174,23 @@ template <int DP> __device__ __forceinline__ void column_operands(bf16x8_t* x, c
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) x[u * (DP / 32) + i] = column_operand<DP>(lds, row0 + 16 * u, i);
 }
-// The operand that stays in registers: columns are rows `row` (per lane) of a tensor.
-template <int DP> __device__ __forceinline__ void load_columns(bf16x8_t* x, const uint16_t* row, int d, bool negative) {
+// The operand that stays in registers: columns are rows `row` (per lane) of a tensor.  DIRECT rows of DP elements are read without a condition, so
+// that all loads are under way at once.
+template <int DP, bool DIRECT> __device__ __forceinline__ void load_columns(bf16x8_t* x, const uint16_t* row, int d) {
   const int h = (threadIdx.x & 63) >> 5;
+  if (DIRECT && d == DP) {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) x[s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const i32x4_t*>(row + 16 * s + 8 * h));
+  } else {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) x[s] = __builtin_bit_cast(bf16x8_t, load_piece(row, d, 16 * s + 8 * h));
+  }
+}
+template <int DP> __device__ __forceinline__ void negate(bf16x8_t* x) {
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) {
-    i32x4_t w = load_piece(row, d, 16 * s + 8 * h);
-    if (negative)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] ^= (int)0x80008000u;
-    x[s] = __builtin_bit_cast(bf16x8_t, w);
+    const uint4 w = __builtin_bit_cast(uint4, x[s]);
+    x[s] = __builtin_bit_cast(bf16x8_t, make_uint4(w.x ^ 0x80008000u, w.y ^ 0x80008000u, w.z ^ 0x80008000u, w.w ^ 0x80008000u));
   }
 }
 
@@ -387,15 +394,24 @@ __device__ __forceinline__ void store_four(uint16_t* row, int d, int at, const f
 // Accumulators [DP / 32] of a column each lane (elements 32 i + 8 q + 4 h + j) times f into a row.
 template <int DP> __device__ __forceinline__ void store_column(const f32x16_t* acc, float f, uint16_t* row, int d) {
   const int h = (threadIdx.x & 63) >> 5;
+  uint16_t* mine = row + 4 * h;
+  if (d == DP) {
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i)
+    for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float x[4] = {acc[i][4 * q] * f, acc[i][4 * q + 1] * f, acc[i][4 * q + 2] * f, acc[i][4 * q + 3] * f};
-      store_four(row, d, 32 * i + 8 * q + 4 * h, x);
-    }
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<u32x2_u_t*>(mine + 32 * i + 8 * q) = u32x2_u_t{round_two(acc[i][4 * q] * f, acc[i][4 * q + 1] * f),
+                                                                        round_two(acc[i][4 * q + 2] * f, acc[i][4 * q + 3] * f)};
+  } else {
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float x[4] = {acc[i][4 * q] * f, acc[i][4 * q + 1] * f, acc[i][4 * q + 2] * f, acc[i][4 * q + 3] * f};
+        store_four(row, d, 32 * i + 8 * q + 4 * h, x);
+      }
+  }
 }
-
 template <int DP> __device__ __forceinline__ void store_part(const f32x16_t* acc, float f, float* row, int d) {
   const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
@@ -542,18 +558,18 @@ __device__ __forceinline__ void forward_block(const self_args& a, const unsigned
   }
 }
 
-// Whether one of the lane's sums is infinite or NaN.
+// Whether one of the lane's sums is infinite or NaN (in eight chains: one would wait for each of its instructions).
 template <int NK> __device__ __forceinline__ bool any_nonfinite(const f32x16_t* acc) {
-  float z = 0.0f;
+  float z[8] = {};
 #pragma unroll
   for (int i = 0; i < NK; ++i)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) z = __builtin_fmaf(acc[i][j], 0.0f, z);
-  return z != 0.0f;              // (NaN: not equal)
+    for (int j = 0; j < 16; ++j) z[j & 7] = __builtin_fmaf(acc[i][j], 0.0f, z[j & 7]);
+  return !(((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7])) == 0.0f);     // (NaN: not equal)
 }
 
 template <int DP, bool DIRECT, bool CAREFUL>
-__device__ __forceinline__ void forward_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, const bf16x8_t* q, f32x16_t* o, float& m,
+__device__ __forceinline__ void forward_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, bf16x8_t* q, f32x16_t* o, float& m,
                                              float& l, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES;
@@ -583,6 +599,10 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
     if (i + 1 < g.n) put(i + 1);
   };
   load(0);
+  if constexpr (!CAREFUL) {                             // (behind the first stage's loads, and under way together with them)
+    load_columns<DP, DIRECT>(q, a.Q + ((int64_t)t.r0 + min(row, t.n - 1)) * a.qs + w.head * a.d, a.d);
+    if (a.scale < 0.0f) negate<DP>(q);
+  }
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) o[i] = f32x16_t{};
   m = -INFINITY;
@@ -622,7 +642,6 @@ __global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) stage::clear(lds + i * stage::BYTES, a.d);
   bf16x8_t q[DP / 16];
-  load_columns<DP>(q, a.Q + ((int64_t)t.r0 + min(row, t.n - 1)) * a.qs + w.head * a.d, a.d, a.scale < 0.0f);
   f32x16_t o[NK];
   float m, l;
   forward_tile<DP, DIRECT, false>(a, w, t, row0, q, o, m, l, lds);
@@ -750,8 +769,8 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
 }
 
 template <int DP, bool DIRECT, bool CAREFUL>
-__device__ __forceinline__ void query_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, const bf16x8_t* q, const bf16x8_t* g,
-                                           f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, float& rounded, unsigned char* lds) {
+__device__ __forceinline__ void query_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, bf16x8_t* q, bf16x8_t* g,
+                                           f32x16_t* dq, f32x16_t* pk, float& lse, float& delta, float& rest, float& rounded, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES;
   const int row = row0 + (threadIdx.x & 31);
@@ -780,6 +799,22 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
     if (i + 1 < st.n) put(i + 1);
   };
   load(0);
+  if constexpr (!CAREFUL) {
+    const int64_t mine = (int64_t)t.r0 + min(row, t.n - 1);
+    bf16x8_t o[DP / 16];
+    load_columns<DP, DIRECT>(q, a.Q + mine * a.qs + w.head * a.d, a.d);
+    load_columns<DP, DIRECT>(g, a.dO + (mine * a.heads + w.head) * a.d, a.d);
+    load_columns<DP, DIRECT>(o, a.O + (mine * a.heads + w.head) * a.d, a.d);
+    lse = a.lse[mine * a.heads + w.head] * SA_LOG2E;
+    if (a.scale < 0.0f) negate<DP>(q);
+    float sum[4] = {};
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j & 3] = __builtin_fmaf((float)o[s][j], (float)g[s][j], sum[j & 3]);
+    delta = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    delta += other_half(delta);
+  }
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = pk[i] = f32x16_t{};
   rest = rounded = 0.0f;
@@ -811,19 +846,7 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
   for (int i = 0; i < 4; ++i) stage::clear(lds + i * stage::BYTES, a.d);
   const int64_t mine = (int64_t)t.r0 + min(row, t.n - 1);
   bf16x8_t q[DP / 16], g[DP / 16];
-  load_columns<DP>(q, a.Q + mine * a.qs + w.head * a.d, a.d, a.scale < 0.0f);
-  load_columns<DP>(g, a.dO + (mine * a.heads + w.head) * a.d, a.d, false);
-  float delta = 0.0f;
-  {
-    bf16x8_t o[DP / 16];
-    load_columns<DP>(o, a.O + (mine * a.heads + w.head) * a.d, a.d, false);
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)o[s][j], (float)g[s][j], delta);
-  }
-  delta += other_half(delta);
-  const float lse = a.lse[mine * a.heads + w.head] * SA_LOG2E;
+  float lse, delta;
   f32x16_t dq[NK], pk[NK];
   float rest, rounded;
   query_tile<DP, DIRECT, false>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rounded, lds);
@@ -962,7 +985,7 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
 }
 
 template <int DP, bool DIRECT, bool CAREFUL>
-__device__ __forceinline__ void token_tile(const self_args& a, int kv_head, const self_tile& t, int tok0, int piece, const bf16x8_t* k, const bf16x8_t* v,
+__device__ __forceinline__ void token_tile(const self_args& a, int kv_head, const self_tile& t, int tok0, int piece, bf16x8_t* k, bf16x8_t* v,
                                            f32x16_t* dk, f32x16_t* dv, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES + SA_STAGE * 8;
@@ -1003,6 +1026,12 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
   if (begin == end) return;
   const int head0 = begin / all.n, head1 = (end - 1) / all.n;
   load(head0, begin - head0 * all.n, 0);
+  if constexpr (!CAREFUL) {
+    const int64_t mine = (int64_t)t.r0 + min(tok, t.n - 1);
+    load_columns<DP, DIRECT>(k, a.K + mine * a.ks + kv_head * a.d, a.d);
+    load_columns<DP, DIRECT>(v, a.V + mine * a.vs + kv_head * a.d, a.d);
+    if (a.scale < 0.0f) negate<DP>(k);
+  }
   put(0);
 #pragma unroll 1
   for (int head = head0; head <= head1; ++head) {
@@ -1053,8 +1082,6 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(s
   for (int i = 0; i < 4; ++i) stage::clear(lds + (i >> 1) * BUF + (i & 1) * stage::BYTES, a.d);
   const int64_t mine = (int64_t)t.r0 + min(tok, t.n - 1);
   bf16x8_t k[DP / 16], v[DP / 16];
-  load_columns<DP>(k, a.K + mine * a.ks + kv_head * a.d, a.d, a.scale < 0.0f);
-  load_columns<DP>(v, a.V + mine * a.vs + kv_head * a.d, a.d, false);
   f32x16_t dk[NK], dv[NK];
   token_tile<DP, DIRECT, false>(a, kv_head, t, tok0, piece, k, v, dk, dv, lds);
   if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dk) || any_nonfinite<NK>(dv)), 0))
@@ -1208,7 +1235,7 @@ extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64
   a.out = (uint16_t*)O; a.lse = lse;
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_FWD, s);
-  const bool direct = a.d % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
+  const bool direct = a.d % 8 == 0 && q_stride % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
   return direct ? launch_forward_d<true>(a, s) : launch_forward_d<false>(a, s);
 }
 
