@@ -168,6 +168,10 @@ template <int DP> __device__ __forceinline__ void row_operands(bf16x8_t* x, cons
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) x[s] = row_operand<DP>(lds, row0, s);
 }
+// (the j-th of columns: block j % (DP / 32) of rows 16 (j / (DP / 32)) ..)
+template <int DP> __device__ __forceinline__ bf16x8_t nth_column_operand(const unsigned char* lds, int row0, int j) {
+  return column_operand<DP>(lds, row0 + 16 * (j / (DP / 32)), j % (DP / 32));
+}
 template <int DP> __device__ __forceinline__ void column_operands(bf16x8_t* x, const unsigned char* lds, int row0) {
 #pragma unroll
   for (int u = 0; u < 2; ++u)
@@ -204,9 +208,8 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 // Two neighbours rounded by one instruction (v_cvt_pk_bf16_f32).
 __device__ __forceinline__ uint32_t round_two(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x, y}, bf16x2_t)); }
 
-// The order of a run of instructions, in steps: PRODUCTS times a product, READS reads of LDS and VALU other vector instructions.  Reads in front of
-// the first step run ahead of the products by as many.
-__device__ __forceinline__ constexpr int at_least_one(int x) { return x < 1 ? 1 : x; }
+// The order of a run of instructions where there is nothing to do beside the products: READS reads of LDS in front, then PRODUCTS times a product
+// and as many more reads.
 template <int READS> __device__ __forceinline__ void reads_first() { __builtin_amdgcn_sched_group_barrier(0x100, READS, 0); }
 template <int PRODUCTS, int READS, int VALU> __device__ __forceinline__ void steps() {
 #pragma unroll
@@ -216,11 +219,22 @@ template <int PRODUCTS, int READS, int VALU> __device__ __forceinline__ void ste
     if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
   }
 }
-// The same, and nothing moves across its end.
-template <int PRODUCTS, int READS, int VALU> __device__ __forceinline__ void phase() {
-  steps<PRODUCTS, READS, VALU>();
-  __builtin_amdgcn_sched_barrier(0);
+// A phase: N steps of a product, the read of an operand that the next phase wants, and a share of the eight pairs of elements of a tile whose
+// exponentials or dS are formed meanwhile.  Nothing moves from step to step: an instruction waits for the one before it to be issued, an exponential
+// takes four slots, and where the compiler puts them in a row the matrix pipe is idle behind them.
+template <int N, typename P, typename R, typename V> __device__ __forceinline__ void phase(P product, R read, V pair) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    product(k);
+    read(k);
+#pragma unroll
+    for (int x = 8 * k / N; x < 8 * (k + 1) / N; ++x) pair(x);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
+struct nothing { template <typename T> __device__ __forceinline__ void operator()(T) const {} };
+// Four pairs as an operand.
+__device__ __forceinline__ bf16x8_t four_pairs(const uint32_t* w) { return __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3])); }
 
 // Eight rows of a tile as the second product's operand (registers 8 u .. 8 u + 7).
 __device__ __forceinline__ bf16x8_t as_operand(const f32x16_t& x, int u) {
@@ -497,24 +511,22 @@ __device__ __forceinline__ void forward_stage(const self_args& a, const unsigned
     steps<3 * NK, 2, 28 / NK>();
     steps<NK, 0, 0>();
   } else {
-    // each phase's operands are read during the one before it, exponentials run beside products
-    constexpr int VE = at_least_one(56 / N);
     ref = m;
+    uint32_t w[2][8];
+    auto pair = [&](int t, int y) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][2 * y], c, -ref)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][2 * y + 1], c, -ref));
+      sum[0] += p0;
+      sum[1] += p1;
+      w[t][y] = round_two(p0, p1);
+    };
+    auto product = [&](int t, int j) { o[j % NK] = mfma(x[t][j], four_pairs(w[t] + 4 * (j / NK)), o[j % NK]); };
     row_operands<DP>(x[0], lk, 0);
+    s[0] = s[1] = f32x16_t{};
     __builtin_amdgcn_sched_barrier(0);
-    row_operands<DP>(x[1], lk, 32);
-    scores(0, x[0]);
-    phase<N, 1, 0>();
-    column_operands<DP>(x[0], lv, 0);
-    scores(1, x[1]);
-    weights(0);
-    phase<N, 2, VE>();
-    column_operands<DP>(x[1], lv, 32);
-    products(0, x[0]);
-    weights(1);
-    phase<N, 2, VE>();
-    products(1, x[1]);
-    __builtin_amdgcn_sched_barrier(0);
+    phase<N>([&](int k) { s[0] = mfma(x[0][k], q[k], s[0]); }, [&](int k) { x[1][k] = row_operand<DP>(lk, 32, k); }, nothing{});
+    phase<N>([&](int k) { s[1] = mfma(x[1][k], q[k], s[1]); }, [&](int k) { x[0][k] = nth_column_operand<DP>(lv, 0, k); }, [&](int y) { pair(0, y); });
+    phase<N>([&](int k) { product(0, k); }, [&](int k) { x[1][k] = nth_column_operand<DP>(lv, 32, k); }, [&](int y) { pair(1, y); });
+    phase<N>([&](int k) { product(1, k); }, nothing{}, nothing{});
   }
   l += sum[0] + sum[1];
 }
@@ -660,8 +672,6 @@ __global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
 // Rows that see one token have p = 1 whatever its score: no gradient passes through it.
 __device__ __forceinline__ bool see_one(const self_args& a, int n) { return n == 1 || a.window == 1; }
 
-// Blocks of 32 tokens that a wavefront has in flight at a time: with two the products of one cover the exponentials of the other.
-template <int DP> constexpr int blocks_in_flight() { return 2; }
 // Wavefronts a SIMD of the backward kernels: their accumulators and both operands that stay take 1.5 DP registers, of 256 or 512.
 template <int DP> constexpr int backward_waves() { return DP > 64 ? 1 : 2; }
 
@@ -671,8 +681,8 @@ template <int DP> constexpr int backward_waves() { return DP > 64 ? 1 : 2; }
 // mean of the k would carry out as well: the true dS add up to nothing.
 template <int DP, bool MASKED, bool CAREFUL>
 __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q,
-                                             const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, float& rounded, int low, int lim) {
-  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : blocks_in_flight<DP>();
+                                             const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, float& rest_odd, float& rounded, int low, int lim) {
+  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : 2;
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
   uint32_t seen[NB];
@@ -723,54 +733,57 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
       }
     }
   };
-  if constexpr (NB == 2) {
-    // Each phase's operands are read during the one before it; the exponentials and dS of a block run beside the products of another phase.
-    constexpr int VE = at_least_one(40 / N), VD = at_least_one(56 / N);
+  if constexpr (CAREFUL) {
     row_operands<DP>(x[0], lk, at);
-    __builtin_amdgcn_sched_barrier(0);
-    row_operands<DP>(x[1], lv, at);
     scores(0, x[0]);
-    phase<N, 1, 0>();
-    row_operands<DP>(x[0], lk, at + 32);
+    row_operands<DP>(x[1], lv, at);
     slopes(0, x[1]);
     weights(0);
-    phase<N, 1, VE>();
-    row_operands<DP>(x[1], lv, at + 32);
-    scores(1, x[0]);
     through(0);
-    phase<N, 1, VD>();
     column_operands<DP>(x[0], lk, at);
-    slopes(1, x[1]);
-    weights(1);
-    phase<N, 2, VE>();
-    column_operands<DP>(x[1], lk, at + 32);
     products(0, x[0]);
-    through(1);
-    phase<2 * N, 1, VD / 2>();
-    products(1, x[1]);
-    __builtin_amdgcn_sched_barrier(0);
   } else {
-    // (one block: no registers for a second set of operands, reads run four products ahead)
+    uint32_t pw[2][8], xw[2][8];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s[b] = f32x16_t{};
+#pragma unroll
+      for (int j = 0; j < 16; ++j) dp[b][j] = -delta;
+      if constexpr (MASKED) seen[b] = bits_between(low - at - 32 * b, lim - at - 32 * b) >> (4 * h);
+    }
+    auto weight = [&](int b, int y) {
+#pragma unroll
+      for (int j = 2 * y; j < 2 * y + 2; ++j) {
+        s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], a.c, -lse));
+        if constexpr (MASKED) s[b][j] = where_set(s[b][j], seen[b], tile_row(j));
+      }
+      pw[b][y] = round_two(s[b][2 * y], s[b][2 * y + 1]);
+    };
+    auto slope = [&](int b, int y) {
+      const float x0 = s[b][2 * y] * dp[b][2 * y], x1 = s[b][2 * y + 1] * dp[b][2 * y + 1];
+      rest += x0;
+      rest_odd += x1;
+      xw[b][y] = round_two(x0, x1);
+      rounded = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, xw[b][y]), bf16x2_t{(__bf16)1.0f, (__bf16)1.0f}, rounded, false);
+    };
+    auto product = [&](int b, int j) {
+      dq[j % NK] = mfma(x[b][j], four_pairs(xw[b] + 4 * (j / NK)), dq[j % NK]);
+      pk[j % NK] = mfma(x[b][j], four_pairs(pw[b] + 4 * (j / NK)), pk[j % NK]);
+    };
     row_operands<DP>(x[0], lk, at);
-    scores(0, x[0]);
-    row_operands<DP>(x[1], lv, at);
-    slopes(0, x[1]);
-    weights(0);
-    through(0);
-    column_operands<DP>(x[0], lk, at);
-    products(0, x[0]);
-    reads_first<4>();
-    steps<N, 1, 0>();
-    steps<N, 1, at_least_one(32 / N)>();
-    __builtin_amdgcn_sched_group_barrier(0x2, 40, 0);
-    steps<2 * N - 4, 1, 0>();
-    steps<4, 0, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    phase<N>([&](int k) { s[0] = mfma(x[0][k], q[k], s[0]); }, [&](int k) { x[1][k] = row_operand<DP>(lv, at, k); }, nothing{});
+    phase<N>([&](int k) { dp[0] = mfma(x[1][k], g[k], dp[0]); }, [&](int k) { x[0][k] = row_operand<DP>(lk, at + 32, k); }, [&](int y) { weight(0, y); });
+    phase<N>([&](int k) { s[1] = mfma(x[0][k], q[k], s[1]); }, [&](int k) { x[1][k] = row_operand<DP>(lv, at + 32, k); }, [&](int y) { slope(0, y); });
+    phase<N>([&](int k) { dp[1] = mfma(x[1][k], g[k], dp[1]); }, [&](int k) { x[0][k] = nth_column_operand<DP>(lk, at, k); }, [&](int y) { weight(1, y); });
+    phase<N>([&](int k) { product(0, k); }, [&](int k) { x[1][k] = nth_column_operand<DP>(lk, at + 32, k); }, [&](int y) { slope(1, y); });
+    phase<N>([&](int k) { product(1, k); }, nothing{}, nothing{});
   }
 }
 
 template <int DP, bool DIRECT, bool CAREFUL>
 __device__ __forceinline__ void query_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, bf16x8_t* q, bf16x8_t* g,
-                                           f32x16_t* dq, f32x16_t* pk, float& lse, float& delta, float& rest, float& rounded, unsigned char* lds) {
+                                           f32x16_t* dq, f32x16_t* pk, float& lse, float& delta, float& rest, float& rest_odd, float& rounded, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES;
   const int row = row0 + (threadIdx.x & 31);
@@ -817,16 +830,16 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
   }
 #pragma unroll
   for (int i = 0; i < DP / 32; ++i) dq[i] = pk[i] = f32x16_t{};
-  rest = rounded = 0.0f;
+  rest = rest_odd = rounded = 0.0f;
   put(0);
   auto use = [&](int i, auto masked) {
     unsigned char* here = lds + (i & 1) * BUF;
     const int j0 = st.first + i * SA_STAGE;
     const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
-    constexpr int NB = CAREFUL ? 1 : blocks_in_flight<DP>();
+    constexpr int NB = CAREFUL ? 1 : 2;
 #pragma unroll 1
     for (int at = 0; at < SA_STAGE; at += 32 * NB)
-      query_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, rounded, low, lim);
+      query_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, low, lim);
   };
   if constexpr (CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
   else in_stages(st, next, store, use);
@@ -848,10 +861,11 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
   bf16x8_t q[DP / 16], g[DP / 16];
   float lse, delta;
   f32x16_t dq[NK], pk[NK];
-  float rest, rounded;
-  query_tile<DP, DIRECT, false>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rounded, lds);
+  float rest, rest_odd, rounded;
+  query_tile<DP, DIRECT, false>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, lds);
   if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dq) || any_nonfinite<NK>(pk)), 0))
-    query_tile<DP, DIRECT, true>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rounded, lds);
+    query_tile<DP, DIRECT, true>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, lds);
+  rest += rest_odd;
   rest += other_half(rest);
   rounded += other_half(rounded);
   if (row >= t.n) return;
@@ -870,11 +884,12 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
 template <int DP, bool MASKED, bool CAREFUL>
 __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned char* lq, const unsigned char* lg, const float* lst, int at, int low, int lim,
                                              const bf16x8_t* k, const bf16x8_t* v, f32x16_t* dk, f32x16_t* dv) {
-  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : blocks_in_flight<DP>();
+  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : 2;
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
   uint32_t seen[NB];
   constexpr int N = DP / 16;
+  const bf16x8_t* k_of = k;      // (`k` counts steps below)
   bf16x8_t o[2][N];              // operands of the present phase and, being read, of the next
   f32x4_t lse[NB][4];            // (-lse log2 e)
   auto sums = [&](int b) {       // and -delta, which dP begins with
@@ -929,58 +944,48 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
       }
     }
   };
-  if constexpr (NB == 2) {
-    // (as in the other kernel)
-    constexpr int VE = at_least_one(40 / N), VD = at_least_one(36 / N);
+  if constexpr (CAREFUL) {
     row_operands<DP>(o[0], lq, at);
-    sums(0);
-    __builtin_amdgcn_sched_barrier(0);
-    row_operands<DP>(o[1], lg, at);
     scores(0, o[0]);
-    phase<N, 1, 0>();
-    row_operands<DP>(o[0], lq, at + 32);
-    sums(1);
+    sums(0);
+    row_operands<DP>(o[1], lg, at);
     slopes(0, o[1]);
     weights(0);
-    phase<N, 2, VE>();
-    row_operands<DP>(o[1], lg, at + 32);
-    scores(1, o[0]);
     through(0);
-    phase<N, 1, VD>();
     column_operands<DP>(o[0], lg, at);
-    slopes(1, o[1]);
-    weights(1);
-    phase<N, 2, VE>();
-    column_operands<DP>(o[1], lq, at);
     value_products(0, o[0]);
-    through(1);
-    phase<N, 2, VD>();
-    column_operands<DP>(o[0], lg, at + 32);
+    column_operands<DP>(o[1], lq, at);
     key_products(0, o[1]);
-    phase<N, 2, 0>();
-    column_operands<DP>(o[1], lq, at + 32);
-    value_products(1, o[0]);
-    phase<N, 2, 0>();
-    key_products(1, o[1]);
-    __builtin_amdgcn_sched_barrier(0);
   } else {
+    uint32_t pw[2][8], xw[2][8];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s[b] = f32x16_t{};
+      if constexpr (MASKED) seen[b] = bits_between(low - at - 32 * b, lim - at - 32 * b) >> (4 * h);
+    }
+    auto weight = [&](int b, int y) {
+#pragma unroll
+      for (int j = 2 * y; j < 2 * y + 2; ++j) {
+        s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], a.c, lse[b][j >> 2][j & 3]));
+        if constexpr (MASKED) s[b][j] = where_set(s[b][j], seen[b], tile_row(j));
+      }
+      pw[b][y] = round_two(s[b][2 * y], s[b][2 * y + 1]);
+    };
+    auto slope = [&](int b, int y) { xw[b][y] = round_two(s[b][2 * y] * dp[b][2 * y], s[b][2 * y + 1] * dp[b][2 * y + 1]); };
+    auto value_product = [&](int b, const bf16x8_t* o, int j) { dv[j % NK] = mfma(o[j], four_pairs(pw[b] + 4 * (j / NK)), dv[j % NK]); };
+    auto key_product = [&](int b, const bf16x8_t* o, int j) { dk[j % NK] = mfma(o[j], four_pairs(xw[b] + 4 * (j / NK)), dk[j % NK]); };
     row_operands<DP>(o[0], lq, at);
-    scores(0, o[0]);
     sums(0);
-    row_operands<DP>(o[1], lg, at);
-    slopes(0, o[1]);
-    weights(0);
-    through(0);
-    column_operands<DP>(o[0], lg, at);
-    value_products(0, o[0]);
-    column_operands<DP>(o[1], lq, at);
-    key_products(0, o[1]);
-    reads_first<8>();
-    steps<N, 1, 0>();
-    steps<N, 2, at_least_one(32 / N)>();
-    __builtin_amdgcn_sched_group_barrier(0x2, 24, 0);
-    steps<2 * N - 4, 2, 0>();
-    steps<4, 0, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    phase<N>([&](int k) { s[0] = mfma(o[0][k], k_of[k], s[0]); }, [&](int k) { o[1][k] = row_operand<DP>(lg, at, k); }, nothing{});
+    sums(1);
+    phase<N>([&](int k) { dp[0] = mfma(o[1][k], v[k], dp[0]); }, [&](int k) { o[0][k] = row_operand<DP>(lq, at + 32, k); }, [&](int y) { weight(0, y); });
+    phase<N>([&](int k) { s[1] = mfma(o[0][k], k_of[k], s[1]); }, [&](int k) { o[1][k] = row_operand<DP>(lg, at + 32, k); }, [&](int y) { slope(0, y); });
+    phase<N>([&](int k) { dp[1] = mfma(o[1][k], v[k], dp[1]); }, [&](int k) { o[0][k] = nth_column_operand<DP>(lg, at, k); }, [&](int y) { weight(1, y); });
+    phase<N>([&](int k) { value_product(0, o[0], k); }, [&](int k) { o[1][k] = nth_column_operand<DP>(lq, at, k); }, [&](int y) { slope(1, y); });
+    phase<N>([&](int k) { key_product(0, o[1], k); }, [&](int k) { o[0][k] = nth_column_operand<DP>(lg, at + 32, k); }, nothing{});
+    phase<N>([&](int k) { value_product(1, o[0], k); }, [&](int k) { o[1][k] = nth_column_operand<DP>(lq, at + 32, k); }, nothing{});
+    phase<N>([&](int k) { key_product(1, o[1], k); }, nothing{}, nothing{});
   }
 }
 
@@ -1057,7 +1062,7 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
       const float* lst = reinterpret_cast<const float*>(here + 2 * stage::BYTES);
       const int i0 = st.first + i * SA_STAGE;
       const int low = (a.causal ? tok : 0) - i0, lim = first_blind_row(a, t.n, tok) - 1 - i0;      // the rows that see the lane's token
-      constexpr int NB = CAREFUL ? 1 : blocks_in_flight<DP>();
+      constexpr int NB = CAREFUL ? 1 : 2;
 #pragma unroll 1
       for (int x = 0; x < SA_STAGE; x += 32 * NB)
         token_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, lst, x, low, lim, k, v, dk, dv);
