@@ -664,42 +664,46 @@ def rope_freqs(rot_dim, base=10000.0, factor=1.0, original_len=0, low=1.0, high=
     return (f * (keep + (1.0 - keep) / factor)).to(device)
 
 
-def _index_check(dev, what, *tensors):
-    for t, n in tensors:
-        if t is not None:
-            if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
-                raise PQError(f"{what} are contiguous int32 tensors on the rows' device")
-            if t.numel() < n:
-                raise PQError(f"{what}: {t.numel()} entries where the descriptor asks for {n}")
+def _index_check(dev, what, t, n):
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
+        raise PQError(f"{what} is a contiguous int32 tensor on the rows' device")
+    if t.numel() < n:
+        raise PQError(f"{what}: {t.numel()} entries where the descriptor asks for {n}")
 
 
 def rope(desc, Q, K, freqs, Qr, Kr, row_start=None, lens=None):
     """Q [T, n_heads, d_head] and K [T, n_kv_heads, d_head] (or None) turned into Qr and Kr, which may be Q and K themselves."""
-    d, B, dt = desc.d_head, desc.n_seqs, _KV_DT.get(Q.dtype)
-    dev = Q.get_device()
+    d, B, Hk, dtype, dev = desc.d_head, desc.n_seqs, desc.n_kv_heads, Q.dtype, Q.get_device()
+    dt = _KV_DT.get(dtype)
     T, qs = _rows(Q, desc.n_heads, d)
     Tr, qrs = _rows(Qr, desc.n_heads, d)
-    if dev < 0 or dt is None or Qr.dtype is not Q.dtype or T != Tr or Qr.get_device() != dev:
+    if dev < 0 or dt is None or Qr.dtype is not dtype or T != Tr or Qr.get_device() != dev:
         raise PQError("Q and Qr are fp32 or bf16 tensors of as many rows on one GPU")
+    k = kr = None
     ks = krs = 0
-    if desc.n_kv_heads:
+    if Hk:
         if K is None or Kr is None:
             raise PQError("the descriptor has key heads: K and Kr are wanted")
-        Tk, ks = _rows(K, desc.n_kv_heads, d)
-        Tkr, krs = _rows(Kr, desc.n_kv_heads, d)
-        if Tk != T or Tkr != T or K.dtype is not Q.dtype or Kr.dtype is not Q.dtype or K.get_device() != dev or Kr.get_device() != dev:
+        Tk, ks = _rows(K, Hk, d)
+        Tkr, krs = _rows(Kr, Hk, d)
+        if Tk != T or Tkr != T or K.dtype is not dtype or Kr.dtype is not dtype or K.get_device() != dev or Kr.get_device() != dev:
             raise PQError("K and Kr have Q's rows, type and device")
+        k, kr = K.data_ptr(), Kr.data_ptr()
     elif K is not None or Kr is not None:
         raise PQError("the descriptor has no key heads")
     if freqs.dtype is not torch.float64 or freqs.get_device() != dev or not freqs.is_contiguous() or freqs.numel() != desc.rot_dim // 2:
         raise PQError(f"freqs is a contiguous fp64 tensor of rot_dim / 2 = {desc.rot_dim // 2} values on Q's device")
-    _index_check(dev, "row_start and lens", (row_start, B + 1), (lens, B))
+    rs = ln = None
+    if row_start is not None:
+        _index_check(dev, "row_start", row_start, B + 1)
+        rs = row_start.data_ptr()
+    if lens is not None:
+        _index_check(dev, "lens", lens, B)
+        ln = lens.data_ptr()
     if _current_device() != dev:
         with torch.cuda.device(dev):
             return rope(desc, Q, K, freqs, Qr, Kr, row_start, lens)
-    rc = lib().pq_rope(C.byref(desc), Q.data_ptr(), qs, None if K is None else K.data_ptr(), ks, dt, T, freqs.data_ptr(),
-                       None if row_start is None else row_start.data_ptr(), None if lens is None else lens.data_ptr(), Qr.data_ptr(), qrs,
-                       None if Kr is None else Kr.data_ptr(), krs, _raw_stream(dev))
+    rc = lib().pq_rope(C.byref(desc), Q.data_ptr(), qs, k, ks, dt, T, freqs.data_ptr(), rs, ln, Qr.data_ptr(), qrs, kr, krs, _raw_stream(dev))
     if rc:
         _check(rc)
     return Qr, Kr
@@ -729,7 +733,7 @@ def _self_attn_check(desc, Q, K, V, row_start, O, lse):
         raise PQError("lse is a contiguous fp32 tensor of one value per row and head")
     if dev < 0 or K.get_device() != dev or V.get_device() != dev or O.get_device() != dev or lse.get_device() != dev:
         raise PQError("Q, K, V, O and lse are on one GPU")
-    _index_check(dev, "row_start", (row_start, desc.n_seqs + 1))
+    _index_check(dev, "row_start", row_start, desc.n_seqs + 1)
     return T, qs, ks, vs, dev
 
 
