@@ -822,10 +822,13 @@ class AdamWTensors:
                                   + (" (steps: [ceil(n / 256), 2])" if name == "steps" else ""))
                 if n:
                     written.append((t.data_ptr(), t.data_ptr() + n * t.element_size(), name))
-        written.sort()
-        for (_, end, a), (begin, _, b) in zip(written, written[1:]):
-            if begin < end and not a == b == "grads":
-                raise PQError(f"{a} and {b} overlap")
+        written.sort()                                                  # (gradients are only read and may share memory among themselves)
+        reach = {True: (0, ""), False: (0, "")}
+        for begin, end, name in written:
+            for read_only, (to, other) in reach.items():
+                if begin < to and not (read_only and name == "grads"):
+                    raise PQError(f"{other} and {name} overlap")
+            reach[name == "grads"] = max(reach[name == "grads"], (end, name))
         self.desc = AdamWDesc(len(params), _dt(params[0]), _dt(grads[0]), state, int(masters is not None), int(m_values is not None), beta1, beta2, eps)
         lists = [params, grads, masters, m, v, steps, m_values, v_values]
         self.params, self.grads, self.masters, self.m, self.v, self.steps, self.m_values, self.v_values = lists

@@ -1234,6 +1234,7 @@ extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64
   if (int e = check_stride("K", k_stride, d->n_kv_heads, d->d_head)) return e;
   if (int e = check_stride("V", v_stride, d->n_kv_heads, d->d_head)) return e;
   PQ_REQUIRE(at16(Q) && at16(K) && at16(V) && at16(O), PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
+  PQ_REQUIRE(O != Q && O != K && O != V, PQ_ERR_BAD_ARG, "the output in place of an input");
   self_args a = make_args(d, T, row_start);
   a.Q = (const uint16_t*)Q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
   a.qs = q_stride; a.ks = k_stride; a.vs = v_stride;
@@ -1266,6 +1267,7 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   if (int e = check_stride("dV", dv_stride, d->n_kv_heads, d->d_head)) return e;
   PQ_REQUIRE(at16(dO) && at16(Q) && at16(K) && at16(V) && at16(O) && at16(dQ) && at16(dK) && at16(dV) && at16(workspace), PQ_ERR_SHAPE,
              "buffers must be 16-byte aligned");
+  PQ_REQUIRE(dQ != Q && dK != K && dV != V && dQ != dO && dQ != O, PQ_ERR_BAD_ARG, "gradients in place of what they are formed from");
   PQ_REQUIRE(workspace_bytes >= pq_self_attn_bwd_workspace_bytes(d, T), PQ_ERR_WORKSPACE, "workspace %zu < %zu", workspace_bytes,
              pq_self_attn_bwd_workspace_bytes(d, T));
   self_args a = make_args(d, T, row_start);

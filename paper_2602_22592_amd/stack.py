@@ -204,6 +204,8 @@ class CachedAttention:
     buffers are made by the call; those of a decoding step are the object's, so that a step can be captured into a graph.  freqs [rot_dim / 2]
     (rope_freqs): rotary positions of queries and keys, turned before the keys are written."""
 
+    freqs = None
+
     def __init__(self, weights, n_heads, n_kv_heads, n_pages, n_seqs, max_pages, page_tokens=64, kv_kind=pq.PQ_KV_INT8, max_len=0,
                  device="cuda", freqs=None, rot_dim=0, rope_layout=pq.PQ_ROPE_HALF, rope_scale=1.0):
         d = weights["Wq"].shape[1]
@@ -217,8 +219,8 @@ class CachedAttention:
         if dev.type != "cuda" or want.type != "cuda" or want.index not in (None, dev.index) or any(weights["W" + n].device != dev for n in "kvo"):
             raise pq.PQError(f"the weights are on one GPU, that of device={device}")
         self.d, self.H, self.Hk, self.dh, self.B = d, n_heads, n_kv_heads, d // n_heads, n_seqs
-        self.freqs = freqs
         if freqs is not None:
+            self.freqs = freqs
             self.turn = pq.make_rope_desc(n_heads, n_kv_heads, self.dh, n_seqs, rot_dim=rot_dim, layout=rope_layout, scale=rope_scale)
         with torch.cuda.device(dev):                                     # (whichever is current)
             self._build(weights, n_pages, n_seqs, max_pages, page_tokens, kv_kind, max_len, dev)

@@ -171,3 +171,33 @@ def test_a_captured_step_is_replayed_with_other_scalars_and_gradients():
         torch.cuda.synchronize()
         for a, b in zip(t.params + t.m + t.v + t.steps, u.params + u.m + u.v + u.steps):
             assert torch.equal(a, b)
+
+
+def test_tensors_that_share_memory_are_refused():
+    x = torch.zeros(2048, device="cuda")
+    new = lambda n=256: torch.zeros(n, device="cuda")
+    with pytest.raises(pq.PQError, match="overlap"):
+        pq.AdamWTensors([x[:256], x[:256]], [new(), new()])
+    with pytest.raises(pq.PQError, match="overlap"):
+        pq.AdamWTensors([x[128:384], new(4)], [x[:256], new(4)])
+    with pytest.raises(pq.PQError, match="overlap"):                  # (behind a shorter gradient inside of a longer one)
+        pq.AdamWTensors([new(1024), new(16), x[512:768]], [x[:1024], x[16:32], new()])
+    with pytest.raises(pq.PQError, match="overlap"):
+        pq.AdamWTensors([x[:256]], [new()], m=[x[252:508]], v=[new()])
+    t = pq.AdamWTensors([new(), new()], [x[:256], x[:256]])            # one gradient for two tensors
+    pq.adamw_step(t, pq.adamw_scalars(t, 1, 1e-3))
+
+
+def test_empty_tensors_and_another_stream():
+    p = [torch.ones(n, device="cuda") for n in (0, 5, 0)]
+    g = [torch.ones(n, device="cuda") for n in (0, 5, 0)]
+    t = pq.AdamWTensors(p, g, state=pq.PQ_STATE_8BIT)
+    s = pq.adamw_scalars(t, 1, 0.5)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        pq.adamw_step(t, s)
+    side.synchronize()
+    assert (p[1] - 0.5).abs().max() < 1e-5                            # (the first step is lr, whatever the gradient's size)
+    with pytest.raises(pq.PQError, match="read back"):
+        pq.adamw_read(t)

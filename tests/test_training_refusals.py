@@ -50,12 +50,15 @@ def attn(**k):
     return pq.make_self_attn_desc(**dict(dict(n_heads=4, n_kv_heads=2, d_head=64, n_seqs=2), **k))
 
 
-def fwd(lib, d, T=4, Q=fake, qs=256, ks=128, vs=128, rs=fake, O=fake, lse=fake):
+out = C.c_void_p(0x2000)
+
+
+def fwd(lib, d, T=4, Q=fake, qs=256, ks=128, vs=128, rs=fake, O=out, lse=fake):
     return lib.pq_self_attn_fwd(C.byref(d), Q, qs, fake, ks, fake, vs, T, rs, O, lse, None)
 
 
-def bwd(lib, d, T=4, dO=fake, ws=fake, n=big, dqs=256):
-    return lib.pq_self_attn_bwd(C.byref(d), dO, fake, 256, fake, 128, fake, 128, fake, fake, T, fake, fake, dqs, fake, 128, fake, 128, ws, n, None)
+def bwd(lib, d, T=4, dO=fake, ws=fake, n=big, dqs=256, dQ=out, dK=out):
+    return lib.pq_self_attn_bwd(C.byref(d), dO, fake, 256, fake, 128, fake, 128, fake, fake, T, fake, dQ, dqs, dK, 128, out, 128, ws, n, None)
 
 
 @pytest.mark.parametrize("bad,code", [(dict(n_heads=3), -2), (dict(n_kv_heads=0), -2), (dict(d_head=63), -2), (dict(d_head=130), -2), (dict(d_head=0, scale=1.0), -2),
@@ -78,6 +81,7 @@ def test_attention_arguments(lib):
     assert fwd(lib, d, O=C.c_void_p(0x1004)) == -2
     need = lib.pq_self_attn_bwd_workspace_bytes(C.byref(d), 4)
     assert need > 0 and bwd(lib, d, n=C.c_size_t(need - 1)) == -4
+    assert bwd(lib, d, dQ=fake) == -1 and bwd(lib, d, dK=fake) == -1 and fwd(lib, d, O=fake) == -1        # in place
     assert bwd(lib, d, ws=None) == -1 and bwd(lib, d, dO=None) == -1 and bwd(lib, d, dqs=255) == -2
 
 
