@@ -11,6 +11,13 @@ namespace {
 
 constexpr int ROPE_TABLE = 2048;       // sines and cosines in LDS, of all rows of a workgroup
 
+// i / by for i * by < 2^32, by a product (a division costs more than an element's bytes).
+struct divisor {
+  uint32_t by, inverse;
+  __host__ void set(int x) { by = (uint32_t)x; inverse = (uint32_t)((0xffffffffull + x) / x); }
+  __device__ __forceinline__ int into(int i) const { return by == 1 ? i : (int)__umulhi((uint32_t)i, inverse); }
+};
+
 struct rope_args {
   kv_view v;                     // row_start, lens, n_seqs, T
   const void *q, *k;
@@ -18,6 +25,7 @@ struct rope_args {
   int64_t qs, ks, qrs, krs;      // elements between rows
   const double* freqs;
   int heads, total_heads, d, half, pieces, rows;   // pieces: of a head's pairs, VEC each;  rows: of a workgroup
+  divisor by_half, by_row, by_piece;               // by_row: pieces of a row
   int inverse, whole;            // whole: sequences are the call's rows
   float scale;
 };
@@ -70,7 +78,7 @@ __global__ __launch_bounds__(256) void rope_kernel(rope_args a) {
   }
   __syncthreads();
   for (int i = threadIdx.x; i < a.rows * a.half; i += 256) {
-    const int r = i / a.half, f = i - r * a.half, pos = places[r];
+    const int r = a.by_half.into(i), f = i - r * a.half, pos = places[r];
     float s = 0.0f, c = 1.0f;
     if (pos != INT32_MIN) sine_cosine((double)pos * a.freqs[f], s, c);
     table[i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
@@ -79,7 +87,7 @@ __global__ __launch_bounds__(256) void rope_kernel(rope_args a) {
   typedef run<T, VEC> R;
   const int per_row = a.total_heads * a.pieces, all = a.rows * per_row;
   for (int i = threadIdx.x; i < all; i += 256) {
-    const int r = i / per_row, x = i - r * per_row, head = x / a.pieces, at = (x - head * a.pieces) * VEC;   // pairs at .. at + VEC - 1
+    const int r = a.rows > 1 ? a.by_row.into(i) : 0, x = i - r * per_row, head = a.by_piece.into(x), at = (x - head * a.pieces) * VEC;   // pairs at .. at + VEC - 1
     if (places[r] == INT32_MIN) continue;
     const bool is_k = head >= a.heads;
     const int64_t row = row0 + r;
@@ -179,6 +187,9 @@ extern "C" int pq_rope(const pq_rope_desc* d, const void* Q, int64_t q_stride, c
   if (rows > 64) rows = 64;
   if (rows < 1) rows = 1;
   a.rows = rows;
+  a.by_half.set(a.half);         // (at most ROPE_TABLE, ..
+  a.by_row.set(per_row);         // .. 1024 where there are several rows ..
+  a.by_piece.set(a.pieces);      // .. and 2^16 heads of 2^7 pieces are divided)
   const unsigned grid = (unsigned)((T + rows - 1) / rows);
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_ROPE, s);
