@@ -10,7 +10,7 @@ namespace {
   do { if (!(cond)) return pq_set_error(code, __VA_ARGS__); } while (0)
 
 constexpr int AW_BLOCK = 256;      // elements that share the steps of their 8-bit states
-constexpr int AW_PIECE = 4096;     // elements of a workgroup ..
+constexpr int AW_PIECE = 2048;     // elements of a workgroup ..
 constexpr int AW_SMALL = 1024;     // .. and where that leaves CUs without work
 
 // What a workgroup works on: `n` elements that begin at a multiple of AW_BLOCK of their tensor.
