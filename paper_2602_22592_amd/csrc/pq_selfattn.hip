@@ -7,6 +7,7 @@
 // No tensor of scores exists: tiles of 32 x 32 scores are formed by v_mfma_f32_32x32x16_bf16, used, and formed again from lse in the backward pass.
 #include "pq_kv.h"
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -1150,13 +1151,23 @@ int check_stride(const char* name, int64_t stride, int heads, int d) {
 }
 bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Pieces of a token tile's work, where there are fewer tiles than CUs: as many as give 512 workgroups, of 8 stages each at least.
+// Pieces of a token tile's work, whose parts are joined in their order.  As many as give 512 workgroups, of 8 stages each at least (16 heads of 64 on one,
+// 2000 rows: 91 us, 713 in one piece; 4 heads of 128 on one, 1000 rows: 72, in pieces of 16 stages 83, in one 168).  Tiles of causal rows differ
+// in length and come in few rounds, so long ones are cut further: to 2048 workgroups of 64 stages where two share a CU (32 heads of 64 on four, 10000
+// rows: 1560 us, uncut 2500; on eight, 8192 rows: 1060 and 1230; cut to 4096 1616 and 1124), to 1024 of 32 where one has it alone (32 heads of 128
+// on eight, 5000 rows: 900, uncut 1040, cut to 2048 980; 8192 rows, which stay whole: 2150, cut 2210).  Stages by the window (5000 rows, a window of 512:
+// 311 uncut, 335 and 411 in pieces) and, for the second cut, by the sequences' mean length (16 of 512 rows: 295, cut 387).
 int token_pieces(const pq_self_attn_desc* d, int T) {
-  const int64_t tiles = ((int64_t)T / SA_ROWS + d->n_seqs) * d->n_kv_heads, steps = (int64_t)d->n_heads / d->n_kv_heads * (T / SA_STAGE + 1);
-  if (tiles == 0 || tiles > 256) return 1;
-  int64_t pieces = 512 / tiles;
-  if (pieces > steps / 8) pieces = steps / 8;
-  return pieces < 1 ? 1 : pieces > 32 ? 32 : (int)pieces;
+  const int64_t tiles = ((int64_t)T / SA_ROWS + d->n_seqs) * d->n_kv_heads, group = d->n_heads / d->n_kv_heads;
+  if (tiles == 0 || d->n_seqs == 0) return 1;
+  auto stages = [&](int64_t rows) {
+    if (d->window > 0 && rows > (int64_t)d->window + SA_ROWS) rows = (int64_t)d->window + SA_ROWS;
+    return group * (rows / SA_STAGE + 1);
+  };
+  const bool alone = d->d_head > 64;           // a workgroup on its CU
+  const int64_t few = std::min(512 / tiles, stages(T) / 8);
+  const int64_t even = std::min((alone ? 1024 : 2048) / tiles, stages(T / d->n_seqs) / (alone ? 32 : 64));
+  return (int)std::min<int64_t>(std::max<int64_t>(std::max(few, even), 1), 32);
 }
 size_t stats_bytes(const pq_self_attn_desc* d, int T) { return pq_align_up((size_t)T * d->n_heads * sizeof(float2), 256); }
 

@@ -85,6 +85,17 @@ def test_attention_arguments(lib):
     assert bwd(lib, d, ws=None) == -1 and bwd(lib, d, dO=None) == -1 and bwd(lib, d, dqs=255) == -2
 
 
+def test_attention_workspace(lib):
+    """Room for lse and delta, and for a tile's pieces where there are few tiles with much work; no sequences need no more."""
+    def size(T, **k):
+        return lib.pq_self_attn_bwd_workspace_bytes(C.byref(attn(**k)), T)
+    assert size(1 << 20, n_seqs=0) <= (1 << 20) * 64 + 512
+    long, cut = dict(n_heads=32, n_kv_heads=8, d_head=64), 8192 * 8 * 2 * 64 * 4
+    assert size(8192, **long) == 8192 * 32 * 8 + 3 * cut + 256                                             # 520 tiles, 4 heads of 129 stages
+    assert size(8192, window=100, **long) == 8192 * 32 * 8 + 256                                           # a tile's rows are 4 stages
+    assert size(8192, n_heads=32, n_kv_heads=32, d_head=64) == 8192 * 32 * 8 + 256
+
+
 def tensors(n=300, **k):
     t = pq.AdamWTensor(0x1000, 0x2000, None, 0x3000, 0x4000, None, None, None, n)
     for a, b in k.items():
