@@ -481,9 +481,9 @@ int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const voi
  *   Q [T][n_heads][d_head], K, V [T][n_kv_heads][d_head] bf16, rows *_stride elements apart (even, at most 2^23);  O [T][n_heads][d_head] bf16 out and
  *   lse [T][n_heads] fp32 out, both contiguous.  Rows of no sequence are neither read nor written.  Buffers 16-byte aligned; what a call
  *   writes must not overlap what it reads, in both calls.
- * Scores, sums and lse are fp32; exp(s_j - m) is rounded to bf16 for the product with v (m: up to 16 powers of two below the largest s_j), o once more at the
- * end.  Tokens that a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite
- * or NaN.  At most 2^29 rows, rows * n_heads < 2^31.  The result does not depend on the order in which workgroups run. */
+ * Scores, sums and lse are fp32; exp(s_j - m) is rounded to bf16 for the product with v (m: the largest s_j among the first up to 64 tokens that the row
+ * sees, or among all where sums with it are not finite), o once more at the end; sums hold |v| up to 2^80.  Tokens that
+ * a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite or NaN.  At most 2^29 rows, rows * n_heads < 2^31.  The result does not depend on the order in which workgroups run. */
 typedef struct pq_self_attn_desc {
   int32_t n_heads;    /* query heads, a multiple of n_kv_heads */
   int32_t n_kv_heads;

@@ -10,8 +10,10 @@ namespace {
   do { if (!(cond)) return pq_set_error(code, __VA_ARGS__); } while (0)
 
 constexpr int AW_BLOCK = 256;      // elements that share the steps of their 8-bit states
-constexpr int AW_PIECE = 2048;     // elements of a workgroup ..
-constexpr int AW_SMALL = 1024;     // .. and where that leaves CUs without work
+// Elements of a workgroup, and where that leaves CUs without work.  With 8-bit states, 20M elements: 30 us in pieces of 4096, 28 of 2048, 26 of 1024; two
+// layers of the 1.3B shape: 476, 468 and 493.  1.5M elements: 16.7 us in pieces of 4096, 12.4 of 1024.
+constexpr int AW_PIECE = 2048;
+constexpr int AW_SMALL = 1024;
 
 // What a workgroup works on: `n` elements that begin at a multiple of AW_BLOCK of their tensor.
 struct adamw_piece {
@@ -69,8 +71,9 @@ __device__ __forceinline__ void block_step(uint32_t top_bits, float inv_square, 
   }
 }
 
-// A lane has four neighbouring elements, so a wavefront has a block and takes its maxima by exchanges.  Bound by memory where the states are fp32; with
-// 8-bit states the arithmetic of an element is as long as its bytes.
+// A lane has four neighbouring elements, so a wavefront has a block and takes its maxima by exchanges.  Bound by memory: 28 bytes an element with fp32
+// masters and states, bf16 weights and gradients (10M elements: 61 us, 4.6 TB/s, of inputs that are not in the last-level cache), 12 with 8-bit states, bf16
+// weights and fp32 gradients, where the arithmetic of an element (roots and the nearest codes, exactly) is nearly as long as its bytes.
 template <typename P, typename G, bool EIGHT, bool MASTER>
 __global__ __launch_bounds__(256) void adamw_kernel(const adamw_piece* __restrict__ pieces, adamw_consts k, const float* __restrict__ scalars) {
   const adamw_piece t = pieces[blockIdx.x];

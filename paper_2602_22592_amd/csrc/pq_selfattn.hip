@@ -5,6 +5,9 @@
 //     dQ_i = scale sum_j dS_ij k_j,   dK_j = scale sum_i dS_ij q_i,   dV_j = sum_i p_ij dO_i     (j's sums over the heads that share it, too)
 //
 // No tensor of scores exists: tiles of 32 x 32 scores are formed by v_mfma_f32_32x32x16_bf16, used, and formed again from lse in the backward pass.
+// Long sequences are bound by the matrix pipe and by what one wavefront can issue beside it; memory is read once or from the L2.  A score tile's columns
+// are the lanes (queries in the forward pass and for dQ, tokens for dK and dV), so that its weights are the next product's operand as they stand in
+// registers, in an order of the contraction that the other operand's reads follow, and softmax never leaves a lane but for halves of sums.
 #include "pq_kv.h"
 
 #include <algorithm>
@@ -244,6 +247,14 @@ __device__ __forceinline__ bf16x8_t as_operand(const f32x16_t& x, int u) {
   return __builtin_bit_cast(bf16x8_t, w);
 }
 
+// What that left of them, rounded itself.
+__device__ __forceinline__ bf16x8_t as_remainder(const f32x16_t& x, int u, bf16x8_t r) {
+  uint32_t w[4];
+#pragma unroll
+  for (int y = 0; y < 4; ++y) w[y] = round_two(x[8 * u + 2 * y] - (float)r[2 * y], x[8 * u + 2 * y + 1] - (float)r[2 * y + 1]);
+  return four_pairs(w);
+}
+
 // The sum of an operand's eight elements and x.
 __device__ __forceinline__ float sum_of(bf16x8_t a, float x) {
   const uint4 w = __builtin_bit_cast(uint4, a);
@@ -338,6 +349,10 @@ __device__ __forceinline__ int first_token(const self_args& a, int row) { return
 
 // The stages that a tile needs, and of them those of which a wavefront's 32 rows (or tokens) see something, from .. to - 1: these are a loop of their own,
 // since a branch around accumulators costs a second copy of them all.  Those from `all` to `part` - 1 are seen by all of its rows.
+// FINE stages of the gradients: p and dS as sums of two bf16 numbers.  Of rows that see at most 64 tokens, which is where few large elements make a row's
+// part of the gradients and where these rows' parts are large: with one rounding each the gradients' error comes to 1.4 times that of their own
+// rounding on average, and in one of ten short calls to more than 1.5 times.  A sequence has one such stage a head, so it costs long ones nothing.
+enum { PLAIN, FINE, CAREFUL };
 struct stages_of { int first, n, from, all, part, to, begin; };     // begin: the first of those that are taken at all
 // Stages of tokens that rows row0 .. row0 + 31 of the tile see.
 __device__ __forceinline__ stages_of token_stages(const self_args& a, const self_tile& t, int row0) {
@@ -370,11 +385,16 @@ __device__ __forceinline__ stages_of row_stages(const self_args& a, const self_t
 // `next` waits for a stage and has the loads of the one behind it started, `store` puts away what came through registers; `use` is told whether the
 // stage needs its mask.  (Masked and unmasked stages are loops in turn inside a loop, so that each is there once: heads of 128, 8192 and 130 tokens,
 // always masked 2320 and 29.1 us, two masked loops around an unmasked one 2150 and 33.)
-template <typename N, typename S, typename U>
-__device__ __forceinline__ void in_stages(const stages_of& g, N next, S store, U use) {
+struct fine_t { static constexpr bool value = true; };              // (masked, and one by itself)
+template <bool ANY_FINE, typename N, typename S, typename U>
+__device__ __forceinline__ void in_stages(const stages_of& g, N next, S store, U use, bool fine = false) {
   int i = g.begin;
 #pragma unroll 1
   for (; i < min(g.from, g.n); ++i) { next(i); store(i); }
+  if constexpr (ANY_FINE) {
+#pragma unroll 1
+    for (; i < min(fine ? 1 : 0, g.to); ++i) { next(i); use(i, fine_t{}); store(i); }
+  }
   int masked = min(g.all, g.to);
   const int part = min(g.part, g.to);
 #pragma unroll 1
@@ -452,6 +472,12 @@ __device__ __forceinline__ self_place place_of(const self_args& a) {
 // sees in its first stage serves for all others (it has p = 1, so nothing that counts is lost below; what overflows above ends as infinity or NaN,
 // and the tile is taken once more with care).  So the stages have no maximum to keep and no accumulators to rescale.
 // MASKED: stages that some row sees in part, or as its first.
+//
+// 128 rows a workgroup, 32 a wavefront; stages of 64 tokens, the next one's loads on their way to LDS.  Two workgroups share a CU: one's softmax runs beside
+// the other's products (one wavefront a SIMD: 627 us where two take 525).  A phase is a row of products with what the next phase needs read between
+// them and the other half's softmax in the gaps, in an order that the compiler is held to.  8192 causal rows, 32 heads of 128 on eight: 525 us,
+// 1.05 PFLOP/s, the matrix pipe busy 60 % of the cycles at the 1.7 GHz that the power limit leaves, LDS without bank conflicts; the rest is
+// the issue of softmax (exponentials, sums, conversion) in two wavefronts a SIMD.  Four stages in LDS instead of two: 545 us.
 template <int DP, bool MASKED>
 __device__ __forceinline__ void forward_stage(const self_args& a, const unsigned char* lk, const unsigned char* lv, const bf16x8_t* q, f32x16_t* o,
                                               float& m, float& l, int low, int lim) {
@@ -638,7 +664,7 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
     // (the stage of the last row's first token is masked as well: there its reference is found)
     stages_of f = g;
     f.all = (first_token(a, min(row0 + 31, t.n - 1)) - g.first) / SA_STAGE + 1;
-    in_stages(f, next, store, use);
+    in_stages<false>(f, next, store, use);
   }
 }
 
@@ -673,17 +699,26 @@ __global__ __launch_bounds__(256, 2) void self_forward_kernel(self_args a) {
 // Rows that see one token have p = 1 whatever its score: no gradient passes through it.
 __device__ __forceinline__ bool see_one(const self_args& a, int n) { return n == 1 || a.window == 1; }
 
-// Wavefronts a SIMD of the backward kernels: their accumulators and both operands that stay take 1.5 DP registers, of 256 or 512.
+// Wavefronts a SIMD of the backward kernels: their accumulators and both operands that stay take 1.5 DP registers, of 256 or 512 (heads of 96 with two
+// wavefronts spill).
 template <int DP> constexpr int backward_waves() { return DP > 64 ? 1 : 2; }
 
 // delta is dO . O with O as it was rounded to bf16, which costs dS as much as all else together; what is missing to sum_j p_ij dP_ij is the sum of
 // the dS themselves, known at the end.  So the products with p are kept beside those with dS (they share their other operand), and dQ is put right by
 // them: dQ = sum (dS - p sum dS) k.  With the sum of the dS as they were rounded for the product, which takes the part of their roundings that the
-// mean of the k would carry out as well: the true dS add up to nothing.
-template <int DP, bool MASKED, bool CAREFUL>
+// mean of the k would carry out as well: the true dS add up to nothing.  (Relative error of dQ: 3.6e-3 to 4.7e-3 with delta from the rounded O, 2.8e-3 to
+// 3.1e-3 with the exact sum of the dS, 2.4e-3 so.  The other kernel gets delta with the exact sum; with that of the rounded dS, dK's error
+// was 2.6e-3 instead of 2.3e-3.)
+//
+// Four products a tile (scores, dP, dS k, p k), as many as the kernel below: eight in all where five would do if dQ were added to by the workgroups of
+// all tokens, with atomics whose order changes results or parts of it in memory.  8192 causal rows, 32 heads of 128 on eight: 1050 us a kernel, 650
+// TFLOP/s of the five products, 1040 of the eight; the matrix pipe is busy 47 % of the cycles (46 % below; heads of 64: 45 % and 43 %).  A lone
+// wavefront takes 1.9 us for a stage and still 1.4 us with its products left out, so what bounds both is the issue of one wavefront's vector
+// instructions (one in about 5 cycles), not LDS (no bank conflicts) or loads.
+template <int DP, bool MASKED, int CARE>
 __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned char* lk, const unsigned char* lv, int at, const bf16x8_t* q,
                                              const bf16x8_t* g, f32x16_t* dq, f32x16_t* pk, float lse, float delta, float& rest, float& rest_odd, float& rounded, int low, int lim) {
-  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : 2;
+  constexpr int NK = DP / 32, NB = CARE == PLAIN ? 2 : 1;
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
   uint32_t seen[NB];
@@ -712,7 +747,7 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       // (without care 0 times what is not finite is NaN, and has the tile taken with care)
-      dp[b][j] = CAREFUL ? where_set(s[b][j] * dp[b][j], seen[b], tile_row(j)) : s[b][j] * dp[b][j];
+      dp[b][j] = CARE == CAREFUL ? where_set(s[b][j] * dp[b][j], seen[b], tile_row(j)) : s[b][j] * dp[b][j];
       rest += dp[b][j];
     }
   };
@@ -721,20 +756,26 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
     for (int u = 0; u < 2; ++u) {
       const bf16x8_t x = as_operand(dp[b], u), p = as_operand(s[b], u);
       rounded = sum_of(x, rounded);
+      bf16x8_t left;
+      if constexpr (CARE == FINE) {
+        left = as_remainder(dp[b], u, x);
+        rounded = sum_of(left, rounded);
+      }
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
         const bf16x8_t k = o[u * NK + i];
-        if constexpr (CAREFUL) {
+        if constexpr (CARE == CAREFUL) {
           dq[i] = mfma_seen(k, x, register_bits(seen[b], u), dq[i]);
           pk[i] = mfma_seen(k, p, register_bits(seen[b], u), pk[i]);
         } else {
           dq[i] = mfma(k, x, dq[i]);
           pk[i] = mfma(k, p, pk[i]);
+          if constexpr (CARE == FINE) dq[i] = mfma(k, left, dq[i]);
         }
       }
     }
   };
-  if constexpr (CAREFUL) {
+  if constexpr (CARE != PLAIN) {
     row_operands<DP>(x[0], lk, at);
     scores(0, x[0]);
     row_operands<DP>(x[1], lv, at);
@@ -782,7 +823,7 @@ __device__ __forceinline__ void query_blocks(const self_args& a, const unsigned 
   }
 }
 
-template <int DP, bool DIRECT, bool CAREFUL>
+template <int DP, bool DIRECT, int CARE>
 __device__ __forceinline__ void query_tile(const self_args& a, const self_place& w, const self_tile& t, int row0, bf16x8_t* q, bf16x8_t* g,
                                            f32x16_t* dq, f32x16_t* pk, float& lse, float& delta, float& rest, float& rest_odd, float& rounded, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
@@ -791,6 +832,7 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
   const uint16_t* K = a.K + (int64_t)t.r0 * a.ks + w.kv_head * a.d;
   const uint16_t* V = a.V + (int64_t)t.r0 * a.vs + w.kv_head * a.d;
   const stages_of st = token_stages(a, t, row0);
+  const bool fine = a.causal ? row0 < SA_STAGE : t.n <= SA_STAGE;
   stage k, v;
   k.begin(K, a.ks, a.d, t.n, t.r0 + t.n == a.T);
   v.begin(V, a.vs, a.d, t.n, t.r0 + t.n == a.T);
@@ -813,7 +855,7 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
     if (i + 1 < st.n) put(i + 1);
   };
   load(0);
-  if constexpr (!CAREFUL) {
+  if constexpr (CARE != CAREFUL) {
     const int64_t mine = (int64_t)t.r0 + min(row, t.n - 1);
     bf16x8_t o[DP / 16];
     load_columns<DP, DIRECT>(q, a.Q + mine * a.qs + w.head * a.d, a.d);
@@ -837,13 +879,13 @@ __device__ __forceinline__ void query_tile(const self_args& a, const self_place&
     unsigned char* here = lds + (i & 1) * BUF;
     const int j0 = st.first + i * SA_STAGE;
     const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
-    constexpr int NB = CAREFUL ? 1 : 2;
+    constexpr int HERE = std::is_same<decltype(masked), fine_t>::value ? FINE : CARE, NB = HERE == PLAIN ? 2 : 1;
 #pragma unroll 1
     for (int at = 0; at < SA_STAGE; at += 32 * NB)
-      query_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, low, lim);
+      query_blocks<DP, decltype(masked)::value, HERE>(a, here, here + stage::BYTES, at, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, low, lim);
   };
-  if constexpr (CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
-  else in_stages(st, next, store, use);
+  if constexpr (CARE == CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
+  else in_stages<true>(st, next, store, use, fine);
 }
 
 template <int DP, bool DIRECT>
@@ -863,9 +905,9 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
   float lse, delta;
   f32x16_t dq[NK], pk[NK];
   float rest, rest_odd, rounded;
-  query_tile<DP, DIRECT, false>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, lds);
+  query_tile<DP, DIRECT, PLAIN>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, lds);
   if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dq) || any_nonfinite<NK>(pk)), 0))
-    query_tile<DP, DIRECT, true>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, lds);
+    query_tile<DP, DIRECT, CAREFUL>(a, w, t, row0, q, g, dq, pk, lse, delta, rest, rest_odd, rounded, lds);
   rest += rest_odd;
   rest += other_half(rest);
   rounded += other_half(rounded);
@@ -882,10 +924,10 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_query_kernel(s
 // ---------------------------------------------------------------------------------------------
 // Gradients of the keys and values
 // ---------------------------------------------------------------------------------------------
-template <int DP, bool MASKED, bool CAREFUL>
+template <int DP, bool MASKED, int CARE>
 __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned char* lq, const unsigned char* lg, const float* lst, int at, int low, int lim,
                                              const bf16x8_t* k, const bf16x8_t* v, f32x16_t* dk, f32x16_t* dv) {
-  constexpr int NK = DP / 32, NB = CAREFUL ? 1 : 2;
+  constexpr int NK = DP / 32, NB = CARE == PLAIN ? 2 : 1;
   const int h = (threadIdx.x & 63) >> 5;
   f32x16_t s[NB], dp[NB];
   uint32_t seen[NB];
@@ -921,7 +963,7 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
   };
   auto through = [&](int b) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) dp[b][j] = CAREFUL ? where_set(s[b][j] * dp[b][j], seen[b], tile_row(j)) : s[b][j] * dp[b][j];
+    for (int j = 0; j < 16; ++j) dp[b][j] = CARE == CAREFUL ? where_set(s[b][j] * dp[b][j], seen[b], tile_row(j)) : s[b][j] * dp[b][j];
   };
   auto value_products = [&](int b, const bf16x8_t* o) {
 #pragma unroll
@@ -929,8 +971,9 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
       const bf16x8_t x = as_operand(s[b], u);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        if constexpr (CAREFUL) dv[i] = mfma_seen(o[u * NK + i], x, register_bits(seen[b], u), dv[i]);
+        if constexpr (CARE == CAREFUL) dv[i] = mfma_seen(o[u * NK + i], x, register_bits(seen[b], u), dv[i]);
         else dv[i] = mfma(o[u * NK + i], x, dv[i]);
+        if constexpr (CARE == FINE) dv[i] = mfma(o[u * NK + i], as_remainder(s[b], u, x), dv[i]);
       }
     }
   };
@@ -940,12 +983,13 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
       const bf16x8_t x = as_operand(dp[b], u);
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        if constexpr (CAREFUL) dk[i] = mfma_seen(o[u * NK + i], x, register_bits(seen[b], u), dk[i]);
+        if constexpr (CARE == CAREFUL) dk[i] = mfma_seen(o[u * NK + i], x, register_bits(seen[b], u), dk[i]);
         else dk[i] = mfma(o[u * NK + i], x, dk[i]);
+        if constexpr (CARE == FINE) dk[i] = mfma(o[u * NK + i], as_remainder(dp[b], u, x), dk[i]);
       }
     }
   };
-  if constexpr (CAREFUL) {
+  if constexpr (CARE != PLAIN) {
     row_operands<DP>(o[0], lq, at);
     scores(0, o[0]);
     sums(0);
@@ -990,13 +1034,14 @@ __device__ __forceinline__ void token_blocks(const self_args& a, const unsigned 
   }
 }
 
-template <int DP, bool DIRECT, bool CAREFUL>
+template <int DP, bool DIRECT, int CARE>
 __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, const self_tile& t, int tok0, int piece, bf16x8_t* k, bf16x8_t* v,
                                            f32x16_t* dk, f32x16_t* dv, unsigned char* lds) {
   typedef stage_t<DP, DIRECT> stage;
   constexpr int BUF = 2 * stage::BYTES + SA_STAGE * 8;
   const int tok = tok0 + (threadIdx.x & 31);
   const stages_of all = row_stages(a, t, tok0);
+  const bool fine = all.first == 0 && (a.causal || t.n <= SA_STAGE);
   // The stages of the heads that share the tile one behind the other, and of these the piece's.
   const int steps = all.n * a.group, begin = (int)((int64_t)steps * piece / a.pieces), end = (int)((int64_t)steps * (piece + 1) / a.pieces);
   const uint16_t* Q = a.Q + (int64_t)t.r0 * a.qs + (int64_t)kv_head * a.group * a.d;
@@ -1032,7 +1077,7 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
   if (begin == end) return;
   const int head0 = begin / all.n, head1 = (end - 1) / all.n;
   load(head0, begin - head0 * all.n, 0);
-  if constexpr (!CAREFUL) {
+  if constexpr (CARE != CAREFUL) {
     const int64_t mine = (int64_t)t.r0 + min(tok, t.n - 1);
     load_columns<DP, DIRECT>(k, a.K + mine * a.ks + kv_head * a.d, a.d);
     load_columns<DP, DIRECT>(v, a.V + mine * a.vs + kv_head * a.d, a.d);
@@ -1063,13 +1108,13 @@ __device__ __forceinline__ void token_tile(const self_args& a, int kv_head, cons
       const float* lst = reinterpret_cast<const float*>(here + 2 * stage::BYTES);
       const int i0 = st.first + i * SA_STAGE;
       const int low = (a.causal ? tok : 0) - i0, lim = first_blind_row(a, t.n, tok) - 1 - i0;      // the rows that see the lane's token
-      constexpr int NB = CAREFUL ? 1 : 2;
+      constexpr int HERE = std::is_same<decltype(masked), fine_t>::value ? FINE : CARE, NB = HERE == PLAIN ? 2 : 1;
 #pragma unroll 1
       for (int x = 0; x < SA_STAGE; x += 32 * NB)
-        token_blocks<DP, decltype(masked)::value, CAREFUL>(a, here, here + stage::BYTES, lst, x, low, lim, k, v, dk, dv);
+        token_blocks<DP, decltype(masked)::value, HERE>(a, here, here + stage::BYTES, lst, x, low, lim, k, v, dk, dv);
     };
-    if constexpr (CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
-    else in_stages(st, next, store, use);
+    if constexpr (CARE == CAREFUL) in_stages_alike(st, next, store, [&](int i) { use(i, std::true_type{}); });
+    else in_stages<true>(st, next, store, use, fine);
   }
 }
 
@@ -1089,9 +1134,9 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(s
   const int64_t mine = (int64_t)t.r0 + min(tok, t.n - 1);
   bf16x8_t k[DP / 16], v[DP / 16];
   f32x16_t dk[NK], dv[NK];
-  token_tile<DP, DIRECT, false>(a, kv_head, t, tok0, piece, k, v, dk, dv, lds);
+  token_tile<DP, DIRECT, PLAIN>(a, kv_head, t, tok0, piece, k, v, dk, dv, lds);
   if (__builtin_expect(__syncthreads_or(any_nonfinite<NK>(dk) || any_nonfinite<NK>(dv)), 0))
-    token_tile<DP, DIRECT, true>(a, kv_head, t, tok0, piece, k, v, dk, dv, lds);
+    token_tile<DP, DIRECT, CAREFUL>(a, kv_head, t, tok0, piece, k, v, dk, dv, lds);
   if (tok >= t.n) return;
   const float f = see_one(a, t.n) ? 0.0f : a.scale;
   if (a.pieces == 1) {
@@ -1104,7 +1149,8 @@ __global__ __launch_bounds__(256, backward_waves<DP>()) void self_token_kernel(s
   }
 }
 
-// The pieces' parts of dK and dV added in their order, two neighbouring elements a lane.  Rows of no sequence are left alone.
+// The pieces' parts of dK and dV added in their order, two neighbouring elements a lane.  Rows of no sequence are left alone.  Bound by memory, most of it
+// from the last-level cache.
 __global__ __launch_bounds__(256) void self_join_kernel(self_args a) {
   const int half = a.d / 2, per_row = a.kv_heads * 2 * half;
   const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, row = x / per_row;
