@@ -499,7 +499,8 @@ int pq_self_attn_fwd(const pq_self_attn_desc* desc, const void* Q, int64_t q_str
  *     p_j = exp(s_j - lse),   delta = sum_j p_j dO . v_j,   dS_j = p_j (dO . v_j - delta)
  *     dQ = scale sum_j dS_j k_j,   dK_j = scale sum dS_j q,   dV_j = sum p_j dO      (the last two over the rows that see j, and over the heads
  *                                                                                      that share it)
- *   dQ, dK, dV bf16 out with strides of their own (even); p and dS are rounded to bf16 for the products, the sums are fp32.  (delta is
+ *   dQ, dK, dV bf16 out with strides of their own (even); p and dS are rounded to bf16 for the products (the first 64 rows' of a causal
+ *   sequence, and those of whole ones of up to 64 rows, are sums of two bf16 numbers), the sums are fp32.  (delta is
  *   begun as dO . O, with O as it was rounded, and put right by the sum of the dS: O may be off by its rounding, not be something else.)  A row
  *   that sees one token has dS = 0.  Tokens and rows that do not see each other have no effect on each other, as above.
  *   workspace: pq_self_attn_bwd_workspace_bytes() bytes of scratch (0: refused arguments); calls that may overlap need one each. */

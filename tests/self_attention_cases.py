@@ -93,8 +93,9 @@ class Packed:
             assert not bad.any(), (here, h, np.argwhere(bad)[:4], np.abs(O[here, h] - o).max())
             assert (np.abs(lse[here, h] - l) <= e[:, 0] + len(q) * F + 2 * F * np.abs(l)).all(), (here, h)
 
-    def check_backward(self, O, lse, out):
-        """Against the formula in 64 bits on the lse that the call was given (O is where delta begins, not what it is)."""
+    def check_backward(self, O, lse, out, operand=U):
+        """Against the formula in 64 bits on the lse that the call was given (O is where delta begins, not what it is).  `operand`: what p and dS are off
+        by, relative, as operands of the second products (U; U U where they are sums of two bf16 numbers, but for p in m)."""
         dQ, dK, dV = (x.float().cpu().numpy() for x in out)
         for x in (dQ, dK, dV):
             assert (x[self.others()] == 7).all()
@@ -117,14 +118,14 @@ class Packed:
             # m exact), so the error is sum r_j (k_j - m), at most U sum |x_j| (|k_j| + |m|), and (sum D_j) (m~ - m), at most (rest + U sum |x_j|) U sum p |k|.
             many = seen.sum(1, keepdims=True) > 1
             rest = np.abs((do * o).sum(1, keepdims=True) - (p * (do @ v.T)).sum(1, keepdims=True)) * many
-            dse = (np.abs(ds) * (U + e) + p * diff * (1 + e)) * (1 + U)
-            dsq = dse + p * rest * (U + 2 * e)
+            dse = (np.abs(ds) * (operand + e) + p * diff * (1 + e)) * (1 + U)
+            dsq = dse + p * rest * (operand + 2 * e)
             x = (np.abs(ds) + p * rest) * many
-            mean = U * x.sum(1, keepdims=True) * np.abs(p @ k) + (rest + U * x.sum(1, keepdims=True)) * U * (p @ np.abs(k))
+            mean = operand * x.sum(1, keepdims=True) * np.abs(p @ k) + (rest + operand * x.sum(1, keepdims=True)) * U * (p @ np.abs(k))
             n = len(q) * self.H // self.Hk + 4
             add("dQ", here, h, dq, abs(self.scale) * (dsq @ np.abs(k) + mean + n * F * np.abs(ds) @ np.abs(k)))
             add("dK", here, hk, dk, abs(self.scale) * (dse.T @ np.abs(q) + n * F * np.abs(ds).T @ np.abs(q)))
-            add("dV", here, hk, dv, (p * (U + e + n * F)).T @ np.abs(do))
+            add("dV", here, hk, dv, (p * (operand + e + n * F)).T @ np.abs(do))
         mine = ~self.others()
         for name, x in (("dQ", dQ), ("dK", dK), ("dV", dV)):
             value, error = want[name]

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from self_attention_cases import Packed
+from self_attention_cases import Packed, U
 from paper_2602_22592_amd import binding as pq
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +56,13 @@ def test_against_the_definition(name):
     c.check_backward(O, lse, out)
     again = c.backward(O, lse, dev)
     assert all(torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16)) for a, b in zip(out, again))   # (whatever the order of workgroups)
+
+
+@pytest.mark.parametrize("case", [dict(rows=[1, 2, 17, 64, 3], H=4, Hk=2, d=64), dict(rows=[50, 64], H=8, Hk=1, d=128), dict(rows=[5, 33], H=3, Hk=3, d=90),
+                                  dict(rows=[64, 2], H=2, Hk=2, d=32, causal=False), dict(rows=[60, 9], H=4, Hk=4, d=96, window=7)],
+                         ids=["grouped", "one_head", "odd", "whole", "window"])
+def test_short_sequences_have_the_outputs_rounding_alone(case):
+    """Rows that see at most 64 tokens: p and dS are two bf16 numbers each."""
+    c = Packed(**case)
+    O, lse = c.forward()
+    c.check_backward(O, lse, c.backward(O, lse), operand=U * U)
