@@ -2,6 +2,7 @@
 #include "pq_internal.h"
 
 #include <cmath>
+#include <type_traits>
 #include <cstring>
 
 namespace {
@@ -55,10 +56,19 @@ __device__ __forceinline__ float square_code(float y, float top) {
   else if (c > 0.0f && (y < d2 || (y == d2 && odd))) c -= 1.0f;
   return fminf(c, top);
 }
+// The largest x of a wavefront, by lanes' neighbours without LDS: in fours, eights, rows of sixteen, rows 1 and 3, row 3's last lane.
 __device__ __forceinline__ uint32_t wave_max_bits(uint32_t x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o, 64));
-  return x;
+  auto from = [](uint32_t v, auto control, auto rows) {                     // (0 where a row is left out)
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(control)::value, decltype(rows)::value, 0xf, false);
+  };
+  typedef std::integral_constant<int, 0xf> all;
+  x = max(x, from(x, std::integral_constant<int, 0xb1>{}, all{}));          // quad_perm 1 0 3 2
+  x = max(x, from(x, std::integral_constant<int, 0x4e>{}, all{}));          // quad_perm 2 3 0 1
+  x = max(x, from(x, std::integral_constant<int, 0x141>{}, all{}));         // row_half_mirror
+  x = max(x, from(x, std::integral_constant<int, 0x140>{}, all{}));         // row_mirror
+  x = max(x, from(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{}));   // row_bcast 15
+  x = max(x, from(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{}));   // row_bcast 31
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 // Step of a block from the largest |x| as bits (those of infinities and NaN are above every finite value's), and its inverse; NaN and zero where it
 // is not finite.
