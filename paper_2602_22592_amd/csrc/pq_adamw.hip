@@ -45,16 +45,13 @@ __device__ __forceinline__ float load1(const uint16_t* p) { return bf16_to_f32(*
 __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void store1(uint16_t* p, float x) { *p = f32_to_bf16(x); }
 
-// The nearest code c to y = |x| / step under the law c^2: the one with (c - 1/2)^2 <= y <= (c + 1/2)^2, even where y is a border.  Borders below 2^16 are
-// fp32 numbers, so a root that is off in its last place is put right exactly.
-__device__ __forceinline__ float square_code(float y, float top) {
-  float c = __builtin_rintf(__builtin_amdgcn_sqrtf(y));
-  const float up = c + 0.5f, down = c - 0.5f;
-  const float u2 = up * up, d2 = down * down;
-  const bool odd = ((int)c) & 1;
-  if (y > u2 || (y == u2 && odd)) c += 1.0f;
-  else if (c > 0.0f && (y < d2 || (y == d2 && odd))) c -= 1.0f;
-  return fminf(c, top);
+// The nearest code c to y = |x| / step under the law c^2: the one with (c - 1/2)^2 <= y <= (c + 1/2)^2, of a tie the even one.  Borders below 2^16 are
+// fp32 numbers, so a root that is off in its last place is put right exactly; as bits, so that an odd c counts its upper border as passed and its lower
+// one as not reached (below 0 it is negative).
+__device__ __forceinline__ int square_code(float y, int top) {
+  const float c = __builtin_rintf(__builtin_amdgcn_sqrtf(y)), up = c + 0.5f, down = c - 0.5f;
+  const int code = (int)c, odd = code & 1, bits = __float_as_int(y);
+  return min(code + (bits + odd > __float_as_int(up * up) ? 1 : 0) - (bits < __float_as_int(down * fabsf(down)) + odd ? 1 : 0), top);
 }
 // The largest x of a wavefront, by lanes' neighbours without LDS: in fours, eights, rows of sixteen, rows 1 and 3, row 3's last lane.
 __device__ __forceinline__ uint32_t wave_max_bits(uint32_t x) {
@@ -152,11 +149,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(const adamw_piece* __restric
       qm = qr = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float c = square_code(fabsf(m[j]) * im, 127.0f);
-        float u = square_code(r[j] * ir, 255.0f);
-        if (r[j] > 0.0f) u = fmaxf(u, 1.0f);
-        qm |= ((uint32_t)(int)(m[j] < 0.0f ? -c : c) & 0xffu) << (8 * j);
-        qr |= (uint32_t)u << (8 * j);
+        const int c = square_code(fabsf(m[j]) * im, 127), u = square_code(r[j] * ir, 255);
+        qm |= ((uint32_t)(m[j] < 0.0f ? -c : c) & 0xffu) << (8 * j);
+        qr |= (uint32_t)max(u, r[j] > 0.0f ? 1 : 0) << (8 * j);
       }
       if ((threadIdx.x & 63) == 0) *reinterpret_cast<float2*>(t.steps + 2 * (at >> 8)) = make_float2(sm, sr);
     }
