@@ -12,7 +12,8 @@ namespace {
 
 constexpr int AW_BLOCK = 256;      // elements that share the steps of their 8-bit states
 // Elements of a workgroup, and where that leaves CUs without work.  With 8-bit states, 20M elements: 30 us in pieces of 4096, 28 of 2048, 26 of 1024; two
-// layers of the 1.3B shape: 476, 468 and 493.  1.5M elements: 16.7 us in pieces of 4096, 12.4 of 1024.
+// layers of the 1.3B shape, read back as well: 476, 468 and 493 (441 to 457 with maxima and codes as they are now).  1.5M elements: 16.7 us in
+// pieces of 4096, 12.4 of 1024.
 constexpr int AW_PIECE = 2048;
 constexpr int AW_SMALL = 1024;
 
