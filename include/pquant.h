@@ -503,7 +503,8 @@ int pq_self_attn_fwd(const pq_self_attn_desc* desc, const void* Q, int64_t q_str
  *   sequence, and those of whole ones of up to 64 rows, are sums of two bf16 numbers), the sums are fp32.  (delta is
  *   begun as dO . O, with O as it was rounded, and put right by the sum of the dS: O may be off by its rounding, not be something else.)  A row
  *   that sees one token has dS = 0.  Tokens and rows that do not see each other have no effect on each other, as above.
- *   workspace: pq_self_attn_bwd_workspace_bytes() bytes of scratch (0: refused arguments); calls that may overlap need one each. */
+ *   workspace: pq_self_attn_bwd_workspace_bytes() bytes of scratch (0: refused arguments; fewer rows may want more: one for more
+ *   rows serves them too, their work then cut into the pieces that it holds); calls that may overlap need one each. */
 size_t pq_self_attn_bwd_workspace_bytes(const pq_self_attn_desc* desc, int32_t T);
 int pq_self_attn_bwd(const pq_self_attn_desc* desc, const void* dO, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
                      int64_t v_stride, const void* O, const float* lse, int32_t T, const int32_t* row_start, void* dQ, int64_t dq_stride, void* dK,

@@ -1216,6 +1216,7 @@ int token_pieces(const pq_self_attn_desc* d, int T) {
   const int64_t even = std::min((alone ? 1024 : 2048) / tiles, stages(T / d->n_seqs) / (alone ? 32 : 64));
   return (int)std::min<int64_t>(std::max<int64_t>(std::max(few, even), 1), 32);
 }
+size_t part_bytes(const pq_self_attn_desc* d, int T) { return (size_t)T * d->n_kv_heads * 2 * d->d_head * sizeof(float); }
 size_t stats_bytes(const pq_self_attn_desc* d, int T) { return pq_align_up((size_t)T * d->n_heads * sizeof(float2), 256); }
 
 self_args make_args(const pq_self_attn_desc* d, int T, const int32_t* row_start) {
@@ -1306,7 +1307,7 @@ extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64
 extern "C" size_t pq_self_attn_bwd_workspace_bytes(const pq_self_attn_desc* d, int32_t T) {
   if (check_self(d) || check_rows(d, T)) return 0;
   const int pieces = token_pieces(d, T);
-  return stats_bytes(d, T) + (pieces > 1 ? (size_t)pieces * T * d->n_kv_heads * 2 * d->d_head * sizeof(float) : 0) + 256;
+  return stats_bytes(d, T) + (pieces > 1 ? pieces * part_bytes(d, T) : 0) + 256;
 }
 
 extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
@@ -1326,8 +1327,9 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   PQ_REQUIRE(at16(dO) && at16(Q) && at16(K) && at16(V) && at16(O) && at16(dQ) && at16(dK) && at16(dV) && at16(workspace), PQ_ERR_SHAPE,
              "buffers must be 16-byte aligned");
   PQ_REQUIRE(dQ != Q && dK != K && dV != V && dQ != dO && dQ != O, PQ_ERR_BAD_ARG, "gradients in place of what they are formed from");
-  PQ_REQUIRE(workspace_bytes >= pq_self_attn_bwd_workspace_bytes(d, T), PQ_ERR_WORKSPACE, "workspace %zu < %zu", workspace_bytes,
-             pq_self_attn_bwd_workspace_bytes(d, T));
+  // (fewer rows may want more pieces and more room for them: a workspace for more rows serves fewer with the pieces that it holds)
+  const size_t least = stats_bytes(d, T) + 256;
+  PQ_REQUIRE(workspace_bytes >= least, PQ_ERR_WORKSPACE, "workspace %zu < %zu", workspace_bytes, least);
   self_args a = make_args(d, T, row_start);
   a.Q = (const uint16_t*)Q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V; a.O = (const uint16_t*)O; a.dO = (const uint16_t*)dO;
   a.qs = q_stride; a.ks = k_stride; a.vs = v_stride;
@@ -1336,7 +1338,7 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   a.lse = const_cast<float*>(lse);
   a.stats = (float2*)workspace;
   a.parts = (float*)((char*)workspace + stats_bytes(d, T));
-  a.pieces = token_pieces(d, T);
+  a.pieces = (int)std::max<size_t>(1, std::min<size_t>(token_pieces(d, T), (workspace_bytes - least) / part_bytes(d, T)));
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_BWD, s);
   const bool direct = a.d % 8 == 0 && q_stride % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;

@@ -54,10 +54,14 @@ class Packed:
         torch.cuda.synchronize()
         return O, lse
 
-    def backward(self, O, lse, dev=None):
+    def backward(self, O, lse, dev=None, pieces=None):
         Q, K, V = dev or self.inputs()
         out, desc = self.gradients(), self.desc()
         ws = pq.self_attn_bwd_workspace(desc, self.T)
+        if pieces is not None:                               # a workspace with room for so many pieces of dK and dV, less than the call would take
+            few = (self.T * self.H * 8 + 255) // 256 * 256 + 256 + pieces * self.T * self.Hk * 2 * self.d * 4
+            assert few < ws.numel()
+            ws = ws[:few]
         ws.fill_(255)
         pq.self_attn_bwd(desc, self.gpu(self.do, 0), Q, K, V, O, lse, self.row_start(), *out, ws)
         torch.cuda.synchronize()

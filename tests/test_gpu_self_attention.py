@@ -66,3 +66,10 @@ def test_short_sequences_have_the_outputs_rounding_alone(case):
     c = Packed(**case)
     O, lse = c.forward()
     c.check_backward(O, lse, c.backward(O, lse), operand=U * U)
+
+
+@pytest.mark.parametrize("pieces", [0, 1, 2, 3])
+def test_a_workspace_with_room_for_fewer_pieces(pieces):
+    c = Packed(rows=[330, 70], H=8, Hk=1, d=64)
+    O, lse = c.forward()
+    c.check_backward(O, lse, c.backward(O, lse, pieces=pieces))
