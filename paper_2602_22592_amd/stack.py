@@ -30,7 +30,8 @@ class AttentionCore:
     """What stands between the q, k, v projections and the o projection in training: rotary positions and attention over packed sequences.
 
     row_start [n_seqs + 1] int32 on the GPU: the sequences' rows among the `tokens` of a call; it may change from step to step.  Rows of no sequence come
-    out as zeros and have no gradient.  freqs [rot_dim / 2] (rope_freqs), or None for attention without positions."""
+    out as zeros and have no gradient: the kernels leave them alone, so every call clears what it is about to write (the products that read it take all
+    rows).  freqs [rot_dim / 2] (rope_freqs), or None for attention without positions."""
 
     def __init__(self, tokens, n_heads, n_kv_heads, d_head, n_seqs, freqs=None, rot_dim=0, layout=pq.PQ_ROPE_HALF, rope_scale=1.0, window=0, causal=True,
                  device="cuda"):
@@ -51,12 +52,13 @@ class AttentionCore:
         """s: a layer's buffers with the projections in q, k and v.  Turns q and k in place and returns the output [T, n_heads * d_head]."""
         if self.freqs is not None:
             pq.rope(self.turn, s["q"], s["k"], self.freqs, s["q"], s["k"], row_start=row_start)
+        s["o"].zero_()
         pq.self_attn_fwd(self.attn, s["q"], s["k"], s["v"], row_start, s["o"], s["lse"])
         return s["o"].view(self.T, -1)
 
     def backward(self, dm, s, row_start, dq, dk, dv):
         """The gradients of the projections, [T, heads * d_head] each, from that of the output."""
-        three = [x.view(self.T, -1, self.dh) for x in (dq, dk, dv)]
+        three = [x.zero_().view(self.T, -1, self.dh) for x in (dq, dk, dv)]
         pq.self_attn_bwd(self.attn, dm, s["q"], s["k"], s["v"], s["o"], s["lse"], row_start, *three, self.ws)
         if self.freqs is not None:
             pq.rope(self.turn_back, three[0], three[1], self.freqs, three[0], three[1], row_start=row_start)
