@@ -48,6 +48,12 @@ class AttentionCore:
         z = lambda heads: torch.zeros((self.T, heads, self.dh), dtype=torch.bfloat16, device=device)
         return dict(q=z(self.H), k=z(self.Hk), v=z(self.Hk), o=z(self.H), lse=torch.zeros((self.T, self.H), dtype=torch.float32, device=device))
 
+    def check(self, row_start):
+        """For whoever launches something in front of the core's calls: a refusal between them would leave buffers that nobody has filled."""
+        if row_start is None:
+            raise pq.PQError("row_start: a stack with an AttentionCore is given its sequences' rows")
+        pq._index_check(self.ws.get_device(), "row_start", row_start, self.attn.n_seqs + 1)
+
     def forward(self, s, row_start):
         """s: a layer's buffers with the projections in q, k and v.  Turns q and k in place and returns the output [T, n_heads * d_head]."""
         if self.freqs is not None:
@@ -125,6 +131,7 @@ class Stack:
 
     def _forward_core(self, h0, weights, row_start):
         h, core = h0, self.core
+        core.check(row_start)
         o, f = self.t[:2]
         for ly, w in zip(self.layers, weights):
             ly["h"].copy_(h)
@@ -177,6 +184,8 @@ class Stack:
 
     def backward(self, dY, weights, grads, row_start=None):
         """grads: per-layer dict of fp32 tensors shaped like the weights (plus 'dab' [2])."""
+        if self.core is not None:
+            self.core.check(row_start)
         d_cur, d_tmp = self.dh
         d_cur.copy_(dY)
         dq, dk, dv, dm, dx = self.t
