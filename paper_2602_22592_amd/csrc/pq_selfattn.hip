@@ -651,7 +651,9 @@ __device__ __forceinline__ void forward_tile(const self_args& a, const self_plac
   auto use = [&](int i, auto masked) {
     unsigned char* here = lds + (i & 1) * BUF;
     const int j0 = g.first + i * SA_STAGE;
-    const int lim = (a.causal ? min(row, t.n - 1) : t.n - 1) - j0, low = first_token(a, row) - j0;
+    // (lanes behind the sequence's last row are that row once more, its window too: with one of their own they could see nothing of the masked stages, have
+    // no reference in the others, and have the tile taken with care)
+    const int last = min(row, t.n - 1), lim = (a.causal ? last : t.n - 1) - j0, low = first_token(a, last) - j0;
     if constexpr (CAREFUL) {
 #pragma unroll 1
       for (int at = 0; at < SA_STAGE; at += 32) forward_block<DP>(a, here, here + stage::BYTES, at, q, o, m, l, low, lim);
