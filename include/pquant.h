@@ -469,8 +469,8 @@ typedef struct pq_rope_desc {
   float scale;        /* finite; usually 1 */
 } pq_rope_desc;
 /* Q [T][n_heads][d_head], K [T][n_kv_heads][d_head] of `dtype` (PQ_F32 or PQ_BF16), rows q_stride / k_stride elements apart (even, at least
- * the heads' elements); Qr, Kr the same shapes with strides of their own.  Qr may be Q and Kr may be K, with the same stride (in place); otherwise they
- * must not overlap.  All 16-byte aligned. */
+ * the heads' elements); Qr, Kr the same shapes with strides of their own.  Qr may be Q and Kr may be K, with the same stride (in place); otherwise what is
+ * written must share no byte with what is read, or with the other output (refused; rows between each other's rows are no overlap).  All 16-byte aligned. */
 int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, int32_t dtype, int32_t T,
             const double* freqs, const int32_t* row_start, const int32_t* lens, void* Qr, int64_t qr_stride, void* Kr, int64_t kr_stride, void* stream);
 
@@ -479,8 +479,8 @@ int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const voi
  * these the last `window` if window > 0.  Query head h reads key-value head h / (n_heads / n_kv_heads).
  *     s_j = scale q . k_j,   lse = log sum_j exp s_j,   o = sum_j exp(s_j - lse) v_j
  *   Q [T][n_heads][d_head], K, V [T][n_kv_heads][d_head] bf16, rows *_stride elements apart (even, at most 2^23);  O [T][n_heads][d_head] bf16 out and
- *   lse [T][n_heads] fp32 out, both contiguous.  Rows of no sequence are neither read nor written.  Buffers 16-byte aligned; what a call
- *   writes must not overlap what it reads, in both calls.
+ *   lse [T][n_heads] fp32 out, both contiguous.  Rows of no sequence are neither read nor written.  Buffers 16-byte aligned; in both
+ *   calls what is written must share no byte with what is read or with another output (refused; rows between each other's rows are no overlap).
  * Scores, sums and lse are fp32; exp(s_j - m) is rounded to bf16 for the product with v (m: the largest s_j among the first up to 64 tokens that the row
  * sees, or among all where sums with it are not finite), o once more at the end; sums hold |v| up to 2^80.  Tokens that
  * a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite or NaN.  At most 2^29 rows, rows * n_heads < 2^31.  The result does not depend on the order in which workgroups run. */

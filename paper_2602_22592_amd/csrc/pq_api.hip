@@ -14,6 +14,48 @@ int pq_set_error(int code, const char* fmt, ...) {
   return code;
 }
 
+namespace {
+bool regions_overlap(pq_region a, pq_region b) {
+  for (pq_region* r : {&a, &b})
+    if (r->stride == r->bytes || r->rows == 1) {           // (one long row)
+      r->bytes *= r->rows;
+      r->stride = r->bytes;
+      r->rows = r->bytes > 0 ? 1 : 0;
+    }
+  if (a.rows <= 0 || b.rows <= 0 || a.bytes <= 0 || b.bytes <= 0) return false;
+  if (a.rows > b.rows) { const pq_region t = a; a = b; b = t; }
+  // Row 0 of b begins `from` behind row 0 of a; rows i of a and j of b meet where 0 < from + j b.stride - i a.stride + b.bytes and what is in front of
+  // that is below a.bytes.
+  const int64_t from = (int64_t)(b.at - a.at);
+  if (from >= (a.rows - 1) * a.stride + a.bytes || -from >= (b.rows - 1) * b.stride + b.bytes) return false;
+  // first j >= least at which row j of b ends behind x, and whether it begins in front of x + a.bytes
+  auto meets = [&](int64_t x, int64_t least) {
+    int64_t j = least;
+    const int64_t gap = x - from - b.bytes - least * b.stride;       // of that row's end
+    if (gap >= 0) j += gap / b.stride + 1;
+    return j < b.rows && from + j * b.stride < x + a.bytes;
+  };
+  if (a.stride == b.stride) return meets(0, -(a.rows - 1));          // (only j - i counts)
+  for (int64_t i = 0; i < a.rows; ++i)
+    if (meets(i * a.stride, 0)) return true;
+  return false;
+}
+}  // namespace
+
+int pq_refuse_overlap(const pq_region* written, int n_written, const pq_region* read, int n_read) {
+  for (int i = 0; i < n_written; ++i) {
+    const pq_region& w = written[i];
+    for (int j = i + 1; j < n_written; ++j)
+      if (regions_overlap(w, written[j])) return pq_set_error(PQ_ERR_BAD_ARG, "%s and %s are written and overlap", w.name, written[j].name);
+    for (int j = 0; j < n_read; ++j) {
+      const pq_region& r = read[j];
+      if (w.in_place && w.in_place == r.in_place && w.at == r.at && w.stride == r.stride) continue;
+      if (regions_overlap(w, r)) return pq_set_error(PQ_ERR_BAD_ARG, "%s is written and overlaps %s, which is read", w.name, r.name);
+    }
+  }
+  return PQ_OK;
+}
+
 extern "C" const char* pq_last_error_string(void) { return g_err; }
 extern "C" int pq_version(void) { return 100; }
 

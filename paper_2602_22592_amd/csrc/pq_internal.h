@@ -14,6 +14,17 @@ struct pq_prof_scope {   // records an event pair around the launches made while
   ~pq_prof_scope();
 };
 
+// ---- buffers of a call that must not share memory (pq_api.hip) ------------------------------
+struct pq_region {       // `rows` rows of `bytes` bytes, `stride` bytes apart (at least `bytes`)
+  const char* name;
+  uintptr_t at;
+  int64_t rows, stride, bytes;
+  int in_place;          // a written and a read region of the same number, not 0, may be one and the same
+};
+inline pq_region pq_flat_region(const char* name, const void* p, int64_t bytes) { return {name, (uintptr_t)p, 1, bytes, bytes, 0}; }
+// PQ_ERR_BAD_ARG where a written region shares a byte with a read one or with another written one.  Rows between each other's rows are no overlap.
+int pq_refuse_overlap(const pq_region* written, int n_written, const pq_region* read, int n_read);
+
 // ---- pq_quant.hip -------------------------------------------------------------------------
 // Per-token AbsMax INT8 quantiser.  Xt (optional, bf16) receives q/gamma, the de-quantised
 // activation that the STE backward multiplies with.

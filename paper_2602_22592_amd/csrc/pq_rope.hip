@@ -169,6 +169,13 @@ extern "C" int pq_rope(const pq_rope_desc* d, const void* Q, int64_t q_stride, c
   PQ_REQUIRE(((((uintptr_t)Q | (uintptr_t)Qr | (uintptr_t)(has_k ? K : nullptr) | (uintptr_t)(has_k ? Kr : nullptr)) & 15) == 0) &&
                  ((uintptr_t)freqs & 7) == 0, PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
   PQ_REQUIRE((Q != Qr || q_stride == qr_stride) && (!has_k || K != Kr || k_stride == kr_stride), PQ_ERR_SHAPE, "in place, both strides are the same");
+  const int size = dtype == PQ_F32 ? 4 : 2;
+  const pq_region written[] = {{"Qr", (uintptr_t)Qr, T, qr_stride * size, qn * size, 1}, {"Kr", (uintptr_t)Kr, has_k ? T : 0, kr_stride * size, kn * size, 2}};
+  const pq_region read[] = {{"Q", (uintptr_t)Q, T, q_stride * size, qn * size, 1}, {"K", (uintptr_t)K, has_k ? T : 0, k_stride * size, kn * size, 2},
+                            pq_flat_region("freqs", freqs, (int64_t)d->rot_dim / 2 * 8),
+                            pq_flat_region("row_start", row_start, row_start ? ((int64_t)d->n_seqs + 1) * 4 : 0),
+                            pq_flat_region("lens", lens, lens ? (int64_t)d->n_seqs * 4 : 0)};
+  if (int e = pq_refuse_overlap(written, 2, read, 5)) return e;
   rope_args a = {};
   a.v.lens = lens; a.v.row_start = row_start; a.v.n_seqs = d->n_seqs; a.v.T = T;
   a.whole = lens == nullptr;

@@ -1199,6 +1199,13 @@ int check_stride(const char* name, int64_t stride, int heads, int d) {
   return PQ_OK;
 }
 bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// T rows of `heads` heads, `stride` elements apart.
+pq_region rows_region(const char* name, const void* p, int T, int64_t stride, int heads, int d) {
+  return {name, (uintptr_t)p, T, stride * 2, (int64_t)heads * d * 2, 0};
+}
+pq_region row_start_region(const pq_self_attn_desc* d, const int32_t* row_start) {
+  return pq_flat_region("row_start", row_start, ((int64_t)d->n_seqs + 1) * 4);
+}
 
 // Pieces of a token tile's work, whose parts are joined in their order.  As many as give 512 workgroups, of 8 stages each at least (16 heads of 64 on one,
 // 2000 rows: 91 us, 713 in one piece; 4 heads of 128 on one, 1000 rows: 72, in pieces of 16 stages 83, in one 168).  Tiles of causal rows differ
@@ -1295,7 +1302,11 @@ extern "C" int pq_self_attn_fwd(const pq_self_attn_desc* d, const void* Q, int64
   if (int e = check_stride("K", k_stride, d->n_kv_heads, d->d_head)) return e;
   if (int e = check_stride("V", v_stride, d->n_kv_heads, d->d_head)) return e;
   PQ_REQUIRE(at16(Q) && at16(K) && at16(V) && at16(O), PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
-  PQ_REQUIRE(O != Q && O != K && O != V, PQ_ERR_BAD_ARG, "the output in place of an input");
+  const int H = d->n_heads, Hk = d->n_kv_heads, dh = d->d_head;
+  const pq_region written[] = {rows_region("O", O, T, (int64_t)H * dh, H, dh), pq_flat_region("lse", lse, (int64_t)T * H * 4)};
+  const pq_region read[] = {rows_region("Q", Q, T, q_stride, H, dh), rows_region("K", K, T, k_stride, Hk, dh), rows_region("V", V, T, v_stride, Hk, dh),
+                            row_start_region(d, row_start)};
+  if (int e = pq_refuse_overlap(written, 2, read, 4)) return e;
   self_args a = make_args(d, T, row_start);
   a.Q = (const uint16_t*)Q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V;
   a.qs = q_stride; a.ks = k_stride; a.vs = v_stride;
@@ -1328,10 +1339,17 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   if (int e = check_stride("dV", dv_stride, d->n_kv_heads, d->d_head)) return e;
   PQ_REQUIRE(at16(dO) && at16(Q) && at16(K) && at16(V) && at16(O) && at16(dQ) && at16(dK) && at16(dV) && at16(workspace), PQ_ERR_SHAPE,
              "buffers must be 16-byte aligned");
-  PQ_REQUIRE(dQ != Q && dK != K && dV != V && dQ != dO && dQ != O, PQ_ERR_BAD_ARG, "gradients in place of what they are formed from");
   // (fewer rows may want more pieces and more room for them: a workspace for more rows serves fewer with the pieces that it holds)
   const size_t least = stats_bytes(d, T) + 256;
   PQ_REQUIRE(workspace_bytes >= least, PQ_ERR_WORKSPACE, "workspace %zu < %zu", workspace_bytes, least);
+  const int pieces = (int)std::max<size_t>(1, std::min<size_t>(token_pieces(d, T), (workspace_bytes - least) / part_bytes(d, T)));
+  const int H = d->n_heads, Hk = d->n_kv_heads, dh = d->d_head;
+  const pq_region written[] = {rows_region("dQ", dQ, T, dq_stride, H, dh), rows_region("dK", dK, T, dk_stride, Hk, dh), rows_region("dV", dV, T, dv_stride, Hk, dh),
+                               pq_flat_region("workspace", workspace, (int64_t)(stats_bytes(d, T) + (pieces > 1 ? pieces * part_bytes(d, T) : 0)))};
+  const pq_region read[] = {rows_region("dO", dO, T, (int64_t)H * dh, H, dh), rows_region("Q", Q, T, q_stride, H, dh), rows_region("K", K, T, k_stride, Hk, dh),
+                            rows_region("V", V, T, v_stride, Hk, dh), rows_region("O", O, T, (int64_t)H * dh, H, dh),
+                            pq_flat_region("lse", lse, (int64_t)T * H * 4), row_start_region(d, row_start)};
+  if (int e = pq_refuse_overlap(written, 4, read, 7)) return e;
   self_args a = make_args(d, T, row_start);
   a.Q = (const uint16_t*)Q; a.K = (const uint16_t*)K; a.V = (const uint16_t*)V; a.O = (const uint16_t*)O; a.dO = (const uint16_t*)dO;
   a.qs = q_stride; a.ks = k_stride; a.vs = v_stride;
@@ -1340,7 +1358,7 @@ extern "C" int pq_self_attn_bwd(const pq_self_attn_desc* d, const void* dO, cons
   a.lse = const_cast<float*>(lse);
   a.stats = (float2*)workspace;
   a.parts = (float*)((char*)workspace + stats_bytes(d, T));
-  a.pieces = (int)std::max<size_t>(1, std::min<size_t>(token_pieces(d, T), (workspace_bytes - least) / part_bytes(d, T)));
+  a.pieces = pieces;
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_SELF_ATTN_BWD, s);
   const bool direct = a.d % 8 == 0 && q_stride % 8 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0;
