@@ -470,7 +470,8 @@ typedef struct pq_rope_desc {
 } pq_rope_desc;
 /* Q [T][n_heads][d_head], K [T][n_kv_heads][d_head] of `dtype` (PQ_F32 or PQ_BF16), rows q_stride / k_stride elements apart (even, at least
  * the heads' elements); Qr, Kr the same shapes with strides of their own.  Qr may be Q and Kr may be K, with the same stride (in place); otherwise what is
- * written must share no byte with what is read, or with the other output (refused; rows between each other's rows are no overlap).  All 16-byte aligned. */
+ * written must share no byte with what is read, or with the other output (refused; rows between each other's rows are no overlap).  All 16-byte aligned.
+ * 2^24 - 1 rows of any length are taken, up to 2^29 short ones; what wants more workgroups than a launch has is refused. */
 int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, int32_t dtype, int32_t T,
             const double* freqs, const int32_t* row_start, const int32_t* lens, void* Qr, int64_t qr_stride, void* Kr, int64_t kr_stride, void* stream);
 
@@ -483,7 +484,8 @@ int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const voi
  *   calls what is written must share no byte with what is read or with another output (refused; rows between each other's rows are no overlap).
  * Scores, sums and lse are fp32; exp(s_j - m) is rounded to bf16 for the product with v (m: the largest s_j among the first up to 64 tokens that the row
  * sees, or among all where sums with it are not finite), o once more at the end; sums hold |v| up to 2^80.  Tokens that
- * a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite or NaN.  At most 2^29 rows, rows * n_heads < 2^31.  The result does not depend on the order in which workgroups run. */
+ * a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite or NaN.  At most 2^29 rows, rows * n_heads < 2^31 and
+ * (rows / 128 + n_seqs) * n_heads < 2^24 (more is refused).  The result does not depend on the order in which workgroups run. */
 typedef struct pq_self_attn_desc {
   int32_t n_heads;    /* query heads, a multiple of n_kv_heads */
   int32_t n_kv_heads;
@@ -543,7 +545,7 @@ typedef struct pq_adamw_desc {
 } pq_adamw_desc;
 /* A plan lists the pieces of all tensors.  pq_adamw_plan writes pq_adamw_plan_bytes() bytes of HOST memory (plan, 8-byte aligned); the caller copies them to device
  * memory and keeps them for as long as the tensors' addresses hold.  Every buffer is 16-byte aligned (steps: 8); written buffers must not overlap.
- * `tensors` is host memory, read only by these two calls.  (0 bytes: refused arguments.)  pq_adamw_step and pq_adamw_read want exactly that many bytes. */
+ * `tensors` is host memory, read only by these two calls.  (0 bytes: refused arguments, among them tensors of 2^24 and more blocks of 2048 elements.)  pq_adamw_step and pq_adamw_read want exactly that many bytes. */
 size_t pq_adamw_plan_bytes(const pq_adamw_desc* desc, const pq_adamw_tensor* tensors);
 int pq_adamw_plan(const pq_adamw_desc* desc, const pq_adamw_tensor* tensors, void* plan, size_t plan_bytes);
 /* scalars: device memory, so that a captured step can be replayed with others; fp32 { 1 - lr weight_decay, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t),

@@ -251,7 +251,7 @@ int check_tensors(const pq_adamw_desc* d, const pq_adamw_tensor* t, int64_t* pie
     small += (t[i].n + AW_SMALL - 1) / AW_SMALL;
     large += (t[i].n + AW_PIECE - 1) / AW_PIECE;
   }
-  PQ_REQUIRE(large <= 0x7fffffff, PQ_ERR_SHAPE, "too many elements for one call");
+  PQ_REQUIRE(large <= PQ_MOST_WORKGROUPS, PQ_ERR_SHAPE, "too many elements for one call");
   *size = large < 1024 ? AW_SMALL : AW_PIECE;
   *pieces = large < 1024 ? small : large;
   if (*pieces == 0) *pieces = 1;       // (one without elements)
@@ -277,7 +277,7 @@ int check_plan(const pq_adamw_desc* d, const void* plan, size_t plan_bytes) {
   if (int e = check_adamw(d)) return e;
   PQ_REQUIRE(plan, PQ_ERR_BAD_ARG, "NULL plan");
   PQ_REQUIRE(((uintptr_t)plan & 15) == 0, PQ_ERR_SHAPE, "buffers must be 16-byte aligned");
-  PQ_REQUIRE(plan_bytes > 0 && plan_bytes % sizeof(adamw_piece) == 0 && plan_bytes / sizeof(adamw_piece) <= 0x7fffffff, PQ_ERR_WORKSPACE,
+  PQ_REQUIRE(plan_bytes > 0 && plan_bytes % sizeof(adamw_piece) == 0 && plan_bytes / sizeof(adamw_piece) <= PQ_MOST_WORKGROUPS, PQ_ERR_WORKSPACE,
              "a plan has pq_adamw_plan_bytes() bytes, not %zu", plan_bytes);
   return PQ_OK;
 }

@@ -14,6 +14,9 @@ struct pq_prof_scope {   // records an event pair around the launches made while
   ~pq_prof_scope();
 };
 
+// Workgroups of 256 threads that a launch takes at most (it has fewer than 2^32 threads).
+constexpr int64_t PQ_MOST_WORKGROUPS = (1 << 24) - 1;
+
 // ---- buffers of a call that must not share memory (pq_api.hip) ------------------------------
 struct pq_region {       // `rows` rows of `bytes` bytes, `stride` bytes apart (at least `bytes`)
   const char* name;

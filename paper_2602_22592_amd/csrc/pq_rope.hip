@@ -203,6 +203,7 @@ extern "C" int pq_rope(const pq_rope_desc* d, const void* Q, int64_t q_stride, c
   a.by_row.set(per_row);         // .. 1024 where there are several rows ..
   a.by_piece.set(a.pieces);      // .. and 2^16 heads of 2^7 pieces are divided)
   const unsigned grid = (unsigned)((T + rows - 1) / rows);
+  PQ_REQUIRE(grid <= PQ_MOST_WORKGROUPS, PQ_ERR_SHAPE, "T=%d rows of %d heads of %d are too many for one call", T, a.total_heads, a.d);
   hipStream_t s = (hipStream_t)stream;
   pq_prof_scope prof(PQP_ROPE, s);
   if (dtype == PQ_BF16) {

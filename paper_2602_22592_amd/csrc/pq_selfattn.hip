@@ -1189,7 +1189,7 @@ int check_self(const pq_self_attn_desc* d) {
 int check_rows(const pq_self_attn_desc* d, int T) {
   PQ_REQUIRE(T >= 0, PQ_ERR_BAD_ARG, "T=%d is negative", T);
   PQ_REQUIRE(T <= (1 << 29) && (int64_t)T * d->n_heads <= 0x7fffffff &&
-                 ((int64_t)T / SA_ROWS + d->n_seqs) * d->n_heads <= 0x7fffffff, PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call",
+                 ((int64_t)T / SA_ROWS + d->n_seqs) * d->n_heads <= PQ_MOST_WORKGROUPS, PQ_ERR_SHAPE, "%d rows of %d heads in %d sequences are too many for one call",
              T, d->n_heads, d->n_seqs);
   return PQ_OK;
 }

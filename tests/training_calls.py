@@ -46,7 +46,8 @@ def _child(shim_path, lib_path):
         f = getattr(lib, name)
         f.restype = C.c_size_t if name.endswith("_bytes") else C.c_int
         rc = f(*[kinds[k](x) for k, x in args])
-        out.append([rc, lib.pq_last_error_string().decode() if rc else "", [shim.trace_name(i).decode() for i in range(shim.trace_count())]])
+        failed = rc == 0 if name.endswith("_bytes") else rc != 0
+        out.append([rc, lib.pq_last_error_string().decode() if failed else "", [shim.trace_name(i).decode() for i in range(shim.trace_count())]])
     json.dump(out, sys.stdout)
 
 
