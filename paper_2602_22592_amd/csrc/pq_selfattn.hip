@@ -65,7 +65,9 @@ __device__ __forceinline__ i32x4_t load_piece(const uint16_t* q, int d, int at) 
 }
 
 // Sixteen bytes a lane from memory to LDS, lane by lane from `lds` on: from base + offset, the base and `lds` the same for all lanes.  (Not through the
-// compiler's builtin: it would wait for these loads in front of every later read of LDS, of the other buffer as well.)
+// compiler's builtin: it would wait for these loads in front of every later read of LDS, of the other buffer as well.  m0 is a
+// register that the compiler keeps for itself and sets where it needs it: naming it as clobbered is taken with a warning and no promise.  It needs it nowhere
+// in these kernels, and forms the base by scalar instructions, which need no wait states in front of the load; both are tested on what is built.)
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
