@@ -483,8 +483,9 @@ int pq_rope(const pq_rope_desc* desc, const void* Q, int64_t q_stride, const voi
  *   lse [T][n_heads] fp32 out, both contiguous.  Rows of no sequence are neither read nor written.  Buffers 16-byte aligned; in both
  *   calls what is written must share no byte with what is read or with another output (refused; rows between each other's rows are no overlap).
  * Scores, sums and lse are fp32; exp(s_j - m) is rounded to bf16 for the product with v (m: the largest s_j among the first up to 64 tokens that the row
- * sees, or among all where sums with it are not finite), o once more at the end; sums hold |v| up to 2^80.  Tokens that
- * a row does not see have no effect on it, whatever they hold; an infinity or a NaN that it sees makes what it reaches infinite or NaN.  At most 2^29 rows, rows * n_heads < 2^31 and
+ * sees, or among all where sums with it are not finite), o once more at the end; sums hold |v| up to 2^80.  An infinity or a NaN
+ * that a row sees makes what it reaches infinite or NaN.  Tokens that it does not see have no effect on it, but that one
+ * which is not finite can have the 128 rows of a tile that reads it formed with the other m: their results differ by a rounding.  At most 2^29 rows, rows * n_heads < 2^31 and
  * (rows / 128 + n_seqs) * n_heads < 2^24 (more is refused).  The result does not depend on the order in which workgroups run. */
 typedef struct pq_self_attn_desc {
   int32_t n_heads;    /* query heads, a multiple of n_kv_heads */
@@ -501,12 +502,14 @@ int pq_self_attn_fwd(const pq_self_attn_desc* desc, const void* Q, int64_t q_str
  *     p_j = exp(s_j - lse),   delta = sum_j p_j dO . v_j,   dS_j = p_j (dO . v_j - delta)
  *     dQ = scale sum_j dS_j k_j,   dK_j = scale sum dS_j q,   dV_j = sum p_j dO      (the last two over the rows that see j, and over the heads
  *                                                                                      that share it)
- *   dQ, dK, dV bf16 out with strides of their own (even); p and dS are rounded to bf16 for the products (the first 64 rows' of a causal
- *   sequence, and those of whole ones of up to 64 rows, are sums of two bf16 numbers), the sums are fp32.  (delta is
+ *   dQ, dK, dV bf16 out with strides of their own (even); p and dS are rounded to bf16 for the products, by up to 2^-8 of themselves (the
+ *   first 64 rows' of a causal sequence, and those of whole ones of up to 64 rows, are sums of two bf16 numbers, off by up to 2^-16; not in
+ *   tiles that read something that is not finite), the sums are fp32.  (delta is
  *   begun as dO . O, with O as it was rounded, and put right by the sum of the dS: O may be off by its rounding, not be something else.)  A row
  *   that sees one token has dS = 0.  Tokens and rows that do not see each other have no effect on each other, as above.
  *   workspace: pq_self_attn_bwd_workspace_bytes() bytes of scratch (0: refused arguments; fewer rows may want more: one for more
- *   rows serves them too, their work then cut into the pieces that it holds); calls that may overlap need one each. */
+ *   rows serves them too, their work then cut into the pieces that it holds); calls that may overlap need one each.  Pieces are
+ *   added in their order, so that the last bits of dK and dV follow from workspace_bytes, and from nothing else but the arguments. */
 size_t pq_self_attn_bwd_workspace_bytes(const pq_self_attn_desc* desc, int32_t T);
 int pq_self_attn_bwd(const pq_self_attn_desc* desc, const void* dO, const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* V,
                      int64_t v_stride, const void* O, const float* lse, int32_t T, const int32_t* row_start, void* dQ, int64_t dq_stride, void* dK,

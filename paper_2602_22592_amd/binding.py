@@ -779,7 +779,8 @@ class AdamWTensors:
     params: contiguous tensors of one type, fp32 or bf16, on one GPU; grads: of the same sizes, fp32 or bf16, read anew by every step; masters: fp32, of bf16
     params, or None.  States m and v that are not given are made here and begin at zero, of `state` (PQ_STATE_F32 or PQ_STATE_8BIT: int8 m, uint8 v and
     steps [ceil(n / 256), 2] fp32); those that are given say by their type which it is.  m_values, v_values: fp32, where adamw_read writes 8-bit
-    states as the values they stand for, or None.  The tensors must stay where they are."""
+    states as the values they stand for, or None.  The tensors must stay where they are: gradients too, which are written into the same memory by every
+    backward.  (Laying out fifty tensors anew takes 190 us, seventy 260, many times a small step.)"""
 
     def __init__(self, params, grads, m=None, v=None, steps=None, masters=None, m_values=None, v_values=None, beta1=0.9, beta2=0.999, eps=1e-8,
                  state=PQ_STATE_F32):
@@ -843,7 +844,9 @@ class AdamWTensors:
 
 
 def adamw_scalars(tensors, step, lr, weight_decay=0.0, grad_scale=1.0, out=None):
-    """What changes from step to step (counted from 1), as the device tensor that adamw_step reads; `out`: into that tensor, for steps that are captured."""
+    """What changes from step to step (counted from 1), as the device tensor that adamw_step reads; `out`: into that tensor, for steps that are captured.
+    Formed on the host and copied by a transfer that the host waits for, on the current stream behind all that is there: about 16 us of every step that
+    takes new ones, and no run-ahead of the host across it."""
     if step < 1 or lr < 0.0 or weight_decay < 0.0:
         raise PQError(f"step={step} counts from 1, lr={lr} and weight_decay={weight_decay} are not negative")
     d = tensors.desc

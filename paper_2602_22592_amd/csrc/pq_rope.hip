@@ -61,8 +61,9 @@ template <> __device__ __forceinline__ float rounded<float>(float x) { return x;
 template <> __device__ __forceinline__ uint16_t rounded<uint16_t>(float x) { return f32_to_bf16(x); }
 
 // Bound by memory: a workgroup forms the sines and cosines of its rows once, for all heads, then turns them piece by piece, 16 bytes of x and of y a lane
-// where everything is aligned to that (32768 rows, 32+8 heads of 128, bf16: 131 us, 5.1 TB/s; a pair a lane 251), else a pair a lane
-// (8192 rows, 32+32 heads of 90, pairs of neighbours: bf16 53 us, 3.6 TB/s; four bytes a lane and load).  The turns are fp64: near position 2^23
+// where everything is aligned to that (32768 rows, 32+8 heads of 128, bf16: 131 us, 5.1 TB/s; a pair a lane 251), else a pair a lane, since heads
+// of 90 begin at multiples of four bytes and a piece of 16 would hold pairs of two of them (8192 rows, 32+32 heads of 90, bf16: pairs of neighbours, four bytes a
+// lane and load, 52 us, 3.6 TB/s; halves, two bytes, 56; fp32 80 and 86).  The turns are fp64: near position 2^23
 // fp32 would be off by 2^-4 of a turn, fp64 is by 2^-32.
 template <typename T, int LAYOUT, int VEC>
 __global__ __launch_bounds__(256) void rope_kernel(rope_args a) {

@@ -306,7 +306,9 @@ __device__ __forceinline__ uint32_t register_bits(uint32_t rows, int u) {
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
 
 // Which sequence and which of its tiles of SA_ROWS rows workgroup tile vt is.  Up to 8 sequences: the longest first, of each the tiles with most work
-// first (`down`: its last ones), so that long tiles do not start when the others end.  Up to 63: from one load of all of row_start.  Any number: virtual
+// first (`down`: its last ones), so that long tiles do not start when the others end (32 heads of 128 on eight, 8 ragged sequences of up to 1166 rows: 64 us
+// and 300 for the gradients, otherwise 68 and 315; 16 of up to 868: 85 and 351 in this order, 81 and 379 without; 60 of up to 292: 107 and 391 to 74 and 318, the
+// search for the order takes longer).  Up to 63: from one load of all of row_start.  Any number: virtual
 // tiles, of which sequence b owns those from floor(first row / SA_ROWS) + b on, at least as many as it has.
 struct self_tile { int r0, n, at; };     // rows r0 .. r0 + n - 1 of the call, the tile's first row among them (n == 0: none)
 __device__ __forceinline__ self_tile find_self_tile(const self_args& a, int vt, bool down) {
@@ -351,10 +353,10 @@ __device__ __forceinline__ int first_token(const self_args& a, int row) { return
 
 // The stages that a tile needs, and of them those of which a wavefront's 32 rows (or tokens) see something, from .. to - 1: these are a loop of their own,
 // since a branch around accumulators costs a second copy of them all.  Those from `all` to `part` - 1 are seen by all of its rows.
-// FINE stages of the gradients: p and dS as sums of two bf16 numbers.  The first 64 rows of causal sequences and whole ones of up to 64 rows: they see
-// few tokens, so that few large elements make their parts of the gradients, and these parts are the largest.  With one rounding each the gradients' error
-// comes to 1.4 times that of their own rounding, in one of ten short calls to more than 1.5 times (with two: in one of a hundred).  A sequence has one
-// such stage a head: 130 tokens 32 us instead of 31, longer ones as before.
+// FINE stages of the gradients: p and dS as sums of two bf16 numbers, off by 2^-16 of themselves instead of 2^-8.  The first 64 rows of causal sequences and
+// whole ones of up to 64 rows: they see few tokens, so that few large elements make their parts of the gradients, and these parts are the largest.  What the
+// gradients of short sequences are off by is then the outputs' own rounding alone; with one rounding each it came to 1.4 times that, in one of ten short
+// calls to more than 1.5 times.  A sequence has one such stage a head: 130 tokens 32 us instead of 31.  (Stages taken with care have one rounding.)
 enum { PLAIN, FINE, CAREFUL };
 struct stages_of { int first, n, from, all, part, to, begin; };     // begin: the first of those that are taken at all
 // Stages of tokens that rows row0 .. row0 + 31 of the tile see.
@@ -1213,7 +1215,8 @@ pq_region row_start_region(const pq_self_attn_desc* d, const int32_t* row_start)
 // 2000 rows: 91 us, 713 in one piece; 4 heads of 128 on one, 1000 rows: 72, in pieces of 16 stages 83, in one 168).  Tiles of causal rows differ
 // in length and come in few rounds, so long ones are cut further: to 2048 workgroups of 64 stages where two share a CU (32 heads of 64 on four, 10000
 // rows: 1560 us, uncut 2500; on eight, 8192 rows: 1060 and 1230; cut to 4096 1616 and 1124), to 1024 of 32 where one has it alone (32 heads of 128
-// on eight, 5000 rows: 900, uncut 1040, cut to 2048 980; 8192 rows, which stay whole: 2150, cut 2210).  Stages by the window (5000 rows, a window of 512:
+// on eight, 5000 rows: 900, uncut 1040, cut to 2048 980; 8192 rows, which stay whole: 2150, cut 2210).  Whole sequences gain as well, from fewer
+// tiles (of 2000 rows, 32 heads of 64 on eight: 159 us, uncut 244; 5000 rows of 128: 1700 and 2056; 8192 of 64 lose 2 %).  Stages by the window (5000 rows, a window of 512:
 // 311 uncut, 335 and 411 in pieces) and, for the second cut, by the sequences' mean length (16 of 512 rows: 295, cut 387).
 int token_pieces(const pq_self_attn_desc* d, int T) {
   const int64_t tiles = ((int64_t)T / SA_ROWS + d->n_seqs) * d->n_kv_heads, group = d->n_heads / d->n_kv_heads;

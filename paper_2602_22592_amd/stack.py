@@ -8,7 +8,8 @@ Stack: a stack of transformer-shaped layers made of pQuant linears only (no atte
                 h2 = h1 + FFN(h1)                   decoupled FFN with routed experts (Sec. 3.2, 3.3)
 
 It exists to time the linears of a 24-layer 1.3B-shaped model end to end.  With an AttentionCore m is attention(rotary(q), rotary(k), v) in its place, and
-Stack.optimizer lays out the AdamW step of all layers' weights: forward, backward and that step are a training step.
+Stack.optimizer lays out the AdamW step of all layers' weights: forward, backward and that step train these.  An FFN's alpha and beta are host numbers
+(`layers[l]["ffn_desc"].alpha` and `.beta`, read by every call, fixed in a captured one); their gradients are in backward's "dab", and nothing here applies them.
 
 CachedAttention: the attention half of a layer at inference, on packed weights and a paged key-value cache:
 
@@ -31,7 +32,7 @@ class AttentionCore:
 
     row_start [n_seqs + 1] int32 on the GPU: the sequences' rows among the `tokens` of a call; it may change from step to step.  Rows of no sequence come
     out as zeros and have no gradient: the kernels leave them alone, so every call clears what it is about to write (the products that read it take all
-    rows).  freqs [rot_dim / 2] (rope_freqs), or None for attention without positions."""
+    rows).  freqs [rot_dim / 2] (rope_freqs), or None for attention without positions.  The workspace is the core's: calls that may overlap need one each."""
 
     def __init__(self, tokens, n_heads, n_kv_heads, d_head, n_seqs, freqs=None, rot_dim=0, layout=pq.PQ_ROPE_HALF, rope_scale=1.0, window=0, causal=True,
                  device="cuda"):
@@ -157,8 +158,8 @@ class Stack:
         return [dxq, dxk, dxv]
 
     def optimizer(self, weights, grads, names=None, **kw):
-        """The AdamW step over all layers' weights with backward's gradients (`names`: all of a layer's tensors unless given).  kw: as AdamWTensors takes
-        them; masters=True makes fp32 masters of the weights as they are."""
+        """The AdamW step over all layers' weights with backward's gradients (`names`: all of a layer's tensors unless given; alpha and beta are none of
+        them).  kw: as AdamWTensors takes them; masters=True makes fp32 masters of the weights as they are."""
         pairs = [(w[n], g[n]) for w, g in zip(weights, grads) for n in (names or [n for n in w if n in g])]
         if kw.get("masters") is True:
             kw["masters"] = [p.float() for p, _ in pairs]

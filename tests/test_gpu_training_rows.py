@@ -94,3 +94,20 @@ def test_a_core_clears_what_it_is_given():
     for g in grads:
         assert torch.isfinite(g).all() and (g[outside] == 0).all()
     assert (grads[2][~outside] != 0).any(1).all()
+
+
+def test_alpha_and_beta_are_those_of_the_descriptors_at_the_call():
+    """What nothing in the stack trains: whoever does writes them into the layers' descriptors."""
+    c, x, dY = _case()
+    rows, a = t32([0, 60, 128]), Steps(c)
+    before = a.run(x, dY, rows)[0]
+    for w, ly in zip(c["layers"], a.stack.layers):
+        w["alpha"], w["beta"] = 1.5 * w["alpha"], 0.5 * w["beta"]
+        ly["ffn_desc"].alpha, ly["ffn_desc"].beta = w["alpha"], w["beta"]
+    b = Steps(c)
+    got, want = a.run(x, dY, rows), b.run(x, dY, rows)
+    assert not torch.equal(got[0], before)
+    for p, q in zip(got, want):
+        assert torch.equal(p, q)
+    for (name, p), q in zip(a.left().items(), b.left().values()):
+        assert torch.equal(p, q), name
